@@ -2,10 +2,12 @@
 
     python -m paper_2510_05361_amd.build
 
-compiles csrc/mtdao.hip (host code + kernels) with hipcc for gfx950 into
-paper_2510_05361_amd/libmtdao.so, and csrc/stream_ref.hip (reference copy /
-read / fill kernels used only by the benchmark) into libstream_ref.so.  Packed-fp32 instruction selection is
-switched off for the device code.
+compiles csrc/mtdao.hip (the optimizer: host code + kernels) and the
+operators' sources (OPS_SRCS) side by side with hipcc for gfx950, links them
+into paper_2510_05361_amd/libmtdao.so, and compiles csrc/stream_ref.hip
+(reference copy / read / fill kernels used only by the benchmark) into
+libstream_ref.so.  Packed-fp32 instruction selection is switched off for the
+device code.
 """
 
 from __future__ import annotations
@@ -13,11 +15,15 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "mtdao.hip")
-HEADERS = [os.path.join(PKG, "csrc", "kernels.hpp"), os.path.join(ROOT, "include", "mtdao.h")]
+OPS_SRCS = [os.path.join(PKG, "csrc", f) for f in ("adamw.hip", "peri_norm.hip", "product8.hip")]
+HEADERS = [os.path.join(PKG, "csrc", f) for f in ("kernels.hpp", "host.hpp", "ops_device.hpp")] + \
+    [os.path.join(ROOT, "include", f) for f in ("mtdao.h", "mtdao_ops.h")]
 LIB = os.path.join(PKG, "libmtdao.so")
 STREAM_SRC = os.path.join(PKG, "csrc", "stream_ref.hip")
 STREAM_LIB = os.path.join(PKG, "libstream_ref.so")
@@ -40,7 +46,7 @@ def source_hash() -> str:
     """Hash of the device sources the kernels are compiled from."""
     import hashlib
     h = hashlib.sha256()
-    for f in [SRC, *HEADERS]:
+    for f in [SRC, *OPS_SRCS, *HEADERS]:
         with open(f, "rb") as fh:
             h.update(fh.read())
     return h.hexdigest()[:16]
@@ -65,34 +71,47 @@ def resource_rows(remarks: str):
     return rows
 
 
-def _compile(src: str, out: str, extra=(), libs=(), resources: str = "") -> str:
-    """hipcc src into out; with ``resources``, also write the register,
-    scratch and occupancy figures of every kernel there."""
-    tmp = out + ".tmp"
-    cmd = [HIPCC, *FLAGS, *extra, "-I", os.path.join(ROOT, "include"), "-o", tmp, src, *libs]
-    if resources:
-        cmd.append(_REMARK)
+def _run(cmd) -> str:
+    """Run hipcc; its stderr, with what is no resource remark passed through."""
     r = subprocess.run(cmd, stderr=subprocess.PIPE, text=True)
-    # pass everything that is not a resource remark through
     sys.stderr.write("".join(l + "\n" for l in r.stderr.splitlines() if "kernel-resource-usage" not in l))
     if r.returncode != 0:
         raise subprocess.CalledProcessError(r.returncode, cmd)
-    if resources:
-        with open(resources, "w") as f:
-            f.write(f"# source {source_hash()}\n")
-            for row in resource_rows(r.stderr):
-                f.write(" ".join(f"{k}={v}" for k, v in row.items()) + "\n")
+    return r.stderr
+
+
+def _compile(src: str, out: str, extra=(), libs=()) -> str:
+    """hipcc src into the shared library out."""
+    tmp = out + ".tmp"
+    _run([HIPCC, *FLAGS, *extra, "-I", os.path.join(ROOT, "include"), "-o", tmp, src, *libs])
     os.replace(tmp, out)
     return out
 
 
 def build(out: str = LIB, extra=()) -> str:
-    """The optimizer library (always) and the benchmark's stream-reference
-    kernels (libstream_ref.so)."""
-    _compile(STREAM_SRC, STREAM_LIB, extra)
-    # roctx ranges (MTDAO_ROCTX=1) come from the rocprofiler-sdk marker library
-    return _compile(SRC, out, extra, libs=("-L/opt/rocm/lib", "-lrocprofiler-sdk-roctx", "-Wl,-rpath,/opt/rocm/lib"),
-                    resources=RESOURCES)
+    """The library (always) and the benchmark's stream-reference kernels
+    (libstream_ref.so).  The register, scratch and occupancy figures of every
+    kernel go to RESOURCES."""
+    flags = [f for f in FLAGS if f != "-shared"]
+    with tempfile.TemporaryDirectory() as d, ThreadPoolExecutor(4) as pool:
+        def compile_one(src):
+            obj = os.path.join(d, os.path.basename(src) + ".o")
+            return obj, _run([HIPCC, *flags, *extra, "-I", os.path.join(ROOT, "include"), "-c", "-o", obj, src, _REMARK])
+
+        stream = pool.submit(_compile, STREAM_SRC, STREAM_LIB, extra)
+        done = list(pool.map(compile_one, [SRC, *OPS_SRCS]))
+        stream.result()
+        # roctx ranges (MTDAO_ROCTX=1) come from the rocprofiler-sdk marker library
+        tmp = out + ".tmp"
+        _run([HIPCC, "--offload-arch=gfx950", "-fPIC", "-shared", "-o", tmp, *[obj for obj, _ in done],
+              "-L/opt/rocm/lib", "-lrocprofiler-sdk-roctx", "-Wl,-rpath,/opt/rocm/lib"])
+    with open(RESOURCES, "w") as f:
+        f.write(f"# source {source_hash()}\n")
+        for _, remarks in done:
+            for row in resource_rows(remarks):
+                f.write(" ".join(f"{k}={v}" for k, v in row.items()) + "\n")
+    os.replace(tmp, out)
+    return out
 
 
 if __name__ == "__main__":

@@ -3,14 +3,10 @@
 // The arithmetic of every step runs in the kernels of kernels.hpp.
 
 #include <hip/hip_runtime.h>
-#include <rocprofiler-sdk-roctx/roctx.h>
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
 #include <cstddef>
-#include <cstdio>
-#include <cstdlib>
 #include <cstring>
 #include <mutex>
 #include <string>
@@ -18,9 +14,14 @@
 #include <vector>
 
 #include "../../include/mtdao.h"
+#include "host.hpp"
 #include "kernels.hpp"
 
 using namespace mtdao;
+
+namespace mtdao {
+thread_local std::string g_err;
+}
 
 static_assert(sizeof(DeviceStep) == sizeof(mtdao_device_step) && offsetof(DeviceStep, s) == offsetof(mtdao_device_step, s),
               "DeviceStep mirrors mtdao_device_step");
@@ -44,34 +45,6 @@ struct mtdao_handle {
 
 namespace {
 
-thread_local std::string g_err;
-
-// roctx ranges around every enqueueing call, for timelines of
-// rocprofv3 --marker-trace: on when MTDAO_ROCTX=1 in the environment.
-bool roctx_on() {
-  static const bool on = [] {
-    const char* e = std::getenv("MTDAO_ROCTX");
-    return e != nullptr && e[0] == '1';
-  }();
-  return on;
-}
-
-struct RoctxRange {
-  bool on;
-  explicit RoctxRange(const char* fmt, ...) : on(roctx_on()) {
-    if (!on) return;
-    char buf[128];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    roctxRangePushA(buf);
-  }
-  ~RoctxRange() {
-    if (on) roctxRangePop();
-  }
-};
-
 // Piece length of the tile -> element map (tile_elem): one wavefront's
 // access, 64 lanes of V elements (1 KiB of fp32 for V = 4).
 constexpr int piece_for(int V) { return 64 * V; }
@@ -79,17 +52,6 @@ constexpr int kStepNT = 3;     // nontemporal hints of the local step (bit 0 loa
 constexpr bool kMeanNT = true; // nontemporal hints of the replica mean
 constexpr int kNormU = 8;      // vector slots per thread in the norm pass
 
-int32_t fail(std::string* sink, int32_t code, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  *sink = buf;
-  return code;
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
 bool has_v(const mtdao_config& c) { return c.form != MTDAO_SGDM; }
 
@@ -195,17 +157,6 @@ size_t workspace_for(const mtdao_config& c) {
   if (!(c.clip_rho > 0.0f) || c.form == MTDAO_ADOPT) return 0;
   const size_t scale_bytes = ((size_t)c.replicas * sizeof(float) + 255) / 256 * 256;
   return scale_bytes + (size_t)c.replicas * (size_t)norm_blocks_for(c.numel) * sizeof(double);
-}
-
-// Non-overlap of two [lo, lo + bytes) device ranges.
-bool overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes) {
-  const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b;
-  return a0 < b0 + (uintptr_t)bbytes && b0 < a0 + (uintptr_t)abytes;
-}
-
-int32_t hip_check(std::string* e, hipError_t r, const char* what) {
-  if (r != hipSuccess) return fail(e, MTDAO_ERR_HIP, "%s: %s", what, hipGetErrorString(r));
-  return MTDAO_OK;
 }
 
 // ---------------------------------------------------------------- dispatch

@@ -1,0 +1,693 @@
+// The boundary of a Peri-LN block (include/mtdao_ops.h): norm after the block,
+// gate and residual scale, norm before the next block, in one pass over the
+// rows, and its backward pass.
+//
+// A row of D elements lies in the registers of TPR threads (a wave or more),
+// eight consecutive elements per thread and vector, so every tensor is read
+// and written once and the statistics are formed from registers (the mean
+// first, then the centred squares).  Both passes are bound by HBM: forward
+// reads x, f and writes x', n; backward reads dx', dn, x', f and writes dx,
+// df.  The backward pass forms the statistics again rather than reading
+// stored ones: the rows pass through registers anyway.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <string>
+#include <type_traits>
+
+#include "../../include/mtdao_ops.h"
+#include "host.hpp"
+#include "ops_device.hpp"
+
+using namespace mtdao;
+using namespace mtdao::ops;
+
+namespace {
+
+constexpr int kE = 8;         // elements of a thread's vector
+constexpr int kGroup = 256;   // smallest workgroup
+
+struct Args {
+  int64_t rows, rows_per_gate, ld_x, ld_f, ld_d_out, ld_dn;
+  const void *x, *f, *w_post, *w_pre, *gate, *d_out, *dn;
+  void *x_out, *n_out, *df;
+  float *d_w_post, *d_w_pre, *d_gate;
+  float* partial;           // backward: [3][blocks][D], sums of a workgroup's rows
+  int64_t per_block;        // backward: rows of a workgroup, or gates (whole_gates)
+  int64_t parts;            // backward: workgroups of a gate
+  int32_t d, whole_gates, weight_bf16;
+  float eps, scale, inv_d;
+};
+
+// Sums of N values over the TPR threads of a row, in all of them.  `buf` has
+// N floats per wave of the workgroup; consecutive calls use different ones.
+template <int TPR, int N>
+__device__ __forceinline__ void sum_row(float (&v)[N], float* buf) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = sum64(v[i]);
+  if constexpr (TPR > 64) {
+    constexpr int W = TPR / 64;
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, first = wave / W * W;
+    if (lane == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) buf[wave * N + i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float s = 0.0f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) s += buf[(first + w) * N + i];
+      v[i] = s;
+    }
+  }
+}
+
+__device__ __forceinline__ void load_weight(const void* p, bool bf16, int64_t at, int n, float (&o)[kE]) {
+  if (n <= 0) {
+#pragma unroll
+    for (int t = 0; t < kE; ++t) o[t] = 0.0f;
+  } else if (bf16) {
+    load_some<kE>(reinterpret_cast<const bf16_t*>(p) + at, n, o);
+  } else {
+    load_some<kE>(reinterpret_cast<const float*>(p) + at, n, o);
+  }
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void load_or_zero(const T* p, int n, float (&o)[N]) {
+  if (n > 0) {
+    load_some<N>(p, n, o);
+  } else {
+#pragma unroll
+    for (int t = 0; t < N; ++t) o[t] = 0.0f;
+  }
+}
+
+// z centred (LayerNorm) in place, 1 / sqrt(mean square + eps) returned.
+template <int TPR, int NV, bool LAYER>
+__device__ __forceinline__ float normalize(float (&z)[NV][kE], const int (&n)[NV], const Args& a, float* buf) {
+  if constexpr (LAYER) {
+    float m[1] = {0.0f};
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int t = 0; t < kE; ++t) m[0] += z[v][t];
+    sum_row<TPR>(m, buf);
+    const float mean = m[0] * a.inv_d;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int t = 0; t < kE; ++t) z[v][t] = t < n[v] ? z[v][t] - mean : 0.0f;
+    buf += kGroup / 64 * (TPR > kGroup ? TPR / kGroup : 1);
+  }
+  float q[1] = {0.0f};
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int t = 0; t < kE; ++t) q[0] = fmaf(z[v][t], z[v][t], q[0]);
+  sum_row<TPR>(q, buf);
+  return 1.0f / sqrtf(fmaf(q[0], a.inv_d, a.eps));
+}
+
+template <typename ST, typename BT, bool LAYER, int TPR, int NV>
+__global__ __launch_bounds__(TPR > kGroup ? TPR : kGroup) void k_peri_norm(Args a) {
+  constexpr int kThreads = TPR > kGroup ? TPR : kGroup, kWaves = kThreads / 64;
+  __shared__ float buf[4 * kWaves];
+  const int lane = threadIdx.x % TPR;
+  const int64_t row_or_past = (int64_t)blockIdx.x * (kThreads / TPR) + threadIdx.x / TPR;
+  const bool live = row_or_past < a.rows;
+  if (TPR == 64 && !live) return;  // (wider rows fill a workgroup or meet at barriers)
+  const int64_t row = live ? row_or_past : a.rows - 1;
+  const ST* x = reinterpret_cast<const ST*>(a.x) + row * a.ld_x;
+  float xa[NV][kE], fa[NV][kE];
+  int n[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int e = (v * TPR + lane) * kE;
+    n[v] = a.d - e;
+    load_or_zero<kE>(x + e, n[v], xa[v]);
+    if (a.f) load_or_zero<kE>(reinterpret_cast<const BT*>(a.f) + row * a.ld_f + e, n[v], fa[v]);
+  }
+  const bool wb = a.weight_bf16 != 0;
+  if (a.f) {
+    const float r = normalize<TPR, NV, LAYER>(fa, n, a, buf) * a.scale;
+    const int64_t gate_row = a.gate ? row / a.rows_per_gate * a.d : 0;
+    ST* out = reinterpret_cast<ST*>(a.x_out) + row * a.d;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int e = (v * TPR + lane) * kE;
+      float w[kE], g[kE];
+      load_weight(a.w_post, wb, e, n[v], w);
+      if (a.gate) load_weight(a.gate, wb, gate_row + e, n[v], g);
+#pragma unroll
+      for (int t = 0; t < kE; ++t) {
+        const float h = fa[v][t] * r * w[t];
+        xa[v][t] += a.gate ? h * g[t] : h;
+      }
+      if (live && n[v] > 0) store_some<kE>(out + e, n[v], xa[v]);
+    }
+  }
+  if (a.w_pre) {
+    const float r = normalize<TPR, NV, LAYER>(xa, n, a, buf + 2 * kWaves);
+    BT* out = reinterpret_cast<BT*>(a.n_out) + row * a.d;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int e = (v * TPR + lane) * kE;
+      float w[kE];
+      load_weight(a.w_pre, wb, e, n[v], w);
+#pragma unroll
+      for (int t = 0; t < kE; ++t) xa[v][t] = xa[v][t] * r * w[t];
+      if (live && n[v] > 0) store_some<kE>(out + e, n[v], xa[v]);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ backward
+
+// Rows of a workgroup: either one range of rows whose gate (if any) is one,
+// split over the workgroup's row groups, or `per_block` whole gates, each
+// taken by one row group (whole_gates).  A thread keeps the sums of its
+// columns over its rows; the workgroup joins its row groups at the end and
+// writes a row of partial sums, which k_peri_columns adds up.
+template <typename ST, typename BT, bool LAYER, int TPR, int NV, int R>
+__global__ __launch_bounds__(TPR > kGroup ? TPR : kGroup) void k_peri_norm_backward(Args a) {
+  constexpr int kThreads = TPR > kGroup ? TPR : kGroup, kWaves = kThreads / 64, kGroups = kThreads / TPR;
+  constexpr int kMost = 3 * R * kWaves;  // floats of one exchange
+  __shared__ float buf[3 * kMost];
+  __shared__ float joined[kGroups > 1 ? kThreads * kE : 1];
+  const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
+  const bool wb = a.weight_bf16 != 0;
+  float w_pre[NV][kE], w_post[NV][kE], gate[NV][kE], s_pre[NV][kE], s_post[NV][kE], s_gate[NV][kE];
+  int n[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int e = (v * TPR + lane) * kE;
+    n[v] = a.d - e;
+#pragma unroll
+    for (int t = 0; t < kE; ++t) {
+      w_pre[v][t] = w_post[v][t] = s_pre[v][t] = s_post[v][t] = s_gate[v][t] = 0.0f;
+      gate[v][t] = 1.0f;
+    }
+    if (a.w_pre) load_weight(a.w_pre, wb, e, n[v], w_pre[v]);
+    if (a.f) load_weight(a.w_post, wb, e, n[v], w_post[v]);
+  }
+  const int64_t block = blockIdx.x;
+  const int64_t gates = a.gate ? (a.rows + a.rows_per_gate - 1) / a.rows_per_gate : 0;
+  const int64_t rounds = a.whole_gates ? (a.per_block + kGroups - 1) / kGroups : 1;
+  for (int64_t round = 0; round < rounds; ++round) {
+    int64_t at, end, step, longest, my_gate;
+    bool mine = true;
+    if (a.whole_gates) {
+      const int64_t k = round * kGroups + group;
+      my_gate = block * a.per_block + k;
+      mine = k < a.per_block && my_gate < gates;
+      at = my_gate * a.rows_per_gate;
+      end = mine ? (at + a.rows_per_gate < a.rows ? at + a.rows_per_gate : a.rows) : at;
+      step = 1;
+      longest = a.rows_per_gate;
+    } else {
+      my_gate = block / a.parts;
+      const int64_t base = a.gate ? my_gate * a.rows_per_gate : 0;
+      const int64_t stop = a.gate && base + a.rows_per_gate < a.rows ? base + a.rows_per_gate : a.rows;
+      const int64_t from = base + (block - my_gate * a.parts) * a.per_block;
+      end = from + a.per_block < stop ? from + a.per_block : stop;
+      at = from + group;
+      step = kGroups;
+      longest = (a.per_block + kGroups - 1) / kGroups;
+    }
+    if (a.gate) {
+      const int64_t row = (mine ? my_gate : 0) * a.d;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) load_weight(a.gate, wb, row + (v * TPR + lane) * kE, n[v], gate[v]);
+    }
+    for (int64_t done = 0; done < longest; done += R) {
+      float x[R][NV][kE], f[R][NV][kE], d[R][NV][kE], y[R][NV][kE];
+      bool live[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int64_t want = at + (done + i) * step;
+        live[i] = want < end;
+        const int64_t row = live[i] ? want : 0;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          const int e = (v * TPR + lane) * kE;
+          const int m = live[i] ? n[v] : 0;
+          load_or_zero<kE>(reinterpret_cast<const ST*>(a.x) + row * a.ld_x + e, a.w_pre ? m : 0, x[i][v]);
+          load_or_zero<kE>(reinterpret_cast<const BT*>(a.f) + row * a.ld_f + e, a.f ? m : 0, f[i][v]);
+          load_or_zero<kE>(reinterpret_cast<const ST*>(a.d_out) + row * a.ld_d_out + e, a.d_out ? m : 0, d[i][v]);
+          load_or_zero<kE>(reinterpret_cast<const BT*>(a.dn) + row * a.ld_dn + e, a.dn ? m : 0, y[i][v]);
+        }
+      }
+      float* now = buf;
+      if constexpr (LAYER) {  // centre x and f
+        float m[2 * R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          m[2 * i] = m[2 * i + 1] = 0.0f;
+#pragma unroll
+          for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int t = 0; t < kE; ++t) {
+              m[2 * i] += x[i][v][t];
+              m[2 * i + 1] += f[i][v][t];
+            }
+        }
+        sum_row<TPR>(m, now);
+        now += kMost;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int t = 0; t < kE; ++t) {
+              x[i][v][t] = t < n[v] ? x[i][v][t] - m[2 * i] * a.inv_d : 0.0f;
+              f[i][v][t] = t < n[v] ? f[i][v][t] - m[2 * i + 1] * a.inv_d : 0.0f;
+            }
+      }
+      float q[3 * R];  // squares of x and f, and dn w_pre against x
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        q[3 * i] = q[3 * i + 1] = q[3 * i + 2] = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int t = 0; t < kE; ++t) {
+            q[3 * i] = fmaf(x[i][v][t], x[i][v][t], q[3 * i]);
+            q[3 * i + 1] = fmaf(f[i][v][t], f[i][v][t], q[3 * i + 1]);
+            q[3 * i + 2] = fmaf(y[i][v][t] * w_pre[v][t], x[i][v][t], q[3 * i + 2]);
+          }
+      }
+      sum_row<TPR>(q, now);
+      now += kMost;
+      float yw[LAYER ? R : 1];  // sum of dn w_pre: the mean part of the norm's gradient
+      if constexpr (LAYER) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          yw[i] = 0.0f;
+#pragma unroll
+          for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int t = 0; t < kE; ++t) yw[i] = fmaf(y[i][v][t], w_pre[v][t], yw[i]);
+        }
+        sum_row<TPR>(yw, buf);  // (every thread has read the means: it has met at the barrier of q)
+      }
+      float c[2 * R];  // a = dh w_post against f, and its sum
+      float rf[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const float rx = 1.0f / sqrtf(fmaf(q[3 * i], a.inv_d, a.eps));
+        rf[i] = 1.0f / sqrtf(fmaf(q[3 * i + 1], a.inv_d, a.eps));
+        const float along = q[3 * i + 2] * rx * a.inv_d;
+        const float mean = LAYER ? yw[LAYER ? i : 0] * a.inv_d : 0.0f;
+        c[2 * i] = c[2 * i + 1] = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+          for (int t = 0; t < kE; ++t) {
+            const float xh = x[i][v][t] * rx, fh = f[i][v][t] * rf[i];
+            s_pre[v][t] = fmaf(y[i][v][t], xh, s_pre[v][t]);
+            const float through = fmaf(-xh, along, fmaf(y[i][v][t], w_pre[v][t], -mean));
+            const float dd = fmaf(rx, through, d[i][v][t]);
+            d[i][v][t] = dd;
+            const float dh = dd * gate[v][t] * a.scale;
+            s_post[v][t] = fmaf(dh, fh, s_post[v][t]);
+            s_gate[v][t] = fmaf(dd, fh * w_post[v][t], s_gate[v][t]);
+            const float aw = dh * w_post[v][t];
+            y[i][v][t] = aw;
+            f[i][v][t] = fh;
+            c[2 * i] = fmaf(aw, fh, c[2 * i]);
+            if constexpr (LAYER) c[2 * i + 1] += t < n[v] ? aw : 0.0f;
+          }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+          const int e = (v * TPR + lane) * kE;
+          if (live[i] && n[v] > 0)
+            store_some<kE>(reinterpret_cast<ST*>(a.x_out) + (at + (done + i) * step) * a.d + e, n[v], d[i][v]);
+        }
+      }
+      if (a.f) {
+        sum_row<TPR>(c, now);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int v = 0; v < NV; ++v) {
+            const int e = (v * TPR + lane) * kE;
+#pragma unroll
+            for (int t = 0; t < kE; ++t)
+              y[i][v][t] = rf[i] * fmaf(-f[i][v][t], c[2 * i] * a.inv_d, LAYER ? y[i][v][t] - c[2 * i + 1] * a.inv_d : y[i][v][t]);
+            if (live[i] && n[v] > 0)
+              store_some<kE>(reinterpret_cast<BT*>(a.df) + (at + (done + i) * step) * a.d + e, n[v], y[i][v]);
+          }
+      }
+      // The next rows' first exchange goes where the one before the last was:
+      // everyone has read it once all have met at the last one's barrier.
+      if (TPR > 64 && !a.f) __syncthreads();
+    }
+    if (a.whole_gates) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        if (mine && n[v] > 0) {
+          float o[kE];
+#pragma unroll
+          for (int t = 0; t < kE; ++t) o[t] = s_gate[v][t] * a.scale;
+          store_some<kE>(a.d_gate + my_gate * a.d + (v * TPR + lane) * kE, n[v], o);
+        }
+#pragma unroll
+        for (int t = 0; t < kE; ++t) s_gate[v][t] = 0.0f;
+      }
+    }
+  }
+  // join the row groups, in order, and write the workgroup's sums
+  auto write = [&](float (&s)[NV][kE], float* out, float factor) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if constexpr (kGroups > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kE; ++t) joined[t * kThreads + threadIdx.x] = s[v][t];
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+          for (int t = 0; t < kE; ++t)
+#pragma unroll
+            for (int g = 1; g < kGroups; ++g) s[v][t] += joined[t * kThreads + g * TPR + lane];
+        }
+      }
+      if (group == 0 && n[v] > 0) {
+        float o[kE];
+#pragma unroll
+        for (int t = 0; t < kE; ++t) o[t] = s[v][t] * factor;
+        store_some<kE>(out + (v * TPR + lane) * kE, n[v], o);
+      }
+    }
+  };
+  const int64_t plane = (int64_t)gridDim.x * a.d;
+  if (a.w_pre) write(s_pre, a.partial + block * a.d, 1.0f);
+  if (a.f) write(s_post, a.partial + plane + block * a.d, 1.0f);
+  if (a.gate && !a.whole_gates) write(s_gate, a.partial + 2 * plane + block * a.d, a.scale);
+}
+
+// Sums of the workgroups' partial rows: job 0 and 1 of all of them (w_pre,
+// w_post), job 2 + j of those of gate j.  32 columns x 32 rows at once.
+constexpr int kCols = 32;
+__global__ __launch_bounds__(kCols * 32) void k_peri_columns(Args a, int64_t blocks) {
+  __shared__ float part[32][kCols + 1];
+  const int col = threadIdx.x % kCols, lane = threadIdx.x / kCols;
+  const int64_t c = (int64_t)blockIdx.x * kCols + col;
+  const int64_t job = blockIdx.y;
+  float* out = job == 0 ? a.d_w_pre : job == 1 ? a.d_w_post : a.d_gate + (job - 2) * a.d;
+  if ((job == 0 && !a.w_pre) || (job == 1 && !a.f)) return;
+  const int64_t from = job < 2 ? 0 : (job - 2) * a.parts, count = job < 2 ? blocks : a.parts;
+  const float* in = a.partial + ((job < 2 ? job : 2) * blocks + from) * a.d;
+  float s = 0.0f;
+  if (c < a.d) {
+#pragma unroll 8
+    for (int64_t r = lane; r < count; r += 32) s += in[r * a.d + c];
+  }
+  part[lane][col] = s;
+  __syncthreads();
+  if (lane == 0 && c < a.d) {
+    s = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 32; ++r) s += part[r][col];
+    out[c] = s;
+  }
+}
+
+// --------------------------------------------------------------------- host
+
+int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
+bool is_type(int32_t dt) { return dt == MTDAO_F32 || dt == MTDAO_BF16; }
+int64_t gates_of(const mtdao_peri_norm_args& a) {
+  return a.gate ? (a.rows + a.rows_per_gate - 1) / a.rows_per_gate : 0;
+}
+
+int32_t validate_sizes(const mtdao_peri_norm_args* p, std::string* e) {
+  if (!p) return fail(e, MTDAO_ERR_INVALID_ARG, "args is NULL");
+  const mtdao_peri_norm_args& a = *p;
+  if (a.rows < 0) return fail(e, MTDAO_ERR_INVALID_ARG, "rows < 0");
+  if (a.d < 1 || a.d > MTDAO_PERI_MAX_D)
+    return fail(e, MTDAO_ERR_INVALID_ARG, "d %lld outside [1, %d]", (long long)a.d, MTDAO_PERI_MAX_D);
+  if (a.rows > (INT64_C(1) << 40) / a.d) return fail(e, MTDAO_ERR_INVALID_ARG, "rows * d exceeds 2^40");
+  if (a.kind != MTDAO_NORM_RMS && a.kind != MTDAO_NORM_LAYER)
+    return fail(e, MTDAO_ERR_INVALID_ARG, "kind %d is not RMS(0) or LAYER(1)", a.kind);
+  if (!is_type(a.stream_dtype) || !is_type(a.branch_dtype) || !is_type(a.weight_dtype))
+    return fail(e, MTDAO_ERR_INVALID_ARG, "stream_dtype, branch_dtype, weight_dtype must be F32(0) or BF16(1)");
+  if (a.stream_dtype == MTDAO_BF16 && a.branch_dtype == MTDAO_F32)
+    return fail(e, MTDAO_ERR_INVALID_ARG, "an fp32 branch needs an fp32 stream");
+  if (!(a.eps >= 0.0f) || !std::isfinite(a.eps)) return fail(e, MTDAO_ERR_INVALID_ARG, "eps=%g must be finite and >= 0", a.eps);
+  if (!std::isfinite(a.scale)) return fail(e, MTDAO_ERR_INVALID_ARG, "scale is not finite");
+  if (a.gate && !a.f) return fail(e, MTDAO_ERR_INVALID_ARG, "a gate needs f");
+  if (a.gate && a.rows_per_gate < 1) return fail(e, MTDAO_ERR_INVALID_ARG, "rows_per_gate < 1");
+  if (!a.f && !a.w_pre) return fail(e, MTDAO_ERR_INVALID_ARG, "neither f nor w_pre is given");
+  return MTDAO_OK;
+}
+
+int32_t check_pointer(const void* p, int64_t align, const char* name, std::string* e) {
+  if (!p) return fail(e, MTDAO_ERR_INVALID_ARG, "%s is NULL", name);
+  if (!aligned_to(p, (uintptr_t)align)) return fail(e, MTDAO_ERR_ALIGN, "%s is not aligned to its element", name);
+  return MTDAO_OK;
+}
+
+// An input of [rows][d] with row stride ld.
+int32_t check_rows(const mtdao_peri_norm_args& a, const void* p, int64_t ld, int32_t dt, const char* name, std::string* e) {
+  if (ld < a.d || ld > (INT64_C(1) << 40) / (a.rows < 1 ? 1 : a.rows))
+    return fail(e, MTDAO_ERR_INVALID_ARG, "row stride %lld of %s is below d or exceeds 2^40 elements in all", (long long)ld, name);
+  return check_pointer(p, esize(dt), name, e);
+}
+
+// The written [rows][d] buffer `out` against an input; the same rows in
+// place are fine (`same`).
+int32_t check_apart(const mtdao_peri_norm_args& a, const void* out, int32_t out_dt, const void* in, int64_t ld, int32_t dt,
+                    bool same, const char* name, std::string* e) {
+  if (!in || !out) return MTDAO_OK;
+  if (same && out == in && ld == a.d && out_dt == dt) return MTDAO_OK;
+  if (overlap(out, a.rows * a.d * esize(out_dt), in, ((a.rows - 1) * ld + a.d) * esize(dt)))
+    return fail(e, MTDAO_ERR_INVALID_ARG, "an output overlaps %s", name);
+  return MTDAO_OK;
+}
+
+int32_t check_weights(const mtdao_peri_norm_args& a, std::string* e) {
+  int32_t r = MTDAO_OK;
+  if (a.f) r = check_pointer(a.w_post, esize(a.weight_dtype), "w_post", e);
+  if (r == MTDAO_OK && a.w_pre) r = check_pointer(a.w_pre, esize(a.weight_dtype), "w_pre", e);
+  if (r == MTDAO_OK && a.gate) r = check_pointer(a.gate, esize(a.weight_dtype), "gate", e);
+  return r;
+}
+
+Args device_args(const mtdao_peri_norm_args& a) {
+  Args k = {};
+  k.rows = a.rows;
+  k.rows_per_gate = a.gate ? a.rows_per_gate : 1;
+  k.ld_x = a.ld_x;
+  k.ld_f = a.ld_f;
+  k.ld_d_out = a.ld_d_out;
+  k.ld_dn = a.ld_dn;
+  k.x = a.x;
+  k.f = a.f;
+  k.w_post = a.w_post;
+  k.w_pre = a.w_pre;
+  k.gate = a.gate;
+  k.d_out = a.d_out;
+  k.dn = a.dn;
+  k.x_out = a.x_out;
+  k.n_out = a.n_out;
+  k.df = a.df;
+  k.d_w_post = a.d_w_post;
+  k.d_w_pre = a.d_w_pre;
+  k.d_gate = a.d_gate;
+  k.d = (int32_t)a.d;
+  k.weight_bf16 = a.weight_dtype == MTDAO_BF16;
+  k.eps = a.eps;
+  k.scale = a.scale;
+  k.inv_d = 1.0f / (float)a.d;
+  return k;
+}
+
+template <int V>
+using Int = std::integral_constant<int, V>;
+
+// f(stream type, branch type, layer)
+template <typename F>
+void with_types(const mtdao_peri_norm_args& a, F&& f) {
+  auto kind = [&](auto s, auto b) {
+    if (a.kind == MTDAO_NORM_LAYER) f(s, b, std::true_type{});
+    else f(s, b, std::false_type{});
+  };
+  if (a.stream_dtype == MTDAO_BF16) kind(bf16_t{}, bf16_t{});
+  else if (a.branch_dtype == MTDAO_BF16) kind(float{}, bf16_t{});
+  else kind(float{}, float{});
+}
+
+// Threads of a row, backward: one vector a thread up to D = 4096, which leaves
+// registers for two rows in flight and the sums of the thread's columns.
+int backward_threads(int64_t d) { return d <= 64 * kE ? 64 : d <= 128 * kE ? 128 : d <= 256 * kE ? 256 : 512; }
+
+// How the rows go over the workgroups, backward: at most kBlocks of them, at
+// least eight rows each, none across gates unless it has them whole.
+constexpr int64_t kBlocks = 512;
+struct Plan {
+  int64_t blocks, per_block, parts;
+  bool whole_gates;
+};
+Plan backward_plan(const mtdao_peri_norm_args& a) {
+  Plan p;
+  const int64_t rows = std::max<int64_t>(8, (a.rows + kBlocks - 1) / kBlocks);
+  const int64_t gates = gates_of(a);
+  if (gates > 1 && a.rows_per_gate <= rows / 2) {
+    p.per_block = rows / a.rows_per_gate;
+    p.parts = 1;
+    p.blocks = (gates + p.per_block - 1) / p.per_block;
+    p.whole_gates = true;
+  } else {
+    const int64_t each = gates > 1 ? a.rows_per_gate : a.rows;
+    p.parts = (each + rows - 1) / rows;
+    p.per_block = (each + p.parts - 1) / p.parts;
+    p.parts = (each + p.per_block - 1) / p.per_block;
+    p.blocks = p.parts * std::max<int64_t>(1, gates);
+    p.whole_gates = false;
+  }
+  return p;
+}
+
+size_t backward_bytes(const mtdao_peri_norm_args& a) {
+  return a.rows == 0 ? 0 : (size_t)3 * (size_t)backward_plan(a).blocks * (size_t)a.d * sizeof(float);
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t mtdao_peri_norm(const mtdao_peri_norm_args* args, void* hip_stream) {
+  std::string* e = &g_err;
+  int32_t r = validate_sizes(args, e);
+  if (r != MTDAO_OK) return r;
+  const mtdao_peri_norm_args& a = *args;
+  if (a.rows == 0) return MTDAO_OK;
+  r = check_weights(a, e);
+  if (r == MTDAO_OK) r = check_rows(a, a.x, a.ld_x, a.stream_dtype, "x", e);
+  if (r == MTDAO_OK && a.f) r = check_rows(a, a.f, a.ld_f, a.branch_dtype, "f", e);
+  if (r == MTDAO_OK && a.f) r = check_pointer(a.x_out, esize(a.stream_dtype), "x_out", e);
+  if (r == MTDAO_OK && a.w_pre) r = check_pointer(a.n_out, esize(a.branch_dtype), "n_out", e);
+  if (r != MTDAO_OK) return r;
+  if (a.f) {
+    r = check_apart(a, a.x_out, a.stream_dtype, a.x, a.ld_x, a.stream_dtype, true, "x", e);
+    if (r == MTDAO_OK) r = check_apart(a, a.x_out, a.stream_dtype, a.f, a.ld_f, a.branch_dtype, true, "f", e);
+    if (r == MTDAO_OK && a.w_pre)
+      r = check_apart(a, a.x_out, a.stream_dtype, a.n_out, a.d, a.branch_dtype, false, "n_out", e);
+    if (r != MTDAO_OK) return r;
+  }
+  if (a.w_pre) {
+    r = check_apart(a, a.n_out, a.branch_dtype, a.x, a.ld_x, a.stream_dtype, true, "x", e);
+    if (r == MTDAO_OK) r = check_apart(a, a.n_out, a.branch_dtype, a.f, a.ld_f, a.branch_dtype, true, "f", e);
+    if (r != MTDAO_OK) return r;
+  }
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  RoctxRange range("mtdao_peri_norm rows=%lld d=%lld", (long long)a.rows, (long long)a.d);
+  const Args k = device_args(a);
+  // a wave per row up to D = 2048, else four
+  const int64_t per = a.d <= 2048 ? kGroup / 64 : 1;
+  const int64_t blocks = (a.rows + per - 1) / per;
+  if (blocks > 0x7fffffff) return fail(e, MTDAO_ERR_INVALID_ARG, "rows exceed the largest launch");
+  with_types(a, [&](auto s, auto b, auto layer) {
+    using ST = decltype(s);
+    using BT = decltype(b);
+    constexpr bool L = decltype(layer)::value;
+    auto go = [&](auto tpr, auto nv) {
+      constexpr int T = decltype(tpr)::value;
+      hipLaunchKernelGGL((k_peri_norm<ST, BT, L, T, decltype(nv)::value>), dim3((unsigned)blocks),
+                         dim3(T > kGroup ? T : kGroup), 0, st, k);
+    };
+    if (a.d <= 512) go(Int<64>{}, Int<1>{});
+    else if (a.d <= 1024) go(Int<64>{}, Int<2>{});
+    else if (a.d <= 2048) go(Int<64>{}, Int<4>{});
+    else if (a.d <= 4096) go(Int<256>{}, Int<2>{});
+    else go(Int<256>{}, Int<4>{});
+  });
+  return hip_check(e, hipGetLastError(), "mtdao_peri_norm launch");
+}
+
+int32_t mtdao_peri_norm_backward_workspace_bytes(const mtdao_peri_norm_args* a, size_t* bytes) {
+  const int32_t r = validate_sizes(a, &g_err);
+  if (r != MTDAO_OK) return r;
+  if (!bytes) return fail(&g_err, MTDAO_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = backward_bytes(*a);
+  return MTDAO_OK;
+}
+
+int32_t mtdao_peri_norm_backward(const mtdao_peri_norm_args* args, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream) {
+  std::string* e = &g_err;
+  int32_t r = validate_sizes(args, e);
+  if (r != MTDAO_OK) return r;
+  const mtdao_peri_norm_args& a = *args;
+  r = check_weights(a, e);
+  if (r == MTDAO_OK && a.f) r = check_pointer(a.d_w_post, 4, "d_w_post", e);
+  if (r == MTDAO_OK && a.w_pre) r = check_pointer(a.d_w_pre, 4, "d_w_pre", e);
+  if (r == MTDAO_OK && a.gate) r = check_pointer(a.d_gate, 4, "d_gate", e);
+  if (r != MTDAO_OK) return r;
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  Args k = device_args(a);
+  const Plan plan = backward_plan(a);
+  const size_t need = backward_bytes(a);
+  if (a.rows > 0) {
+    if (a.w_pre) r = check_rows(a, a.x, a.ld_x, a.stream_dtype, "x", e);
+    if (r == MTDAO_OK && a.f) r = check_rows(a, a.f, a.ld_f, a.branch_dtype, "f", e);
+    if (r == MTDAO_OK && a.d_out) r = check_rows(a, a.d_out, a.ld_d_out, a.stream_dtype, "d_out", e);
+    if (r == MTDAO_OK && a.dn) r = check_rows(a, a.dn, a.ld_dn, a.branch_dtype, "dn", e);
+    if (r == MTDAO_OK) r = check_pointer(a.x_out, esize(a.stream_dtype), "x_out", e);
+    if (r == MTDAO_OK && a.f) r = check_pointer(a.df, esize(a.branch_dtype), "df", e);
+    if (r != MTDAO_OK) return r;
+    const void* outs[2] = {a.x_out, a.f ? a.df : nullptr};
+    const int32_t types[2] = {a.stream_dtype, a.branch_dtype};
+    for (int o = 0; o < 2 && r == MTDAO_OK; ++o) {
+      r = check_apart(a, outs[o], types[o], a.w_pre ? a.x : nullptr, a.ld_x, a.stream_dtype, true, "x", e);
+      if (r == MTDAO_OK) r = check_apart(a, outs[o], types[o], a.f, a.ld_f, a.branch_dtype, true, "f", e);
+      if (r == MTDAO_OK) r = check_apart(a, outs[o], types[o], a.d_out, a.ld_d_out, a.stream_dtype, true, "d_out", e);
+      if (r == MTDAO_OK) r = check_apart(a, outs[o], types[o], a.dn, a.ld_dn, a.branch_dtype, true, "dn", e);
+    }
+    if (r == MTDAO_OK) r = check_apart(a, a.x_out, a.stream_dtype, outs[1], a.d, a.branch_dtype, false, "df", e);
+    if (r != MTDAO_OK) return r;
+    if (!workspace || workspace_bytes < need)
+      return fail(e, MTDAO_ERR_WORKSPACE, "workspace of %zu bytes required, %zu given", need,
+                  workspace ? workspace_bytes : (size_t)0);
+    if (!aligned_to(workspace, 256)) return fail(e, MTDAO_ERR_ALIGN, "workspace is not 256-byte aligned");
+    if (plan.blocks > 0x7fffffff) return fail(e, MTDAO_ERR_INVALID_ARG, "rows exceed the largest launch");
+  }
+  k.partial = static_cast<float*>(workspace);
+  k.per_block = plan.per_block;
+  k.parts = plan.parts;
+  k.whole_gates = plan.whole_gates;
+  RoctxRange range("mtdao_peri_norm_backward rows=%lld d=%lld", (long long)a.rows, (long long)a.d);
+  if (a.rows > 0) {
+    with_types(a, [&](auto s, auto b, auto layer) {
+      using ST = decltype(s);
+      using BT = decltype(b);
+      constexpr bool L = decltype(layer)::value;
+      auto go = [&](auto tpr, auto nv, auto rows) {
+        constexpr int T = decltype(tpr)::value;
+        hipLaunchKernelGGL((k_peri_norm_backward<ST, BT, L, T, decltype(nv)::value, decltype(rows)::value>),
+                           dim3((unsigned)plan.blocks), dim3(T > kGroup ? T : kGroup), 0, st, k);
+      };
+      switch (backward_threads(a.d)) {
+        case 64: go(Int<64>{}, Int<1>{}, Int<2>{}); break;
+        case 128: go(Int<128>{}, Int<1>{}, Int<2>{}); break;
+        case 256: go(Int<256>{}, Int<1>{}, Int<2>{}); break;
+        default:
+          if (a.d <= 512 * kE) go(Int<512>{}, Int<1>{}, Int<2>{});
+          else go(Int<512>{}, Int<2>{}, Int<1>{});
+      }
+    });
+  }
+  const int64_t jobs = 2 + (plan.whole_gates || a.rows == 0 ? 0 : gates_of(a));
+  const int64_t blocks = a.rows > 0 ? plan.blocks : 0;  // no rows: sums of nothing
+  // (gates that are not whole hold over a 1024th of the rows each, so jobs fit a launch)
+  hipLaunchKernelGGL(k_peri_columns, dim3((unsigned)((a.d + kCols - 1) / kCols), (unsigned)jobs), dim3(kCols * 32), 0, st, k,
+                     blocks);
+  return hip_check(e, hipGetLastError(), "mtdao_peri_norm_backward launch");
+}
+
+}  // extern "C"

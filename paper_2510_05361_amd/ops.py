@@ -1,0 +1,387 @@
+"""Operators of a Peri-LN training step next to the optimizer, on torch
+tensors: AdamW over many tensors, the boundary of a Peri-LN block, linear
+layers in 8-bit floating point.
+
+As in ``optimizer.py``, torch only allocates device memory and supplies the
+current HIP stream; the work runs in the library's kernels through
+``mtdao_ops.py`` (include/mtdao_ops.h has the formulas).  Outputs and
+workspaces are allocated from torch's caching allocator on the current
+stream; inputs that belong to another stream are the caller's to order, as
+for any torch operation.  There is no CPU path.
+"""
+
+from __future__ import annotations
+
+from typing import Dict, List, Optional, Sequence, Tuple, Union
+
+import torch
+
+from . import mtdao as abi
+from . import mtdao_ops as c_ops
+
+_TYPES = {torch.float32: abi.MTDAO_F32, torch.bfloat16: abi.MTDAO_BF16}
+_KINDS = {"rms": c_ops.MTDAO_NORM_RMS, "layer": c_ops.MTDAO_NORM_LAYER}
+CODE, SCALE = torch.float8_e4m3fn, torch.float8_e8m0fnu
+BLOCK = c_ops.MTDAO_BLOCK8
+
+
+def _stream(t: torch.Tensor) -> int:
+    return torch.cuda.current_stream(t.device).cuda_stream
+
+
+def _type(t: torch.Tensor, what: str) -> int:
+    if t.dtype not in _TYPES:
+        raise TypeError(f"{what} must be float32 or bfloat16, not {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _on_device(*named) -> torch.device:
+    """The one HIP device of the given (name, tensor) pairs; None is skipped."""
+    device = None
+    for name, t in named:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name} is on {t.device}: the operators run on the GPU only")
+        if device is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the others on {device}")
+        device = t.device
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {device}, the current device is {torch.cuda.current_device()}")
+    return device
+
+
+# ------------------------------------------------------------------- AdamW
+
+
+class AdamW:
+    """AdamW over a list of tensors, one launch for all of them (three with
+    clipping); states in 32 or 8 bits (``state_bits``).
+
+    ``params`` and ``grads`` are lists of contiguous tensors, each list of one
+    type (float32 or bfloat16); the gradients are read from these tensors at
+    every step until ``set_grads`` names others.  ``weight_decay`` is one
+    value or one per tensor; ``max_norm`` > 0 clips by the global norm.
+    ``states`` takes states to go on from (lists "m", "v", with 8 bits also
+    "m_scale", "v_scale", as in the attributes of the same names), zeros
+    otherwise.  8-bit states are e4m3 codes with an e8m0 scale per 128
+    elements; v holds sqrt(v).
+    """
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], *,
+                 betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
+                 weight_decay: Union[float, Sequence[float]] = 0.0, max_norm: float = 0.0, state_bits: int = 32,
+                 start_step: int = 0, states: Optional[Dict[str, List[torch.Tensor]]] = None):
+        self.handle = None
+        self.params = list(params)
+        n = len(self.params)
+        if n == 0:
+            raise ValueError("no parameters")
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [float(weight_decay)] * n
+        if len(decay) != n:
+            raise ValueError(f"{len(decay)} values of weight_decay for {n} tensors")
+        device = _on_device(*((f"params[{i}]", p) for i, p in enumerate(self.params)))
+        for i, p in enumerate(self.params):
+            if p.dtype != self.params[0].dtype or not p.is_contiguous():
+                raise ValueError(f"params[{i}]: parameters are contiguous and of one type")
+        self._grads_ok(grads, torch.float32 if len(grads) == 0 else grads[0].dtype)
+        self.grads = list(grads)
+        eight = state_bits == 8
+        kinds = {"m": CODE if eight else torch.float32, "v": CODE if eight else torch.float32}
+        if eight:
+            kinds.update(m_scale=SCALE, v_scale=SCALE)
+        for name, dtype in kinds.items():
+            sizes = [-(-p.numel() // BLOCK) if name.endswith("scale") else p.numel() for p in self.params]
+            if states is None:
+                made = [torch.zeros(s, dtype=torch.uint8 if eight else dtype, device=device).view(dtype) for s in sizes]
+            else:
+                made = list(states[name])
+                _on_device((name, self.params[0]), *((f"{name}[{i}]", t) for i, t in enumerate(made)))
+                if len(made) != n or any(t.dtype != dtype or t.numel() != s or not t.is_contiguous()
+                                         for t, s in zip(made, sizes)):
+                    raise ValueError(f"states['{name}']: {n} contiguous tensors of {dtype}, as large as their parameters "
+                                     "(scales: one per 128 elements)")
+            setattr(self, name, made)
+        if not eight:
+            self.m_scale = self.v_scale = None
+        rows = (c_ops.AdamwTensor * n)()
+        for i, r in enumerate(rows):
+            r.p, r.g, r.m, r.v = (t[i].data_ptr() for t in (self.params, self.grads, self.m, self.v))
+            if eight:
+                r.m_scale, r.v_scale = self.m_scale[i].data_ptr(), self.v_scale[i].data_ptr()
+            r.numel, r.weight_decay = self.params[i].numel(), decay[i]
+        cfg = c_ops.AdamwConfig(_type(self.params[0], "params"), _type(self.grads[0], "grads"), state_bits, n, betas[0],
+                                betas[1], eps, max_norm, start_step)
+        need = c_ops.mtdao_adamw_workspace_bytes(cfg, rows)
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        self.handle = c_ops.mtdao_adamw_init(cfg, rows, self.workspace.data_ptr(), need, _stream(self.workspace))
+
+    def _grads_ok(self, grads, dtype) -> None:
+        if len(grads) != len(self.params):
+            raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
+        _on_device(("params", self.params[0]), *((f"grads[{i}]", g) for i, g in enumerate(grads)))
+        for i, (p, g) in enumerate(zip(self.params, grads)):
+            if g.dtype != dtype or g.numel() != p.numel() or not g.is_contiguous():
+                raise ValueError(f"grads[{i}]: gradients are contiguous, of one type and as large as their parameters")
+
+    def set_grads(self, grads: Sequence[torch.Tensor]) -> None:
+        """Take the gradients from these tensors from here on."""
+        self._grads_ok(grads, self.grads[0].dtype)
+        c_ops.mtdao_adamw_set_grads(self.handle, [g.data_ptr() for g in grads], _stream(self.workspace))
+        self.grads = list(grads)
+
+    def step(self, lr: float) -> None:
+        c_ops.mtdao_adamw_step(self.handle, lr, torch.cuda.current_stream().cuda_stream)
+
+    @property
+    def step_count(self) -> int:
+        return c_ops.mtdao_adamw_step_count(self.handle)
+
+    def close(self) -> None:
+        if self.handle:
+            c_ops.mtdao_adamw_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# -------------------------------------------------------- Peri-LN boundary
+
+
+def _rows(t: Optional[torch.Tensor], shape, what: str) -> Tuple[Optional[torch.Tensor], int]:
+    """t as [rows, d] with contiguous rows, and its row stride."""
+    if t is None:
+        return None, shape[-1]
+    if t.shape != shape:
+        raise ValueError(f"{what} is {tuple(t.shape)}, not {tuple(shape)}")
+    t = t.reshape(-1, shape[-1])
+    if t.stride(1) != 1 and t.shape[1] > 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        t = t.contiguous()
+    return t, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _peri_args(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch):
+    if kind not in _KINDS:
+        raise ValueError(f"kind {kind!r} is not 'rms' or 'layer'")
+    if (f is None) != (w_post is None):
+        raise ValueError("f and w_post come together")
+    weights = [w for w in (w_post, w_pre, gate) if w is not None]
+    if not weights:
+        raise ValueError("neither f nor w_pre is given")
+    d = x.shape[-1]
+    a = c_ops.PeriNormArgs()
+    a.rows, a.d, a.kind = (x.numel() // d if d else 0), d, _KINDS[kind]
+    a.stream_dtype, a.branch_dtype, a.weight_dtype = _type(x, "x"), _TYPES[branch], _type(weights[0], "weights")
+    a.eps, a.scale = eps, scale
+    for name, w in (("w_post", w_post), ("w_pre", w_pre), ("gate", gate)):
+        if w is None:
+            continue
+        if w.dtype != weights[0].dtype or not w.is_contiguous():
+            raise ValueError(f"{name}: w_post, w_pre and gate are contiguous and of one type")
+        if name != "gate" and w.numel() != d:
+            raise ValueError(f"{name} has {w.numel()} elements, rows have {d}")
+    if gate is not None:
+        a.rows_per_gate = rows_per_gate if rows_per_gate > 0 else max(1, a.rows)
+        if gate.numel() != max(1, -(-a.rows // a.rows_per_gate)) * d:
+            raise ValueError(f"gate is {tuple(gate.shape)}: one row of {d} per {a.rows_per_gate} rows of {a.rows}")
+    a.w_post, a.w_pre, a.gate = _ptr(w_post), _ptr(w_pre), _ptr(gate)
+    return a
+
+
+def peri_norm(x: torch.Tensor, f: Optional[torch.Tensor], w_post: Optional[torch.Tensor],
+              w_pre: Optional[torch.Tensor], *, gate: Optional[torch.Tensor] = None, rows_per_gate: int = 0,
+              scale: float = 1.0, eps: float = 1e-5, kind: str = "rms",
+              branch_dtype: Optional[torch.dtype] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """x' = x + scale gate norm(f) w_post and n = norm(x') w_pre over the last
+    axis; returns (x', n).
+
+    ``f`` None: x' is x (the first norm of a model).  ``w_pre`` None: n is
+    None.  ``gate`` has one row of D per ``rows_per_gate`` rows of x (0: one
+    row for all).  n has f's type (``branch_dtype``, x's by default, without
+    f)."""
+    _on_device(("x", x), ("f", f), ("w_post", w_post), ("w_pre", w_pre), ("gate", gate))
+    branch = f.dtype if f is not None else branch_dtype or x.dtype
+    if branch not in _TYPES:
+        raise TypeError(f"f must be float32 or bfloat16, not {branch}")
+    a = _peri_args(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch)
+    x2, a.ld_x = _rows(x, x.shape, "x")
+    f2, a.ld_f = _rows(f, x.shape, "f")
+    a.x, a.f = _ptr(x2), _ptr(f2)
+    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if f is not None else x
+    n = torch.empty(x.shape, dtype=branch, device=x.device) if w_pre is not None else None
+    a.x_out, a.n_out = (_ptr(out) if f is not None else None), _ptr(n)
+    if a.rows:
+        c_ops.mtdao_peri_norm(a, _stream(x))
+    return out, n
+
+
+def peri_norm_backward(d_out: Optional[torch.Tensor], dn: Optional[torch.Tensor], x_out: torch.Tensor,
+                       f: Optional[torch.Tensor], w_post: Optional[torch.Tensor], w_pre: Optional[torch.Tensor], *,
+                       gate: Optional[torch.Tensor] = None, rows_per_gate: int = 0, scale: float = 1.0,
+                       eps: float = 1e-5, kind: str = "rms"):
+    """Gradients of ``peri_norm`` from those of its outputs (either may be
+    None: zero), its output x' and its input f: (dx, df, d_w_post, d_w_pre,
+    d_gate), those of weights in float32, None for what was not given."""
+    _on_device(("x_out", x_out), ("f", f), ("w_post", w_post), ("w_pre", w_pre), ("gate", gate), ("d_out", d_out), ("dn", dn))
+    branch = f.dtype if f is not None else dn.dtype if dn is not None else x_out.dtype
+    if branch not in _TYPES:
+        raise TypeError(f"f must be float32 or bfloat16, not {branch}")
+    if d_out is not None and d_out.dtype != x_out.dtype or dn is not None and dn.dtype != branch:
+        raise TypeError("d_out has the type of x_out, dn that of f")
+    a = _peri_args(x_out, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch)
+    d = x_out.shape[-1]
+    x2, a.ld_x = _rows(x_out, x_out.shape, "x_out")
+    f2, a.ld_f = _rows(f, x_out.shape, "f")
+    d2, a.ld_d_out = _rows(d_out, x_out.shape, "d_out")
+    y2, a.ld_dn = _rows(dn, x_out.shape, "dn")
+    a.x, a.f, a.d_out, a.dn = _ptr(x2), _ptr(f2), _ptr(d2), _ptr(y2)
+    dev = x_out.device
+    dx = torch.empty(x_out.shape, dtype=x_out.dtype, device=dev)
+    df = torch.empty(x_out.shape, dtype=branch, device=dev) if f is not None else None
+    dw_post = torch.empty(d, dtype=torch.float32, device=dev) if f is not None else None
+    dw_pre = torch.empty(d, dtype=torch.float32, device=dev) if w_pre is not None else None
+    dgate = torch.empty(gate.shape, dtype=torch.float32, device=dev) if gate is not None else None
+    if a.rows == 0:
+        for t in (dw_post, dw_pre, dgate):
+            if t is not None:
+                t.zero_()
+        return dx, df, dw_post, dw_pre, dgate
+    a.x_out, a.df, a.d_w_post, a.d_w_pre, a.d_gate = (_ptr(t) for t in (dx, df, dw_post, dw_pre, dgate))
+    need = c_ops.mtdao_peri_norm_backward_workspace_bytes(a)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    c_ops.mtdao_peri_norm_backward(a, ws.data_ptr(), need, _stream(x_out))
+    return dx, df, dw_post, dw_pre, dgate
+
+
+# ------------------------------------------------------------ 8-bit blocks
+
+
+class Matrix8:
+    """A [rows, cols] matrix of 8-bit blocks: ``codes`` (e4m3, [rows, cols up
+    to a multiple of 128]) and ``scales`` (e8m0, one row per ``scale_rows``
+    rows, one column per 128 columns up to a multiple of 4)."""
+
+    def __init__(self, rows: int, cols: int, device, scale_rows: int = 1):
+        self.rows, self.cols, self.scale_rows = rows, cols, scale_rows
+        ld = -(-cols // BLOCK) * BLOCK
+        scale_ld = -(-(ld // BLOCK) // 4) * 4
+        srows = -(-rows // scale_rows)
+        buf = torch.empty(rows * ld + srows * scale_ld, dtype=torch.uint8, device=device)
+        self._buf = buf
+        self.args = c_ops.Matrix8(buf.data_ptr(), buf.data_ptr() + rows * ld, rows, cols, ld, scale_ld, scale_rows)
+
+    @property
+    def codes(self) -> torch.Tensor:
+        a = self.args
+        return self._buf[:a.rows * a.ld].view(CODE).view(a.rows, a.ld)
+
+    @property
+    def scales(self) -> torch.Tensor:
+        a = self.args
+        return self._buf[a.rows * a.ld:].view(SCALE).view(-1, a.scale_ld)
+
+    def dequantize(self) -> torch.Tensor:
+        """The values as float32 [rows, cols]."""
+        a = self.args
+        s = self.scales.float()[:, :a.ld // BLOCK]
+        if self.scale_rows > 1:
+            s = s.repeat_interleave(self.scale_rows, 0)[:self.rows]
+        return (self.codes.float().view(self.rows, -1, BLOCK) * s[:, :, None]).view(self.rows, a.ld)[:, :self.cols]
+
+
+def _matrix(x: torch.Tensor) -> torch.Tensor:
+    if x.dim() != 2:
+        raise ValueError(f"a matrix is wanted, not {tuple(x.shape)}")
+    if x.stride(1) != 1 and x.shape[1] > 1 or x.shape[0] > 1 and x.stride(0) < x.shape[1]:
+        x = x.contiguous()
+    return x
+
+
+def _ld(x: torch.Tensor) -> int:
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _quantize(x: torch.Tensor, q: Optional[Matrix8], qt: Optional[Matrix8]) -> None:
+    c_ops.mtdao_quantize8(x.data_ptr(), _type(x, "x"), _ld(x), q.args if q is not None else None,
+                          qt.args if qt is not None else None, _stream(x))
+
+
+def quantize8(x: torch.Tensor, *, rows: bool = True, transposed: bool = False):
+    """x [r, c] as 8-bit blocks of 1 x 128: along its rows (``rows``), and/or
+    transposed, along its columns (``transposed``).  Returns the one asked
+    for, or both in one pass over x."""
+    _on_device(("x", x))
+    x = _matrix(x)
+    q = Matrix8(x.shape[0], x.shape[1], x.device) if rows else None
+    qt = Matrix8(x.shape[1], x.shape[0], x.device) if transposed else None
+    if q is None and qt is None:
+        raise ValueError("neither rows nor transposed is asked for")
+    _quantize(x, q, qt)
+    return (q, qt) if rows and transposed else q if rows else qt
+
+
+def product8(a: Matrix8, b: Matrix8, *, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
+             accumulate: bool = False) -> torch.Tensor:
+    """a b^T [a.rows, b.rows], summed in float32.  ``out``: written in place
+    of a new tensor (contiguous rows); ``accumulate``: added to (float32)."""
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty((a.rows, b.rows), dtype=dtype, device=a._buf.device)
+    elif tuple(out.shape) != (a.rows, b.rows) or out.shape[1] > 1 and out.stride(1) != 1:
+        raise ValueError(f"out is {tuple(out.shape)} with strides {out.stride()}, not [{a.rows}, {b.rows}] with contiguous rows")
+    _on_device(("a", a._buf), ("b", b._buf), ("out", out))
+    need = c_ops.mtdao_product8_workspace_bytes(a.rows, b.rows, a.cols)
+    ws = torch.empty(need, dtype=torch.uint8, device=out.device) if need else None
+    c_ops.mtdao_product8(a.args, b.args, out.data_ptr(), _type(out, "out"), _ld(out), accumulate, _ptr(ws), need,
+                         _stream(out))
+    return out
+
+
+class Weight8:
+    """The weight [out, in] of a linear layer in 8-bit blocks of 128 x 128,
+    with its transpose for the gradient of the input (the same values).
+    ``update`` takes the weight again after an optimizer step, in place."""
+
+    def __init__(self, w: torch.Tensor):
+        _on_device(("w", w))
+        w = _matrix(w)
+        self.q = Matrix8(w.shape[0], w.shape[1], w.device, BLOCK)
+        self.qt = Matrix8(w.shape[1], w.shape[0], w.device, BLOCK)
+        _quantize(w, self.q, self.qt)
+
+    def update(self, w: torch.Tensor) -> None:
+        _on_device(("w", w), ("weight", self.q._buf))
+        if tuple(w.shape) != (self.q.rows, self.q.cols):
+            raise ValueError(f"the weight is [{self.q.rows}, {self.q.cols}], not {tuple(w.shape)}")
+        _quantize(_matrix(w), self.q, self.qt)
+
+
+def linear8(x: torch.Tensor, w: Weight8, *, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """x W^T over the last axis of x, x in 8-bit blocks along it; in x's type
+    unless ``dtype`` is given."""
+    if x.shape[-1] != w.q.cols:
+        raise ValueError(f"x has {x.shape[-1]} columns, the weight {w.q.cols}")
+    q = quantize8(x.reshape(-1, x.shape[-1]))
+    return product8(q, w.q, dtype=dtype or x.dtype).view(*x.shape[:-1], w.q.rows)
+
+
+def linear8_backward(dy: torch.Tensor, x: torch.Tensor, w: Weight8, *, dw: Optional[torch.Tensor] = None,
+                     accumulate: bool = False) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(dx, dw) of ``linear8``: dx = dy W in dy's type, with dy in 8-bit
+    blocks along its rows; dw = dy^T x in float32, with dy and x in 8-bit
+    blocks along the tokens.  ``dw`` / ``accumulate``: as in product8."""
+    if x.shape[-1] != w.q.cols or dy.shape[-1] != w.q.rows or x.shape[:-1] != dy.shape[:-1]:
+        raise ValueError(f"dy is {tuple(dy.shape)}, x {tuple(x.shape)}, the weight [{w.q.rows}, {w.q.cols}]")
+    q, qt = quantize8(dy.reshape(-1, dy.shape[-1]), transposed=True)
+    xt = quantize8(x.reshape(-1, x.shape[-1]), rows=False, transposed=True)
+    dx = product8(q, w.qt, dtype=dy.dtype).view(x.shape)
+    return dx, product8(qt, xt, dtype=torch.float32, out=dw, accumulate=accumulate)
