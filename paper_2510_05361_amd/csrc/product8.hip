@@ -20,8 +20,8 @@ namespace {
 struct Mat {
   uint8_t* codes;
   uint8_t* scales;
-  int64_t rows, ld;
-  int32_t blocks, scale_ld;  // blocks of a row, and bytes from row to row of the scales
+  int64_t rows, ld, scale_rows;  // scale_rows: rows of scales
+  int32_t blocks, scale_ld;      // blocks of a row, and bytes from row to row of the scales
 };
 
 // --------------------------------------------------------------- quantizers
@@ -179,13 +179,12 @@ __global__ __launch_bounds__(kThreads) void k_quantize8_tile(const T* x, int64_t
 
 // ------------------------------------------------------------------ product
 //
-// Every matrix instruction takes 16 x 128 codes of each side and their
-// scales: a block of 128 is its whole contraction, and as the scales are
-// powers of two in the instruction's own format, sums stay in its
-// accumulators from the first block to the last.  Which 16-byte chunks of a
-// block a lane holds is free as long as both sides agree, since they share
-// one scale.  Rows of b go in as the instruction's rows, so that a lane ends
-// with four consecutive columns of a row of c.
+// Every matrix instruction takes 32 x 64 codes of each side, half a block, and
+// their scales: as these are powers of two in the instruction's own format,
+// sums stay in its accumulators from the first block to the last.  Which
+// 16-byte chunks of a block a lane holds is free as long as both sides agree,
+// since they share one scale.  Rows of b go in as the instruction's rows, so
+// that a lane ends with sixteen consecutive columns of a row of c.
 //
 // Within a group of products the 8-bit instructions drop what lies more than
 // 13 bits below the largest one (measured: 65536 + 4 gives 65536, in the
@@ -197,7 +196,7 @@ __global__ __launch_bounds__(kThreads) void k_quantize8_tile(const T* x, int64_t
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef int v4i __attribute__((ext_vector_type(4)));
-typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 
@@ -205,17 +204,28 @@ struct Product {
   Mat a, b;
   void* c;
   int64_t ldc;
-  int32_t a_scale_rows, b_scale_rows, accumulate;
+  int32_t a_scale_shift, b_scale_shift;  // rows of a scale: 1 << shift
+  int32_t accumulate, tiles_m, tiles_n, group;
 };
 
-// A 128-byte row of a tile in LDS: its eight 16-byte chunks, at the places
-// that eight consecutive rows need to be read from different banks.
-__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ (row & 7)) << 4); }
+// A 128-byte row of a tile in LDS: its eight 16-byte chunks, each at the place
+// that its number and the row's key give, so that the eight rows that a
+// quarter wave reads at once lie in different banks.  For a these are
+// consecutive rows; for b a lane group's rows are 16 apart (row_of_b).
+template <bool B>
+__device__ __forceinline__ int row_key(int row) { return B ? (row & 3) | ((row >> 2) & 4) : row & 7; }
 
-__device__ __forceinline__ v8i fragment(const uint8_t* tile, int row, int group) {
-  const v4i lo = *reinterpret_cast<const v4i*>(tile + chunk_at(row, group));
-  const v4i hi = *reinterpret_cast<const v4i*>(tile + chunk_at(row, group + 4));
-  return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ row_key<false>(row)) << 4); }
+
+// The row of b's fragment that the instruction's row r takes: results of a lane
+// are rows 8 q + 4 h + t, so these are sixteen consecutive columns of c.
+__device__ __forceinline__ int row_of_b(int r) { return ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3); }
+
+// Two chunks of a row, as the instruction's operand.  lo, hi: where the
+// lane's chunks of row lane % 16 of the tile are.
+__device__ __forceinline__ v8i fragment(const uint8_t* lo, const uint8_t* hi, int at) {
+  const v4i a = *reinterpret_cast<const v4i*>(lo + at), b = *reinterpret_cast<const v4i*>(hi + at);
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 // Eight codes (two of a fragment's words) times their scale, as bf16: exact
@@ -239,93 +249,380 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t* p, in
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)(bytes < most ? bytes : most), 0x00027000);
 }
 
-template <int BM, int BN, typename CT>
-__global__ __launch_bounds__(256) void k_product8(Product p) {
-  constexpr int kWM = BM / 2, kWN = BN / 2, kMI = kWM / 16, kNI = kWN / 16;
-  __shared__ __attribute__((aligned(1024))) uint8_t ta[BM * 128];
-  __shared__ __attribute__((aligned(1024))) uint8_t tb[BN * 128];
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int64_t row0 = (int64_t)blockIdx.y * BM, col0 = (int64_t)blockIdx.x * BN;
-  const auto ra = buffer_of(p.a.codes + row0 * p.a.ld, (p.a.rows - row0) * p.a.ld);
-  const auto rb = buffer_of(p.b.codes + col0 * p.b.ld, (p.b.rows - col0) * p.b.ld);
-  // a wave loads eight rows at once: lane l the chunk that belongs at place l % 8 of row l / 8
-  const int lr = lane / 8, lc = (lane % 8) ^ (lr & 7);
-  const int wm = wave / 2 * kWM, wn = wave % 2 * kWN, fr = lane % 16, fg = lane / 16;
-  const uint8_t *sa[kMI], *sb[kNI];
+// Every wave of the workgroup has come here; nothing is moved across.
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+// This wave's loads (global memory to registers or LDS; LDS to registers)
+// have arrived.
+__device__ __forceinline__ void loads_landed() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void reads_landed() { __builtin_amdgcn_s_waitcnt(0xc07f); }  // lgkmcnt(0)
+
+// Tile t of c's tiles in the order in which they are worked on: groups of
+// p.group tile rows, down the rows first, so that tiles in work at one time
+// share their rows of a and b in the L2.
+struct Place {
+  int64_t row0, col0;
+};
+template <int BM, int BN>
+__device__ __forceinline__ Place place_of(const Product& p, int t) {
+  const int group = t / (p.group * p.tiles_n), in_group = t - group * p.group * p.tiles_n;
+  const int rows_here = p.tiles_m - group * p.group < p.group ? p.tiles_m - group * p.group : p.group;
+  return {(int64_t)(group * p.group + in_group % rows_here) * BM, (int64_t)(in_group / rows_here) * BN};
+}
+
+// The fragments' products of half a block, into acc.
+template <int MI, int NI, bool WIDE>
+__device__ __forceinline__ void multiply(const v8i (&fa)[MI], const v8i (&fb)[NI], const uint32_t (&ea)[MI], const uint32_t (&eb)[NI],
+                                         v16f (&acc)[MI][NI]) {
+  if constexpr (!WIDE) {
 #pragma unroll
-  for (int i = 0; i < kMI; ++i) {
-    const int64_t r = row0 + wm + i * 16 + fr;
-    sa[i] = p.a.scales + (r < p.a.rows ? r : p.a.rows - 1) / p.a_scale_rows * p.a.scale_ld;
-  }
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-  for (int j = 0; j < kNI; ++j) {
-    const int64_t r = col0 + wn + j * 16 + fr;
-    sb[j] = p.b.scales + (r < p.b.rows ? r : p.b.rows - 1) / p.b_scale_rows * p.b.scale_ld;
-  }
-  v4f acc[kMI][kNI];
+      for (int j = 0; j < NI; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[i], acc[i][j], 0, 0, 0, eb[j], 0, ea[i]);
+  } else {
 #pragma unroll
-  for (int i = 0; i < kMI; ++i)
+    for (int k = 0; k < 4; ++k) {
+      v8bf wb[NI];
 #pragma unroll
-    for (int j = 0; j < kNI; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int kb = 0; kb < p.a.blocks; ++kb) {
-    for (int r = wave * 8; r < BM; r += 32)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (__attribute__((address_space(3))) void*)(ta + r * 128), 16,
-                                               (r + lr) * (int)p.a.ld + lc * 16, kb * 128, 0, 0);
-    for (int r = wave * 8; r < BN; r += 32)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (__attribute__((address_space(3))) void*)(tb + r * 128), 16,
-                                               (r + lr) * (int)p.b.ld + lc * 16, kb * 128, 0, 0);
-    __syncthreads();
-    v8i fb[kNI];
-    int eb[kNI];
+      for (int j = 0; j < NI; ++j) wb[j] = widened(fb[j], k, scale_of(eb[j] & 255u));
 #pragma unroll
-    for (int j = 0; j < kNI; ++j) {
-      fb[j] = fragment(tb, wn + j * 16 + fr, fg);
-      eb[j] = sb[j][kb];
+      for (int i = 0; i < MI; ++i) {
+        const v8bf wa = widened(fa[i], k, scale_of(ea[i] & 255u));
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j], wa, acc[i][j], 0, 0, 0);
+      }
     }
+  }
+  // (without a use here the instructions would be moved past the next barrier)
 #pragma unroll
-    for (int i = 0; i < kMI; ++i) {
-      const v8i fa = fragment(ta, wm + i * 16 + fr, fg);
-      const int ea = sa[i][kb];
-      if constexpr (sizeof(CT) == 2) {
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j) asm volatile("" : "+v"(acc[i][j]));
+}
+
+// A wave's 32 x 64 (bf16) or 32 x 32 (fp32) results to c, by way of 4 KiB of
+// LDS of its own: rows of 128 bytes, of which eight lanes then store one.
+template <typename CT>
+__device__ __forceinline__ void store_rows(const Product& p, uint8_t* own, const float* o, int64_t row0, int64_t col0, int lane) {
+  constexpr int kPer = 16 / (int)sizeof(CT), kChunks = sizeof(CT) == 2 ? 4 : 4;  // elements of a chunk; chunks a lane writes
+  const int fr = lane % 32, fg = lane / 32;
+#pragma unroll
+  for (int k = 0; k < kChunks; ++k) {
+    // chunks of the row: bf16 four of each fragment, two a lane; fp32 eight of one fragment, four a lane
+    const int chunk = sizeof(CT) == 2 ? (k >> 1) * 4 + fg * 2 + (k & 1) : fg * 4 + k;
+    float v[kPer];
+#pragma unroll
+    for (int t = 0; t < kPer; ++t) v[t] = o[k * kPer + t];
+    store_full<kPer>(reinterpret_cast<CT*>(own + chunk_at(fr, chunk)), v);
+  }
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int r = q * 8 + lane / 8, chunk = (lane % 8) ^ (r & 7);
+    float v[kPer];
+    load_full<kPer>(reinterpret_cast<const CT*>(own + r * 128 + (lane % 8) * 16), v);
+    const int64_t row = row0 + r, col = col0 + chunk * kPer, left = p.b.rows - col;
+    if (row < p.a.rows && left > 0) {
+      const int n = left > kPer ? kPer : (int)left;
+      CT* at = reinterpret_cast<CT*>(p.c) + row * p.ldc + col;
+      if (p.accumulate) {
+        float before[kPer];
+        load_some<kPer>(at, n, before);
+#pragma unroll
+        for (int t = 0; t < kPer; ++t) v[t] += before[t];
+      }
+      store_some<kPer>(at, n, v);
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Large products: tiles of 256 x 256 over eight waves of 128 x 64, one
+// workgroup per CU that goes from tile to tile.  LDS holds two blocks of each
+// side: the next one, of the next tile after a tile's last, is loaded,
+// straight into LDS, while this one is multiplied.  The two halves of the
+// waves take turns, four a block: one multiplies the half block that it has
+// read while the other reads; a SIMD holds a wave of each.
+constexpr int kBig = 256, kBigStage = 2 * kBig * 128, kBigLds = 2 * kBigStage + 8 * 4096;
+
+template <typename CT>
+__global__ __launch_bounds__(512, 1) void k_product8_big(Product p) {
+  constexpr int kMI = 4, kNI = 2, kLoads = kBig / 64;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int tiles = p.tiles_m * p.tiles_n, per = (tiles + 7) / 8, xcd = blockIdx.x % 8;
+  // this XCD's share of the tiles, and this workgroup's among them
+  const int first = xcd * per + blockIdx.x / 8, past = xcd * per + per < tiles ? xcd * per + per : tiles, stride = gridDim.x / 8;
+  if (first >= past) return;
+  const int blocks = p.a.blocks;
+
+  // A wave loads eight rows at once: lane l the chunk that belongs at place l
+  // % 8 of row l / 8.  Rows go into the lane's offset, which the hardware
+  // holds against the matrix's end; the block into the scalar offset.
+  const int lr = wave * 8 + lane / 8, lda = (int)p.a.ld, ldb = (int)p.b.ld;
+  int va = lr * lda + ((lane % 8) ^ row_key<false>(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key<true>(lr)) * 16;
+  int l_tile = first, l_kb = 0, l_stage = 0;  // what is loaded next
+  Place l_at = place_of<kBig, kBig>(p, l_tile);
+  auto load = [&]() {
+    const auto ra = buffer_of(p.a.codes + l_at.row0 * p.a.ld, (p.a.rows - l_at.row0) * p.a.ld);
+    const auto rb = buffer_of(p.b.codes + l_at.col0 * p.b.ld, (p.b.rows - l_at.col0) * p.b.ld);
+    uint8_t* to = lds + l_stage + wave * 1024;
+    asm("" : "+v"(va), "+v"(vb));  // (offsets of further rows are formed anew: they would each hold a register)
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (__attribute__((address_space(3))) void*)(to + k * 8192), 16, va + k * 64 * lda,
+                                               l_kb * 128, 0, 0);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (__attribute__((address_space(3))) void*)(to + kBig * 128 + k * 8192), 16,
+                                               vb + k * 64 * ldb, l_kb * 128, 0, 0);
+    l_stage ^= kBigStage;
+    // (past the last block of the last tile its first one is loaded, and not used)
+    if (++l_kb == blocks) {
+      l_kb = 0;
+      if (l_tile + stride < past) {
+        l_tile += stride;
+        l_at = place_of<kBig, kBig>(p, l_tile);
+      }
+    }
+  };
+
+  const int wm = wave / 4 * 128, wn = wave % 4 * 64, fr = lane % 32, fg = lane / 32;
+  // Four blocks' scales of each of the lane's rows at once, as the blocks
+  // before them end; rows past the end read zeros.
+  const int step_a = p.a_scale_shift ? 0 : p.a.scale_ld, step_b = p.b_scale_shift ? 0 : p.b.scale_ld;
+  int vsa = ((wm + fr) >> p.a_scale_shift) * p.a.scale_ld, vsb = ((wn + row_of_b(fr)) >> p.b_scale_shift) * p.b.scale_ld;
+  uint32_t ea[kMI], eb[kNI], next_a[kMI], next_b[kNI];
+  auto load_scales = [&](const Place& at, int kb) {
+    const int64_t r = at.row0 >> p.a_scale_shift, c = at.col0 >> p.b_scale_shift;
+    const auto rsa = buffer_of(p.a.scales + r * p.a.scale_ld, (p.a.scale_rows - r) * p.a.scale_ld);
+    const auto rsb = buffer_of(p.b.scales + c * p.b.scale_ld, (p.b.scale_rows - c) * p.b.scale_ld);
+    asm("" : "+v"(vsa), "+v"(vsb));
+#pragma unroll
+    for (int i = 0; i < kMI; ++i) next_a[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsa, vsa + i * 32 * step_a, kb, 0);
+#pragma unroll
+    for (int j = 0; j < kNI; ++j) next_b[j] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsb, vsb + j * 32 * step_b, kb, 0);
+  };
+  auto take_scales = [&]() {
+#pragma unroll
+    for (int i = 0; i < kMI; ++i) ea[i] = next_a[i];
+#pragma unroll
+    for (int j = 0; j < kNI; ++j) eb[j] = next_b[j];
+  };
+
+  // Where the lane's two chunks of its first row are; the block's other half
+  // is 64 bytes away, up or down as the row's key says.
+  const int key_a = row_key<false>(fr), key_b = row_key<true>(row_of_b(fr));
+  const int a0 = (wm + fr) * 128 + ((2 * fg ^ key_a) << 4), b0 = (kBig + wn + row_of_b(fr)) * 128 + ((2 * fg ^ key_b) << 4);
+
+  load();
+  load_scales(l_at, 0);  // (of the first tile also where it has one block alone: no other tile is begun before)
+  loads_landed();
+  take_scales();
+  meet();
+  // A stage is free for the block after next when both halves have read it,
+  // and has to be there when the first half reads it four turns later, so both
+  // load it in the same turn: the first half when it reads, the second, one
+  // turn behind, when it multiplies.
+  auto turns = [&](auto which) {
+    constexpr bool second = decltype(which)::value;
+    if (second) {
+      load();
+      meet();
+    }
+    int stage = 0;
+    for (int tile = first; tile < past; tile += stride) {
+      const Place at = place_of<kBig, kBig>(p, tile);
+      v16f acc[kMI][kNI];
+#pragma unroll
+      for (int i = 0; i < kMI; ++i)
 #pragma unroll
         for (int j = 0; j < kNI; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa, acc[i][j], 0, 0, 0, eb[j], 0, ea);
-      } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const v8bf wa = widened(fa, k, scale_of((uint32_t)ea));
+          for (int t = 0; t < 16; ++t) acc[i][j][t] = 0.0f;
+      for (int kb = 0; kb < blocks; ++kb) {
+        const bool renew = (kb & 3) == 3 || kb + 1 == blocks;
+        uint32_t sa[kMI], sb[kNI];
+#pragma unroll
+        for (int i = 0; i < kMI; ++i) sa[i] = ea[i] >> 8 * (kb & 3);
+#pragma unroll
+        for (int j = 0; j < kNI; ++j) sb[j] = eb[j] >> 8 * (kb & 3);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          if (half == 0) {
+            if (renew) {
+              if (kb + 1 < blocks) load_scales(at, kb + 1);
+              else load_scales(place_of<kBig, kBig>(p, tile + stride < past ? tile + stride : tile), 0);
+            }
+            if (!second) load();
+          }
+          v8i fa[kMI], fb[kNI];
 #pragma unroll
           for (int j = 0; j < kNI; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widened(fb[j], k, scale_of((uint32_t)eb[j])), wa, acc[i][j], 0, 0, 0);
+            fb[j] = fragment(lds + stage + (b0 ^ half * 64), lds + stage + (b0 ^ (half * 64 + 16)), j * 4096);
+#pragma unroll
+          for (int i = 0; i < kMI; ++i)
+            fa[i] = fragment(lds + stage + (a0 ^ half * 64), lds + stage + (a0 ^ (half * 64 + 16)), i * 4096);
+          reads_landed();
+          if (second && half == 1) loads_landed();
+          meet();
+          if (second && half == 1) load();
+          __builtin_amdgcn_s_setprio(1);
+          multiply<kMI, kNI, sizeof(CT) == 4>(fa, fb, sa, sb, acc);
+          __builtin_amdgcn_sched_barrier(0);
+          __builtin_amdgcn_s_setprio(0);
+          if (!second && half == 1) loads_landed();
+          meet();
+        }
+        if (renew) take_scales();
+        stage ^= kBigStage;
+      }
+      uint8_t* own = lds + 2 * kBigStage + wave * 4096;
+#pragma unroll
+      for (int i = 0; i < kMI; ++i) {
+        if constexpr (sizeof(CT) == 2) {
+          float o[32];
+#pragma unroll
+          for (int t = 0; t < 32; ++t) o[t] = acc[i][t / 16][t % 16];
+          store_rows<CT>(p, own, o, at.row0 + wm + i * 32, at.col0 + wn, lane);
+        } else {
+#pragma unroll
+          for (int j = 0; j < kNI; ++j) {
+            float o[16];
+#pragma unroll
+            for (int t = 0; t < 16; ++t) o[t] = acc[i][j][t];
+            store_rows<CT>(p, own, o, at.row0 + wm + i * 32, at.col0 + wn + j * 32, lane);
+          }
         }
       }
     }
-    __syncthreads();
+    if (!second) meet();
+    loads_landed();  // LDS is given back: nothing may still be on its way there
+  };
+  if (wave >= 4) turns(std::true_type{});
+  else turns(std::false_type{});
+}
+
+// Other products: tiles of 128 x 128 over four waves of 64 x 64, one tile a
+// workgroup, several workgroups a CU.
+constexpr int kMid = 128, kMidStage = 2 * kMid * 128, kMidLds = 2 * kMidStage;
+
+template <typename CT>
+__global__ __launch_bounds__(256, 2) void k_product8_mid(Product p) {
+  constexpr int kMI = 2, kNI = 2, kLoads = kMid / 32;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int tiles = p.tiles_m * p.tiles_n, per = (tiles + 7) / 8, tile = blockIdx.x % 8 * per + blockIdx.x / 8;
+  if (tile >= tiles) return;
+  const Place at = place_of<kMid, kMid>(p, tile);
+  const int blocks = p.a.blocks;
+  const int lr = wave * 8 + lane / 8, lda = (int)p.a.ld, ldb = (int)p.b.ld;
+  const int va = lr * lda + ((lane % 8) ^ row_key<false>(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key<true>(lr)) * 16;
+  const auto ra = buffer_of(p.a.codes + at.row0 * p.a.ld, (p.a.rows - at.row0) * p.a.ld);
+  const auto rb = buffer_of(p.b.codes + at.col0 * p.b.ld, (p.b.rows - at.col0) * p.b.ld);
+  auto load = [&](int kb) {
+    uint8_t* to = lds + (kb & 1) * kMidStage + wave * 1024;
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (__attribute__((address_space(3))) void*)(to + k * 4096), 16, va + k * 32 * lda,
+                                               kb * 128, 0, 0);
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (__attribute__((address_space(3))) void*)(to + kMid * 128 + k * 4096), 16,
+                                               vb + k * 32 * ldb, kb * 128, 0, 0);
+  };
+  const int wm = wave / 2 * 64, wn = wave % 2 * 64, fr = lane % 32, fg = lane / 32;
+  const int64_t sr = at.row0 >> p.a_scale_shift, sc = at.col0 >> p.b_scale_shift;
+  const auto rsa = buffer_of(p.a.scales + sr * p.a.scale_ld, (p.a.scale_rows - sr) * p.a.scale_ld);
+  const auto rsb = buffer_of(p.b.scales + sc * p.b.scale_ld, (p.b.scale_rows - sc) * p.b.scale_ld);
+  const int step_a = p.a_scale_shift ? 0 : p.a.scale_ld, step_b = p.b_scale_shift ? 0 : p.b.scale_ld;
+  const int vsa = ((wm + fr) >> p.a_scale_shift) * p.a.scale_ld, vsb = ((wn + row_of_b(fr)) >> p.b_scale_shift) * p.b.scale_ld;
+  uint32_t ea[kMI], eb[kNI], next_a[kMI], next_b[kNI];
+  auto load_scales = [&](int kb) {
+#pragma unroll
+    for (int i = 0; i < kMI; ++i) next_a[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsa, vsa + i * 32 * step_a, kb, 0);
+#pragma unroll
+    for (int j = 0; j < kNI; ++j) next_b[j] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsb, vsb + j * 32 * step_b, kb, 0);
+  };
+  const int key_a = row_key<false>(fr), key_b = row_key<true>(row_of_b(fr));
+  const int a0 = (wm + fr) * 128 + ((2 * fg ^ key_a) << 4), b0 = (kMid + wn + row_of_b(fr)) * 128 + ((2 * fg ^ key_b) << 4);
+  v16f acc[kMI][kNI];
+#pragma unroll
+  for (int i = 0; i < kMI; ++i)
+#pragma unroll
+    for (int j = 0; j < kNI; ++j)
+#pragma unroll
+      for (int t = 0; t < 16; ++t) acc[i][j][t] = 0.0f;
+  if (blocks > 0) {
+    load_scales(0);
+    load(0);
   }
-  CT* c = reinterpret_cast<CT*>(p.c);
+  for (int kb = 0; kb < blocks; ++kb) {
+    loads_landed();
+    meet();
+    if ((kb & 3) == 0) {
+#pragma unroll
+      for (int i = 0; i < kMI; ++i) ea[i] = next_a[i];
+#pragma unroll
+      for (int j = 0; j < kNI; ++j) eb[j] = next_b[j];
+    }
+    if (kb + 1 < blocks) {
+      if ((kb & 3) == 3) load_scales(kb + 1);
+      load(kb + 1);
+    }
+    const uint8_t* stage = lds + (kb & 1) * kMidStage;
+    uint32_t sa[kMI], sb[kNI];
+#pragma unroll
+    for (int i = 0; i < kMI; ++i) sa[i] = ea[i] >> 8 * (kb & 3);
+#pragma unroll
+    for (int j = 0; j < kNI; ++j) sb[j] = eb[j] >> 8 * (kb & 3);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      v8i fa[kMI], fb[kNI];
+#pragma unroll
+      for (int j = 0; j < kNI; ++j) fb[j] = fragment(stage + (b0 ^ half * 64), stage + (b0 ^ (half * 64 + 16)), j * 4096);
+#pragma unroll
+      for (int i = 0; i < kMI; ++i) fa[i] = fragment(stage + (a0 ^ half * 64), stage + (a0 ^ (half * 64 + 16)), i * 4096);
+      multiply<kMI, kNI, sizeof(CT) == 4>(fa, fb, sa, sb, acc);
+    }
+  }
+  meet();  // the stages become the waves' own
+  uint8_t* own = lds + wave * 4096;
 #pragma unroll
   for (int i = 0; i < kMI; ++i) {
-    const int64_t row = row0 + wm + i * 16 + fr;
-    if (row >= p.a.rows) continue;
+    if constexpr (sizeof(CT) == 2) {
+      float o[32];
 #pragma unroll
-    for (int j = 0; j < kNI; ++j) {
-      const int64_t col = col0 + wn + j * 16 + fg * 4, left = p.b.rows - col;
-      if (left <= 0) continue;
-      const int n = left > 4 ? 4 : (int)left;
-      CT* to = c + row * p.ldc + col;
-      float o[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-      if (p.accumulate) {
-        float before[4];
-        load_some<4>(to, n, before);
+      for (int t = 0; t < 32; ++t) o[t] = acc[i][t / 16][t % 16];
+      store_rows<CT>(p, own, o, at.row0 + wm + i * 32, at.col0 + wn, lane);
+    } else {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) o[t] += before[t];
+      for (int j = 0; j < kNI; ++j) {
+        float o[16];
+#pragma unroll
+        for (int t = 0; t < 16; ++t) o[t] = acc[i][j][t];
+        store_rows<CT>(p, own, o, at.row0 + wm + i * 32, at.col0 + wn + j * 32, lane);
       }
-      store_some<4>(to, n, o);
     }
   }
 }
 
 // --------------------------------------------------------------------- host
+
+template <int V>
+using Int = std::integral_constant<int, V>;
 
 int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
@@ -354,6 +651,7 @@ Mat mat_of(const mtdao_matrix8* q) {
   m.codes = q->codes;
   m.scales = q->scales;
   m.rows = q->rows;
+  m.scale_rows = (q->rows + q->scale_rows - 1) / q->scale_rows;
   m.ld = q->ld;
   m.blocks = (int32_t)(q->ld / kBlock8);
   m.scale_ld = (int32_t)q->scale_ld;
@@ -450,17 +748,30 @@ int32_t mtdao_product8(const mtdao_matrix8* a, const mtdao_matrix8* b, void* c, 
   p.b = mat_of(b);
   p.c = c;
   p.ldc = ldc;
-  p.a_scale_rows = a->scale_rows;
-  p.b_scale_rows = b->scale_rows;
+  p.a_scale_shift = a->scale_rows == 1 ? 0 : 7;
+  p.b_scale_shift = b->scale_rows == 1 ? 0 : 7;
   p.accumulate = accumulate;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   RoctxRange range("mtdao_product8 m=%lld n=%lld k=%lld", (long long)a->rows, (long long)b->rows, (long long)a->cols);
-  constexpr int B = 128;
-  const int64_t ty = up(a->rows, B) / B;
-  if (ty > 65535) return fail(e, MTDAO_ERR_INVALID_ARG, "the rows of a exceed the largest launch");
-  const dim3 grid((unsigned)(up(b->rows, B) / B), (unsigned)ty);
-  if (c_dtype == MTDAO_F32) hipLaunchKernelGGL((k_product8<B, B, float>), grid, dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((k_product8<B, B, bf16_t>), grid, dim3(256), 0, st, p);
+  auto go = [&](auto kernel, int tile, unsigned threads, int bytes, int64_t most) {
+    p.tiles_m = (int32_t)(up(a->rows, tile) / tile);
+    p.tiles_n = (int32_t)(up(b->rows, tile) / tile);
+    p.group = 8;
+    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+    if (tiles > INT64_C(0x3fffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "c has more tiles than one launch takes");
+    const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (set != hipSuccess) return hip_check(e, set, "mtdao_product8 LDS");
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(up(tiles, 8), most)), dim3(threads), bytes, st, p);
+    return (int32_t)MTDAO_OK;
+  };
+  auto pick = [&](auto ct) {
+    using CT = decltype(ct);
+    const int64_t big = (up(a->rows, kBig) / kBig) * (up(b->rows, kBig) / kBig);
+    if (big >= 128 && a->cols > 0) return go(k_product8_big<CT>, kBig, 512, kBigLds, 256);
+    return go(k_product8_mid<CT>, kMid, 256, kMidLds, INT64_C(0x3fffff));
+  };
+  r = c_dtype == MTDAO_F32 ? pick(float{}) : pick(bf16_t{});
+  if (r != MTDAO_OK) return r;
   return hip_check(e, hipGetLastError(), "mtdao_product8 launch");
 }
 
