@@ -209,13 +209,13 @@ struct Product {
 };
 
 // A 128-byte row of a tile in LDS: its eight 16-byte chunks, each at the place
-// that its number and the row's key give, so that the eight rows that a
-// quarter wave reads at once lie in different banks.  For a these are
-// consecutive rows; for b a lane group's rows are 16 apart (row_of_b).
-template <bool B>
-__device__ __forceinline__ int row_key(int row) { return B ? (row & 3) | ((row >> 2) & 4) : row & 7; }
-
-__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ row_key<false>(row)) << 4); }
+// that its number and the row's key give.  A 16-byte read of a wave takes 16
+// lanes at once, which have to lie in different ones of the 16 such places of
+// the 64 banks: two rows of eight, told apart by the row's last bit, so the
+// key has the next three.  (With the last three bits as the key half of the
+// reads' cycles were conflicts.)
+__device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ row_key(row)) << 4); }
 
 // The row of b's fragment that the instruction's row r takes: results of a lane
 // are rows 8 q + 4 h + t, so these are sixteen consecutive columns of c.
@@ -279,16 +279,20 @@ __device__ __forceinline__ Place place_of(const Product& p, int t) {
   return {(int64_t)(group * p.group + in_group % rows_here) * BM, (int64_t)(in_group / rows_here) * BN};
 }
 
-// The fragments' products of half a block, into acc.
-template <int MI, int NI, bool WIDE>
+// The fragments' products of half a block, into acc.  between(t) is called
+// after the instructions of products t = 0 .. MI NI - 1: what it issues goes
+// out while the matrix cores work.
+template <int MI, int NI, bool WIDE, typename F>
 __device__ __forceinline__ void multiply(const v8i (&fa)[MI], const v8i (&fb)[NI], const uint32_t (&ea)[MI], const uint32_t (&eb)[NI],
-                                         v16f (&acc)[MI][NI]) {
+                                         v16f (&acc)[MI][NI], F&& between) {
   if constexpr (!WIDE) {
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j)
+      for (int j = 0; j < NI; ++j) {
         acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[i], acc[i][j], 0, 0, 0, eb[j], 0, ea[i]);
+        between(i * NI + j);
+      }
   } else {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -300,6 +304,7 @@ __device__ __forceinline__ void multiply(const v8i (&fa)[MI], const v8i (&fb)[NI
         const v8bf wa = widened(fa[i], k, scale_of(ea[i] & 255u));
 #pragma unroll
         for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j], wa, acc[i][j], 0, 0, 0);
+        if ((k * MI + i) * NI % 4 == 0) between((k * MI + i) * NI / 4);
       }
     }
   }
@@ -329,7 +334,7 @@ __device__ __forceinline__ void store_rows(const Product& p, uint8_t* own, const
   asm volatile("" ::: "memory");
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const int r = q * 8 + lane / 8, chunk = (lane % 8) ^ (r & 7);
+    const int r = q * 8 + lane / 8, chunk = (lane % 8) ^ row_key(r);
     float v[kPer];
     load_full<kPer>(reinterpret_cast<const CT*>(own + r * 128 + (lane % 8) * 16), v);
     const int64_t row = row0 + r, col = col0 + chunk * kPer, left = p.b.rows - col;
@@ -372,22 +377,18 @@ __global__ __launch_bounds__(512, 1) void k_product8_big(Product p) {
   // % 8 of row l / 8.  Rows go into the lane's offset, which the hardware
   // holds against the matrix's end; the block into the scalar offset.
   const int lr = wave * 8 + lane / 8, lda = (int)p.a.ld, ldb = (int)p.b.ld;
-  int va = lr * lda + ((lane % 8) ^ row_key<false>(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key<true>(lr)) * 16;
+  int va = lr * lda + ((lane % 8) ^ row_key(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key(lr)) * 16;
   int l_tile = first, l_kb = 0, l_stage = 0;  // what is loaded next
   Place l_at = place_of<kBig, kBig>(p, l_tile);
-  auto load = [&]() {
-    const auto ra = buffer_of(p.a.codes + l_at.row0 * p.a.ld, (p.a.rows - l_at.row0) * p.a.ld);
-    const auto rb = buffer_of(p.b.codes + l_at.col0 * p.b.ld, (p.b.rows - l_at.col0) * p.b.ld);
-    uint8_t* to = lds + l_stage + wave * 1024;
+  auto load_part = [&](int k) {  // 0 .. 7: four of a, four of b
+    const bool of_b = k >= kLoads;
+    const auto r = of_b ? buffer_of(p.b.codes + l_at.col0 * p.b.ld, (p.b.rows - l_at.col0) * p.b.ld)
+                        : buffer_of(p.a.codes + l_at.row0 * p.a.ld, (p.a.rows - l_at.row0) * p.a.ld);
     asm("" : "+v"(va), "+v"(vb));  // (offsets of further rows are formed anew: they would each hold a register)
-#pragma unroll
-    for (int k = 0; k < kLoads; ++k)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (__attribute__((address_space(3))) void*)(to + k * 8192), 16, va + k * 64 * lda,
-                                               l_kb * 128, 0, 0);
-#pragma unroll
-    for (int k = 0; k < kLoads; ++k)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (__attribute__((address_space(3))) void*)(to + kBig * 128 + k * 8192), 16,
-                                               vb + k * 64 * ldb, l_kb * 128, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + l_stage + wave * 1024 + k * 8192), 16,
+                                             of_b ? vb + (k - kLoads) * 64 * ldb : va + k * 64 * lda, l_kb * 128, 0, 0);
+  };
+  auto load_done = [&]() {
     l_stage ^= kBigStage;
     // (past the last block of the last tile its first one is loaded, and not used)
     if (++l_kb == blocks) {
@@ -397,6 +398,11 @@ __global__ __launch_bounds__(512, 1) void k_product8_big(Product p) {
         l_at = place_of<kBig, kBig>(p, l_tile);
       }
     }
+  };
+  auto load = [&]() {
+#pragma unroll
+    for (int k = 0; k < 2 * kLoads; ++k) load_part(k);
+    load_done();
   };
 
   const int wm = wave / 4 * 128, wn = wave % 4 * 64, fr = lane % 32, fg = lane / 32;
@@ -424,7 +430,7 @@ __global__ __launch_bounds__(512, 1) void k_product8_big(Product p) {
 
   // Where the lane's two chunks of its first row are; the block's other half
   // is 64 bytes away, up or down as the row's key says.
-  const int key_a = row_key<false>(fr), key_b = row_key<true>(row_of_b(fr));
+  const int key_a = row_key(fr), key_b = row_key(row_of_b(fr));
   const int a0 = (wm + fr) * 128 + ((2 * fg ^ key_a) << 4), b0 = (kBig + wn + row_of_b(fr)) * 128 + ((2 * fg ^ key_b) << 4);
 
   load();
@@ -432,10 +438,11 @@ __global__ __launch_bounds__(512, 1) void k_product8_big(Product p) {
   loads_landed();
   take_scales();
   meet();
-  // A stage is free for the block after next when both halves have read it,
-  // and has to be there when the first half reads it four turns later, so both
-  // load it in the same turn: the first half when it reads, the second, one
-  // turn behind, when it multiplies.
+  // A stage is free for the block after next when the second half, which is
+  // one turn behind the first, has read it, and has to be there when the first
+  // half reads it four turns later.  Each half loads its share between the
+  // matrix instructions of its first turn in that time: at other places the
+  // loads' issue (16 cycles each) held up reads or instructions.
   auto turns = [&](auto which) {
     constexpr bool second = decltype(which)::value;
     if (second) {
@@ -466,7 +473,6 @@ __global__ __launch_bounds__(512, 1) void k_product8_big(Product p) {
               if (kb + 1 < blocks) load_scales(at, kb + 1);
               else load_scales(place_of<kBig, kBig>(p, tile + stride < past ? tile + stride : tile), 0);
             }
-            if (!second) load();
           }
           v8i fa[kMI], fb[kNI];
 #pragma unroll
@@ -478,9 +484,16 @@ __global__ __launch_bounds__(512, 1) void k_product8_big(Product p) {
           reads_landed();
           if (second && half == 1) loads_landed();
           meet();
-          if (second && half == 1) load();
           __builtin_amdgcn_s_setprio(1);
-          multiply<kMI, kNI, sizeof(CT) == 4>(fa, fb, sa, sb, acc);
+          const bool loads = half == (second ? 1 : 0);
+          multiply<kMI, kNI, sizeof(CT) == 4>(fa, fb, sa, sb, acc, [&](int t) {
+            if (loads) {
+              __builtin_amdgcn_sched_barrier(0);
+              load_part(t);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          });
+          if (loads) load_done();
           __builtin_amdgcn_sched_barrier(0);
           __builtin_amdgcn_s_setprio(0);
           if (!second && half == 1) loads_landed();
@@ -529,7 +542,7 @@ __global__ __launch_bounds__(256, 2) void k_product8_mid(Product p) {
   const Place at = place_of<kMid, kMid>(p, tile);
   const int blocks = p.a.blocks;
   const int lr = wave * 8 + lane / 8, lda = (int)p.a.ld, ldb = (int)p.b.ld;
-  const int va = lr * lda + ((lane % 8) ^ row_key<false>(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key<true>(lr)) * 16;
+  const int va = lr * lda + ((lane % 8) ^ row_key(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key(lr)) * 16;
   const auto ra = buffer_of(p.a.codes + at.row0 * p.a.ld, (p.a.rows - at.row0) * p.a.ld);
   const auto rb = buffer_of(p.b.codes + at.col0 * p.b.ld, (p.b.rows - at.col0) * p.b.ld);
   auto load = [&](int kb) {
@@ -556,7 +569,7 @@ __global__ __launch_bounds__(256, 2) void k_product8_mid(Product p) {
 #pragma unroll
     for (int j = 0; j < kNI; ++j) next_b[j] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsb, vsb + j * 32 * step_b, kb, 0);
   };
-  const int key_a = row_key<false>(fr), key_b = row_key<true>(row_of_b(fr));
+  const int key_a = row_key(fr), key_b = row_key(row_of_b(fr));
   const int a0 = (wm + fr) * 128 + ((2 * fg ^ key_a) << 4), b0 = (kMid + wn + row_of_b(fr)) * 128 + ((2 * fg ^ key_b) << 4);
   v16f acc[kMI][kNI];
 #pragma unroll
@@ -595,7 +608,7 @@ __global__ __launch_bounds__(256, 2) void k_product8_mid(Product p) {
       for (int j = 0; j < kNI; ++j) fb[j] = fragment(stage + (b0 ^ half * 64), stage + (b0 ^ (half * 64 + 16)), j * 4096);
 #pragma unroll
       for (int i = 0; i < kMI; ++i) fa[i] = fragment(stage + (a0 ^ half * 64), stage + (a0 ^ (half * 64 + 16)), i * 4096);
-      multiply<kMI, kNI, sizeof(CT) == 4>(fa, fb, sa, sb, acc);
+      multiply<kMI, kNI, sizeof(CT) == 4>(fa, fb, sa, sb, acc, [](int) {});
     }
   }
   meet();  // the stages become the waves' own
