@@ -227,16 +227,24 @@ __global__ __launch_bounds__(kThreads) void k_adamw_step(Step s) {
 #pragma unroll
       for (int t = 0; t < kV; ++t) {
         va[t] = sqrtf(va[t]);
-        mm = fmaxf(mm, finite_abs(ma[t]));
-        vm = fmaxf(vm, finite_abs(va[t]));
+        mm = max_abs(mm, ma[t]);
+        vm = max_abs(vm, va[t]);
+      }
+      if (is_infinite(mm) || is_infinite(vm)) {
+        mm = vm = 0.0f;
+#pragma unroll
+        for (int t = 0; t < kV; ++t) {
+          mm = fmaxf(mm, finite_abs(ma[t]));
+          vm = fmaxf(vm, finite_abs(va[t]));
+        }
       }
       // (lanes past the tensor hold zeros)
       const uint32_t mbyte = scale_byte(max32(mm)), vbyte = scale_byte(max32(vm));
       const float mi = inverse_scale_of(mbyte), vi = inverse_scale_of(vbyte);
 #pragma unroll
       for (int t = 0; t < kV; ++t) {
-        ma[t] = nan_if_infinite(ma[t] * mi);
-        va[t] = nan_if_infinite(va[t] > 0.0f ? fmaxf(va[t] * vi, 0x1p-9f) : va[t] * vi);
+        ma[t] *= mi;
+        va[t] = va[t] > 0.0f ? fmaxf(va[t] * vi, 0x1p-9f) : va[t] * vi;
       }
       const uint32_t mq = codes_of(ma[0], ma[1], ma[2], ma[3]), vq = codes_of(va[0], va[1], va[2], va[3]);
       if (n[k] >= kV) {

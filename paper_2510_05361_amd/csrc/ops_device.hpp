@@ -127,8 +127,18 @@ __device__ __forceinline__ float dpp(float x) {
 }
 constexpr int kRor8 = 0x128, kRor4 = 0x124, kRor2 = 0x122, kRor1 = 0x121;  // rotations within rows of 16 lanes
 
-__device__ __forceinline__ float swap16(float x) {  // the lane 16 away, within 32
-  return __uint_as_float((uint32_t)__builtin_amdgcn_ds_swizzle((int)__float_as_uint(x), 0x401f));
+// x of this lane and of the lane 16 (32) away, within 32 (64) lanes: both
+// lanes get the same pair in the same order.
+struct Pair {
+  float a, b;
+};
+__device__ __forceinline__ Pair with16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return {__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ Pair with32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return {__uint_as_float(r[0]), __uint_as_float(r[1])};
 }
 
 // Largest / sum over rows of 16 lanes, groups of 32 lanes or the wave, in
@@ -139,21 +149,31 @@ __device__ __forceinline__ float max16(float x) {
   x = fmaxf(x, dpp<kRor2>(x));
   return fmaxf(x, dpp<kRor1>(x));
 }
-__device__ __forceinline__ float max32(float x) {
-  x = max16(x);
-  return fmaxf(x, swap16(x));
+__device__ __forceinline__ float max_with16(float x) {
+  const Pair p = with16(x);
+  return fmaxf(p.a, p.b);
 }
+__device__ __forceinline__ float max_with32(float x) {
+  const Pair p = with32(x);
+  return fmaxf(p.a, p.b);
+}
+__device__ __forceinline__ float max32(float x) { return max_with16(max16(x)); }
 __device__ __forceinline__ float sum64(float x) {
   x += dpp<kRor8>(x);
   x += dpp<kRor4>(x);
   x += dpp<kRor2>(x);
   x += dpp<kRor1>(x);
-  x += swap16(x);
-  return x + __shfl_xor(x, 32);
+  const Pair p = with16(x);
+  const Pair q = with32(p.a + p.b);
+  return q.a + q.b;
 }
 
 // ------------------------------------------------------------- 8-bit blocks
 
+// Largest |x| so far, NaN left out.  Infinite only where an infinity was seen:
+// then the maximum is formed again from finite_abs.
+__device__ __forceinline__ float max_abs(float m, float x) { return fmaxf(m, fabsf(x)); }
+__device__ __forceinline__ bool is_infinite(float m) { return m > 3.4028234664e38f; }
 // |x| where x is finite, else 0: what a block's scale is formed from.
 __device__ __forceinline__ float finite_abs(float x) {
   const float a = fabsf(x);
@@ -171,14 +191,12 @@ __device__ __forceinline__ uint32_t scale_byte(float amax) {
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
 __device__ __forceinline__ float inverse_scale_of(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 
-// Four scaled values as e4m3 codes (the conversion rounds to nearest even).
-// Values are at most 448 or not finite; infinities are turned into NaN
-// first, as the conversion would saturate them.
+// Four scaled values as e4m3 codes: rounded to nearest even; infinities and
+// NaN give NaN codes (a kernel's floating-point mode does not clamp).
 __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d) {
   int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
-__device__ __forceinline__ float nan_if_infinite(float x) { return fabsf(x) <= 3.4028234664e38f ? x : __builtin_nanf(""); }
 
 __device__ __forceinline__ void values_of(uint32_t codes, float (&o)[4]) {
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false);

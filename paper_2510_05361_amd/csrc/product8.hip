@@ -45,11 +45,16 @@ __global__ __launch_bounds__(kThreads) void k_quantize8_rows(const T* x, int64_t
     for (int t = 0; t < kE; ++t) a[t] = 0.0f;
   }
 #pragma unroll
-  for (int t = 0; t < kE; ++t) most = fmaxf(most, finite_abs(a[t]));
+  for (int t = 0; t < kE; ++t) most = max_abs(most, a[t]);
+  if (is_infinite(most)) {
+    most = 0.0f;
+#pragma unroll
+    for (int t = 0; t < kE; ++t) most = fmaxf(most, finite_abs(a[t]));
+  }
   const uint32_t byte = live ? scale_byte(max16(most)) : 127u;
   const float inv = inverse_scale_of(byte);
 #pragma unroll
-  for (int t = 0; t < kE; ++t) a[t] = nan_if_infinite(a[t] * inv);
+  for (int t = 0; t < kE; ++t) a[t] *= inv;
   if (live) {
     uint2 c = {codes_of(a[0], a[1], a[2], a[3]), codes_of(a[4], a[5], a[6], a[7])};
     *reinterpret_cast<uint2*>(q.codes + row * q.ld + e) = c;
@@ -57,76 +62,105 @@ __global__ __launch_bounds__(kThreads) void k_quantize8_rows(const T* x, int64_t
   if (row < q.rows && threadIdx.x % 16 == 0) q.scales[row * q.scale_ld + kb] = (uint8_t)byte;
 }
 
-// A tile of 128 x 128: a thread holds eight rows of eight columns, so that a
-// transposed row of codes is eight consecutive bytes of it.  SQUARE: one
-// scale for the tile; else blocks along the rows for q, along the columns
-// for qt, which goes through LDS to be written in whole lines.
+// A tile of 128 x 128: a thread holds four rows of eight columns, so that it
+// has four consecutive bytes of each transposed row.  SQUARE: one scale for
+// the tile; else blocks along the rows for q, along the columns for qt.  qt
+// goes through LDS to be written in whole lines.
+constexpr int kTileThreads = 512;
 template <typename T, bool SQUARE>
-__global__ __launch_bounds__(kThreads) void k_quantize8_tile(const T* x, int64_t ld, int64_t cols, int64_t rows, Mat q,
-                                                             Mat qt) {
-  constexpr int kPad = kBlock8 + 16;
-  __shared__ __attribute__((aligned(16))) uint8_t turned[kBlock8 * kPad];
-  __shared__ float most[16][kBlock8];
-  const int c8 = (int)(threadIdx.x % 16) * kE, r8 = (int)(threadIdx.x / 16) * 8;
+__global__ __launch_bounds__(kTileThreads) void k_quantize8_tile(const T* x, int64_t ld, int64_t cols, int64_t rows, Mat q,
+                                                                 Mat qt) {
+  constexpr int kRows = 4, kWaves = kTileThreads / 64;
+  __shared__ __attribute__((aligned(16))) uint8_t turned[kBlock8 * kBlock8];
+  __shared__ __attribute__((aligned(16))) float most[kWaves][kBlock8];
+  __shared__ __attribute__((aligned(8))) uint8_t bytes_of[kBlock8];
+  const int c8 = (int)(threadIdx.x % 16) * kE, r4 = (int)(threadIdx.x / 16) * kRows, wave = threadIdx.x / 64;
   const int64_t row0 = (int64_t)blockIdx.y * kBlock8, col0 = (int64_t)blockIdx.x * kBlock8;
-  const int64_t in_cols = cols - col0 - c8, in_rows = rows - row0 - r8;
+  const int64_t in_cols = cols - col0 - c8, in_rows = rows - row0 - r4;
   const int nc = in_cols < 0 ? 0 : in_cols > kE ? kE : (int)in_cols;
-  float a[8][kE];
+  float a[kRows][kE];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < kRows; ++i) {
     if (i < in_rows && nc > 0) {
-      load_some<kE>(x + (row0 + r8 + i) * ld + col0 + c8, nc, a[i]);
+      load_some<kE>(x + (row0 + r4 + i) * ld + col0 + c8, nc, a[i]);
     } else {
 #pragma unroll
       for (int t = 0; t < kE; ++t) a[i][t] = 0.0f;
     }
   }
-  uint32_t row_byte[8];
-  float all = 0.0f;
+  float rmax[kRows], cmax[kE], all = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    float m = 0.0f;
+  for (int t = 0; t < kE; ++t) cmax[t] = 0.0f;
 #pragma unroll
-    for (int t = 0; t < kE; ++t) m = fmaxf(m, finite_abs(a[i][t]));
-    if constexpr (SQUARE) all = fmaxf(all, m);
-    else row_byte[i] = scale_byte(max16(m));
+  for (int i = 0; i < kRows; ++i) {
+    rmax[i] = 0.0f;
+#pragma unroll
+    for (int t = 0; t < kE; ++t) {
+      rmax[i] = max_abs(rmax[i], a[i][t]);
+      cmax[t] = max_abs(cmax[t], a[i][t]);
+    }
+    all = fmaxf(all, rmax[i]);
   }
-  uint32_t col_byte[kE];
-  if constexpr (SQUARE) {
-    all = max32(all);
-    all = fmaxf(all, __shfl_xor(all, 32));
-    if (threadIdx.x % 64 == 0) most[0][threadIdx.x / 64] = all;
-    __syncthreads();
-    const uint32_t byte = scale_byte(fmaxf(fmaxf(most[0][0], most[0][1]), fmaxf(most[0][2], most[0][3])));
+  if (is_infinite(all)) {
+    all = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) row_byte[i] = col_byte[i] = byte;
+    for (int t = 0; t < kE; ++t) cmax[t] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      rmax[i] = 0.0f;
+#pragma unroll
+      for (int t = 0; t < kE; ++t) {
+        rmax[i] = fmaxf(rmax[i], finite_abs(a[i][t]));
+        cmax[t] = fmaxf(cmax[t], finite_abs(a[i][t]));
+      }
+      all = fmaxf(all, rmax[i]);
+    }
+  }
+  uint32_t row_byte[kRows], col_byte[kE];
+  if constexpr (SQUARE) {
+    all = max_with32(max32(all));
+    if (threadIdx.x % 64 == 0) most[0][wave] = all;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) all = fmaxf(all, most[0][w]);
+    const uint32_t byte = scale_byte(all);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) row_byte[i] = byte;
+#pragma unroll
+    for (int t = 0; t < kE; ++t) col_byte[t] = byte;
   } else {
 #pragma unroll
-    for (int t = 0; t < kE; ++t) {
-      float m = 0.0f;
+    for (int i = 0; i < kRows; ++i) row_byte[i] = scale_byte(max16(rmax[i]));
+    // columns: the four rows of threads of a wave, then the waves
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m = fmaxf(m, finite_abs(a[i][t]));
-      most[threadIdx.x / 16][c8 + t] = m;
+    for (int t = 0; t < kE; ++t) cmax[t] = max_with32(max_with16(cmax[t]));
+    if (threadIdx.x % 64 < 16) {
+#pragma unroll
+      for (int t = 0; t < kE; t += 4)
+        *reinterpret_cast<float4*>(&most[wave][c8 + t]) = float4{cmax[t], cmax[t + 1], cmax[t + 2], cmax[t + 3]};
     }
     __syncthreads();
-#pragma unroll
-    for (int t = 0; t < kE; ++t) {
+    if (threadIdx.x < kBlock8) {
       float m = 0.0f;
 #pragma unroll
-      for (int g = 0; g < 16; ++g) m = fmaxf(m, most[g][c8 + t]);
-      col_byte[t] = scale_byte(m);
+      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, most[w][threadIdx.x]);
+      bytes_of[threadIdx.x] = (uint8_t)scale_byte(m);
     }
+    __syncthreads();
+    const uint2 b = *reinterpret_cast<const uint2*>(bytes_of + c8);
+#pragma unroll
+    for (int t = 0; t < kE; ++t) col_byte[t] = ((t < 4 ? b.x : b.y) >> 8 * (t & 3)) & 255u;
   }
   if (q.codes) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < kRows; ++i) {
       const float inv = inverse_scale_of(row_byte[i]);
       float s[kE];
 #pragma unroll
-      for (int t = 0; t < kE; ++t) s[t] = nan_if_infinite(a[i][t] * inv);
+      for (int t = 0; t < kE; ++t) s[t] = a[i][t] * inv;
       if (i < in_rows) {
         uint2 c = {codes_of(s[0], s[1], s[2], s[3]), codes_of(s[4], s[5], s[6], s[7])};
-        *reinterpret_cast<uint2*>(q.codes + (row0 + r8 + i) * q.ld + col0 + c8) = c;
+        *reinterpret_cast<uint2*>(q.codes + (row0 + r4 + i) * q.ld + col0 + c8) = c;
       }
     }
     const bool last = blockIdx.x + 1 == gridDim.x;
@@ -136,22 +170,25 @@ __global__ __launch_bounds__(kThreads) void k_quantize8_tile(const T* x, int64_t
         q.scales[(int64_t)blockIdx.y * q.scale_ld + blockIdx.x + threadIdx.x] = threadIdx.x == 0 ? (uint8_t)row_byte[0] : 127;
     } else if (threadIdx.x % 16 == 0) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < kRows; ++i)
         if (i < in_rows) {
-          uint8_t* s = q.scales + (row0 + r8 + i) * q.scale_ld + blockIdx.x;
+          uint8_t* s = q.scales + (row0 + r4 + i) * q.scale_ld + blockIdx.x;
           for (int k = 0; k < bytes; ++k) s[k] = k == 0 ? (uint8_t)row_byte[i] : 127;
         }
     }
   }
   if (qt.codes) {
+    // row c of turned: its 16-byte chunk k at place k ^ c / 8 % 8, which
+    // spreads a wave's writes over half of the banks
+    const int chunk = r4 / 16, in_chunk = r4 % 16;
 #pragma unroll
     for (int t = 0; t < kE; ++t) {
       const float inv = inverse_scale_of(col_byte[t]);
-      float s[8];
+      float s[kRows];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] = nan_if_infinite(a[i][t] * inv);
-      uint2 c = {codes_of(s[0], s[1], s[2], s[3]), codes_of(s[4], s[5], s[6], s[7])};
-      *reinterpret_cast<uint2*>(turned + (c8 + t) * kPad + r8) = c;
+      for (int i = 0; i < kRows; ++i) s[i] = a[i][t] * inv;
+      *reinterpret_cast<uint32_t*>(turned + (c8 + t) * kBlock8 + ((chunk ^ (c8 / 8 & 7)) << 4) + in_chunk) =
+          codes_of(s[0], s[1], s[2], s[3]);
     }
     const bool last = blockIdx.y + 1 == gridDim.y;
     const int bytes = last ? qt.scale_ld - (int)blockIdx.y : 1;
@@ -168,11 +205,11 @@ __global__ __launch_bounds__(kThreads) void k_quantize8_tile(const T* x, int64_t
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int at = k * kThreads + (int)threadIdx.x, r = at / 8, c = at % 8 * 16;
+    for (int k = 0; k < kBlock8 * 8 / kTileThreads; ++k) {
+      const int at = k * kTileThreads + (int)threadIdx.x, r = at / 8, c = at % 8;
       if (col0 + r < cols)
-        *reinterpret_cast<uint4*>(qt.codes + (col0 + r) * qt.ld + row0 + c) =
-            *reinterpret_cast<const uint4*>(turned + r * kPad + c);
+        *reinterpret_cast<uint4*>(qt.codes + (col0 + r) * qt.ld + row0 + c * 16) =
+            *reinterpret_cast<const uint4*>(turned + r * kBlock8 + ((c ^ (r / 8 & 7)) << 4));
     }
   }
 }
@@ -716,8 +753,8 @@ int32_t mtdao_quantize8(const void* x, int32_t dtype, int64_t ld, const mtdao_ma
     const int64_t ty = up(rows, kBlock8) / kBlock8;
     if (ty > 65535) return false;
     const dim3 grid((unsigned)(up(cols, kBlock8) / kBlock8), (unsigned)ty);
-    if (square) hipLaunchKernelGGL((k_quantize8_tile<T, true>), grid, dim3(kThreads), 0, st, in, ld, cols, rows, m, mt);
-    else hipLaunchKernelGGL((k_quantize8_tile<T, false>), grid, dim3(kThreads), 0, st, in, ld, cols, rows, m, mt);
+    if (square) hipLaunchKernelGGL((k_quantize8_tile<T, true>), grid, dim3(kTileThreads), 0, st, in, ld, cols, rows, m, mt);
+    else hipLaunchKernelGGL((k_quantize8_tile<T, false>), grid, dim3(kTileThreads), 0, st, in, ld, cols, rows, m, mt);
     return true;
   };
   if (!(dtype == MTDAO_BF16 ? with(bf16_t{}) : with(float{})))
