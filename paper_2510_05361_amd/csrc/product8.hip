@@ -243,6 +243,8 @@ struct Product {
   int64_t ldc;
   int32_t a_scale_shift, b_scale_shift;  // rows of a scale: 1 << shift
   int32_t accumulate, tiles_m, tiles_n, group;
+  int32_t splits, split_blocks;  // parts of the contraction, and their blocks (k_product8_mid)
+  float* partial;                // [splits][rows of a][rows of b] with more than one part
 };
 
 // A 128-byte row of a tile in LDS: its eight 16-byte chunks, each at the place
@@ -295,10 +297,11 @@ __device__ __forceinline__ void meet() {
   asm volatile("" ::: "memory");
 }
 // This wave's loads (global memory to registers or LDS; LDS to registers)
-// have arrived.
+// have arrived, but for the last LEFT of them.
+template <int LEFT = 0>
 __device__ __forceinline__ void loads_landed() {
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (LEFT & 15) | (LEFT >> 4) << 14);  // vmcnt(LEFT)
   asm volatile("" ::: "memory");
 }
 __device__ __forceinline__ void reads_landed() { __builtin_amdgcn_s_waitcnt(0xc07f); }  // lgkmcnt(0)
@@ -389,6 +392,26 @@ __device__ __forceinline__ void store_rows(const Product& p, uint8_t* own, const
   }
   __builtin_amdgcn_wave_barrier();
   asm volatile("" ::: "memory");
+}
+
+// The results of one row of fragments, 32 x 32 NI.
+template <typename CT, int NI>
+__device__ __forceinline__ void store_wave(const Product& p, uint8_t* own, const v16f (&acc)[NI], int64_t row0, int64_t col0, int lane) {
+  if constexpr (sizeof(CT) == 2) {
+    static_assert(NI == 2, "64 columns of bf16");
+    float o[32];
+#pragma unroll
+    for (int t = 0; t < 32; ++t) o[t] = acc[t / 16][t % 16];
+    store_rows<CT>(p, own, o, row0, col0, lane);
+  } else {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      float o[16];
+#pragma unroll
+      for (int t = 0; t < 16; ++t) o[t] = acc[j][t];
+      store_rows<CT>(p, own, o, row0, col0 + j * 32, lane);
+    }
+  }
 }
 
 // Large products: tiles of 256 x 256 over eight waves of 128 x 64, one
@@ -541,22 +564,7 @@ __global__ __launch_bounds__(512, 1) void k_product8_big(Product p) {
       }
       uint8_t* own = lds + 2 * kBigStage + wave * 4096;
 #pragma unroll
-      for (int i = 0; i < kMI; ++i) {
-        if constexpr (sizeof(CT) == 2) {
-          float o[32];
-#pragma unroll
-          for (int t = 0; t < 32; ++t) o[t] = acc[i][t / 16][t % 16];
-          store_rows<CT>(p, own, o, at.row0 + wm + i * 32, at.col0 + wn, lane);
-        } else {
-#pragma unroll
-          for (int j = 0; j < kNI; ++j) {
-            float o[16];
-#pragma unroll
-            for (int t = 0; t < 16; ++t) o[t] = acc[i][j][t];
-            store_rows<CT>(p, own, o, at.row0 + wm + i * 32, at.col0 + wn + j * 32, lane);
-          }
-        }
-      }
+      for (int i = 0; i < kMI; ++i) store_wave<CT, kNI>(p, own, acc[i], at.row0 + wm + i * 32, at.col0 + wn, lane);
     }
     if (!second) meet();
     loads_landed();  // LDS is given back: nothing may still be on its way there
@@ -565,35 +573,40 @@ __global__ __launch_bounds__(512, 1) void k_product8_big(Product p) {
   else turns(std::false_type{});
 }
 
-// Other products: tiles of 128 x 128 over four waves of 64 x 64, one tile a
-// workgroup, several workgroups a CU.
-constexpr int kMid = 128, kMidStage = 2 * kMid * 128, kMidLds = 2 * kMidStage;
+// Other products: tiles of 128 x 128, one a workgroup.  Loads are STAGES - 1
+// blocks ahead: four stages over eight waves of 32 x 64 where a CU gets one
+// workgroup, two over four waves of 64 x 64 where it gets two.
+constexpr int kMid = 128, kMidStage = 2 * kMid * 128;
 
-template <typename CT>
-__global__ __launch_bounds__(256, 2) void k_product8_mid(Product p) {
-  constexpr int kMI = 2, kNI = 2, kLoads = kMid / 32;
+// PART: this workgroup's blocks are one of p.splits parts of the contraction,
+// whose sums go to p.partial.
+template <typename CT, bool PART, int WAVES, int STAGES>
+__global__ __launch_bounds__(64 * WAVES, 2) void k_product8_mid(Product p) {
+  constexpr int kMI = 8 / WAVES, kNI = 2, kLoads = kMid / (8 * WAVES), kAhead = STAGES - 1;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int tiles = p.tiles_m * p.tiles_n, per = (tiles + 7) / 8, tile = blockIdx.x % 8 * per + blockIdx.x / 8;
-  if (tile >= tiles) return;
-  const Place at = place_of<kMid, kMid>(p, tile);
-  const int blocks = p.a.blocks;
+  const int tiles = p.tiles_m * p.tiles_n, items = tiles * p.splits, per = (items + 7) / 8;
+  const int item = blockIdx.x % 8 * per + blockIdx.x / 8;
+  if (blockIdx.x / 8 >= (unsigned)per || item >= items) return;
+  const int split = item / tiles;
+  const Place at = place_of<kMid, kMid>(p, item - split * tiles);
+  const int from = split * p.split_blocks, blocks = from + p.split_blocks < p.a.blocks ? from + p.split_blocks : p.a.blocks;
   const int lr = wave * 8 + lane / 8, lda = (int)p.a.ld, ldb = (int)p.b.ld;
   const int va = lr * lda + ((lane % 8) ^ row_key(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key(lr)) * 16;
   const auto ra = buffer_of(p.a.codes + at.row0 * p.a.ld, (p.a.rows - at.row0) * p.a.ld);
   const auto rb = buffer_of(p.b.codes + at.col0 * p.b.ld, (p.b.rows - at.col0) * p.b.ld);
   auto load = [&](int kb) {
-    uint8_t* to = lds + (kb & 1) * kMidStage + wave * 1024;
+    uint8_t* to = lds + (kb & (STAGES - 1)) * kMidStage + wave * 1024;
 #pragma unroll
     for (int k = 0; k < kLoads; ++k)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (__attribute__((address_space(3))) void*)(to + k * 4096), 16, va + k * 32 * lda,
-                                               kb * 128, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (__attribute__((address_space(3))) void*)(to + k * WAVES * 1024), 16,
+                                               va + k * 8 * WAVES * lda, kb * 128, 0, 0);
 #pragma unroll
     for (int k = 0; k < kLoads; ++k)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (__attribute__((address_space(3))) void*)(to + kMid * 128 + k * 4096), 16,
-                                               vb + k * 32 * ldb, kb * 128, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (__attribute__((address_space(3))) void*)(to + kMid * 128 + k * WAVES * 1024), 16,
+                                               vb + k * 8 * WAVES * ldb, kb * 128, 0, 0);
   };
-  const int wm = wave / 2 * 64, wn = wave % 2 * 64, fr = lane % 32, fg = lane / 32;
+  const int wm = wave / 2 * (32 * kMI), wn = wave % 2 * 64, fr = lane % 32, fg = lane / 32;
   const int64_t sr = at.row0 >> p.a_scale_shift, sc = at.col0 >> p.b_scale_shift;
   const auto rsa = buffer_of(p.a.scales + sr * p.a.scale_ld, (p.a.scale_rows - sr) * p.a.scale_ld);
   const auto rsb = buffer_of(p.b.scales + sc * p.b.scale_ld, (p.b.scale_rows - sc) * p.b.scale_ld);
@@ -615,24 +628,26 @@ __global__ __launch_bounds__(256, 2) void k_product8_mid(Product p) {
     for (int j = 0; j < kNI; ++j)
 #pragma unroll
       for (int t = 0; t < 16; ++t) acc[i][j][t] = 0.0f;
-  if (blocks > 0) {
-    load_scales(0);
-    load(0);
+  if (from < blocks) {
+    load_scales(from & ~3);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (from + k < blocks) load(from + k);
   }
-  for (int kb = 0; kb < blocks; ++kb) {
-    loads_landed();
+  for (int kb = from; kb < blocks; ++kb) {
+    // the loads of this block have landed: at most those of the blocks after it are on their way
+    if (kb + kAhead <= blocks) loads_landed<(kAhead - 1) * 2 * kLoads>();
+    else loads_landed();
     meet();
-    if ((kb & 3) == 0) {
+    if ((kb & 3) == 0 || kb == from) {
 #pragma unroll
       for (int i = 0; i < kMI; ++i) ea[i] = next_a[i];
 #pragma unroll
       for (int j = 0; j < kNI; ++j) eb[j] = next_b[j];
     }
-    if (kb + 1 < blocks) {
-      if ((kb & 3) == 3) load_scales(kb + 1);
-      load(kb + 1);
-    }
-    const uint8_t* stage = lds + (kb & 1) * kMidStage;
+    if ((kb & 3) == 3 && kb + 1 < blocks) load_scales(kb + 1);
+    if (kb + kAhead < blocks) load(kb + kAhead);
+    const uint8_t* stage = lds + (kb & (STAGES - 1)) * kMidStage;
     uint32_t sa[kMI], sb[kNI];
 #pragma unroll
     for (int i = 0; i < kMI; ++i) sa[i] = ea[i] >> 8 * (kb & 3);
@@ -650,23 +665,41 @@ __global__ __launch_bounds__(256, 2) void k_product8_mid(Product p) {
   }
   meet();  // the stages become the waves' own
   uint8_t* own = lds + wave * 4096;
-#pragma unroll
-  for (int i = 0; i < kMI; ++i) {
-    if constexpr (sizeof(CT) == 2) {
-      float o[32];
-#pragma unroll
-      for (int t = 0; t < 32; ++t) o[t] = acc[i][t / 16][t % 16];
-      store_rows<CT>(p, own, o, at.row0 + wm + i * 32, at.col0 + wn, lane);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kNI; ++j) {
-        float o[16];
-#pragma unroll
-        for (int t = 0; t < 16; ++t) o[t] = acc[i][j][t];
-        store_rows<CT>(p, own, o, at.row0 + wm + i * 32, at.col0 + wn + j * 32, lane);
-      }
-    }
+  Product to = p;
+  if (PART) {
+    to.c = p.partial + (int64_t)split * p.a.rows * p.b.rows;
+    to.ldc = p.b.rows;
+    to.accumulate = 0;
   }
+#pragma unroll
+  for (int i = 0; i < kMI; ++i) store_wave<std::conditional_t<PART, float, CT>, kNI>(to, own, acc[i], at.row0 + wm + i * 32, at.col0 + wn, lane);
+}
+
+// c from the parts' sums, added in their order: four columns a thread.
+template <typename CT>
+__global__ __launch_bounds__(kThreads) void k_product8_join(Product p) {
+  const int64_t quads = (p.b.rows + 3) / 4, at = (int64_t)blockIdx.x * kThreads + threadIdx.x, row = at / quads;
+  if (row >= p.a.rows) return;
+  const int64_t col = (at - row * quads) * 4, plane = p.a.rows * p.b.rows;
+  const int n = p.b.rows - col > 4 ? 4 : (int)(p.b.rows - col);
+  const float* in = p.partial + row * p.b.rows + col;
+  float o[4];
+  load_some<4>(in, n, o);
+#pragma unroll 4
+  for (int k = 1; k < p.splits; ++k) {
+    float v[4];
+    load_some<4>(in + k * plane, n, v);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] += v[t];
+  }
+  CT* to = reinterpret_cast<CT*>(p.c) + row * p.ldc + col;
+  if (p.accumulate) {
+    float before[4];
+    load_some<4>(to, n, before);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] += before[t];
+  }
+  store_some<4>(to, n, o);
 }
 
 // --------------------------------------------------------------------- host
@@ -677,6 +710,31 @@ using Int = std::integral_constant<int, V>;
 int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
 constexpr int64_t kMostCols = INT64_C(1) << 22;  // a tile's rows stay within 2^31 bytes
+
+// How a product of m x n x k goes over the chip.  Tiles of 256 x 256 where
+// these give work to half of the CUs.  Else tiles of 128 x 128; where these
+// leave CUs idle, the contraction in parts of at least four blocks.
+struct Shape {
+  bool big, shared;  // shared: two workgroups on a CU
+  int32_t splits, split_blocks;
+};
+Shape shape_of(int64_t m, int64_t n, int64_t k) {
+  const int64_t blocks = up(k, kBlock8) / kBlock8;
+  Shape s = {false, false, 1, (int32_t)blocks};
+  s.big = blocks > 0 && (up(m, kBig) / kBig) * (up(n, kBig) / kBig) >= 128;
+  const int64_t tiles = (up(m, kMid) / kMid) * (up(n, kMid) / kMid);
+  s.shared = tiles > 256;
+  if (!s.big && tiles > 0 && tiles <= 128 && blocks >= 8) {
+    const int64_t parts = std::min<int64_t>(256 / tiles, blocks / 4);
+    s.split_blocks = (int32_t)((blocks + parts - 1) / parts);
+    s.splits = (int32_t)((blocks + s.split_blocks - 1) / s.split_blocks);
+  }
+  return s;
+}
+size_t product_bytes(int64_t m, int64_t n, int64_t k) {
+  const Shape s = shape_of(m, n, k);
+  return s.splits > 1 ? (size_t)s.splits * (size_t)m * (size_t)n * sizeof(float) : 0;
+}
 
 int32_t check_matrix(const mtdao_matrix8& q, const char* name, std::string* e) {
   if (q.rows < 0 || q.cols < 0) return fail(e, MTDAO_ERR_INVALID_ARG, "%s: rows or cols < 0", name);
@@ -765,7 +823,9 @@ int32_t mtdao_quantize8(const void* x, int32_t dtype, int64_t ld, const mtdao_ma
 int32_t mtdao_product8_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t* bytes) {
   if (!bytes) return fail(&g_err, MTDAO_ERR_INVALID_ARG, "bytes is NULL");
   if (m < 0 || n < 0 || k < 0) return fail(&g_err, MTDAO_ERR_INVALID_ARG, "a size is below 0");
-  *bytes = 0;
+  if (m > INT64_C(0x7fffffff) || n > INT64_C(0x7fffffff) || k > kMostCols)
+    return fail(&g_err, MTDAO_ERR_INVALID_ARG, "a size exceeds what mtdao_product8 takes");
+  *bytes = product_bytes(m, n, k);
   return MTDAO_OK;
 }
 
@@ -789,10 +849,10 @@ int32_t mtdao_product8(const mtdao_matrix8* a, const mtdao_matrix8* b, void* c, 
   for (const mtdao_matrix8* m : {a, b})
     if (overlap(c, cbytes, m->codes, m->rows * m->ld) || overlap(c, cbytes, m->scales, scale_bytes(*m)))
       return fail(e, MTDAO_ERR_INVALID_ARG, "c overlaps a or b");
-  size_t need = 0;
-  mtdao_product8_workspace_bytes(a->rows, b->rows, a->cols, &need);
+  const size_t need = product_bytes(a->rows, b->rows, a->cols);
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(e, MTDAO_ERR_WORKSPACE, "workspace of %zu bytes required, %zu given", need, workspace ? workspace_bytes : (size_t)0);
+  if (need > 0 && !aligned_to(workspace, 256)) return fail(e, MTDAO_ERR_ALIGN, "workspace is not 256-byte aligned");
   Product p = {};
   p.a = mat_of(a);
   p.b = mat_of(b);
@@ -803,22 +863,32 @@ int32_t mtdao_product8(const mtdao_matrix8* a, const mtdao_matrix8* b, void* c, 
   p.accumulate = accumulate;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   RoctxRange range("mtdao_product8 m=%lld n=%lld k=%lld", (long long)a->rows, (long long)b->rows, (long long)a->cols);
+  const Shape shape = shape_of(a->rows, b->rows, a->cols);
+  p.splits = shape.splits;
+  p.split_blocks = shape.split_blocks;
+  p.partial = static_cast<float*>(workspace);
   auto go = [&](auto kernel, int tile, unsigned threads, int bytes, int64_t most) {
     p.tiles_m = (int32_t)(up(a->rows, tile) / tile);
     p.tiles_n = (int32_t)(up(b->rows, tile) / tile);
     p.group = 8;
-    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
-    if (tiles > INT64_C(0x3fffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "c has more tiles than one launch takes");
+    const int64_t items = (int64_t)p.tiles_m * p.tiles_n * p.splits;
+    if (items > INT64_C(0x3fffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "c has more tiles than one launch takes");
     const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (set != hipSuccess) return hip_check(e, set, "mtdao_product8 LDS");
-    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(up(tiles, 8), most)), dim3(threads), bytes, st, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(up(items, 8), most)), dim3(threads), bytes, st, p);
     return (int32_t)MTDAO_OK;
   };
   auto pick = [&](auto ct) {
     using CT = decltype(ct);
-    const int64_t big = (up(a->rows, kBig) / kBig) * (up(b->rows, kBig) / kBig);
-    if (big >= 128 && a->cols > 0) return go(k_product8_big<CT>, kBig, 512, kBigLds, 256);
-    return go(k_product8_mid<CT>, kMid, 256, kMidLds, INT64_C(0x3fffff));
+    if (shape.big) return go(k_product8_big<CT>, kBig, 512, kBigLds, 256);
+    const int64_t most = INT64_C(0x3fffff);
+    if (shape.splits == 1 && shape.shared) return go(k_product8_mid<CT, false, 4, 2>, kMid, 256, 2 * kMidStage, most);
+    if (shape.splits == 1) return go(k_product8_mid<CT, false, 8, 4>, kMid, 512, 4 * kMidStage, most);
+    const int32_t done = go(k_product8_mid<CT, true, 8, 4>, kMid, 512, 4 * kMidStage, most);
+    if (done != MTDAO_OK) return done;
+    const int64_t quads = p.a.rows * ((p.b.rows + 3) / 4);
+    hipLaunchKernelGGL(k_product8_join<CT>, dim3((unsigned)((quads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p);
+    return done;
   };
   r = c_dtype == MTDAO_F32 ? pick(float{}) : pick(bf16_t{});
   if (r != MTDAO_OK) return r;
