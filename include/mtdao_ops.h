@@ -187,6 +187,21 @@ int32_t mtdao_product8_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t* 
 int32_t mtdao_product8(const mtdao_matrix8* a, const mtdao_matrix8* b, void* c, int32_t c_dtype, int64_t ldc,
                        int32_t accumulate, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* A linear layer with 8-bit weights w [n][k] (blocks of 128 x 128 or 1 x 128),
+ * m rows (tokens) of x: y [m][n] = x w^T, x in blocks of 1 x 128 along its
+ * rows.  Up to 16 rows it is one launch.
+ * Backward, from dy [m][n] and x (both dtype) and wt [k][n], w transposed:
+ * dx [m][k] = dy w (dtype), dy in blocks along its rows, and dw [n][k] = dy^T x
+ * (fp32; accumulate: dw +=), dy and x in blocks along the tokens.  The same
+ * results as mtdao_quantize8 and mtdao_product8 one after the other, with
+ * their 8-bit matrices in the workspace (256-byte aligned). */
+int32_t mtdao_linear8_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t* forward, size_t* backward);
+int32_t mtdao_linear8(const void* x, int32_t dtype, int64_t rows, int64_t ld, const mtdao_matrix8* w, void* y, int32_t y_dtype,
+                      int64_t ldy, void* workspace, size_t workspace_bytes, void* hip_stream);
+int32_t mtdao_linear8_backward(const void* dy, const void* x, int32_t dtype, int64_t rows, int64_t ld_dy, int64_t ld_x,
+                               const mtdao_matrix8* wt, void* dx, int64_t ld_dx, float* dw, int64_t ld_dw, int32_t accumulate,
+                               void* workspace, size_t workspace_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

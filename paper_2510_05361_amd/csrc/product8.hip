@@ -4,8 +4,12 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <mutex>
+#include <new>
+#include <set>
 #include <string>
 #include <type_traits>
+#include <utility>
 
 #include "../../include/mtdao_ops.h"
 #include "host.hpp"
@@ -233,6 +237,7 @@ __global__ __launch_bounds__(kTileThreads) void k_quantize8_tile(const T* x, int
 
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -702,6 +707,126 @@ __global__ __launch_bounds__(kThreads) void k_product8_join(Product p) {
   store_some<4>(to, n, o);
 }
 
+// Products of a few rows (up to 64): what counts is to read b once, with as
+// many loads in flight as the chip takes.  A workgroup has sixteen rows of b
+// (columns of c), whose blocks its waves take in turn, straight from memory
+// into registers; their sums meet in LDS, in the order of the waves.  XT
+// uint8_t: a is given as 8-bit blocks; else as it is, up to sixteen rows of
+// it, which every workgroup quantizes as it reads them (one launch less).
+struct Few {
+  const void* x;
+  int64_t ldx, m, k;
+  const uint8_t* x_scales;
+  int32_t x_scale_ld, x_scale_shift;
+  Mat b;
+  int32_t b_scale_shift, accumulate;
+  void* c;
+  int64_t ldc;
+};
+
+template <typename XT, typename CT, int MI, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
+  constexpr bool kCodes = sizeof(XT) == 1;
+  static_assert(kCodes || MI == 1, "sixteen rows");
+  __shared__ v4f part[WAVES][MI][64];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
+  const int64_t col0 = (int64_t)blockIdx.x * 16, br = col0 + r < p.b.rows ? col0 + r : p.b.rows - 1;
+  const uint8_t* b = p.b.codes + br * p.b.ld + g * 32;
+  const uint8_t* bs = p.b.scales + (br >> p.b_scale_shift) * p.b.scale_ld;
+  const XT* a[MI];
+  const uint8_t* as[MI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int64_t ar = i * 16 + r < p.m ? i * 16 + r : p.m - 1;
+    a[i] = reinterpret_cast<const XT*>(p.x) + ar * p.ldx + g * 32;
+    as[i] = kCodes ? p.x_scales + (ar >> p.x_scale_shift) * p.x_scale_ld : nullptr;
+  }
+  v4f acc[MI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i) acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 2
+  for (int kb = wave; kb < p.b.blocks; kb += WAVES) {
+    const int e = kb * kBlock8;
+    const v4i b_lo = *reinterpret_cast<const v4i*>(b + e), b_hi = *reinterpret_cast<const v4i*>(b + e + 16);
+    const uint32_t eb = bs[kb];
+    v8i fa[MI];
+    uint32_t ea[MI];
+    if constexpr (kCodes) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const v4i lo = *reinterpret_cast<const v4i*>(a[i] + e), hi = *reinterpret_cast<const v4i*>(a[i] + e + 16);
+        fa[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        ea[i] = as[i][kb];
+      }
+    } else {
+      float x[4][kE], most = 0.0f;
+      const int64_t left = p.k - e - g * 32;
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int64_t n = left - v * kE;
+        if (n > 0) {
+          load_some<kE>(a[0] + e + v * kE, n > kE ? kE : (int)n, x[v]);
+        } else {
+#pragma unroll
+          for (int t = 0; t < kE; ++t) x[v][t] = 0.0f;
+        }
+#pragma unroll
+        for (int t = 0; t < kE; ++t) most = max_abs(most, x[v][t]);
+      }
+      if (is_infinite(most)) {
+        most = 0.0f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+          for (int t = 0; t < kE; ++t) most = fmaxf(most, finite_abs(x[v][t]));
+      }
+      ea[0] = scale_byte(max_with32(max_with16(most)));
+      const float inv = inverse_scale_of(ea[0]);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        fa[0][2 * v] = (int)codes_of(x[v][0] * inv, x[v][1] * inv, x[v][2] * inv, x[v][3] * inv);
+        fa[0][2 * v + 1] = (int)codes_of(x[v][4] * inv, x[v][5] * inv, x[v][6] * inv, x[v][7] * inv);
+      }
+    }
+    const v8i fb = __builtin_shufflevector(b_lo, b_hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    if constexpr (sizeof(CT) == 2) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa[i], acc[i], 0, 0, 0, eb, 0, ea[i]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const v8bf wb = widened(fb, k, scale_of(eb));
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, widened(fa[i], k, scale_of(ea[i])), acc[i], 0, 0, 0);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MI; ++i) part[wave][i][lane] = acc[i];
+  __syncthreads();
+  if (threadIdx.x < 64 * MI) {
+    const int i = threadIdx.x / 64;
+    v4f s = part[0][i][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) s += part[w][i][lane];
+    const int64_t row = i * 16 + r, col = col0 + g * 4, left = p.b.rows - col;
+    if (row < p.m && left > 0) {
+      const int n = left > 4 ? 4 : (int)left;
+      CT* at = reinterpret_cast<CT*>(p.c) + row * p.ldc + col;
+      float o[4] = {s[0], s[1], s[2], s[3]};
+      if (p.accumulate) {
+        float before[4];
+        load_some<4>(at, n, before);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) o[t] += before[t];
+      }
+      store_some<4>(at, n, o);
+    }
+  }
+}
+
 // --------------------------------------------------------------------- host
 
 template <int V>
@@ -711,16 +836,19 @@ int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
 constexpr int64_t kMostCols = INT64_C(1) << 22;  // a tile's rows stay within 2^31 bytes
 
-// How a product of m x n x k goes over the chip.  Tiles of 256 x 256 where
-// these give work to half of the CUs.  Else tiles of 128 x 128; where these
-// leave CUs idle, the contraction in parts of at least four blocks.
+// How a product of m x n x k goes over the chip.  Up to 64 rows the kernel for
+// few rows.  Tiles of 256 x 256 where these give work to half of the CUs.
+// Else tiles of 128 x 128; where these leave CUs idle, the contraction in
+// parts of at least four blocks.
+constexpr int64_t kFew = 64, kFewWhole = 16;  // rows; of which quantized on the way
 struct Shape {
-  bool big, shared;  // shared: two workgroups on a CU
+  bool few, big, shared;  // shared: two workgroups on a CU
   int32_t splits, split_blocks;
 };
 Shape shape_of(int64_t m, int64_t n, int64_t k) {
   const int64_t blocks = up(k, kBlock8) / kBlock8;
-  Shape s = {false, false, 1, (int32_t)blocks};
+  Shape s = {m <= kFew && blocks > 0, false, false, 1, (int32_t)blocks};
+  if (s.few) return s;
   s.big = blocks > 0 && (up(m, kBig) / kBig) * (up(n, kBig) / kBig) >= 128;
   const int64_t tiles = (up(m, kMid) / kMid) * (up(n, kMid) / kMid);
   s.shared = tiles > 256;
@@ -767,36 +895,47 @@ Mat mat_of(const mtdao_matrix8* q) {
 }
 
 int64_t scale_bytes(const mtdao_matrix8& q) { return (q.rows + q.scale_rows - 1) / q.scale_rows * q.scale_ld; }
+int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
 
-}  // namespace
-
-extern "C" {
-
-int32_t mtdao_quantize8(const void* x, int32_t dtype, int64_t ld, const mtdao_matrix8* q, const mtdao_matrix8* qt,
-                        void* hip_stream) {
-  std::string* e = &g_err;
-  if (!q && !qt) return fail(e, MTDAO_ERR_INVALID_ARG, "q and qt are NULL");
+// A [rows][cols] input with row stride ld.
+int32_t check_input(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const char* name, std::string* e) {
   if (dtype != MTDAO_F32 && dtype != MTDAO_BF16) return fail(e, MTDAO_ERR_INVALID_ARG, "dtype must be F32(0) or BF16(1)");
-  int32_t r = MTDAO_OK;
-  if (q) r = check_matrix(*q, "q", e);
-  if (r == MTDAO_OK && qt) r = check_matrix(*qt, "qt", e);
-  if (r != MTDAO_OK) return r;
-  if (q && qt && (q->rows != qt->cols || q->cols != qt->rows || q->scale_rows != qt->scale_rows))
-    return fail(e, MTDAO_ERR_INVALID_ARG, "qt is not q transposed");
-  const int64_t rows = q ? q->rows : qt->cols, cols = q ? q->cols : qt->rows;
   if (rows == 0 || cols == 0) return MTDAO_OK;
-  const int64_t es = dtype == MTDAO_BF16 ? 2 : 4;
   if (ld < cols || ld > (INT64_C(1) << 40) / rows)
-    return fail(e, MTDAO_ERR_INVALID_ARG, "row stride %lld of x is below cols or exceeds 2^40 elements in all", (long long)ld);
-  if (!x) return fail(e, MTDAO_ERR_INVALID_ARG, "x is NULL");
-  if (!aligned_to(x, (uintptr_t)es)) return fail(e, MTDAO_ERR_ALIGN, "x is not aligned to its element");
-  const int64_t xbytes = ((rows - 1) * ld + cols) * es;
-  const mtdao_matrix8* outs[2] = {q, qt};
-  for (const mtdao_matrix8* o : outs)
-    if (o && (overlap(x, xbytes, o->codes, o->rows * o->ld) || overlap(x, xbytes, o->scales, scale_bytes(*o))))
-      return fail(e, MTDAO_ERR_INVALID_ARG, "x overlaps an output");
-  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-  RoctxRange range("mtdao_quantize8 rows=%lld cols=%lld", (long long)rows, (long long)cols);
+    return fail(e, MTDAO_ERR_INVALID_ARG, "row stride %lld of %s is below its columns or exceeds 2^40 elements in all", (long long)ld, name);
+  if (!x) return fail(e, MTDAO_ERR_INVALID_ARG, "%s is NULL", name);
+  if (!aligned_to(x, (uintptr_t)esize(dtype))) return fail(e, MTDAO_ERR_ALIGN, "%s is not aligned to its element", name);
+  return MTDAO_OK;
+}
+
+int32_t check_product(const mtdao_matrix8& a, const mtdao_matrix8& b, const void* c, int32_t c_dtype, int64_t ldc,
+                      int32_t accumulate, std::string* e) {
+  if (a.cols != b.cols) return fail(e, MTDAO_ERR_INVALID_ARG, "a has %lld columns, b has %lld", (long long)a.cols, (long long)b.cols);
+  if (c_dtype != MTDAO_F32 && c_dtype != MTDAO_BF16) return fail(e, MTDAO_ERR_INVALID_ARG, "c_dtype must be F32(0) or BF16(1)");
+  if (accumulate && c_dtype != MTDAO_F32) return fail(e, MTDAO_ERR_INVALID_ARG, "accumulate needs an fp32 c");
+  if (a.rows == 0 || b.rows == 0) return MTDAO_OK;
+  if (ldc < b.rows || ldc > (INT64_C(1) << 40) / a.rows)
+    return fail(e, MTDAO_ERR_INVALID_ARG, "ldc %lld is below the columns of c or exceeds 2^40 elements in all", (long long)ldc);
+  if (!c) return fail(e, MTDAO_ERR_INVALID_ARG, "c is NULL");
+  if (!aligned_to(c, (uintptr_t)esize(c_dtype))) return fail(e, MTDAO_ERR_ALIGN, "c is not aligned to its element");
+  const int64_t cbytes = ((a.rows - 1) * ldc + b.rows) * esize(c_dtype);
+  for (const mtdao_matrix8* m : {&a, &b})
+    if (overlap(c, cbytes, m->codes, m->rows * m->ld) || overlap(c, cbytes, m->scales, scale_bytes(*m)))
+      return fail(e, MTDAO_ERR_INVALID_ARG, "c overlaps a or b");
+  return MTDAO_OK;
+}
+
+int32_t check_workspace(const void* workspace, size_t given, size_t need, std::string* e) {
+  if (need == 0) return MTDAO_OK;
+  if (!workspace || given < need)
+    return fail(e, MTDAO_ERR_WORKSPACE, "workspace of %zu bytes required, %zu given", need, workspace ? given : (size_t)0);
+  if (!aligned_to(workspace, 256)) return fail(e, MTDAO_ERR_ALIGN, "workspace is not 256-byte aligned");
+  return MTDAO_OK;
+}
+
+int32_t launch_quantize(const void* x, int32_t dtype, int64_t ld, const mtdao_matrix8* q, const mtdao_matrix8* qt, hipStream_t st,
+                        std::string* e) {
+  const int64_t rows = q ? q->rows : qt->cols, cols = q ? q->cols : qt->rows;
   const Mat m = mat_of(q), mt = mat_of(qt);
   const bool square = (q ? q : qt)->scale_rows == kBlock8;
   auto with = [&](auto t) {
@@ -817,7 +956,183 @@ int32_t mtdao_quantize8(const void* x, int32_t dtype, int64_t ld, const mtdao_ma
   };
   if (!(dtype == MTDAO_BF16 ? with(bf16_t{}) : with(float{})))
     return fail(e, MTDAO_ERR_INVALID_ARG, "the matrix exceeds the largest launch");
-  return hip_check(e, hipGetLastError(), "mtdao_quantize8 launch");
+  return MTDAO_OK;
+}
+
+// Waves of a workgroup of the kernel for few rows: enough that each has a few blocks.
+template <typename XT, typename CT, int MI>
+void launch_few(const Few& f, hipStream_t st) {
+  const dim3 grid((unsigned)((f.b.rows + 15) / 16));
+  if (f.b.blocks > 32) hipLaunchKernelGGL((k_product8_few<XT, CT, MI, 16>), grid, dim3(1024), 0, st, f);
+  else hipLaunchKernelGGL((k_product8_few<XT, CT, MI, 8>), grid, dim3(512), 0, st, f);
+}
+
+Few few_of(const mtdao_matrix8& b, void* c, int64_t ldc, int32_t accumulate, int64_t m) {
+  Few f = {};
+  f.b = mat_of(&b);
+  f.b_scale_shift = b.scale_rows == 1 ? 0 : 7;
+  f.c = c;
+  f.ldc = ldc;
+  f.accumulate = accumulate;
+  f.m = m;
+  f.k = b.cols;
+  return f;
+}
+
+int32_t launch_few_whole(const void* x, int32_t dtype, int64_t rows, int64_t ld, const mtdao_matrix8& w, void* y, int32_t y_dtype,
+                         int64_t ldy, hipStream_t st) {
+  Few f = few_of(w, y, ldy, 0, rows);
+  f.x = x;
+  f.ldx = ld;
+  if (dtype == MTDAO_BF16 && y_dtype == MTDAO_BF16) launch_few<bf16_t, bf16_t, 1>(f, st);
+  else if (dtype == MTDAO_BF16) launch_few<bf16_t, float, 1>(f, st);
+  else if (y_dtype == MTDAO_BF16) launch_few<float, bf16_t, 1>(f, st);
+  else launch_few<float, float, 1>(f, st);
+  return MTDAO_OK;
+}
+
+// More than 64 KiB of LDS for a kernel, asked for once per kernel and device.
+int32_t allow_lds(const void* kernel, int bytes, std::string* e) try {
+  static std::mutex lock;
+  static std::set<std::pair<const void*, int>> done;
+  int device = 0;
+  int32_t r = hip_check(e, hipGetDevice(&device), "mtdao_product8 device");
+  if (r != MTDAO_OK) return r;
+  std::lock_guard<std::mutex> held(lock);
+  if (done.count({kernel, device})) return MTDAO_OK;
+  r = hip_check(e, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes), "mtdao_product8 LDS");
+  if (r == MTDAO_OK) done.insert({kernel, device});
+  return r;
+} catch (const std::bad_alloc&) {
+  return fail(e, MTDAO_ERR_WORKSPACE, "out of host memory");
+}
+
+// a, b, c: checked; c has elements.
+int32_t launch_product(const mtdao_matrix8& a, const mtdao_matrix8& b, void* c, int32_t c_dtype, int64_t ldc, int32_t accumulate,
+                       void* workspace, hipStream_t st, std::string* e) {
+  const Shape shape = shape_of(a.rows, b.rows, a.cols);
+  if (shape.few) {
+    Few f = few_of(b, c, ldc, accumulate, a.rows);
+    f.x = a.codes;
+    f.ldx = a.ld;
+    f.x_scales = a.scales;
+    f.x_scale_ld = (int32_t)a.scale_ld;
+    f.x_scale_shift = a.scale_rows == 1 ? 0 : 7;
+    auto with = [&](auto ct) {
+      using CT = decltype(ct);
+      if (a.rows <= 16) launch_few<uint8_t, CT, 1>(f, st);
+      else if (a.rows <= 32) launch_few<uint8_t, CT, 2>(f, st);
+      else launch_few<uint8_t, CT, 4>(f, st);
+    };
+    if (c_dtype == MTDAO_F32) with(float{});
+    else with(bf16_t{});
+    return MTDAO_OK;
+  }
+  Product p = {};
+  p.a = mat_of(&a);
+  p.b = mat_of(&b);
+  p.c = c;
+  p.ldc = ldc;
+  p.a_scale_shift = a.scale_rows == 1 ? 0 : 7;
+  p.b_scale_shift = b.scale_rows == 1 ? 0 : 7;
+  p.accumulate = accumulate;
+  p.group = 8;
+  p.splits = shape.splits;
+  p.split_blocks = shape.split_blocks;
+  p.partial = static_cast<float*>(workspace);
+  auto go = [&](auto kernel, int tile, unsigned threads, int bytes, int64_t most) {
+    p.tiles_m = (int32_t)(up(a.rows, tile) / tile);
+    p.tiles_n = (int32_t)(up(b.rows, tile) / tile);
+    const int64_t items = (int64_t)p.tiles_m * p.tiles_n * p.splits;
+    if (items > INT64_C(0x3fffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "c has more tiles than one launch takes");
+    const int32_t r = allow_lds(reinterpret_cast<const void*>(kernel), bytes, e);
+    if (r != MTDAO_OK) return r;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(up(items, 8), most)), dim3(threads), bytes, st, p);
+    return (int32_t)MTDAO_OK;
+  };
+  auto pick = [&](auto ct) {
+    using CT = decltype(ct);
+    if (shape.big) return go(k_product8_big<CT>, kBig, 512, kBigLds, 256);
+    const int64_t most = INT64_C(0x3fffff);
+    if (shape.splits == 1 && shape.shared) return go(k_product8_mid<CT, false, 4, 2>, kMid, 256, 2 * kMidStage, most);
+    if (shape.splits == 1) return go(k_product8_mid<CT, false, 8, 4>, kMid, 512, 4 * kMidStage, most);
+    const int32_t done = go(k_product8_mid<CT, true, 8, 4>, kMid, 512, 4 * kMidStage, most);
+    if (done != MTDAO_OK) return done;
+    const int64_t quads = p.a.rows * ((p.b.rows + 3) / 4);
+    hipLaunchKernelGGL(k_product8_join<CT>, dim3((unsigned)((quads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p);
+    return done;
+  };
+  return c_dtype == MTDAO_F32 ? pick(float{}) : pick(bf16_t{});
+}
+
+// Where a linear layer's 8-bit matrices and partial sums are in its workspace.
+int64_t up256(int64_t n) { return up(n, 256); }
+struct Part {
+  int64_t codes, scales, end;
+};
+Part part_at(int64_t at, int64_t rows, int64_t cols) {
+  const int64_t ld = up(cols, kBlock8), scales = at + up256(rows * ld);
+  return {at, scales, scales + up256(rows * up(ld / kBlock8, 4))};
+}
+mtdao_matrix8 matrix_at(void* workspace, int64_t codes, int64_t scales, int64_t rows, int64_t cols) {
+  mtdao_matrix8 m = {};
+  m.codes = static_cast<uint8_t*>(workspace) + codes;
+  m.scales = static_cast<uint8_t*>(workspace) + scales;
+  m.rows = rows;
+  m.cols = cols;
+  m.ld = up(cols, kBlock8);
+  m.scale_ld = up(m.ld / kBlock8, 4);
+  m.scale_rows = 1;
+  return m;
+}
+struct Forward {
+  int64_t codes, scales, product;
+  size_t bytes;
+};
+Forward forward_layout(int64_t m, int64_t n, int64_t k) {
+  if (m <= kFewWhole || n == 0 || k == 0) return {0, 0, 0, 0};
+  const Part q = part_at(0, m, k);
+  return {q.codes, q.scales, q.end, (size_t)q.end + product_bytes(m, n, k)};
+}
+struct Backward {
+  Part dy, dyt, xt;
+  int64_t product;
+  size_t bytes;
+};
+Backward backward_layout(int64_t m, int64_t n, int64_t k) {
+  Backward b = {};
+  b.dy = part_at(0, m, n);
+  b.dyt = part_at(b.dy.end, n, m);
+  b.xt = part_at(b.dyt.end, k, m);
+  b.product = b.xt.end;
+  b.bytes = (size_t)b.product + std::max(product_bytes(m, k, n), product_bytes(n, k, m));
+  return b;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t mtdao_quantize8(const void* x, int32_t dtype, int64_t ld, const mtdao_matrix8* q, const mtdao_matrix8* qt,
+                        void* hip_stream) {
+  std::string* e = &g_err;
+  if (!q && !qt) return fail(e, MTDAO_ERR_INVALID_ARG, "q and qt are NULL");
+  int32_t r = MTDAO_OK;
+  if (q) r = check_matrix(*q, "q", e);
+  if (r == MTDAO_OK && qt) r = check_matrix(*qt, "qt", e);
+  if (r != MTDAO_OK) return r;
+  if (q && qt && (q->rows != qt->cols || q->cols != qt->rows || q->scale_rows != qt->scale_rows))
+    return fail(e, MTDAO_ERR_INVALID_ARG, "qt is not q transposed");
+  const int64_t rows = q ? q->rows : qt->cols, cols = q ? q->cols : qt->rows;
+  r = check_input(x, dtype, rows, cols, ld, "x", e);
+  if (r != MTDAO_OK || rows == 0 || cols == 0) return r;
+  const int64_t xbytes = ((rows - 1) * ld + cols) * esize(dtype);
+  for (const mtdao_matrix8* o : {q, qt})
+    if (o && (overlap(x, xbytes, o->codes, o->rows * o->ld) || overlap(x, xbytes, o->scales, scale_bytes(*o))))
+      return fail(e, MTDAO_ERR_INVALID_ARG, "x overlaps an output");
+  RoctxRange range("mtdao_quantize8 rows=%lld cols=%lld", (long long)rows, (long long)cols);
+  r = launch_quantize(x, dtype, ld, q, qt, reinterpret_cast<hipStream_t>(hip_stream), e);
+  return r != MTDAO_OK ? r : hip_check(e, hipGetLastError(), "mtdao_quantize8 launch");
 }
 
 int32_t mtdao_product8_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t* bytes) {
@@ -835,64 +1150,92 @@ int32_t mtdao_product8(const mtdao_matrix8* a, const mtdao_matrix8* b, void* c, 
   if (!a || !b) return fail(e, MTDAO_ERR_INVALID_ARG, "a or b is NULL");
   int32_t r = check_matrix(*a, "a", e);
   if (r == MTDAO_OK) r = check_matrix(*b, "b", e);
+  if (r == MTDAO_OK) r = check_product(*a, *b, c, c_dtype, ldc, accumulate, e);
   if (r != MTDAO_OK) return r;
-  if (a->cols != b->cols) return fail(e, MTDAO_ERR_INVALID_ARG, "a has %lld columns, b has %lld", (long long)a->cols, (long long)b->cols);
-  if (c_dtype != MTDAO_F32 && c_dtype != MTDAO_BF16) return fail(e, MTDAO_ERR_INVALID_ARG, "c_dtype must be F32(0) or BF16(1)");
-  if (accumulate && c_dtype != MTDAO_F32) return fail(e, MTDAO_ERR_INVALID_ARG, "accumulate needs an fp32 c");
   if (a->rows == 0 || b->rows == 0) return MTDAO_OK;
-  const int64_t es = c_dtype == MTDAO_BF16 ? 2 : 4;
-  if (ldc < b->rows || ldc > (INT64_C(1) << 40) / a->rows)
-    return fail(e, MTDAO_ERR_INVALID_ARG, "ldc %lld is below the columns of c or exceeds 2^40 elements in all", (long long)ldc);
-  if (!c) return fail(e, MTDAO_ERR_INVALID_ARG, "c is NULL");
-  if (!aligned_to(c, (uintptr_t)es)) return fail(e, MTDAO_ERR_ALIGN, "c is not aligned to its element");
-  const int64_t cbytes = ((a->rows - 1) * ldc + b->rows) * es;
-  for (const mtdao_matrix8* m : {a, b})
-    if (overlap(c, cbytes, m->codes, m->rows * m->ld) || overlap(c, cbytes, m->scales, scale_bytes(*m)))
-      return fail(e, MTDAO_ERR_INVALID_ARG, "c overlaps a or b");
-  const size_t need = product_bytes(a->rows, b->rows, a->cols);
-  if (need > 0 && (!workspace || workspace_bytes < need))
-    return fail(e, MTDAO_ERR_WORKSPACE, "workspace of %zu bytes required, %zu given", need, workspace ? workspace_bytes : (size_t)0);
-  if (need > 0 && !aligned_to(workspace, 256)) return fail(e, MTDAO_ERR_ALIGN, "workspace is not 256-byte aligned");
-  Product p = {};
-  p.a = mat_of(a);
-  p.b = mat_of(b);
-  p.c = c;
-  p.ldc = ldc;
-  p.a_scale_shift = a->scale_rows == 1 ? 0 : 7;
-  p.b_scale_shift = b->scale_rows == 1 ? 0 : 7;
-  p.accumulate = accumulate;
-  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-  RoctxRange range("mtdao_product8 m=%lld n=%lld k=%lld", (long long)a->rows, (long long)b->rows, (long long)a->cols);
-  const Shape shape = shape_of(a->rows, b->rows, a->cols);
-  p.splits = shape.splits;
-  p.split_blocks = shape.split_blocks;
-  p.partial = static_cast<float*>(workspace);
-  auto go = [&](auto kernel, int tile, unsigned threads, int bytes, int64_t most) {
-    p.tiles_m = (int32_t)(up(a->rows, tile) / tile);
-    p.tiles_n = (int32_t)(up(b->rows, tile) / tile);
-    p.group = 8;
-    const int64_t items = (int64_t)p.tiles_m * p.tiles_n * p.splits;
-    if (items > INT64_C(0x3fffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "c has more tiles than one launch takes");
-    const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (set != hipSuccess) return hip_check(e, set, "mtdao_product8 LDS");
-    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(up(items, 8), most)), dim3(threads), bytes, st, p);
-    return (int32_t)MTDAO_OK;
-  };
-  auto pick = [&](auto ct) {
-    using CT = decltype(ct);
-    if (shape.big) return go(k_product8_big<CT>, kBig, 512, kBigLds, 256);
-    const int64_t most = INT64_C(0x3fffff);
-    if (shape.splits == 1 && shape.shared) return go(k_product8_mid<CT, false, 4, 2>, kMid, 256, 2 * kMidStage, most);
-    if (shape.splits == 1) return go(k_product8_mid<CT, false, 8, 4>, kMid, 512, 4 * kMidStage, most);
-    const int32_t done = go(k_product8_mid<CT, true, 8, 4>, kMid, 512, 4 * kMidStage, most);
-    if (done != MTDAO_OK) return done;
-    const int64_t quads = p.a.rows * ((p.b.rows + 3) / 4);
-    hipLaunchKernelGGL(k_product8_join<CT>, dim3((unsigned)((quads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p);
-    return done;
-  };
-  r = c_dtype == MTDAO_F32 ? pick(float{}) : pick(bf16_t{});
+  r = check_workspace(workspace, workspace_bytes, product_bytes(a->rows, b->rows, a->cols), e);
   if (r != MTDAO_OK) return r;
-  return hip_check(e, hipGetLastError(), "mtdao_product8 launch");
+  RoctxRange range("mtdao_product8 m=%lld n=%lld k=%lld", (long long)a->rows, (long long)b->rows, (long long)a->cols);
+  r = launch_product(*a, *b, c, c_dtype, ldc, accumulate, workspace, reinterpret_cast<hipStream_t>(hip_stream), e);
+  return r != MTDAO_OK ? r : hip_check(e, hipGetLastError(), "mtdao_product8 launch");
+}
+
+int32_t mtdao_linear8_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t* forward, size_t* backward) {
+  if (!forward || !backward) return fail(&g_err, MTDAO_ERR_INVALID_ARG, "forward or backward is NULL");
+  if (m < 0 || n < 0 || k < 0 || m > kMostCols || n > kMostCols || k > kMostCols)
+    return fail(&g_err, MTDAO_ERR_INVALID_ARG, "a size is below 0 or above 2^22");
+  *forward = forward_layout(m, n, k).bytes;
+  *backward = backward_layout(m, n, k).bytes;
+  return MTDAO_OK;
+}
+
+int32_t mtdao_linear8(const void* x, int32_t dtype, int64_t rows, int64_t ld, const mtdao_matrix8* w, void* y, int32_t y_dtype,
+                      int64_t ldy, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  std::string* e = &g_err;
+  if (!w) return fail(e, MTDAO_ERR_INVALID_ARG, "w is NULL");
+  int32_t r = check_matrix(*w, "w", e);
+  if (r == MTDAO_OK && (rows < 0 || rows > kMostCols)) r = fail(e, MTDAO_ERR_INVALID_ARG, "rows below 0 or above 2^22");
+  if (r == MTDAO_OK) r = check_input(x, dtype, rows, w->cols, ld, "x", e);
+  if (r != MTDAO_OK) return r;
+  const Forward f = forward_layout(rows, w->rows, w->cols);
+  mtdao_matrix8 q = matrix_at(workspace, f.codes, f.scales, rows, w->cols);
+  r = check_product(q, *w, y, y_dtype, ldy, 0, e);
+  if (r == MTDAO_OK && rows > 0 && w->rows > 0) {
+    r = check_workspace(workspace, workspace_bytes, f.bytes, e);
+    if (r == MTDAO_OK && overlap(y, ((rows - 1) * ldy + w->rows) * esize(y_dtype), x, ((rows - 1) * ld + w->cols) * esize(dtype)))
+      r = fail(e, MTDAO_ERR_INVALID_ARG, "y overlaps x");
+  }
+  if (r != MTDAO_OK || rows == 0 || w->rows == 0) return r;
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  RoctxRange range("mtdao_linear8 m=%lld n=%lld k=%lld", (long long)rows, (long long)w->rows, (long long)w->cols);
+  if (rows <= kFewWhole && w->cols > 0) {
+    r = launch_few_whole(x, dtype, rows, ld, *w, y, y_dtype, ldy, st);
+  } else {
+    r = launch_quantize(x, dtype, ld, &q, nullptr, st, e);
+    if (r == MTDAO_OK)
+      r = launch_product(q, *w, y, y_dtype, ldy, 0, static_cast<char*>(workspace) + f.product, st, e);
+  }
+  return r != MTDAO_OK ? r : hip_check(e, hipGetLastError(), "mtdao_linear8 launch");
+}
+
+int32_t mtdao_linear8_backward(const void* dy, const void* x, int32_t dtype, int64_t rows, int64_t ld_dy, int64_t ld_x,
+                               const mtdao_matrix8* wt, void* dx, int64_t ld_dx, float* dw, int64_t ld_dw, int32_t accumulate,
+                               void* workspace, size_t workspace_bytes, void* hip_stream) {
+  std::string* e = &g_err;
+  if (!wt) return fail(e, MTDAO_ERR_INVALID_ARG, "wt is NULL");
+  int32_t r = check_matrix(*wt, "wt", e);
+  if (r == MTDAO_OK && (rows < 0 || rows > kMostCols)) r = fail(e, MTDAO_ERR_INVALID_ARG, "rows below 0 or above 2^22");
+  const int64_t n = wt->cols, k = wt->rows;
+  if (r == MTDAO_OK) r = check_input(dy, dtype, rows, n, ld_dy, "dy", e);
+  if (r == MTDAO_OK) r = check_input(x, dtype, rows, k, ld_x, "x", e);
+  if (r != MTDAO_OK) return r;
+  const Backward f = backward_layout(rows, n, k);
+  mtdao_matrix8 q = matrix_at(workspace, f.dy.codes, f.dy.scales, rows, n);
+  mtdao_matrix8 qt = matrix_at(workspace, f.dyt.codes, f.dyt.scales, n, rows);
+  mtdao_matrix8 xt = matrix_at(workspace, f.xt.codes, f.xt.scales, k, rows);
+  r = check_product(q, *wt, dx, dtype, ld_dx, 0, e);
+  if (r == MTDAO_OK) r = check_product(qt, xt, dw, MTDAO_F32, ld_dw, accumulate, e);
+  if (r == MTDAO_OK && n > 0 && k > 0) r = check_workspace(workspace, workspace_bytes, f.bytes, e);
+  if (r == MTDAO_OK && rows > 0 && n > 0 && k > 0) {
+    const int64_t es = esize(dtype);
+    const struct { const void* p; int64_t bytes; } out[2] = {{dx, ((rows - 1) * ld_dx + k) * es}, {dw, ((n - 1) * ld_dw + k) * 4}},
+                                                   in[2] = {{dy, ((rows - 1) * ld_dy + n) * es}, {x, ((rows - 1) * ld_x + k) * es}};
+    for (auto& o : out)
+      for (auto& i : in)
+        if (overlap(o.p, o.bytes, i.p, i.bytes)) return fail(e, MTDAO_ERR_INVALID_ARG, "dx or dw overlaps dy or x");
+    if (overlap(out[0].p, out[0].bytes, out[1].p, out[1].bytes)) return fail(e, MTDAO_ERR_INVALID_ARG, "dx overlaps dw");
+  }
+  if (r != MTDAO_OK) return r;
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  RoctxRange range("mtdao_linear8_backward m=%lld n=%lld k=%lld", (long long)rows, (long long)n, (long long)k);
+  if (rows > 0 && n > 0 && k > 0) {
+    r = launch_quantize(dy, dtype, ld_dy, &q, &qt, st, e);
+    if (r == MTDAO_OK) r = launch_quantize(x, dtype, ld_x, nullptr, &xt, st, e);
+  }
+  char* product = static_cast<char*>(workspace) + f.product;
+  if (r == MTDAO_OK && rows > 0 && k > 0) r = launch_product(q, *wt, dx, dtype, ld_dx, 0, product, st, e);
+  if (r == MTDAO_OK && n > 0 && k > 0) r = launch_product(qt, xt, dw, MTDAO_F32, ld_dw, accumulate, product, st, e);
+  return r != MTDAO_OK ? r : hip_check(e, hipGetLastError(), "mtdao_linear8_backward launch");
 }
 
 }  // extern "C"

@@ -8,6 +8,7 @@ are raw pointers, streams raw HIP stream handles, and errors raise
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional, Sequence
 
 from . import mtdao as abi
@@ -58,12 +59,16 @@ def lib() -> ctypes.CDLL:
                 ("mtdao_adamw_step_count", [_VP], _I64),
                 ("mtdao_adamw_last_error", [_VP], ctypes.c_char_p),
                 ("mtdao_adamw_destroy", [_VP], None),
-                ("mtdao_peri_norm", [P(PeriNormArgs), _VP], _I32),
-                ("mtdao_peri_norm_backward_workspace_bytes", [P(PeriNormArgs), P(SZ)], _I32),
-                ("mtdao_peri_norm_backward", [P(PeriNormArgs), _VP, SZ, _VP], _I32),
+                ("mtdao_peri_norm", [_VP, _VP], _I32),
+                ("mtdao_peri_norm_backward_workspace_bytes", [_VP, P(SZ)], _I32),
+                ("mtdao_peri_norm_backward", [_VP, _VP, SZ, _VP], _I32),
                 ("mtdao_quantize8", [_VP, _I32, _I64, P(Matrix8), P(Matrix8), _VP], _I32),
                 ("mtdao_product8_workspace_bytes", [_I64, _I64, _I64, P(SZ)], _I32),
-                ("mtdao_product8", [P(Matrix8), P(Matrix8), _VP, _I32, _I64, _I32, _VP, SZ, _VP], _I32)):
+                ("mtdao_product8", [P(Matrix8), P(Matrix8), _VP, _I32, _I64, _I32, _VP, SZ, _VP], _I32),
+                ("mtdao_linear8_workspace_bytes", [_I64, _I64, _I64, P(SZ), P(SZ)], _I32),
+                ("mtdao_linear8", [_VP, _I32, _I64, _I64, _VP, _VP, _I32, _I64, _VP, SZ, _VP], _I32),
+                ("mtdao_linear8_backward", [_VP, _VP, _I32, _I64, _I64, _I64, _VP, _VP, _I64, _VP, _I64, _I32, _VP, SZ, _VP],
+                 _I32)):
             fn = getattr(L, name)
             fn.argtypes, fn.restype = args, res
         _lib = L
@@ -110,19 +115,28 @@ def mtdao_adamw_destroy(h: Optional[int]) -> None:
     lib().mtdao_adamw_destroy(h)
 
 
-def mtdao_peri_norm(args: PeriNormArgs, stream: Optional[int]) -> None:
-    _check(lib().mtdao_peri_norm(ctypes.byref(args), stream))
+#: An mtdao_peri_norm_args as bytes (PACKED_ARGS.pack(fields in order)), which
+#: the calls below take like the structure: filled in one call, it costs a
+#: fifth of setting 26 fields.
+PACKED_ARGS = struct.Struct("=qqiiiiffqqqqq13Q")
 
 
-def mtdao_peri_norm_backward_workspace_bytes(args: PeriNormArgs) -> int:
+def _args(args):
+    return args if isinstance(args, bytes) else ctypes.byref(args)
+
+
+def mtdao_peri_norm(args, stream: Optional[int]) -> None:
+    _check((_lib or lib()).mtdao_peri_norm(_args(args), stream))
+
+
+def mtdao_peri_norm_backward_workspace_bytes(args) -> int:
     out = ctypes.c_size_t(0)
-    _check(lib().mtdao_peri_norm_backward_workspace_bytes(ctypes.byref(args), ctypes.byref(out)))
+    _check(lib().mtdao_peri_norm_backward_workspace_bytes(_args(args), ctypes.byref(out)))
     return int(out.value)
 
 
-def mtdao_peri_norm_backward(args: PeriNormArgs, workspace: Optional[int], workspace_bytes: int,
-                             stream: Optional[int]) -> None:
-    _check(lib().mtdao_peri_norm_backward(ctypes.byref(args), workspace, int(workspace_bytes), stream))
+def mtdao_peri_norm_backward(args, workspace: Optional[int], workspace_bytes: int, stream: Optional[int]) -> None:
+    _check((_lib or lib()).mtdao_peri_norm_backward(_args(args), workspace, workspace_bytes, stream))
 
 
 def mtdao_quantize8(x: Optional[int], dtype: int, ld: int, q: Optional[Matrix8], qt: Optional[Matrix8],
@@ -141,3 +155,23 @@ def mtdao_product8(a: Matrix8, b: Matrix8, c: Optional[int], c_dtype: int, ldc: 
                    workspace: Optional[int], workspace_bytes: int, stream: Optional[int]) -> None:
     _check(lib().mtdao_product8(ctypes.byref(a), ctypes.byref(b), c, c_dtype, int(ldc), int(accumulate), workspace,
                                 int(workspace_bytes), stream))
+
+
+def mtdao_linear8_workspace_bytes(m: int, n: int, k: int):
+    """(forward, backward) bytes."""
+    f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(lib().mtdao_linear8_workspace_bytes(int(m), int(n), int(k), ctypes.byref(f), ctypes.byref(b)))
+    return int(f.value), int(b.value)
+
+
+def mtdao_linear8(x: Optional[int], dtype: int, rows: int, ld: int, w: Matrix8, y: Optional[int], y_dtype: int, ldy: int,
+                  workspace: Optional[int], workspace_bytes: int, stream: Optional[int]) -> None:
+    _check((_lib or lib()).mtdao_linear8(x, dtype, rows, ld, ctypes.byref(w), y, y_dtype, ldy, workspace, workspace_bytes,
+                                         stream))
+
+
+def mtdao_linear8_backward(dy: Optional[int], x: Optional[int], dtype: int, rows: int, ld_dy: int, ld_x: int, wt: Matrix8,
+                           dx: Optional[int], ld_dx: int, dw: Optional[int], ld_dw: int, accumulate: bool,
+                           workspace: Optional[int], workspace_bytes: int, stream: Optional[int]) -> None:
+    _check((_lib or lib()).mtdao_linear8_backward(dy, x, dtype, rows, ld_dy, ld_x, ctypes.byref(wt), dx, ld_dx, dw, ld_dw,
+                                                  accumulate, workspace, workspace_bytes, stream))

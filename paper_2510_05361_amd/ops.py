@@ -12,6 +12,7 @@ for any torch operation.  There is no CPU path.
 
 from __future__ import annotations
 
+import functools
 from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
@@ -26,29 +27,27 @@ BLOCK = c_ops.MTDAO_BLOCK8
 
 
 def _stream(t: torch.Tensor) -> int:
-    return torch.cuda.current_stream(t.device).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _type(t: torch.Tensor, what: str) -> int:
-    if t.dtype not in _TYPES:
+    code = _TYPES.get(t.dtype)
+    if code is None:
         raise TypeError(f"{what} must be float32 or bfloat16, not {t.dtype}")
-    return _TYPES[t.dtype]
+    return code
 
 
-def _on_device(*named) -> torch.device:
-    """The one HIP device of the given (name, tensor) pairs; None is skipped."""
-    device = None
-    for name, t in named:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError(f"{name} is on {t.device}: the operators run on the GPU only")
-        if device is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, the others on {device}")
-        device = t.device
-    if device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {device}, the current device is {torch.cuda.current_device()}")
-    return device
+def _on_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> torch.device:
+    """The HIP device that all of the tensors are on (None is skipped) and
+    that is the current one."""
+    index = first.get_device()
+    for t in (first, *others):
+        if t is not None and t.get_device() != index or index < 0:
+            raise ValueError(f"a tensor is on {first.device if index < 0 else t.device}: the operators run on the GPU only, "
+                             "all tensors of a call on one")
+    if index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {first.device}, the current device is {torch.cuda.current_device()}")
+    return first.device
 
 
 # ------------------------------------------------------------------- AdamW
@@ -80,7 +79,7 @@ class AdamW:
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [float(weight_decay)] * n
         if len(decay) != n:
             raise ValueError(f"{len(decay)} values of weight_decay for {n} tensors")
-        device = _on_device(*((f"params[{i}]", p) for i, p in enumerate(self.params)))
+        device = _on_device(*self.params)
         for i, p in enumerate(self.params):
             if p.dtype != self.params[0].dtype or not p.is_contiguous():
                 raise ValueError(f"params[{i}]: parameters are contiguous and of one type")
@@ -96,7 +95,7 @@ class AdamW:
                 made = [torch.zeros(s, dtype=torch.uint8 if eight else dtype, device=device).view(dtype) for s in sizes]
             else:
                 made = list(states[name])
-                _on_device((name, self.params[0]), *((f"{name}[{i}]", t) for i, t in enumerate(made)))
+                _on_device(self.params[0], *made)
                 if len(made) != n or any(t.dtype != dtype or t.numel() != s or not t.is_contiguous()
                                          for t, s in zip(made, sizes)):
                     raise ValueError(f"states['{name}']: {n} contiguous tensors of {dtype}, as large as their parameters "
@@ -119,7 +118,7 @@ class AdamW:
     def _grads_ok(self, grads, dtype) -> None:
         if len(grads) != len(self.params):
             raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
-        _on_device(("params", self.params[0]), *((f"grads[{i}]", g) for i, g in enumerate(grads)))
+        _on_device(self.params[0], *grads)
         for i, (p, g) in enumerate(zip(self.params, grads)):
             if g.dtype != dtype or g.numel() != p.numel() or not g.is_contiguous():
                 raise ValueError(f"grads[{i}]: gradients are contiguous, of one type and as large as their parameters")
@@ -131,7 +130,7 @@ class AdamW:
         self.grads = list(grads)
 
     def step(self, lr: float) -> None:
-        c_ops.mtdao_adamw_step(self.handle, lr, torch.cuda.current_stream().cuda_stream)
+        c_ops.mtdao_adamw_step(self.handle, lr, _stream(self.workspace))
 
     @property
     def step_count(self) -> int:
@@ -152,48 +151,51 @@ class AdamW:
 # -------------------------------------------------------- Peri-LN boundary
 
 
-def _rows(t: Optional[torch.Tensor], shape, what: str) -> Tuple[Optional[torch.Tensor], int]:
-    """t as [rows, d] with contiguous rows, and its row stride."""
+def _rows(t: Optional[torch.Tensor], shape, what: str):
+    """t, its address and row stride as [rows, d] with contiguous rows."""
     if t is None:
-        return None, shape[-1]
+        return None, 0, shape[-1]
     if t.shape != shape:
         raise ValueError(f"{what} is {tuple(t.shape)}, not {tuple(shape)}")
-    t = t.reshape(-1, shape[-1])
-    if t.stride(1) != 1 and t.shape[1] > 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    d = shape[-1]
+    if t.is_contiguous():
+        return t, t.data_ptr(), d
+    t = t.reshape(-1, d)
+    if t.stride(1) != 1 and d > 1 or t.shape[0] > 1 and t.stride(0) < d:
         t = t.contiguous()
-    return t, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t, t.data_ptr(), t.stride(0) if t.shape[0] > 1 else d
 
 
-def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
-    return None if t is None else t.data_ptr()
+def _ptr(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
 
 
-def _peri_args(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch):
+def _peri_sizes(x, f, w_post, w_pre, gate, rows_per_gate, kind):
+    """rows, d, weight type, rows per gate of a call whose weights fit."""
     if kind not in _KINDS:
         raise ValueError(f"kind {kind!r} is not 'rms' or 'layer'")
     if (f is None) != (w_post is None):
         raise ValueError("f and w_post come together")
-    weights = [w for w in (w_post, w_pre, gate) if w is not None]
-    if not weights:
+    if f is None and w_pre is None:
         raise ValueError("neither f nor w_pre is given")
     d = x.shape[-1]
-    a = c_ops.PeriNormArgs()
-    a.rows, a.d, a.kind = (x.numel() // d if d else 0), d, _KINDS[kind]
-    a.stream_dtype, a.branch_dtype, a.weight_dtype = _type(x, "x"), _TYPES[branch], _type(weights[0], "weights")
-    a.eps, a.scale = eps, scale
+    rows = x.numel() // d if d else 0
+    weight = (w_post if w_post is not None else w_pre).dtype
     for name, w in (("w_post", w_post), ("w_pre", w_pre), ("gate", gate)):
         if w is None:
             continue
-        if w.dtype != weights[0].dtype or not w.is_contiguous():
+        if w.dtype != weight or not w.is_contiguous():
             raise ValueError(f"{name}: w_post, w_pre and gate are contiguous and of one type")
-        if name != "gate" and w.numel() != d:
+        if w is not gate and w.numel() != d:
             raise ValueError(f"{name} has {w.numel()} elements, rows have {d}")
-    if gate is not None:
-        a.rows_per_gate = rows_per_gate if rows_per_gate > 0 else max(1, a.rows)
-        if gate.numel() != max(1, -(-a.rows // a.rows_per_gate)) * d:
-            raise ValueError(f"gate is {tuple(gate.shape)}: one row of {d} per {a.rows_per_gate} rows of {a.rows}")
-    a.w_post, a.w_pre, a.gate = _ptr(w_post), _ptr(w_pre), _ptr(gate)
-    return a
+    if weight not in _TYPES:
+        raise TypeError(f"weights must be float32 or bfloat16, not {weight}")
+    if gate is None:
+        return rows, d, weight, 1
+    per = rows_per_gate if rows_per_gate > 0 else max(1, rows)
+    if gate.numel() != max(1, -(-rows // per)) * d:
+        raise ValueError(f"gate is {tuple(gate.shape)}: one row of {d} per {per} rows of {rows}")
+    return rows, d, weight, per
 
 
 def peri_norm(x: torch.Tensor, f: Optional[torch.Tensor], w_post: Optional[torch.Tensor],
@@ -207,20 +209,32 @@ def peri_norm(x: torch.Tensor, f: Optional[torch.Tensor], w_post: Optional[torch
     None.  ``gate`` has one row of D per ``rows_per_gate`` rows of x (0: one
     row for all).  n has f's type (``branch_dtype``, x's by default, without
     f)."""
-    _on_device(("x", x), ("f", f), ("w_post", w_post), ("w_pre", w_pre), ("gate", gate))
+    _on_device(x, f, w_post, w_pre, gate)
     branch = f.dtype if f is not None else branch_dtype or x.dtype
     if branch not in _TYPES:
         raise TypeError(f"f must be float32 or bfloat16, not {branch}")
-    a = _peri_args(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch)
-    x2, a.ld_x = _rows(x, x.shape, "x")
-    f2, a.ld_f = _rows(f, x.shape, "f")
-    a.x, a.f = _ptr(x2), _ptr(f2)
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device) if f is not None else x
-    n = torch.empty(x.shape, dtype=branch, device=x.device) if w_pre is not None else None
-    a.x_out, a.n_out = (_ptr(out) if f is not None else None), _ptr(n)
-    if a.rows:
-        c_ops.mtdao_peri_norm(a, _stream(x))
+    rows, d, weight, per = _peri_sizes(x, f, w_post, w_pre, gate, rows_per_gate, kind)
+    stream = _type(x, "x")
+    shape = x.shape
+    x_in, px, ld_x = _rows(x, shape, "x")
+    f_in, pf, ld_f = _rows(f, shape, "f")
+    out = torch.empty(shape, dtype=x.dtype, device=x.device) if f is not None else x
+    n = torch.empty(shape, dtype=branch, device=x.device) if w_pre is not None else None
+    if rows:
+        c_ops.mtdao_peri_norm(
+            c_ops.PACKED_ARGS.pack(rows, d, _KINDS[kind], stream, _TYPES[branch], _TYPES[weight], eps, scale, per, ld_x, ld_f, d, d,
+                                   px, pf, _ptr(w_post), _ptr(w_pre), _ptr(gate), 0, 0, out.data_ptr() if f is not None else 0,
+                                   _ptr(n), 0, 0, 0, 0), _stream(x))
     return out, n
+
+
+@functools.lru_cache(maxsize=256)
+def _peri_workspace(rows: int, d: int, per: int, gated: bool) -> int:
+    """Bytes for these sizes (every part given: at least what any call needs)."""
+    some = 256  # stands for an address; only whether there is one is looked at
+    return c_ops.mtdao_peri_norm_backward_workspace_bytes(
+        c_ops.PACKED_ARGS.pack(rows, d, 0, 0, 0, 0, 0.0, 1.0, per, d, d, d, d, some, some, some, some, some if gated else 0,
+                               *(0,) * 8))
 
 
 def peri_norm_backward(d_out: Optional[torch.Tensor], dn: Optional[torch.Tensor], x_out: torch.Tensor,
@@ -230,34 +244,37 @@ def peri_norm_backward(d_out: Optional[torch.Tensor], dn: Optional[torch.Tensor]
     """Gradients of ``peri_norm`` from those of its outputs (either may be
     None: zero), its output x' and its input f: (dx, df, d_w_post, d_w_pre,
     d_gate), those of weights in float32, None for what was not given."""
-    _on_device(("x_out", x_out), ("f", f), ("w_post", w_post), ("w_pre", w_pre), ("gate", gate), ("d_out", d_out), ("dn", dn))
+    _on_device(x_out, f, w_post, w_pre, gate, d_out, dn)
     branch = f.dtype if f is not None else dn.dtype if dn is not None else x_out.dtype
     if branch not in _TYPES:
         raise TypeError(f"f must be float32 or bfloat16, not {branch}")
     if d_out is not None and d_out.dtype != x_out.dtype or dn is not None and dn.dtype != branch:
         raise TypeError("d_out has the type of x_out, dn that of f")
-    a = _peri_args(x_out, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch)
-    d = x_out.shape[-1]
-    x2, a.ld_x = _rows(x_out, x_out.shape, "x_out")
-    f2, a.ld_f = _rows(f, x_out.shape, "f")
-    d2, a.ld_d_out = _rows(d_out, x_out.shape, "d_out")
-    y2, a.ld_dn = _rows(dn, x_out.shape, "dn")
-    a.x, a.f, a.d_out, a.dn = _ptr(x2), _ptr(f2), _ptr(d2), _ptr(y2)
-    dev = x_out.device
-    dx = torch.empty(x_out.shape, dtype=x_out.dtype, device=dev)
-    df = torch.empty(x_out.shape, dtype=branch, device=dev) if f is not None else None
-    dw_post = torch.empty(d, dtype=torch.float32, device=dev) if f is not None else None
-    dw_pre = torch.empty(d, dtype=torch.float32, device=dev) if w_pre is not None else None
-    dgate = torch.empty(gate.shape, dtype=torch.float32, device=dev) if gate is not None else None
-    if a.rows == 0:
+    rows, d, weight, per = _peri_sizes(x_out, f, w_post, w_pre, gate, rows_per_gate, kind)
+    stream = _type(x_out, "x_out")
+    shape, dev, f32 = x_out.shape, x_out.device, torch.float32
+    x_in, px, ld_x = _rows(x_out, shape, "x_out")
+    f_in, pf, ld_f = _rows(f, shape, "f")
+    d_in, pd, ld_d = _rows(d_out, shape, "d_out")
+    y_in, py, ld_y = _rows(dn, shape, "dn")
+    dx = torch.empty(shape, dtype=x_out.dtype, device=dev)
+    df = torch.empty(shape, dtype=branch, device=dev) if f is not None else None
+    dw_post = torch.empty(d, dtype=f32, device=dev) if f is not None else None
+    dw_pre = torch.empty(d, dtype=f32, device=dev) if w_pre is not None else None
+    dgate = torch.empty(gate.shape, dtype=f32, device=dev) if gate is not None else None
+    if rows == 0:
         for t in (dw_post, dw_pre, dgate):
             if t is not None:
                 t.zero_()
         return dx, df, dw_post, dw_pre, dgate
-    a.x_out, a.df, a.d_w_post, a.d_w_pre, a.d_gate = (_ptr(t) for t in (dx, df, dw_post, dw_pre, dgate))
-    need = c_ops.mtdao_peri_norm_backward_workspace_bytes(a)
+    if d > c_ops.MTDAO_PERI_MAX_D:
+        raise ValueError(f"rows of {d}: at most {c_ops.MTDAO_PERI_MAX_D}")
+    need = _peri_workspace(rows, d, per, gate is not None)
     ws = torch.empty(need, dtype=torch.uint8, device=dev)
-    c_ops.mtdao_peri_norm_backward(a, ws.data_ptr(), need, _stream(x_out))
+    c_ops.mtdao_peri_norm_backward(
+        c_ops.PACKED_ARGS.pack(rows, d, _KINDS[kind], stream, _TYPES[branch], _TYPES[weight], eps, scale, per, ld_x, ld_f, ld_d, ld_y,
+                               px, pf, _ptr(w_post), _ptr(w_pre), _ptr(gate), pd, py, dx.data_ptr(), 0, _ptr(df), _ptr(dw_post),
+                               _ptr(dw_pre), _ptr(dgate)), ws.data_ptr(), need, _stream(x_out))
     return dx, df, dw_post, dw_pre, dgate
 
 
@@ -309,6 +326,16 @@ def _ld(x: torch.Tensor) -> int:
     return x.stride(0) if x.shape[0] > 1 else x.shape[1]
 
 
+@functools.lru_cache(maxsize=256)
+def _product_workspace(m: int, n: int, k: int) -> int:
+    return c_ops.mtdao_product8_workspace_bytes(m, n, k)
+
+
+@functools.lru_cache(maxsize=256)
+def _linear_workspace(m: int, n: int, k: int) -> Tuple[int, int]:
+    return c_ops.mtdao_linear8_workspace_bytes(m, n, k)
+
+
 def _quantize(x: torch.Tensor, q: Optional[Matrix8], qt: Optional[Matrix8]) -> None:
     c_ops.mtdao_quantize8(x.data_ptr(), _type(x, "x"), _ld(x), q.args if q is not None else None,
                           qt.args if qt is not None else None, _stream(x))
@@ -318,7 +345,7 @@ def quantize8(x: torch.Tensor, *, rows: bool = True, transposed: bool = False):
     """x [r, c] as 8-bit blocks of 1 x 128: along its rows (``rows``), and/or
     transposed, along its columns (``transposed``).  Returns the one asked
     for, or both in one pass over x."""
-    _on_device(("x", x))
+    _on_device(x)
     x = _matrix(x)
     q = Matrix8(x.shape[0], x.shape[1], x.device) if rows else None
     qt = Matrix8(x.shape[1], x.shape[0], x.device) if transposed else None
@@ -338,8 +365,8 @@ def product8(a: Matrix8, b: Matrix8, *, dtype: torch.dtype = torch.bfloat16, out
         out = torch.empty((a.rows, b.rows), dtype=dtype, device=a._buf.device)
     elif tuple(out.shape) != (a.rows, b.rows) or out.shape[1] > 1 and out.stride(1) != 1:
         raise ValueError(f"out is {tuple(out.shape)} with strides {out.stride()}, not [{a.rows}, {b.rows}] with contiguous rows")
-    _on_device(("a", a._buf), ("b", b._buf), ("out", out))
-    need = c_ops.mtdao_product8_workspace_bytes(a.rows, b.rows, a.cols)
+    _on_device(out, a._buf, b._buf)
+    need = _product_workspace(a.rows, b.rows, a.cols)
     ws = torch.empty(need, dtype=torch.uint8, device=out.device) if need else None
     c_ops.mtdao_product8(a.args, b.args, out.data_ptr(), _type(out, "out"), _ld(out), accumulate, _ptr(ws), need,
                          _stream(out))
@@ -352,14 +379,14 @@ class Weight8:
     ``update`` takes the weight again after an optimizer step, in place."""
 
     def __init__(self, w: torch.Tensor):
-        _on_device(("w", w))
+        _on_device(w)
         w = _matrix(w)
         self.q = Matrix8(w.shape[0], w.shape[1], w.device, BLOCK)
         self.qt = Matrix8(w.shape[1], w.shape[0], w.device, BLOCK)
         _quantize(w, self.q, self.qt)
 
     def update(self, w: torch.Tensor) -> None:
-        _on_device(("w", w), ("weight", self.q._buf))
+        _on_device(w, self.q._buf)
         if tuple(w.shape) != (self.q.rows, self.q.cols):
             raise ValueError(f"the weight is [{self.q.rows}, {self.q.cols}], not {tuple(w.shape)}")
         _quantize(_matrix(w), self.q, self.qt)
@@ -368,20 +395,44 @@ class Weight8:
 def linear8(x: torch.Tensor, w: Weight8, *, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """x W^T over the last axis of x, x in 8-bit blocks along it; in x's type
     unless ``dtype`` is given."""
-    if x.shape[-1] != w.q.cols:
-        raise ValueError(f"x has {x.shape[-1]} columns, the weight {w.q.cols}")
-    q = quantize8(x.reshape(-1, x.shape[-1]))
-    return product8(q, w.q, dtype=dtype or x.dtype).view(*x.shape[:-1], w.q.rows)
+    wq = w.q
+    if x.shape[-1] != wq.cols:
+        raise ValueError(f"x has {x.shape[-1]} columns, the weight {wq.cols}")
+    dev = _on_device(x, wq._buf)
+    x2 = _matrix(x if x.dim() == 2 else x.reshape(-1, wq.cols))
+    m = x2.shape[0]
+    y = torch.empty((*x.shape[:-1], wq.rows), dtype=dtype or x.dtype, device=dev)
+    need = _linear_workspace(m, wq.rows, wq.cols)[0]
+    ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    c_ops.mtdao_linear8(x2.data_ptr(), _type(x, "x"), m, _ld(x2), wq.args, y.data_ptr(), _type(y, "dtype"), wq.rows, _ptr(ws), need,
+                        _stream(x))
+    return y
 
 
 def linear8_backward(dy: torch.Tensor, x: torch.Tensor, w: Weight8, *, dw: Optional[torch.Tensor] = None,
                      accumulate: bool = False) -> Tuple[torch.Tensor, torch.Tensor]:
     """(dx, dw) of ``linear8``: dx = dy W in dy's type, with dy in 8-bit
     blocks along its rows; dw = dy^T x in float32, with dy and x in 8-bit
-    blocks along the tokens.  ``dw`` / ``accumulate``: as in product8."""
-    if x.shape[-1] != w.q.cols or dy.shape[-1] != w.q.rows or x.shape[:-1] != dy.shape[:-1]:
-        raise ValueError(f"dy is {tuple(dy.shape)}, x {tuple(x.shape)}, the weight [{w.q.rows}, {w.q.cols}]")
-    q, qt = quantize8(dy.reshape(-1, dy.shape[-1]), transposed=True)
-    xt = quantize8(x.reshape(-1, x.shape[-1]), rows=False, transposed=True)
-    dx = product8(q, w.qt, dtype=dy.dtype).view(x.shape)
-    return dx, product8(qt, xt, dtype=torch.float32, out=dw, accumulate=accumulate)
+    blocks along the tokens.  ``dw``: written in place of a new tensor
+    (float32, contiguous rows); ``accumulate``: added to."""
+    n, k = w.q.rows, w.q.cols
+    if x.shape[-1] != k or dy.shape[-1] != n or x.shape[:-1] != dy.shape[:-1]:
+        raise ValueError(f"dy is {tuple(dy.shape)}, x {tuple(x.shape)}, the weight [{n}, {k}]")
+    if dy.dtype != x.dtype:
+        raise TypeError(f"dy is {dy.dtype}, x {x.dtype}")
+    if dw is None:
+        if accumulate:
+            raise ValueError("accumulate needs dw")
+        dw = torch.empty((n, k), dtype=torch.float32, device=x.device)
+    elif tuple(dw.shape) != (n, k) or k > 1 and dw.stride(1) != 1 or dw.dtype != torch.float32:
+        raise ValueError(f"dw is {tuple(dw.shape)}, {dw.dtype} with strides {dw.stride()}, not float32 [{n}, {k}] with contiguous rows")
+    dev = _on_device(x, dy, dw, w.qt._buf)
+    x2 = _matrix(x if x.dim() == 2 else x.reshape(-1, k))
+    dy2 = _matrix(dy if dy.dim() == 2 else dy.reshape(-1, n))
+    m = x2.shape[0]
+    dx = torch.empty(x.shape, dtype=dy.dtype, device=dev)
+    need = _linear_workspace(m, n, k)[1]
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    c_ops.mtdao_linear8_backward(dy2.data_ptr(), x2.data_ptr(), _type(dy, "dy"), m, _ld(dy2), _ld(x2), w.qt.args, dx.data_ptr(), k,
+                                 dw.data_ptr(), _ld(dw), accumulate, ws.data_ptr(), need, _stream(x))
+    return dx, dw
