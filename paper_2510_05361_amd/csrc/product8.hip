@@ -248,42 +248,39 @@ struct Product {
   int64_t ldc;
   int32_t a_scale_shift, b_scale_shift;  // rows of a scale: 1 << shift
   int32_t accumulate, tiles_m, tiles_n, group;
-  int32_t splits, split_blocks;  // parts of the contraction, and their blocks (k_product8_mid)
+  int32_t splits, split_blocks;  // parts of the contraction, and their blocks
   float* partial;                // [splits][rows of a][rows of b] with more than one part
 };
 
-// A 128-byte row of a tile in LDS: its eight 16-byte chunks, each at the place
-// that its number and the row's key give.  A 16-byte read of a wave takes 16
-// lanes at once, which have to lie in different ones of the 16 such places of
-// the 64 banks: two rows of eight, told apart by the row's last bit, so the
-// key has the next three.  (With the last three bits as the key half of the
-// reads' cycles were conflicts.)
-__device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
-__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ row_key(row)) << 4); }
+// Half a block of a tile in LDS: rows of 64 bytes, whose four 16-byte chunks are
+// at the places that their number and the row's key give.  A 16-byte read of a
+// wave takes 16 lanes at once, which have to lie in different ones of the 16
+// such places of the 64 banks: four rows of four, told apart by the row's last
+// two bits, so the key has the next two.  (With 128-byte rows and their last
+// three bits as the key half of the reads' cycles were conflicts.)
+__device__ __forceinline__ int row_key(int row) { return (row >> 2) & 3; }
+
+// A row of 128 bytes of results on their way to memory: the same for eight
+// chunks, two rows to the banks.
+__device__ __forceinline__ int chunk_key(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ chunk_key(row)) << 4); }
 
 // The row of b's fragment that the instruction's row r takes: results of a lane
 // are rows 8 q + 4 h + t, so these are sixteen consecutive columns of c.
 __device__ __forceinline__ int row_of_b(int r) { return ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3); }
 
-// Two chunks of a row, as the instruction's operand.  lo, hi: where the
-// lane's chunks of row lane % 16 of the tile are.
-__device__ __forceinline__ v8i fragment(const uint8_t* lo, const uint8_t* hi, int at) {
-  const v4i a = *reinterpret_cast<const v4i*>(lo + at), b = *reinterpret_cast<const v4i*>(hi + at);
-  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
-// Eight codes (two of a fragment's words) times their scale, as bf16: exact
-// down to bf16's smallest values.
-__device__ __forceinline__ v8bf widened(v8i f, int part, float scale) {
+// Eight codes times their scale, as bf16: exact down to bf16's smallest values.
+__device__ __forceinline__ v8bf widened(int w0, int w1, float scale) {
   v8bf o;
+  const int w[2] = {w0, w1};
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    const v2bf lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)f[2 * part + w], scale, false);
-    const v2bf hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)f[2 * part + w], scale, true);
-    o[4 * w] = lo[0];
-    o[4 * w + 1] = lo[1];
-    o[4 * w + 2] = hi[0];
-    o[4 * w + 3] = hi[1];
+  for (int k = 0; k < 2; ++k) {
+    const v2bf lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w[k], scale, false);
+    const v2bf hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w[k], scale, true);
+    o[4 * k] = lo[0];
+    o[4 * k + 1] = lo[1];
+    o[4 * k + 2] = hi[0];
+    o[4 * k + 3] = hi[1];
   }
   return o;
 }
@@ -324,41 +321,61 @@ __device__ __forceinline__ Place place_of(const Product& p, int t) {
   return {(int64_t)(group * p.group + in_group % rows_here) * BM, (int64_t)(in_group / rows_here) * BN};
 }
 
-// The fragments' products of half a block, into acc.  between(t) is called
-// after the instructions of products t = 0 .. MI NI - 1: what it issues goes
-// out while the matrix cores work.
-template <int MI, int NI, bool WIDE, typename F>
-__device__ __forceinline__ void multiply(const v8i (&fa)[MI], const v8i (&fb)[NI], const uint32_t (&ea)[MI], const uint32_t (&eb)[NI],
-                                         v16f (&acc)[MI][NI], F&& between) {
-  if constexpr (!WIDE) {
+// A step of half a block: what its matrix instructions take of a row, in a
+// lane.  8-bit instructions: one step of two 16-byte chunks (the half block over
+// the two halves of the wave); bf16 instructions: two steps of one chunk.
+template <bool WIDE>
+struct Step8 {
+  static constexpr int kSteps = WIDE ? 2 : 1;
+  using Fragment = std::conditional_t<WIDE, v4i, v8i>;
+  // `row`: where the lane's first chunk is; the second is an exclusive or away.
+  static __device__ __forceinline__ Fragment read(const uint8_t* lds, int row, int offset, int step) {
+    if constexpr (WIDE) {
+      return *reinterpret_cast<const v4i*>(lds + offset + (row ^ step * 16));
+    } else {
+      const v4i a = *reinterpret_cast<const v4i*>(lds + offset + row);
+      const v4i b = *reinterpret_cast<const v4i*>(lds + offset + (row ^ 16));
+      return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+  }
+  // The products of a step, into acc.  between(t) is called after parts of the
+  // instructions, t = 0 .. calls - 1: what it issues goes out while the matrix
+  // cores work.
+  template <int MI, int NI>
+  static constexpr int calls = WIDE ? 2 * MI : MI * NI;
+  template <int MI, int NI, typename F>
+  static __device__ __forceinline__ void multiply(const Fragment (&fa)[MI], const Fragment (&fb)[NI], const uint32_t (&ea)[MI],
+                                                  const uint32_t (&eb)[NI], v16f (&acc)[MI][NI], F&& between) {
+    if constexpr (!WIDE) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[i], acc[i][j], 0, 0, 0, eb[j], 0, ea[i]);
+          between(i * NI + j);
+        }
+    } else {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        v8bf wb[NI];
+#pragma unroll
+        for (int j = 0; j < NI; ++j) wb[j] = widened(fb[j][2 * k], fb[j][2 * k + 1], scale_of(eb[j] & 255u));
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+          const v8bf wa = widened(fa[i][2 * k], fa[i][2 * k + 1], scale_of(ea[i] & 255u));
+#pragma unroll
+          for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j], wa, acc[i][j], 0, 0, 0);
+          between(k * MI + i);
+        }
+      }
+    }
+    // (without a use here the instructions would be moved past the next barrier)
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fb[j], fa[i], acc[i][j], 0, 0, 0, eb[j], 0, ea[i]);
-        between(i * NI + j);
-      }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v8bf wb[NI];
-#pragma unroll
-      for (int j = 0; j < NI; ++j) wb[j] = widened(fb[j], k, scale_of(eb[j] & 255u));
-#pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        const v8bf wa = widened(fa[i], k, scale_of(ea[i] & 255u));
-#pragma unroll
-        for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wb[j], wa, acc[i][j], 0, 0, 0);
-        if ((k * MI + i) * NI % 4 == 0) between((k * MI + i) * NI / 4);
-      }
-    }
+      for (int j = 0; j < NI; ++j) asm volatile("" : "+v"(acc[i][j]));
   }
-  // (without a use here the instructions would be moved past the next barrier)
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int j = 0; j < NI; ++j) asm volatile("" : "+v"(acc[i][j]));
-}
+};
 
 // A wave's 32 x 64 (bf16) or 32 x 32 (fp32) results to c, by way of 4 KiB of
 // LDS of its own: rows of 128 bytes, of which eight lanes then store one.
@@ -379,7 +396,7 @@ __device__ __forceinline__ void store_rows(const Product& p, uint8_t* own, const
   asm volatile("" ::: "memory");
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const int r = q * 8 + lane / 8, chunk = (lane % 8) ^ row_key(r);
+    const int r = q * 8 + lane / 8, chunk = (lane % 8) ^ chunk_key(r);
     float v[kPer];
     load_full<kPer>(reinterpret_cast<const CT*>(own + r * 128 + (lane % 8) * 16), v);
     const int64_t row = row0 + r, col = col0 + chunk * kPer, left = p.b.rows - col;
@@ -419,58 +436,82 @@ __device__ __forceinline__ void store_wave(const Product& p, uint8_t* own, const
   }
 }
 
-// Large products: tiles of 256 x 256 over eight waves of 128 x 64, one
-// workgroup per CU that goes from tile to tile.  LDS holds two blocks of each
-// side: the next one, of the next tile after a tile's last, is loaded,
-// straight into LDS, while this one is multiplied.  The two halves of the
-// waves take turns, four a block: one multiplies the half block that it has
-// read while the other reads; a SIMD holds a wave of each.
-constexpr int kBig = 256, kBigStage = 2 * kBig * 128, kBigLds = 2 * kBigStage + 8 * 4096;
+// Item t: a tile and the blocks of its contraction.
+struct Item {
+  Place at;
+  int from, to, split;
+};
+template <bool PART, int B>
+__device__ __forceinline__ Item item_at(const Product& p, int tiles, int t) {
+  if (!PART) return {place_of<B, B>(p, t), 0, p.a.blocks, 0};
+  const int split = t / tiles, from = split * p.split_blocks;
+  return {place_of<B, B>(p, t - split * tiles), from, from + p.split_blocks < p.a.blocks ? from + p.split_blocks : p.a.blocks, split};
+}
 
-template <typename CT>
-__global__ __launch_bounds__(512, 1) void k_product8_big(Product p) {
-  constexpr int kMI = 4, kNI = 2, kLoads = kBig / 64;
+// Products in tiles of B x B over WR x WC waves, one workgroup per CU that goes
+// from item to item: tiles, or with PART the p.splits parts of the contraction
+// of each, whose sums go to p.partial.
+//
+// LDS holds STAGES half blocks of each side, loaded straight into it and running
+// on into the next item.  A wave reads a step's fragments while the matrix cores
+// work on the step before, so it needs others only when a stage changes hands:
+// once in PERIOD half blocks, before the last step, when the last fragments are
+// in registers, all meet; then the stages read so far are free to be loaded,
+// and those to be read until the next time are there.  Reads and loads are
+// issued between the matrix instructions, one half block's loads in every half
+// block: a 1 KiB load takes 16 cycles to issue, which holds up a wave's matrix
+// instructions where several come together.
+template <typename CT, bool PART, int B, int WR, int WC, int STAGES, int PERIOD>
+__global__ __launch_bounds__(64 * WR * WC, 1) void k_product8_tiles(Product p) {
+  constexpr int kWaves = WR * WC, kMI = B / WR / 32, kNI = B / WC / 32, kLoads = B / (16 * kWaves), kStage = 2 * B * 64;
+  using Step = Step8<sizeof(CT) == 4>;
+  using Fragment = typename Step::Fragment;
+  constexpr int kSteps = Step::kSteps, kCalls = Step::template calls<kMI, kNI>;
+  static_assert(kNI == 2 && 128 % (32 * kMI) == 0, "a wave has 64 columns, and its rows share their block of 128 rows");
+  static_assert(STAGES >= 2 * PERIOD && (PERIOD == 1 || PERIOD == 2) && kLoads > 0, "stages");
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int tiles = p.tiles_m * p.tiles_n, per = (tiles + 7) / 8, xcd = blockIdx.x % 8;
-  // this XCD's share of the tiles, and this workgroup's among them
-  const int first = xcd * per + blockIdx.x / 8, past = xcd * per + per < tiles ? xcd * per + per : tiles, stride = gridDim.x / 8;
+  const int tiles = p.tiles_m * p.tiles_n, items = PART ? tiles * p.splits : tiles, per = (items + 7) / 8, xcd = blockIdx.x % 8;
+  // this XCD's share of the items, and this workgroup's among them
+  const int first = xcd * per + blockIdx.x / 8, past = xcd * per + per < items ? xcd * per + per : items, stride = gridDim.x / 8;
   if (first >= past) return;
-  const int blocks = p.a.blocks;
+  auto item_of = [&](int t) { return item_at<PART, B>(p, tiles, t); };
 
-  // A wave loads eight rows at once: lane l the chunk that belongs at place l
-  // % 8 of row l / 8.  Rows go into the lane's offset, which the hardware
-  // holds against the matrix's end; the block into the scalar offset.
-  const int lr = wave * 8 + lane / 8, lda = (int)p.a.ld, ldb = (int)p.b.ld;
-  int va = lr * lda + ((lane % 8) ^ row_key(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key(lr)) * 16;
-  int l_tile = first, l_kb = 0, l_stage = 0;  // what is loaded next
-  Place l_at = place_of<kBig, kBig>(p, l_tile);
-  auto load_part = [&](int k) {  // 0 .. 7: four of a, four of b
+  // A wave loads sixteen rows at once: lane l the chunk that belongs at place l
+  // % 4 of row l / 4.  Rows go into the lane's offset, which the hardware
+  // holds against the matrix's end; the half block into the scalar offset.
+  const int lr = wave * 16 + lane / 4, lda = (int)p.a.ld, ldb = (int)p.b.ld;
+  int va = lr * lda + ((lane % 4) ^ row_key(lr)) * 16, vb = lr * ldb + ((lane % 4) ^ row_key(lr)) * 16;
+  // What is loaded next: the item's rows, bytes into them, the last of these, and the stage's place.
+  int l_item = first, l_stage = wave * 1024;
+  const Item start = item_of(first);
+  int l_off = start.from * 128, l_from = l_off, l_end = start.to * 128;
+  auto rows_of_a = [&](const Place& at) { return buffer_of(p.a.codes + at.row0 * p.a.ld, (p.a.rows - at.row0) * p.a.ld); };
+  auto rows_of_b = [&](const Place& at) { return buffer_of(p.b.codes + at.col0 * p.b.ld, (p.b.rows - at.col0) * p.b.ld); };
+  __amdgpu_buffer_rsrc_t ra = rows_of_a(start.at), rb = rows_of_b(start.at);
+  auto load_part = [&](int k) {  // 0 .. 2 kLoads - 1: those of a, then those of b
     const bool of_b = k >= kLoads;
-    const auto r = of_b ? buffer_of(p.b.codes + l_at.col0 * p.b.ld, (p.b.rows - l_at.col0) * p.b.ld)
-                        : buffer_of(p.a.codes + l_at.row0 * p.a.ld, (p.a.rows - l_at.row0) * p.a.ld);
     asm("" : "+v"(va), "+v"(vb));  // (offsets of further rows are formed anew: they would each hold a register)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(lds + l_stage + wave * 1024 + k * 8192), 16,
-                                             of_b ? vb + (k - kLoads) * 64 * ldb : va + k * 64 * lda, l_kb * 128, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(of_b ? rb : ra, (__attribute__((address_space(3))) void*)(lds + l_stage + k * kWaves * 1024),
+                                             16, of_b ? vb + (k - kLoads) * 16 * kWaves * ldb : va + k * 16 * kWaves * lda, l_off, 0, 0);
   };
   auto load_done = [&]() {
-    l_stage ^= kBigStage;
-    // (past the last block of the last tile its first one is loaded, and not used)
-    if (++l_kb == blocks) {
-      l_kb = 0;
-      if (l_tile + stride < past) {
-        l_tile += stride;
-        l_at = place_of<kBig, kBig>(p, l_tile);
+    l_stage = l_stage + kStage >= STAGES * kStage ? wave * 1024 : l_stage + kStage;
+    l_off += 64;
+    if (l_off == l_end) {  // past the last item its blocks are loaded again, and not used
+      if (l_item + stride < past) {
+        l_item += stride;
+        const Item it = item_of(l_item);
+        l_from = it.from * 128;
+        l_end = it.to * 128;
+        ra = rows_of_a(it.at);
+        rb = rows_of_b(it.at);
       }
+      l_off = l_from;
     }
   };
-  auto load = [&]() {
-#pragma unroll
-    for (int k = 0; k < 2 * kLoads; ++k) load_part(k);
-    load_done();
-  };
 
-  const int wm = wave / 4 * 128, wn = wave % 4 * 64, fr = lane % 32, fg = lane / 32;
+  const int wm = wave / WC * (32 * kMI), wn = wave % WC * 64, fr = lane % 32, fg = lane / 32;
   // Four blocks' scales of each of the lane's rows at once, as the blocks
   // before them end; rows past the end read zeros.
   const int step_a = p.a_scale_shift ? 0 : p.a.scale_ld, step_b = p.b_scale_shift ? 0 : p.b.scale_ld;
@@ -482,203 +523,106 @@ __global__ __launch_bounds__(512, 1) void k_product8_big(Product p) {
     const auto rsb = buffer_of(p.b.scales + c * p.b.scale_ld, (p.b.scale_rows - c) * p.b.scale_ld);
     asm("" : "+v"(vsa), "+v"(vsb));
 #pragma unroll
-    for (int i = 0; i < kMI; ++i) next_a[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsa, vsa + i * 32 * step_a, kb, 0);
+    for (int i = 0; i < kMI; ++i) next_a[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsa, vsa + i * 32 * step_a, kb & ~3, 0);
 #pragma unroll
-    for (int j = 0; j < kNI; ++j) next_b[j] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsb, vsb + j * 32 * step_b, kb, 0);
+    for (int j = 0; j < kNI; ++j) next_b[j] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsb, vsb + j * 32 * step_b, kb & ~3, 0);
   };
-  auto take_scales = [&]() {
+  auto take_scales = [&](int kb) {
 #pragma unroll
-    for (int i = 0; i < kMI; ++i) ea[i] = next_a[i];
+    for (int i = 0; i < kMI; ++i) ea[i] = next_a[i] >> 8 * (kb & 3);
 #pragma unroll
-    for (int j = 0; j < kNI; ++j) eb[j] = next_b[j];
+    for (int j = 0; j < kNI; ++j) eb[j] = next_b[j] >> 8 * (kb & 3);
   };
 
-  // Where the lane's two chunks of its first row are; the block's other half
-  // is 64 bytes away, up or down as the row's key says.
   const int key_a = row_key(fr), key_b = row_key(row_of_b(fr));
-  const int a0 = (wm + fr) * 128 + ((2 * fg ^ key_a) << 4), b0 = (kBig + wn + row_of_b(fr)) * 128 + ((2 * fg ^ key_b) << 4);
+  const int a0 = (wm + fr) * 64 + ((2 * fg ^ key_a) << 4), b0 = (B + wn + row_of_b(fr)) * 64 + ((2 * fg ^ key_b) << 4);
+  Fragment fa[2][kMI], fb[2][kNI];
+  auto read_part = [&](int k, int stage, int step, int to) {  // 0 .. kNI + kMI - 1
+    if (k < kNI) fb[to][k] = Step::read(lds + stage, b0, k * 2048, step);
+    else fa[to][k - kNI] = Step::read(lds + stage, a0, (k - kNI) * 2048, step);
+  };
 
-  load();
-  load_scales(l_at, 0);  // (of the first tile also where it has one block alone: no other tile is begun before)
-  loads_landed();
-  take_scales();
+  Item item = start;
+  load_scales(item.at, item.from);
+#pragma unroll
+  for (int s = 0; s < STAGES + 1 - PERIOD; ++s) {
+#pragma unroll
+    for (int k = 0; k < 2 * kLoads; ++k) load_part(k);
+    load_done();
+  }
+  take_scales(item.from);
+  loads_landed<(STAGES + 1 - 2 * PERIOD) * 2 * kLoads>();
   meet();
-  // A stage is free for the block after next when the second half, which is
-  // one turn behind the first, has read it, and has to be there when the first
-  // half reads it four turns later.  Each half loads its share between the
-  // matrix instructions of its first turn in that time: at other places the
-  // loads' issue (16 cycles each) held up reads or instructions.
-  auto turns = [&](auto which) {
-    constexpr bool second = decltype(which)::value;
-    if (second) {
-      load();
-      meet();
-    }
-    int stage = 0;
-    for (int tile = first; tile < past; tile += stride) {
-      const Place at = place_of<kBig, kBig>(p, tile);
-      v16f acc[kMI][kNI];
+  int stage = 0;
 #pragma unroll
-      for (int i = 0; i < kMI; ++i)
+  for (int k = 0; k < kNI + kMI; ++k) read_part(k, 0, 0, 0);
+  for (int t = first; t < past; t += stride) {
+    const Item next = t + stride < past ? item_of(t + stride) : item;
+    v16f acc[kMI][kNI];
 #pragma unroll
-        for (int j = 0; j < kNI; ++j)
+    for (int i = 0; i < kMI; ++i)
 #pragma unroll
-          for (int t = 0; t < 16; ++t) acc[i][j][t] = 0.0f;
-      for (int kb = 0; kb < blocks; ++kb) {
-        const bool renew = (kb & 3) == 3 || kb + 1 == blocks;
-        uint32_t sa[kMI], sb[kNI];
+      for (int j = 0; j < kNI; ++j)
 #pragma unroll
-        for (int i = 0; i < kMI; ++i) sa[i] = ea[i] >> 8 * (kb & 3);
-#pragma unroll
-        for (int j = 0; j < kNI; ++j) sb[j] = eb[j] >> 8 * (kb & 3);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          if (half == 0) {
-            if (renew) {
-              if (kb + 1 < blocks) load_scales(at, kb + 1);
-              else load_scales(place_of<kBig, kBig>(p, tile + stride < past ? tile + stride : tile), 0);
-            }
-          }
-          v8i fa[kMI], fb[kNI];
-#pragma unroll
-          for (int j = 0; j < kNI; ++j)
-            fb[j] = fragment(lds + stage + (b0 ^ half * 64), lds + stage + (b0 ^ (half * 64 + 16)), j * 4096);
-#pragma unroll
-          for (int i = 0; i < kMI; ++i)
-            fa[i] = fragment(lds + stage + (a0 ^ half * 64), lds + stage + (a0 ^ (half * 64 + 16)), i * 4096);
-          reads_landed();
-          if (second && half == 1) loads_landed();
-          meet();
-          __builtin_amdgcn_s_setprio(1);
-          const bool loads = half == (second ? 1 : 0);
-          multiply<kMI, kNI, sizeof(CT) == 4>(fa, fb, sa, sb, acc, [&](int t) {
-            if (loads) {
-              __builtin_amdgcn_sched_barrier(0);
-              load_part(t);
-              __builtin_amdgcn_sched_barrier(0);
-            }
-          });
-          if (loads) load_done();
-          __builtin_amdgcn_sched_barrier(0);
-          __builtin_amdgcn_s_setprio(0);
-          if (!second && half == 1) loads_landed();
-          meet();
-        }
-        if (renew) take_scales();
-        stage ^= kBigStage;
+        for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.0f;
+    for (int kb = item.from; kb < item.to; ++kb) {
+      const bool ends = kb + 1 == item.to, renew = (kb & 3) == 3 || ends;
+      if (renew) {
+        if (ends) load_scales(next.at, next.from);
+        else load_scales(item.at, kb + 1);
       }
-      uint8_t* own = lds + 2 * kBigStage + wave * 4096;
 #pragma unroll
-      for (int i = 0; i < kMI; ++i) store_wave<CT, kNI>(p, own, acc[i], at.row0 + wm + i * 32, at.col0 + wn, lane);
+      for (int half = 0; half < 2; ++half) {
+        const int after = stage + kStage == STAGES * kStage ? 0 : stage + kStage;
+#pragma unroll
+        for (int step = 0; step < kSteps; ++step) {
+          const bool last = step + 1 == kSteps;
+          const int now = (half * kSteps + step) & 1;
+          if (last && (PERIOD == 1 || half == 1)) {
+            reads_landed();
+            loads_landed<(STAGES - 2 * PERIOD) * 2 * kLoads>();
+            meet();
+          }
+          Step::template multiply<kMI, kNI>(fa[now], fb[now], ea, eb, acc, [&](int c) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int k = 0; k < kNI + kMI; ++k)
+              if (k * kCalls / (kNI + kMI) == c) read_part(k, last ? after : stage, last ? 0 : step + 1, now ^ 1);
+            if (last) {
+#pragma unroll
+              for (int k = 0; k < 2 * kLoads; ++k)
+                if (k * kCalls / (2 * kLoads) == c) load_part(k);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          });
+        }
+        load_done();
+        stage = after;
+      }
+      if (renew) {
+        take_scales(ends ? next.from : kb + 1);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kMI; ++i) ea[i] >>= 8;
+#pragma unroll
+        for (int j = 0; j < kNI; ++j) eb[j] >>= 8;
+      }
     }
-    if (!second) meet();
-    loads_landed();  // LDS is given back: nothing may still be on its way there
-  };
-  if (wave >= 4) turns(std::true_type{});
-  else turns(std::false_type{});
+    uint8_t* own = lds + STAGES * kStage + wave * 4096;
+    Product to = p;
+    if (PART) {
+      to.c = p.partial + (int64_t)item.split * p.a.rows * p.b.rows;
+      to.ldc = p.b.rows;
+      to.accumulate = 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kMI; ++i)
+      store_wave<std::conditional_t<PART, float, CT>, kNI>(to, own, acc[i], item.at.row0 + wm + i * 32, item.at.col0 + wn, lane);
+    item = next;
+  }
+  loads_landed();  // LDS is given back: nothing may still be on its way there
 }
-
-// Other products: tiles of 128 x 128, one a workgroup.  Loads are STAGES - 1
-// blocks ahead: four stages over eight waves of 32 x 64 where a CU gets one
-// workgroup, two over four waves of 64 x 64 where it gets two.
-constexpr int kMid = 128, kMidStage = 2 * kMid * 128;
-
-// PART: this workgroup's blocks are one of p.splits parts of the contraction,
-// whose sums go to p.partial.
-template <typename CT, bool PART, int WAVES, int STAGES>
-__global__ __launch_bounds__(64 * WAVES, 2) void k_product8_mid(Product p) {
-  constexpr int kMI = 8 / WAVES, kNI = 2, kLoads = kMid / (8 * WAVES), kAhead = STAGES - 1;
-  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int tiles = p.tiles_m * p.tiles_n, items = tiles * p.splits, per = (items + 7) / 8;
-  const int item = blockIdx.x % 8 * per + blockIdx.x / 8;
-  if (blockIdx.x / 8 >= (unsigned)per || item >= items) return;
-  const int split = item / tiles;
-  const Place at = place_of<kMid, kMid>(p, item - split * tiles);
-  const int from = split * p.split_blocks, blocks = from + p.split_blocks < p.a.blocks ? from + p.split_blocks : p.a.blocks;
-  const int lr = wave * 8 + lane / 8, lda = (int)p.a.ld, ldb = (int)p.b.ld;
-  const int va = lr * lda + ((lane % 8) ^ row_key(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key(lr)) * 16;
-  const auto ra = buffer_of(p.a.codes + at.row0 * p.a.ld, (p.a.rows - at.row0) * p.a.ld);
-  const auto rb = buffer_of(p.b.codes + at.col0 * p.b.ld, (p.b.rows - at.col0) * p.b.ld);
-  auto load = [&](int kb) {
-    uint8_t* to = lds + (kb & (STAGES - 1)) * kMidStage + wave * 1024;
-#pragma unroll
-    for (int k = 0; k < kLoads; ++k)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (__attribute__((address_space(3))) void*)(to + k * WAVES * 1024), 16,
-                                               va + k * 8 * WAVES * lda, kb * 128, 0, 0);
-#pragma unroll
-    for (int k = 0; k < kLoads; ++k)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (__attribute__((address_space(3))) void*)(to + kMid * 128 + k * WAVES * 1024), 16,
-                                               vb + k * 8 * WAVES * ldb, kb * 128, 0, 0);
-  };
-  const int wm = wave / 2 * (32 * kMI), wn = wave % 2 * 64, fr = lane % 32, fg = lane / 32;
-  const int64_t sr = at.row0 >> p.a_scale_shift, sc = at.col0 >> p.b_scale_shift;
-  const auto rsa = buffer_of(p.a.scales + sr * p.a.scale_ld, (p.a.scale_rows - sr) * p.a.scale_ld);
-  const auto rsb = buffer_of(p.b.scales + sc * p.b.scale_ld, (p.b.scale_rows - sc) * p.b.scale_ld);
-  const int step_a = p.a_scale_shift ? 0 : p.a.scale_ld, step_b = p.b_scale_shift ? 0 : p.b.scale_ld;
-  const int vsa = ((wm + fr) >> p.a_scale_shift) * p.a.scale_ld, vsb = ((wn + row_of_b(fr)) >> p.b_scale_shift) * p.b.scale_ld;
-  uint32_t ea[kMI], eb[kNI], next_a[kMI], next_b[kNI];
-  auto load_scales = [&](int kb) {
-#pragma unroll
-    for (int i = 0; i < kMI; ++i) next_a[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsa, vsa + i * 32 * step_a, kb, 0);
-#pragma unroll
-    for (int j = 0; j < kNI; ++j) next_b[j] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsb, vsb + j * 32 * step_b, kb, 0);
-  };
-  const int key_a = row_key(fr), key_b = row_key(row_of_b(fr));
-  const int a0 = (wm + fr) * 128 + ((2 * fg ^ key_a) << 4), b0 = (kMid + wn + row_of_b(fr)) * 128 + ((2 * fg ^ key_b) << 4);
-  v16f acc[kMI][kNI];
-#pragma unroll
-  for (int i = 0; i < kMI; ++i)
-#pragma unroll
-    for (int j = 0; j < kNI; ++j)
-#pragma unroll
-      for (int t = 0; t < 16; ++t) acc[i][j][t] = 0.0f;
-  if (from < blocks) {
-    load_scales(from & ~3);
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k)
-      if (from + k < blocks) load(from + k);
-  }
-  for (int kb = from; kb < blocks; ++kb) {
-    // the loads of this block have landed: at most those of the blocks after it are on their way
-    if (kb + kAhead <= blocks) loads_landed<(kAhead - 1) * 2 * kLoads>();
-    else loads_landed();
-    meet();
-    if ((kb & 3) == 0 || kb == from) {
-#pragma unroll
-      for (int i = 0; i < kMI; ++i) ea[i] = next_a[i];
-#pragma unroll
-      for (int j = 0; j < kNI; ++j) eb[j] = next_b[j];
-    }
-    if ((kb & 3) == 3 && kb + 1 < blocks) load_scales(kb + 1);
-    if (kb + kAhead < blocks) load(kb + kAhead);
-    const uint8_t* stage = lds + (kb & (STAGES - 1)) * kMidStage;
-    uint32_t sa[kMI], sb[kNI];
-#pragma unroll
-    for (int i = 0; i < kMI; ++i) sa[i] = ea[i] >> 8 * (kb & 3);
-#pragma unroll
-    for (int j = 0; j < kNI; ++j) sb[j] = eb[j] >> 8 * (kb & 3);
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      v8i fa[kMI], fb[kNI];
-#pragma unroll
-      for (int j = 0; j < kNI; ++j) fb[j] = fragment(stage + (b0 ^ half * 64), stage + (b0 ^ (half * 64 + 16)), j * 4096);
-#pragma unroll
-      for (int i = 0; i < kMI; ++i) fa[i] = fragment(stage + (a0 ^ half * 64), stage + (a0 ^ (half * 64 + 16)), i * 4096);
-      multiply<kMI, kNI, sizeof(CT) == 4>(fa, fb, sa, sb, acc, [](int) {});
-    }
-  }
-  meet();  // the stages become the waves' own
-  uint8_t* own = lds + wave * 4096;
-  Product to = p;
-  if (PART) {
-    to.c = p.partial + (int64_t)split * p.a.rows * p.b.rows;
-    to.ldc = p.b.rows;
-    to.accumulate = 0;
-  }
-#pragma unroll
-  for (int i = 0; i < kMI; ++i) store_wave<std::conditional_t<PART, float, CT>, kNI>(to, own, acc[i], at.row0 + wm + i * 32, at.col0 + wn, lane);
-}
+constexpr int kBig = 256, kMid = 128;
 
 // c from the parts' sums, added in their order: four columns a thread.
 template <typename CT>
@@ -796,10 +740,10 @@ __global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
     } else {
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const v8bf wb = widened(fb, k, scale_of(eb));
+        const v8bf wb = widened(fb[2 * k], fb[2 * k + 1], scale_of(eb));
 #pragma unroll
         for (int i = 0; i < MI; ++i)
-          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, widened(fa[i], k, scale_of(ea[i])), acc[i], 0, 0, 0);
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, widened(fa[i][2 * k], fa[i][2 * k + 1], scale_of(ea[i])), acc[i], 0, 0, 0);
       }
     }
   }
@@ -842,16 +786,15 @@ constexpr int64_t kMostCols = INT64_C(1) << 22;  // a tile's rows stay within 2^
 // parts of at least four blocks.
 constexpr int64_t kFew = 64, kFewWhole = 16;  // rows; of which quantized on the way
 struct Shape {
-  bool few, big, shared;  // shared: two workgroups on a CU
+  bool few, big;
   int32_t splits, split_blocks;
 };
 Shape shape_of(int64_t m, int64_t n, int64_t k) {
   const int64_t blocks = up(k, kBlock8) / kBlock8;
-  Shape s = {m <= kFew && blocks > 0, false, false, 1, (int32_t)blocks};
+  Shape s = {m <= kFew && blocks > 0, false, 1, (int32_t)blocks};
   if (s.few) return s;
   s.big = blocks > 0 && (up(m, kBig) / kBig) * (up(n, kBig) / kBig) >= 128;
   const int64_t tiles = (up(m, kMid) / kMid) * (up(n, kMid) / kMid);
-  s.shared = tiles > 256;
   if (!s.big && tiles > 0 && tiles <= 128 && blocks >= 8) {
     const int64_t parts = std::min<int64_t>(256 / tiles, blocks / 4);
     s.split_blocks = (int32_t)((blocks + parts - 1) / parts);
@@ -1040,23 +983,22 @@ int32_t launch_product(const mtdao_matrix8& a, const mtdao_matrix8& b, void* c, 
   p.splits = shape.splits;
   p.split_blocks = shape.split_blocks;
   p.partial = static_cast<float*>(workspace);
-  auto go = [&](auto kernel, int tile, unsigned threads, int bytes, int64_t most) {
+  auto go = [&](auto kernel, int tile, int stages) {
     p.tiles_m = (int32_t)(up(a.rows, tile) / tile);
     p.tiles_n = (int32_t)(up(b.rows, tile) / tile);
     const int64_t items = (int64_t)p.tiles_m * p.tiles_n * p.splits;
-    if (items > INT64_C(0x3fffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "c has more tiles than one launch takes");
+    if (items > INT64_C(0x3fffffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "c has more tiles than one launch takes");
+    const int bytes = stages * 2 * tile * 64 + 8 * 4096;
     const int32_t r = allow_lds(reinterpret_cast<const void*>(kernel), bytes, e);
     if (r != MTDAO_OK) return r;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(up(items, 8), most)), dim3(threads), bytes, st, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(up(items, 8), 256)), dim3(512), bytes, st, p);
     return (int32_t)MTDAO_OK;
   };
   auto pick = [&](auto ct) {
     using CT = decltype(ct);
-    if (shape.big) return go(k_product8_big<CT>, kBig, 512, kBigLds, 256);
-    const int64_t most = INT64_C(0x3fffff);
-    if (shape.splits == 1 && shape.shared) return go(k_product8_mid<CT, false, 4, 2>, kMid, 256, 2 * kMidStage, most);
-    if (shape.splits == 1) return go(k_product8_mid<CT, false, 8, 4>, kMid, 512, 4 * kMidStage, most);
-    const int32_t done = go(k_product8_mid<CT, true, 8, 4>, kMid, 512, 4 * kMidStage, most);
+    if (shape.big) return go(k_product8_tiles<CT, false, kBig, 2, 4, 4, 1>, kBig, 4);
+    if (shape.splits == 1) return go(k_product8_tiles<CT, false, kMid, 4, 2, 8, 2>, kMid, 8);
+    const int32_t done = go(k_product8_tiles<CT, true, kMid, 4, 2, 8, 2>, kMid, 8);
     if (done != MTDAO_OK) return done;
     const int64_t quads = p.a.rows * ((p.b.rows + 3) / 4);
     hipLaunchKernelGGL(k_product8_join<CT>, dim3((unsigned)((quads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p);
