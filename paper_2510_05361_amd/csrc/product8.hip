@@ -252,18 +252,14 @@ struct Product {
   float* partial;                // [splits][rows of a][rows of b] with more than one part
 };
 
-// Half a block of a tile in LDS: rows of 64 bytes, whose four 16-byte chunks are
-// at the places that their number and the row's key give.  A 16-byte read of a
-// wave takes 16 lanes at once, which have to lie in different ones of the 16
-// such places of the 64 banks: four rows of four, told apart by the row's last
-// two bits, so the key has the next two.  (With 128-byte rows and their last
-// three bits as the key half of the reads' cycles were conflicts.)
-__device__ __forceinline__ int row_key(int row) { return (row >> 2) & 3; }
-
-// A row of 128 bytes of results on their way to memory: the same for eight
-// chunks, two rows to the banks.
-__device__ __forceinline__ int chunk_key(int row) { return (row >> 1) & 7; }
-__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ chunk_key(row)) << 4); }
+// A 128-byte row in LDS: its eight 16-byte chunks, each at the place that its
+// number and the row's key give.  A 16-byte read of a wave takes 16 lanes at
+// once, which have to lie in different ones of the 16 such places of the 64
+// banks: two rows of eight, told apart by the row's last bit, so the key has
+// the next three.  (With the last three bits as the key half of the reads'
+// cycles were conflicts.)
+__device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ row_key(row)) << 4); }
 
 // The row of b's fragment that the instruction's row r takes: results of a lane
 // are rows 8 q + 4 h + t, so these are sixteen consecutive columns of c.
@@ -396,7 +392,7 @@ __device__ __forceinline__ void store_rows(const Product& p, uint8_t* own, const
   asm volatile("" ::: "memory");
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const int r = q * 8 + lane / 8, chunk = (lane % 8) ^ chunk_key(r);
+    const int r = q * 8 + lane / 8, chunk = (lane % 8) ^ row_key(r);
     float v[kPer];
     load_full<kPer>(reinterpret_cast<const CT*>(own + r * 128 + (lane % 8) * 16), v);
     const int64_t row = row0 + r, col = col0 + chunk * kPer, left = p.b.rows - col;
@@ -452,23 +448,25 @@ __device__ __forceinline__ Item item_at(const Product& p, int tiles, int t) {
 // from item to item: tiles, or with PART the p.splits parts of the contraction
 // of each, whose sums go to p.partial.
 //
-// LDS holds STAGES half blocks of each side, loaded straight into it and running
-// on into the next item.  A wave reads a step's fragments while the matrix cores
-// work on the step before, so it needs others only when a stage changes hands:
-// once in PERIOD half blocks, before the last step, when the last fragments are
-// in registers, all meet; then the stages read so far are free to be loaded,
-// and those to be read until the next time are there.  Reads and loads are
-// issued between the matrix instructions, one half block's loads in every half
-// block: a 1 KiB load takes 16 cycles to issue, which holds up a wave's matrix
-// instructions where several come together.
-template <typename CT, bool PART, int B, int WR, int WC, int STAGES, int PERIOD>
+// LDS holds STAGES blocks of each side, loaded straight into it and running on
+// into the next item.  (Loads take whole 128-byte lines: of half lines the L2
+// gives half as many bytes, 65 GB/s a CU in place of 120.)  A wave reads a
+// step's fragments while the matrix cores work on the step before, so it needs
+// others only once a block: before the last step, when the block's last
+// fragments are in registers, all meet; then its stage is free to be loaded,
+// and the next block's is there.  Reads and loads are issued between the matrix
+// instructions; a 1 KiB load takes 16 cycles to issue, which holds up a wave's
+// matrix instructions where several come together, so with more than two stages
+// a block's loads are spread over its halves.
+template <typename CT, bool PART, int B, int WR, int WC, int STAGES>
 __global__ __launch_bounds__(64 * WR * WC, 1) void k_product8_tiles(Product p) {
-  constexpr int kWaves = WR * WC, kMI = B / WR / 32, kNI = B / WC / 32, kLoads = B / (16 * kWaves), kStage = 2 * B * 64;
+  constexpr int kWaves = WR * WC, kMI = B / WR / 32, kNI = B / WC / 32, kLoads = B / (8 * kWaves), kStage = 2 * B * 128;
+  constexpr bool kSpread = STAGES > 2;
   using Step = Step8<sizeof(CT) == 4>;
   using Fragment = typename Step::Fragment;
   constexpr int kSteps = Step::kSteps, kCalls = Step::template calls<kMI, kNI>;
   static_assert(kNI == 2 && 128 % (32 * kMI) == 0, "a wave has 64 columns, and its rows share their block of 128 rows");
-  static_assert(STAGES >= 2 * PERIOD && (PERIOD == 1 || PERIOD == 2) && kLoads > 0, "stages");
+  static_assert((STAGES * kStage & (STAGES * kStage - 1)) == 0, "the stages' bytes are a power of two");
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int tiles = p.tiles_m * p.tiles_n, items = PART ? tiles * p.splits : tiles, per = (items + 7) / 8, xcd = blockIdx.x % 8;
@@ -477,11 +475,11 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_product8_tiles(Product p) {
   if (first >= past) return;
   auto item_of = [&](int t) { return item_at<PART, B>(p, tiles, t); };
 
-  // A wave loads sixteen rows at once: lane l the chunk that belongs at place l
-  // % 4 of row l / 4.  Rows go into the lane's offset, which the hardware
-  // holds against the matrix's end; the half block into the scalar offset.
-  const int lr = wave * 16 + lane / 4, lda = (int)p.a.ld, ldb = (int)p.b.ld;
-  int va = lr * lda + ((lane % 4) ^ row_key(lr)) * 16, vb = lr * ldb + ((lane % 4) ^ row_key(lr)) * 16;
+  // A wave loads eight rows at once: lane l the chunk that belongs at place l
+  // % 8 of row l / 8.  Rows go into the lane's offset, which the hardware
+  // holds against the matrix's end; the block into the scalar offset.
+  const int lr = wave * 8 + lane / 8, lda = (int)p.a.ld, ldb = (int)p.b.ld;
+  int va = lr * lda + ((lane % 8) ^ row_key(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key(lr)) * 16;
   // What is loaded next: the item's rows, bytes into them, the last of these, and the stage's place.
   int l_item = first, l_stage = wave * 1024;
   const Item start = item_of(first);
@@ -493,11 +491,11 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_product8_tiles(Product p) {
     const bool of_b = k >= kLoads;
     asm("" : "+v"(va), "+v"(vb));  // (offsets of further rows are formed anew: they would each hold a register)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(of_b ? rb : ra, (__attribute__((address_space(3))) void*)(lds + l_stage + k * kWaves * 1024),
-                                             16, of_b ? vb + (k - kLoads) * 16 * kWaves * ldb : va + k * 16 * kWaves * lda, l_off, 0, 0);
+                                             16, of_b ? vb + (k - kLoads) * 8 * kWaves * ldb : va + k * 8 * kWaves * lda, l_off, 0, 0);
   };
   auto load_done = [&]() {
-    l_stage = l_stage + kStage >= STAGES * kStage ? wave * 1024 : l_stage + kStage;
-    l_off += 64;
+    l_stage = (l_stage + kStage) & (STAGES * kStage - 1);
+    l_off += 128;
     if (l_off == l_end) {  // past the last item its blocks are loaded again, and not used
       if (l_item + stride < past) {
         l_item += stride;
@@ -535,27 +533,30 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_product8_tiles(Product p) {
   };
 
   const int key_a = row_key(fr), key_b = row_key(row_of_b(fr));
-  const int a0 = (wm + fr) * 64 + ((2 * fg ^ key_a) << 4), b0 = (B + wn + row_of_b(fr)) * 64 + ((2 * fg ^ key_b) << 4);
+  const int a0 = (wm + fr) * 128 + ((2 * fg ^ key_a) << 4), b0 = (B + wn + row_of_b(fr)) * 128 + ((2 * fg ^ key_b) << 4);
   Fragment fa[2][kMI], fb[2][kNI];
-  auto read_part = [&](int k, int stage, int step, int to) {  // 0 .. kNI + kMI - 1
-    if (k < kNI) fb[to][k] = Step::read(lds + stage, b0, k * 2048, step);
-    else fa[to][k - kNI] = Step::read(lds + stage, a0, (k - kNI) * 2048, step);
+  auto read_part = [&](int k, int stage, int half, int step, int to) {  // 0 .. kNI + kMI - 1
+    if (k < kNI) fb[to][k] = Step::read(lds + stage, b0 ^ half * 64, k * 4096, step);
+    else fa[to][k - kNI] = Step::read(lds + stage, a0 ^ half * 64, (k - kNI) * 4096, step);
   };
 
   Item item = start;
   load_scales(item.at, item.from);
 #pragma unroll
-  for (int s = 0; s < STAGES + 1 - PERIOD; ++s) {
+  for (int s = 0; s < STAGES; ++s) {
+    // (spread: the last one's second half follows in the first block)
+    const int parts = kSpread && s + 1 == STAGES ? kLoads : 2 * kLoads;
 #pragma unroll
-    for (int k = 0; k < 2 * kLoads; ++k) load_part(k);
-    load_done();
+    for (int k = 0; k < 2 * kLoads; ++k)
+      if (k < parts) load_part(k);
+    if (parts == 2 * kLoads) load_done();
   }
   take_scales(item.from);
-  loads_landed<(STAGES + 1 - 2 * PERIOD) * 2 * kLoads>();
+  loads_landed<(STAGES - 1) * 2 * kLoads - (kSpread ? kLoads : 0)>();
   meet();
   int stage = 0;
 #pragma unroll
-  for (int k = 0; k < kNI + kMI; ++k) read_part(k, 0, 0, 0);
+  for (int k = 0; k < kNI + kMI; ++k) read_part(k, 0, 0, 0, 0);
   for (int t = first; t < past; t += stride) {
     const Item next = t + stride < past ? item_of(t + stride) : item;
     v16f acc[kMI][kNI];
@@ -571,34 +572,36 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_product8_tiles(Product p) {
         if (ends) load_scales(next.at, next.from);
         else load_scales(item.at, kb + 1);
       }
+      const int after = (stage + kStage) & (STAGES * kStage - 1);
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const int after = stage + kStage == STAGES * kStage ? 0 : stage + kStage;
 #pragma unroll
         for (int step = 0; step < kSteps; ++step) {
-          const bool last = step + 1 == kSteps;
+          const bool ends_half = step + 1 == kSteps, ends_block = ends_half && half == 1;
           const int now = (half * kSteps + step) & 1;
-          if (last && (PERIOD == 1 || half == 1)) {
+          if (ends_block) {
             reads_landed();
-            loads_landed<(STAGES - 2 * PERIOD) * 2 * kLoads>();
+            loads_landed<(STAGES - 2) * 2 * kLoads>();
             meet();
           }
           Step::template multiply<kMI, kNI>(fa[now], fb[now], ea, eb, acc, [&](int c) {
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < kNI + kMI; ++k)
-              if (k * kCalls / (kNI + kMI) == c) read_part(k, last ? after : stage, last ? 0 : step + 1, now ^ 1);
-            if (last) {
+              if (k * kCalls / (kNI + kMI) == c)
+                read_part(k, ends_block ? after : stage, ends_half ? half ^ 1 : half, ends_half ? 0 : step + 1, now ^ 1);
 #pragma unroll
-              for (int k = 0; k < 2 * kLoads; ++k)
-                if (k * kCalls / (2 * kLoads) == c) load_part(k);
+            for (int k = 0; k < 2 * kLoads; ++k) {
+              if (!kSpread && ends_block && k * kCalls / (2 * kLoads) == c) load_part(k);
+              // the first half at the block's end, the second in the next block
+              if (kSpread && ends_half && half == (k < kLoads) && (k % kLoads) * kCalls / kLoads == c) load_part(k);
             }
             __builtin_amdgcn_sched_barrier(0);
           });
+          if (ends_half && half == (kSpread ? 0 : 1)) load_done();
         }
-        load_done();
-        stage = after;
       }
+      stage = after;
       if (renew) {
         take_scales(ends ? next.from : kb + 1);
       } else {
@@ -988,7 +991,7 @@ int32_t launch_product(const mtdao_matrix8& a, const mtdao_matrix8& b, void* c, 
     p.tiles_n = (int32_t)(up(b.rows, tile) / tile);
     const int64_t items = (int64_t)p.tiles_m * p.tiles_n * p.splits;
     if (items > INT64_C(0x3fffffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "c has more tiles than one launch takes");
-    const int bytes = stages * 2 * tile * 64 + 8 * 4096;
+    const int bytes = stages * 2 * tile * 128 + 8 * 4096;
     const int32_t r = allow_lds(reinterpret_cast<const void*>(kernel), bytes, e);
     if (r != MTDAO_OK) return r;
     hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(up(items, 8), 256)), dim3(512), bytes, st, p);
@@ -996,9 +999,9 @@ int32_t launch_product(const mtdao_matrix8& a, const mtdao_matrix8& b, void* c, 
   };
   auto pick = [&](auto ct) {
     using CT = decltype(ct);
-    if (shape.big) return go(k_product8_tiles<CT, false, kBig, 2, 4, 4, 1>, kBig, 4);
-    if (shape.splits == 1) return go(k_product8_tiles<CT, false, kMid, 4, 2, 8, 2>, kMid, 8);
-    const int32_t done = go(k_product8_tiles<CT, true, kMid, 4, 2, 8, 2>, kMid, 8);
+    if (shape.big) return go(k_product8_tiles<CT, false, kBig, 2, 4, 2>, kBig, 2);
+    if (shape.splits == 1) return go(k_product8_tiles<CT, false, kMid, 4, 2, 4>, kMid, 4);
+    const int32_t done = go(k_product8_tiles<CT, true, kMid, 4, 2, 4>, kMid, 4);
     if (done != MTDAO_OK) return done;
     const int64_t quads = p.a.rows * ((p.b.rows + 3) / 4);
     hipLaunchKernelGGL(k_product8_join<CT>, dim3((unsigned)((quads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p);
