@@ -163,19 +163,22 @@ int32_t mtdao_peri_norm_backward(const mtdao_peri_norm_args* a, void* workspace,
  * A matrix of 8-bit blocks, rows x cols.  Blocks are 1 x 128 (scale_rows =
  * 1) or 128 x 128 (scale_rows = 128), the last ones short. */
 typedef struct mtdao_matrix8 {
-  uint8_t* codes;      /* [rows][ld], 16-byte aligned; zeros in columns cols..ld-1     */
-  uint8_t* scales;     /* [ceil(rows / scale_rows)][scale_ld], 4-byte aligned          */
+  uint8_t* codes;      /* [rows][ld], 16-byte aligned; zeros past cols up to the next  */
+                       /* multiple of 128, nothing after it                            */
+  uint8_t* scales;     /* [ceil(blocks of a row / 4)][ceil(rows / scale_rows)][4]:     */
+                       /* rows of four blocks' bytes together, 4-byte aligned          */
   int64_t rows, cols;
-  int64_t ld;          /* cols rounded up to a multiple of 128                         */
-  int64_t scale_ld;    /* ld / 128 rounded up to a multiple of 4                       */
+  int64_t ld;          /* a multiple of 128 from cols on; odd multiples load fastest   */
+  int64_t scale_ld;    /* bytes of four blocks' scales: 4 ceil(rows / scale_rows)      */
   int32_t scale_rows;  /* 1 or 128                                                     */
 } mtdao_matrix8;
 
 /* x [rows][cols] (dtype, row stride ld elements) as 8-bit blocks, into q
  * and/or, transposed, into qt (qt->rows = cols; either may be NULL).  q and
  * qt have the same scale_rows; with 128 both hold the same values, with 1
- * the blocks of qt lie along the rows of x.  Columns past cols and scale
- * bytes past the last block are written too (codes 0, scale 1). */
+ * the blocks of qt lie along the rows of x.  Columns past cols up to a whole
+ * block and scale bytes past the last block are written too (codes 0, scale
+ * 1). */
 int32_t mtdao_quantize8(const void* x, int32_t dtype, int64_t ld, const mtdao_matrix8* q, const mtdao_matrix8* qt,
                         void* hip_stream);
 

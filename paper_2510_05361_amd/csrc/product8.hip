@@ -25,20 +25,24 @@ struct Mat {
   uint8_t* codes;
   uint8_t* scales;
   int64_t rows, ld, scale_rows;  // scale_rows: rows of scales
-  int32_t blocks, scale_ld;      // blocks of a row, and bytes from row to row of the scales
+  int64_t scale_ld;              // bytes from four blocks' scales to the next four's: 4 scale_rows
+  int32_t blocks;                // blocks of a row
 };
+__device__ __forceinline__ uint8_t* scale_at(const Mat& m, int64_t scale_row, int block) {
+  return m.scales + (block >> 2) * m.scale_ld + scale_row * 4 + (block & 3);
+}
 
 // --------------------------------------------------------------- quantizers
 
 constexpr int kThreads = 256;
 constexpr int kE = 8;  // elements of a thread's vector: 16 threads hold a block
 
-// Blocks along the rows: sixteen of a workgroup, in the order of the scales.
+// Blocks along the rows: four of each of four rows a workgroup, a row a wave.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_quantize8_rows(const T* x, int64_t ld, int64_t cols, Mat q) {
-  const int64_t b = (int64_t)blockIdx.x * (kThreads / 16) + threadIdx.x / 16;
-  const int64_t row = b / q.scale_ld;
-  const int kb = (int)(b - row * q.scale_ld), e = kb * kBlock8 + (int)(threadIdx.x % 16) * kE;
+__global__ __launch_bounds__(kThreads) void k_quantize8_rows(const T* x, int64_t ld, int64_t cols, int groups, Mat q) {
+  const int64_t four = blockIdx.x / (unsigned)groups;
+  const int64_t row = four * 4 + threadIdx.x / 64;
+  const int kb = (int)(blockIdx.x - four * groups) * 4 + (int)threadIdx.x % 64 / 16, e = kb * kBlock8 + (int)(threadIdx.x % 16) * kE;
   float a[kE], most = 0.0f;
   const bool live = row < q.rows && kb < q.blocks;
   const int64_t n = live ? cols - e : 0;
@@ -63,7 +67,7 @@ __global__ __launch_bounds__(kThreads) void k_quantize8_rows(const T* x, int64_t
     uint2 c = {codes_of(a[0], a[1], a[2], a[3]), codes_of(a[4], a[5], a[6], a[7])};
     *reinterpret_cast<uint2*>(q.codes + row * q.ld + e) = c;
   }
-  if (row < q.rows && threadIdx.x % 16 == 0) q.scales[row * q.scale_ld + kb] = (uint8_t)byte;
+  if (row < q.rows && threadIdx.x % 16 == 0) *scale_at(q, row, kb) = (uint8_t)byte;
 }
 
 // A tile of 128 x 128: a thread holds four rows of eight columns, so that it
@@ -167,18 +171,16 @@ __global__ __launch_bounds__(kTileThreads) void k_quantize8_tile(const T* x, int
         *reinterpret_cast<uint2*>(q.codes + (row0 + r4 + i) * q.ld + col0 + c8) = c;
       }
     }
-    const bool last = blockIdx.x + 1 == gridDim.x;
-    const int bytes = last ? q.scale_ld - (int)blockIdx.x : 1;  // the row's unused bytes too
+    // (the last block's thread writes the unused bytes of its four too)
+    const int past = blockIdx.x + 1 == gridDim.x ? (blockIdx.x & ~3u) + 4 : blockIdx.x + 1;
     if constexpr (SQUARE) {
-      if (threadIdx.x < (unsigned)bytes)
-        q.scales[(int64_t)blockIdx.y * q.scale_ld + blockIdx.x + threadIdx.x] = threadIdx.x == 0 ? (uint8_t)row_byte[0] : 127;
+      if (threadIdx.x == 0)
+        for (int k = blockIdx.x; k < past; ++k) *scale_at(q, blockIdx.y, k) = k == (int)blockIdx.x ? (uint8_t)row_byte[0] : 127;
     } else if (threadIdx.x % 16 == 0) {
 #pragma unroll
       for (int i = 0; i < kRows; ++i)
-        if (i < in_rows) {
-          uint8_t* s = q.scales + (row0 + r4 + i) * q.scale_ld + blockIdx.x;
-          for (int k = 0; k < bytes; ++k) s[k] = k == 0 ? (uint8_t)row_byte[i] : 127;
-        }
+        if (i < in_rows)
+          for (int k = blockIdx.x; k < past; ++k) *scale_at(q, row0 + r4 + i, k) = k == (int)blockIdx.x ? (uint8_t)row_byte[i] : 127;
     }
   }
   if (qt.codes) {
@@ -194,18 +196,15 @@ __global__ __launch_bounds__(kTileThreads) void k_quantize8_tile(const T* x, int
       *reinterpret_cast<uint32_t*>(turned + (c8 + t) * kBlock8 + ((chunk ^ (c8 / 8 & 7)) << 4) + in_chunk) =
           codes_of(s[0], s[1], s[2], s[3]);
     }
-    const bool last = blockIdx.y + 1 == gridDim.y;
-    const int bytes = last ? qt.scale_ld - (int)blockIdx.y : 1;
+    const int past = blockIdx.y + 1 == gridDim.y ? (blockIdx.y & ~3u) + 4 : blockIdx.y + 1;
     if constexpr (SQUARE) {
-      if (threadIdx.x < (unsigned)bytes)
-        qt.scales[(int64_t)blockIdx.x * qt.scale_ld + blockIdx.y + threadIdx.x] = threadIdx.x == 0 ? (uint8_t)col_byte[0] : 127;
+      if (threadIdx.x == 0)
+        for (int k = blockIdx.y; k < past; ++k) *scale_at(qt, blockIdx.x, k) = k == (int)blockIdx.y ? (uint8_t)col_byte[0] : 127;
     } else if (threadIdx.x < 16) {
 #pragma unroll
       for (int t = 0; t < kE; ++t)
-        if (t < nc) {
-          uint8_t* s = qt.scales + (col0 + c8 + t) * qt.scale_ld + blockIdx.y;
-          for (int k = 0; k < bytes; ++k) s[k] = k == 0 ? (uint8_t)col_byte[t] : 127;
-        }
+        if (t < nc)
+          for (int k = blockIdx.y; k < past; ++k) *scale_at(qt, col0 + c8 + t, k) = k == (int)blockIdx.y ? (uint8_t)col_byte[t] : 127;
     }
     __syncthreads();
 #pragma unroll
@@ -512,18 +511,18 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_product8_tiles(Product p) {
   const int wm = wave / WC * (32 * kMI), wn = wave % WC * 64, fr = lane % 32, fg = lane / 32;
   // Four blocks' scales of each of the lane's rows at once, as the blocks
   // before them end; rows past the end read zeros.
-  const int step_a = p.a_scale_shift ? 0 : p.a.scale_ld, step_b = p.b_scale_shift ? 0 : p.b.scale_ld;
-  int vsa = ((wm + fr) >> p.a_scale_shift) * p.a.scale_ld, vsb = ((wn + row_of_b(fr)) >> p.b_scale_shift) * p.b.scale_ld;
+  const int step_a = p.a_scale_shift ? 0 : 32 * 4, step_b = p.b_scale_shift ? 0 : 32 * 4;
+  int vsa = ((wm + fr) >> p.a_scale_shift) * 4, vsb = ((wn + row_of_b(fr)) >> p.b_scale_shift) * 4;
   uint32_t ea[kMI], eb[kNI], next_a[kMI], next_b[kNI];
   auto load_scales = [&](const Place& at, int kb) {
     const int64_t r = at.row0 >> p.a_scale_shift, c = at.col0 >> p.b_scale_shift;
-    const auto rsa = buffer_of(p.a.scales + r * p.a.scale_ld, (p.a.scale_rows - r) * p.a.scale_ld);
-    const auto rsb = buffer_of(p.b.scales + c * p.b.scale_ld, (p.b.scale_rows - c) * p.b.scale_ld);
+    const auto rsa = buffer_of(scale_at(p.a, r, kb & ~3), (p.a.scale_rows - r) * 4);
+    const auto rsb = buffer_of(scale_at(p.b, c, kb & ~3), (p.b.scale_rows - c) * 4);
     asm("" : "+v"(vsa), "+v"(vsb));
 #pragma unroll
-    for (int i = 0; i < kMI; ++i) next_a[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsa, vsa + i * 32 * step_a, kb & ~3, 0);
+    for (int i = 0; i < kMI; ++i) next_a[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsa, vsa + i * step_a, 0, 0);
 #pragma unroll
-    for (int j = 0; j < kNI; ++j) next_b[j] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsb, vsb + j * 32 * step_b, kb & ~3, 0);
+    for (int j = 0; j < kNI; ++j) next_b[j] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(rsb, vsb + j * step_b, 0, 0);
   };
   auto take_scales = [&](int kb) {
 #pragma unroll
@@ -663,8 +662,8 @@ __global__ __launch_bounds__(kThreads) void k_product8_join(Product p) {
 struct Few {
   const void* x;
   int64_t ldx, m, k;
-  const uint8_t* x_scales;
-  int32_t x_scale_ld, x_scale_shift;
+  Mat a;  // a's blocks, or nothing
+  int32_t a_scale_shift;
   Mat b;
   int32_t b_scale_shift, accumulate;
   void* c;
@@ -679,14 +678,14 @@ __global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
   const int64_t col0 = (int64_t)blockIdx.x * 16, br = col0 + r < p.b.rows ? col0 + r : p.b.rows - 1;
   const uint8_t* b = p.b.codes + br * p.b.ld + g * 32;
-  const uint8_t* bs = p.b.scales + (br >> p.b_scale_shift) * p.b.scale_ld;
+  const int64_t bs = br >> p.b_scale_shift;
   const XT* a[MI];
-  const uint8_t* as[MI];
+  int64_t as[MI];
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int64_t ar = i * 16 + r < p.m ? i * 16 + r : p.m - 1;
     a[i] = reinterpret_cast<const XT*>(p.x) + ar * p.ldx + g * 32;
-    as[i] = kCodes ? p.x_scales + (ar >> p.x_scale_shift) * p.x_scale_ld : nullptr;
+    as[i] = ar >> p.a_scale_shift;
   }
   v4f acc[MI];
 #pragma unroll
@@ -695,7 +694,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
   for (int kb = wave; kb < p.b.blocks; kb += WAVES) {
     const int e = kb * kBlock8;
     const v4i b_lo = *reinterpret_cast<const v4i*>(b + e), b_hi = *reinterpret_cast<const v4i*>(b + e + 16);
-    const uint32_t eb = bs[kb];
+    const uint32_t eb = *scale_at(p.b, bs, kb);
     v8i fa[MI];
     uint32_t ea[MI];
     if constexpr (kCodes) {
@@ -703,7 +702,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
       for (int i = 0; i < MI; ++i) {
         const v4i lo = *reinterpret_cast<const v4i*>(a[i] + e), hi = *reinterpret_cast<const v4i*>(a[i] + e + 16);
         fa[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        ea[i] = as[i][kb];
+        ea[i] = *scale_at(p.a, as[i], kb);
       }
     } else {
       float x[4][kE], most = 0.0f;
@@ -814,11 +813,12 @@ int32_t check_matrix(const mtdao_matrix8& q, const char* name, std::string* e) {
   if (q.rows < 0 || q.cols < 0) return fail(e, MTDAO_ERR_INVALID_ARG, "%s: rows or cols < 0", name);
   if (q.cols > kMostCols) return fail(e, MTDAO_ERR_INVALID_ARG, "%s: cols exceed 2^22", name);
   if (q.rows > INT64_C(0x7fffffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "%s: rows exceed 2^31", name);
-  if (q.ld != up(q.cols, kBlock8)) return fail(e, MTDAO_ERR_INVALID_ARG, "%s: ld is not cols rounded up to 128", name);
-  if (q.scale_ld != up(q.ld / kBlock8, 4))
-    return fail(e, MTDAO_ERR_INVALID_ARG, "%s: scale_ld is not ld / 128 rounded up to 4", name);
+  if (q.ld % kBlock8 != 0 || q.ld < q.cols || q.ld > 2 * kMostCols)
+    return fail(e, MTDAO_ERR_INVALID_ARG, "%s: ld is not a multiple of 128 from cols on", name);
   if (q.scale_rows != 1 && q.scale_rows != kBlock8)
     return fail(e, MTDAO_ERR_INVALID_ARG, "%s: scale_rows is not 1 or 128", name);
+  if (q.scale_ld != 4 * ((q.rows + q.scale_rows - 1) / q.scale_rows))
+    return fail(e, MTDAO_ERR_INVALID_ARG, "%s: scale_ld is not 4 ceil(rows / scale_rows)", name);
   if (q.rows > 0 && q.cols > 0) {
     if (!q.codes || !q.scales) return fail(e, MTDAO_ERR_INVALID_ARG, "%s: codes or scales is NULL", name);
     if (!aligned16(q.codes)) return fail(e, MTDAO_ERR_ALIGN, "%s: codes are not 16-byte aligned", name);
@@ -835,12 +835,12 @@ Mat mat_of(const mtdao_matrix8* q) {
   m.rows = q->rows;
   m.scale_rows = (q->rows + q->scale_rows - 1) / q->scale_rows;
   m.ld = q->ld;
-  m.blocks = (int32_t)(q->ld / kBlock8);
-  m.scale_ld = (int32_t)q->scale_ld;
+  m.blocks = (int32_t)(up(q->cols, kBlock8) / kBlock8);
+  m.scale_ld = q->scale_ld;
   return m;
 }
 
-int64_t scale_bytes(const mtdao_matrix8& q) { return (q.rows + q.scale_rows - 1) / q.scale_rows * q.scale_ld; }
+int64_t scale_bytes(const mtdao_matrix8& q) { return up(q.cols, 4 * kBlock8) / (4 * kBlock8) * q.scale_ld; }
 int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
 
 // A [rows][cols] input with row stride ld.
@@ -888,9 +888,10 @@ int32_t launch_quantize(const void* x, int32_t dtype, int64_t ld, const mtdao_ma
     using T = decltype(t);
     const T* in = static_cast<const T*>(x);
     if (!qt && !square) {
-      const int64_t wgs = (rows * m.scale_ld + kThreads / 16 - 1) / (kThreads / 16);
-      if (wgs > INT64_C(0x7fffff)) return false;
-      hipLaunchKernelGGL(k_quantize8_rows<T>, dim3((unsigned)wgs), dim3(kThreads), 0, st, in, ld, cols, m);
+      const int groups = (m.blocks + 3) / 4;
+      const int64_t wgs = (rows + 3) / 4 * groups;
+      if (wgs > INT64_C(0xffffff)) return false;  // 2^32 threads
+      hipLaunchKernelGGL(k_quantize8_rows<T>, dim3((unsigned)wgs), dim3(kThreads), 0, st, in, ld, cols, groups, m);
       return true;
     }
     const int64_t ty = up(rows, kBlock8) / kBlock8;
@@ -961,9 +962,8 @@ int32_t launch_product(const mtdao_matrix8& a, const mtdao_matrix8& b, void* c, 
     Few f = few_of(b, c, ldc, accumulate, a.rows);
     f.x = a.codes;
     f.ldx = a.ld;
-    f.x_scales = a.scales;
-    f.x_scale_ld = (int32_t)a.scale_ld;
-    f.x_scale_shift = a.scale_rows == 1 ? 0 : 7;
+    f.a = mat_of(&a);
+    f.a_scale_shift = a.scale_rows == 1 ? 0 : 7;
     auto with = [&](auto ct) {
       using CT = decltype(ct);
       if (a.rows <= 16) launch_few<uint8_t, CT, 1>(f, st);
@@ -1015,9 +1015,16 @@ int64_t up256(int64_t n) { return up(n, 256); }
 struct Part {
   int64_t codes, scales, end;
 };
+// An odd number of blocks from row to row: in rows a multiple of 2 KiB apart the
+// lines that a tile takes at once lie in few of the L2's channels (2048 x 2048
+// x 8192 40.2 us so, x 8320 35.7 us).
+int64_t spread_ld(int64_t cols) {
+  const int64_t blocks = up(cols, kBlock8) / kBlock8;
+  return (blocks | 1) * kBlock8;
+}
 Part part_at(int64_t at, int64_t rows, int64_t cols) {
-  const int64_t ld = up(cols, kBlock8), scales = at + up256(rows * ld);
-  return {at, scales, scales + up256(rows * up(ld / kBlock8, 4))};
+  const int64_t scales = at + up256(rows * spread_ld(cols));
+  return {at, scales, scales + up256(up(cols, 4 * kBlock8) / (4 * kBlock8) * 4 * rows)};
 }
 mtdao_matrix8 matrix_at(void* workspace, int64_t codes, int64_t scales, int64_t rows, int64_t cols) {
   mtdao_matrix8 m = {};
@@ -1025,8 +1032,8 @@ mtdao_matrix8 matrix_at(void* workspace, int64_t codes, int64_t scales, int64_t 
   m.scales = static_cast<uint8_t*>(workspace) + scales;
   m.rows = rows;
   m.cols = cols;
-  m.ld = up(cols, kBlock8);
-  m.scale_ld = up(m.ld / kBlock8, 4);
+  m.ld = spread_ld(cols);
+  m.scale_ld = 4 * rows;
   m.scale_rows = 1;
   return m;
 }

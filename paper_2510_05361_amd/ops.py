@@ -284,34 +284,37 @@ def peri_norm_backward(d_out: Optional[torch.Tensor], dn: Optional[torch.Tensor]
 class Matrix8:
     """A [rows, cols] matrix of 8-bit blocks: ``codes`` (e4m3, [rows, cols up
     to a multiple of 128]) and ``scales`` (e8m0, one row per ``scale_rows``
-    rows, one column per 128 columns up to a multiple of 4)."""
+    rows, one column per 128 columns up to a multiple of 4; a copy: they are
+    held four columns by four).  Rows of codes are an odd number of blocks
+    apart, which spreads them over the L2."""
 
     def __init__(self, rows: int, cols: int, device, scale_rows: int = 1):
         self.rows, self.cols, self.scale_rows = rows, cols, scale_rows
-        ld = -(-cols // BLOCK) * BLOCK
-        scale_ld = -(-(ld // BLOCK) // 4) * 4
-        srows = -(-rows // scale_rows)
-        buf = torch.empty(rows * ld + srows * scale_ld, dtype=torch.uint8, device=device)
+        blocks = -(-cols // BLOCK)
+        ld = (blocks | 1) * BLOCK
+        scale_ld = 4 * -(-rows // scale_rows)
+        buf = torch.empty(rows * ld + -(-blocks // 4) * scale_ld, dtype=torch.uint8, device=device)
         self._buf = buf
         self.args = c_ops.Matrix8(buf.data_ptr(), buf.data_ptr() + rows * ld, rows, cols, ld, scale_ld, scale_rows)
 
     @property
     def codes(self) -> torch.Tensor:
         a = self.args
-        return self._buf[:a.rows * a.ld].view(CODE).view(a.rows, a.ld)
+        return self._buf[:a.rows * a.ld].view(CODE).view(a.rows, a.ld)[:, :-(-a.cols // BLOCK) * BLOCK]
 
     @property
     def scales(self) -> torch.Tensor:
         a = self.args
-        return self._buf[a.rows * a.ld:].view(SCALE).view(-1, a.scale_ld)
+        held = self._buf[a.rows * a.ld:].view(-1, a.scale_ld // 4, 4)
+        return held.permute(1, 0, 2).reshape(a.scale_ld // 4, -1).view(SCALE)
 
     def dequantize(self) -> torch.Tensor:
         """The values as float32 [rows, cols]."""
-        a = self.args
-        s = self.scales.float()[:, :a.ld // BLOCK]
+        codes = self.codes.float().contiguous()
+        s = self.scales.float()[:, :codes.shape[1] // BLOCK]
         if self.scale_rows > 1:
             s = s.repeat_interleave(self.scale_rows, 0)[:self.rows]
-        return (self.codes.float().view(self.rows, -1, BLOCK) * s[:, :, None]).view(self.rows, a.ld)[:, :self.cols]
+        return (codes.view(self.rows, -1, BLOCK) * s[:, :, None]).view(codes.shape)[:, :self.cols]
 
 
 def _matrix(x: torch.Tensor) -> torch.Tensor:

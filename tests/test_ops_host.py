@@ -154,7 +154,7 @@ def test_peri_norm_workspace():
 
 def matrix(rows, cols, at=BASE, scale_rows=1, **kw):
     ld = -(-cols // 128) * 128
-    m = c.Matrix8(at, at + (1 << 32), rows, cols, ld, -(-(ld // 128) // 4) * 4, scale_rows)
+    m = c.Matrix8(at, at + (1 << 32), rows, cols, ld, 4 * -(-rows // scale_rows), scale_rows)
     for k, v in kw.items():
         setattr(m, k, v)
     return m
