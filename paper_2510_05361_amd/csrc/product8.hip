@@ -372,28 +372,22 @@ struct Step8 {
   }
 };
 
-// A wave's 32 x 64 (bf16) or 32 x 32 (fp32) results to c, by way of 4 KiB of
-// LDS of its own: rows of 128 bytes, of which eight lanes then store one.
-template <typename CT>
-__device__ __forceinline__ void store_rows(const Product& p, uint8_t* own, const float* o, int64_t row0, int64_t col0, int lane) {
-  constexpr int kPer = 16 / (int)sizeof(CT), kChunks = sizeof(CT) == 2 ? 4 : 4;  // elements of a chunk; chunks a lane writes
-  const int fr = lane % 32, fg = lane / 32;
-#pragma unroll
-  for (int k = 0; k < kChunks; ++k) {
-    // chunks of the row: bf16 four of each fragment, two a lane; fp32 eight of one fragment, four a lane
-    const int chunk = sizeof(CT) == 2 ? (k >> 1) * 4 + fg * 2 + (k & 1) : fg * 4 + k;
-    float v[kPer];
-#pragma unroll
-    for (int t = 0; t < kPer; ++t) v[t] = o[k * kPer + t];
-    store_full<kPer>(reinterpret_cast<CT*>(own + chunk_at(fr, chunk)), v);
-  }
+// Results to c, by way of the wave's own part of LDS: ROWS rows of BYTES bytes
+// (64 or 128), of which BYTES / 16 lanes then store one.
+template <int BYTES>
+__device__ __forceinline__ uint8_t* staged(uint8_t* own, int row, int chunk) {
+  return own + row * BYTES + ((chunk ^ ((row * BYTES / 256) & (BYTES / 16 - 1))) << 4);
+}
+template <typename CT, int ROWS, int BYTES>
+__device__ __forceinline__ void store_staged(const Product& p, uint8_t* own, int64_t row0, int64_t col0, int lane) {
+  constexpr int kPer = 16 / (int)sizeof(CT), kChunks = BYTES / 16, kAtOnce = 64 / kChunks;
   __builtin_amdgcn_wave_barrier();
   asm volatile("" ::: "memory");
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int r = q * 8 + lane / 8, chunk = (lane % 8) ^ row_key(r);
+  for (int q = 0; q < ROWS / kAtOnce; ++q) {
+    const int r = q * kAtOnce + lane / kChunks, chunk = lane % kChunks;
     float v[kPer];
-    load_full<kPer>(reinterpret_cast<const CT*>(own + r * 128 + (lane % 8) * 16), v);
+    load_full<kPer>(reinterpret_cast<const CT*>(staged<BYTES>(own, r, chunk)), v);
     const int64_t row = row0 + r, col = col0 + chunk * kPer, left = p.b.rows - col;
     if (row < p.a.rows && left > 0) {
       const int n = left > kPer ? kPer : (int)left;
@@ -411,24 +405,31 @@ __device__ __forceinline__ void store_rows(const Product& p, uint8_t* own, const
   asm volatile("" ::: "memory");
 }
 
-// The results of one row of fragments, 32 x 32 NI.
-template <typename CT, int NI>
+// The results of one row of fragments, 32 x 32 NI: a lane's are sixteen
+// consecutive columns of each fragment.  OWN: bytes of the wave's part of LDS.
+template <typename CT, int NI, int OWN>
 __device__ __forceinline__ void store_wave(const Product& p, uint8_t* own, const v16f (&acc)[NI], int64_t row0, int64_t col0, int lane) {
-  if constexpr (sizeof(CT) == 2) {
-    static_assert(NI == 2, "64 columns of bf16");
-    float o[32];
+  constexpr int kPer = 16 / (int)sizeof(CT), kEach = 16 / kPer;  // elements of a chunk; a lane's chunks of a fragment
+  constexpr int kTogether = sizeof(CT) == 2 ? NI : 1;            // fragments staged at once
+  constexpr int kBytes = kTogether * 32 * (int)sizeof(CT), kRows = OWN / kBytes < 32 ? OWN / kBytes : 32;
+  const int fr = lane % 32, fg = lane / 32;
 #pragma unroll
-    for (int t = 0; t < 32; ++t) o[t] = acc[t / 16][t % 16];
-    store_rows<CT>(p, own, o, row0, col0, lane);
-  } else {
+  for (int j0 = 0; j0 < NI; j0 += kTogether)
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      float o[16];
+    for (int r0 = 0; r0 < 32; r0 += kRows) {
+      if (kRows == 32 || fr / kRows == r0 / kRows) {
 #pragma unroll
-      for (int t = 0; t < 16; ++t) o[t] = acc[j][t];
-      store_rows<CT>(p, own, o, row0, col0 + j * 32, lane);
+        for (int j = 0; j < kTogether; ++j)
+#pragma unroll
+          for (int k = 0; k < kEach; ++k) {
+            float v[kPer];
+#pragma unroll
+            for (int t = 0; t < kPer; ++t) v[t] = acc[j0 + j][k * kPer + t];
+            store_full<kPer>(reinterpret_cast<CT*>(staged<kBytes>(own, fr % kRows, (j * 2 + fg) * kEach + k)), v);
+          }
+      }
+      store_staged<CT, kRows, kBytes>(p, own, row0 + r0, col0 + j0 * 32, lane);
     }
-  }
 }
 
 // Item t: a tile and the blocks of its contraction.
@@ -457,7 +458,7 @@ __device__ __forceinline__ Item item_at(const Product& p, int tiles, int t) {
 // instructions; a 1 KiB load takes 16 cycles to issue, which holds up a wave's
 // matrix instructions where several come together, so with more than two stages
 // a block's loads are spread over its halves.
-template <typename CT, bool PART, int B, int WR, int WC, int STAGES>
+template <typename CT, bool PART, int B, int WR, int WC, int STAGES, int OWN>
 __global__ __launch_bounds__(64 * WR * WC, 1) void k_product8_tiles(Product p) {
   constexpr int kWaves = WR * WC, kMI = B / WR / 32, kNI = B / WC / 32, kLoads = B / (8 * kWaves), kStage = 2 * B * 128;
   constexpr bool kSpread = STAGES > 2;
@@ -610,7 +611,7 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_product8_tiles(Product p) {
         for (int j = 0; j < kNI; ++j) eb[j] >>= 8;
       }
     }
-    uint8_t* own = lds + STAGES * kStage + wave * 4096;
+    uint8_t* own = lds + STAGES * kStage + wave * OWN;
     Product to = p;
     if (PART) {
       to.c = p.partial + (int64_t)item.split * p.a.rows * p.b.rows;
@@ -619,7 +620,7 @@ __global__ __launch_bounds__(64 * WR * WC, 1) void k_product8_tiles(Product p) {
     }
 #pragma unroll
     for (int i = 0; i < kMI; ++i)
-      store_wave<std::conditional_t<PART, float, CT>, kNI>(to, own, acc[i], item.at.row0 + wm + i * 32, item.at.col0 + wn, lane);
+      store_wave<std::conditional_t<PART, float, CT>, kNI, OWN>(to, own, acc[i], item.at.row0 + wm + i * 32, item.at.col0 + wn, lane);
     item = next;
   }
   loads_landed();  // LDS is given back: nothing may still be on its way there
@@ -783,20 +784,24 @@ int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 constexpr int64_t kMostCols = INT64_C(1) << 22;  // a tile's rows stay within 2^31 bytes
 
 // How a product of m x n x k goes over the chip.  Up to 64 rows the kernel for
-// few rows.  Tiles of 256 x 256 where these give work to half of the CUs.
-// Else tiles of 128 x 128; where these leave CUs idle, the contraction in
-// parts of at least four blocks.
+// few rows.  Tiles of 256 x 256 from two tiles of 128 x 128 a CU on, unless
+// that pads more than a quarter (2000 x 4000 x 1024, 512 such tiles: 17.5 us
+// in 128 large ones, 14.4 us).  Else tiles of 128 x 128: with more than one a
+// CU two workgroups a CU of two stages each (`shared`; 1999 x 2304 x 768 12.1
+// us one after the other, 10.5 us); where they leave CUs idle, the contraction
+// in parts of at least four blocks (1536 x 512 x 8191 45 us whole, 19 us).
 constexpr int64_t kFew = 64, kFewWhole = 16;  // rows; of which quantized on the way
 struct Shape {
-  bool few, big;
+  bool few, big, shared;
   int32_t splits, split_blocks;
 };
 Shape shape_of(int64_t m, int64_t n, int64_t k) {
   const int64_t blocks = up(k, kBlock8) / kBlock8;
-  Shape s = {m <= kFew && blocks > 0, false, 1, (int32_t)blocks};
+  Shape s = {m <= kFew && blocks > 0, false, false, 1, (int32_t)blocks};
   if (s.few) return s;
-  s.big = blocks > 0 && (up(m, kBig) / kBig) * (up(n, kBig) / kBig) >= 128;
-  const int64_t tiles = (up(m, kMid) / kMid) * (up(n, kMid) / kMid);
+  const int64_t big = (up(m, kBig) / kBig) * (up(n, kBig) / kBig), tiles = (up(m, kMid) / kMid) * (up(n, kMid) / kMid);
+  s.big = blocks > 0 && tiles > 512 && 4 * big <= tiles + tiles / 4;
+  s.shared = !s.big && tiles > 256;
   if (!s.big && tiles > 0 && tiles <= 128 && blocks >= 8) {
     const int64_t parts = std::min<int64_t>(256 / tiles, blocks / 4);
     s.split_blocks = (int32_t)((blocks + parts - 1) / parts);
@@ -986,22 +991,24 @@ int32_t launch_product(const mtdao_matrix8& a, const mtdao_matrix8& b, void* c, 
   p.splits = shape.splits;
   p.split_blocks = shape.split_blocks;
   p.partial = static_cast<float*>(workspace);
-  auto go = [&](auto kernel, int tile, int stages) {
+  // own: LDS of a wave for its results; each: workgroups of a CU
+  auto go = [&](auto kernel, int tile, int stages, int own, int each) {
     p.tiles_m = (int32_t)(up(a.rows, tile) / tile);
     p.tiles_n = (int32_t)(up(b.rows, tile) / tile);
     const int64_t items = (int64_t)p.tiles_m * p.tiles_n * p.splits;
     if (items > INT64_C(0x3fffffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "c has more tiles than one launch takes");
-    const int bytes = stages * 2 * tile * 128 + 8 * 4096;
+    const int bytes = stages * 2 * tile * 128 + 8 * own;
     const int32_t r = allow_lds(reinterpret_cast<const void*>(kernel), bytes, e);
     if (r != MTDAO_OK) return r;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(up(items, 8), 256)), dim3(512), bytes, st, p);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(up(items, 8), 256 * each)), dim3(512), bytes, st, p);
     return (int32_t)MTDAO_OK;
   };
   auto pick = [&](auto ct) {
     using CT = decltype(ct);
-    if (shape.big) return go(k_product8_tiles<CT, false, kBig, 2, 4, 2>, kBig, 2);
-    if (shape.splits == 1) return go(k_product8_tiles<CT, false, kMid, 4, 2, 4>, kMid, 4);
-    const int32_t done = go(k_product8_tiles<CT, true, kMid, 4, 2, 4>, kMid, 4);
+    if (shape.big) return go(k_product8_tiles<CT, false, kBig, 2, 4, 2, 4096>, kBig, 2, 4096, 1);
+    if (shape.shared) return go(k_product8_tiles<CT, false, kMid, 4, 2, 2, 2048>, kMid, 2, 2048, 2);
+    if (shape.splits == 1) return go(k_product8_tiles<CT, false, kMid, 4, 2, 4, 4096>, kMid, 4, 4096, 1);
+    const int32_t done = go(k_product8_tiles<CT, true, kMid, 4, 2, 4, 4096>, kMid, 4, 4096, 1);
     if (done != MTDAO_OK) return done;
     const int64_t quads = p.a.rows * ((p.b.rows + 3) / 4);
     hipLaunchKernelGGL(k_product8_join<CT>, dim3((unsigned)((quads + kThreads - 1) / kThreads)), dim3(kThreads), 0, st, p);
