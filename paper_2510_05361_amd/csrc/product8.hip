@@ -671,15 +671,64 @@ struct Few {
   int64_t ldc;
 };
 
-template <typename XT, typename CT, int MI, int WAVES>
+// Eight elements of a row as they are in memory, zeros from n on.
+struct RawBf16 {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const bf16_t* p, int64_t n) {
+    if (n >= kE) {
+      const u32v4h v = vec_load<false, u32v4h>(p);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) w[t] = v[t];
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        w[t] = (2 * t < n ? (uint32_t)p[2 * t] : 0u) | (2 * t + 1 < n ? (uint32_t)p[2 * t + 1] << 16 : 0u);
+    }
+  }
+  __device__ __forceinline__ void values(float (&o)[kE]) const {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      o[2 * t] = __uint_as_float(w[t] << 16);
+      o[2 * t + 1] = __uint_as_float(w[t] & 0xffff0000u);
+    }
+  }
+};
+struct RawF32 {
+  float w[kE];
+  __device__ __forceinline__ void load(const float* p, int64_t n) {
+    if (n > 0) {
+      load_some<kE>(p, n > kE ? kE : (int)n, w);
+    } else {
+#pragma unroll
+      for (int t = 0; t < kE; ++t) w[t] = 0.0f;
+    }
+  }
+  __device__ __forceinline__ void values(float (&o)[kE]) const {
+#pragma unroll
+    for (int t = 0; t < kE; ++t) o[t] = w[t];
+  }
+};
+
+// NJ: sixteens of columns of a workgroup, two from seventeen rows on, where a's
+// blocks are most of what is read; kAtOnce: blocks that a wave has in flight
+// (more of them do not fit the registers).
+template <typename XT, typename CT, int MI, int NJ, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
   constexpr bool kCodes = sizeof(XT) == 1;
+  constexpr int kAtOnce = sizeof(XT) == 4 || MI > 1 || (sizeof(XT) == 2 && WAVES > 8) ? 2 : 4;
   static_assert(kCodes || MI == 1, "sixteen rows");
-  __shared__ v4f part[WAVES][MI][64];
+  using Raw = std::conditional_t<sizeof(XT) == 4, RawF32, RawBf16>;
+  __shared__ v4f part[WAVES][MI * NJ][64];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
-  const int64_t col0 = (int64_t)blockIdx.x * 16, br = col0 + r < p.b.rows ? col0 + r : p.b.rows - 1;
-  const uint8_t* b = p.b.codes + br * p.b.ld + g * 32;
-  const int64_t bs = br >> p.b_scale_shift;
+  const int64_t col0 = (int64_t)blockIdx.x * (16 * NJ);
+  const uint8_t* b[NJ];
+  int64_t bs[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int64_t br = col0 + j * 16 + r < p.b.rows ? col0 + j * 16 + r : p.b.rows - 1;
+    b[j] = p.b.codes + br * p.b.ld + g * 32;
+    bs[j] = br >> p.b_scale_shift;
+  }
   const XT* a[MI];
   int64_t as[MI];
 #pragma unroll
@@ -688,77 +737,95 @@ __global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
     a[i] = reinterpret_cast<const XT*>(p.x) + ar * p.ldx + g * 32;
     as[i] = ar >> p.a_scale_shift;
   }
-  v4f acc[MI];
+  v4f acc[MI][NJ];
 #pragma unroll
-  for (int i = 0; i < MI; ++i) acc[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 2
-  for (int kb = wave; kb < p.b.blocks; kb += WAVES) {
-    const int e = kb * kBlock8;
-    const v4i b_lo = *reinterpret_cast<const v4i*>(b + e), b_hi = *reinterpret_cast<const v4i*>(b + e + 16);
-    const uint32_t eb = *scale_at(p.b, bs, kb);
-    v8i fa[MI];
-    uint32_t ea[MI];
-    if constexpr (kCodes) {
+  for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int i = 0; i < MI; ++i) {
-        const v4i lo = *reinterpret_cast<const v4i*>(a[i] + e), hi = *reinterpret_cast<const v4i*>(a[i] + e + 16);
-        fa[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        ea[i] = *scale_at(p.a, as[i], kb);
+    for (int j = 0; j < NJ; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int k0 = wave; k0 < p.b.blocks; k0 += kAtOnce * WAVES) {
+    v8i fb[kAtOnce][NJ], fa[kAtOnce][MI];
+    uint32_t eb[kAtOnce][NJ], ea[kAtOnce][MI];
+    Raw raw[kCodes ? 1 : kAtOnce][4];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int kb = k0 + u * WAVES, e = kb * kBlock8;
+      if (kb >= p.b.blocks) break;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const v4i lo = *reinterpret_cast<const v4i*>(b[j] + e), hi = *reinterpret_cast<const v4i*>(b[j] + e + 16);
+        fb[u][j] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        eb[u][j] = *scale_at(p.b, bs[j], kb);
       }
-    } else {
-      float x[4][kE], most = 0.0f;
-      const int64_t left = p.k - e - g * 32;
+      if constexpr (kCodes) {
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int64_t n = left - v * kE;
-        if (n > 0) {
-          load_some<kE>(a[0] + e + v * kE, n > kE ? kE : (int)n, x[v]);
-        } else {
-#pragma unroll
-          for (int t = 0; t < kE; ++t) x[v][t] = 0.0f;
+        for (int i = 0; i < MI; ++i) {
+          const v4i lo = *reinterpret_cast<const v4i*>(a[i] + e), hi = *reinterpret_cast<const v4i*>(a[i] + e + 16);
+          fa[u][i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+          ea[u][i] = *scale_at(p.a, as[i], kb);
         }
+      } else {
 #pragma unroll
-        for (int t = 0; t < kE; ++t) most = max_abs(most, x[v][t]);
-      }
-      if (is_infinite(most)) {
-        most = 0.0f;
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-#pragma unroll
-          for (int t = 0; t < kE; ++t) most = fmaxf(most, finite_abs(x[v][t]));
-      }
-      ea[0] = scale_byte(max_with32(max_with16(most)));
-      const float inv = inverse_scale_of(ea[0]);
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        fa[0][2 * v] = (int)codes_of(x[v][0] * inv, x[v][1] * inv, x[v][2] * inv, x[v][3] * inv);
-        fa[0][2 * v + 1] = (int)codes_of(x[v][4] * inv, x[v][5] * inv, x[v][6] * inv, x[v][7] * inv);
+        for (int v = 0; v < 4; ++v) raw[u][v].load(a[0] + e + v * kE, p.k - e - g * 32 - v * kE);
       }
     }
-    const v8i fb = __builtin_shufflevector(b_lo, b_hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    if constexpr (sizeof(CT) == 2) {
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
-        acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb, fa[i], acc[i], 0, 0, 0, eb, 0, ea[i]);
-    } else {
+    for (int u = 0; u < kAtOnce; ++u) {
+      if (k0 + u * WAVES >= p.b.blocks) break;
+      if constexpr (!kCodes) {
+        float x[4][kE], most = 0.0f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const v8bf wb = widened(fb[2 * k], fb[2 * k + 1], scale_of(eb));
+        for (int v = 0; v < 4; ++v) {
+          raw[u][v].values(x[v]);
+#pragma unroll
+          for (int t = 0; t < kE; ++t) most = max_abs(most, x[v][t]);
+        }
+        if (is_infinite(most)) {
+          most = 0.0f;
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+#pragma unroll
+            for (int t = 0; t < kE; ++t) most = fmaxf(most, finite_abs(x[v][t]));
+        }
+        ea[u][0] = scale_byte(max_with32(max_with16(most)));
+        const float inv = inverse_scale_of(ea[u][0]);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          fa[u][0][2 * v] = (int)codes_of(x[v][0] * inv, x[v][1] * inv, x[v][2] * inv, x[v][3] * inv);
+          fa[u][0][2 * v + 1] = (int)codes_of(x[v][4] * inv, x[v][5] * inv, x[v][6] * inv, x[v][7] * inv);
+        }
+      }
+      if constexpr (sizeof(CT) == 2) {
 #pragma unroll
         for (int i = 0; i < MI; ++i)
-          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, widened(fa[i][2 * k], fa[i][2 * k + 1], scale_of(ea[i])), acc[i], 0, 0, 0);
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[u][j], fa[u][i], acc[i][j], 0, 0, 0, eb[u][j], 0, ea[u][i]);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          v8bf wb[NJ];
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) wb[j] = widened(fb[u][j][2 * k], fb[u][j][2 * k + 1], scale_of(eb[u][j]));
+#pragma unroll
+          for (int i = 0; i < MI; ++i) {
+            const v8bf wa = widened(fa[u][i][2 * k], fa[u][i][2 * k + 1], scale_of(ea[u][i]));
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j], wa, acc[i][j], 0, 0, 0);
+          }
+        }
       }
     }
   }
 #pragma unroll
-  for (int i = 0; i < MI; ++i) part[wave][i][lane] = acc[i];
-  __syncthreads();
-  if (threadIdx.x < 64 * MI) {
-    const int i = threadIdx.x / 64;
-    v4f s = part[0][i][lane];
+  for (int i = 0; i < MI; ++i)
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) s += part[w][i][lane];
-    const int64_t row = i * 16 + r, col = col0 + g * 4, left = p.b.rows - col;
+    for (int j = 0; j < NJ; ++j) part[wave][i * NJ + j][lane] = acc[i][j];
+  __syncthreads();
+  for (int f = wave; f < MI * NJ; f += WAVES) {
+    v4f s = part[0][f][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) s += part[w][f][lane];
+    const int64_t row = f / NJ * 16 + r, col = col0 + f % NJ * 16 + g * 4, left = p.b.rows - col;
     if (row < p.m && left > 0) {
       const int n = left > 4 ? 4 : (int)left;
       CT* at = reinterpret_cast<CT*>(p.c) + row * p.ldc + col;
@@ -914,9 +981,10 @@ int32_t launch_quantize(const void* x, int32_t dtype, int64_t ld, const mtdao_ma
 // Waves of a workgroup of the kernel for few rows: enough that each has a few blocks.
 template <typename XT, typename CT, int MI>
 void launch_few(const Few& f, hipStream_t st) {
-  const dim3 grid((unsigned)((f.b.rows + 15) / 16));
-  if (f.b.blocks > 32) hipLaunchKernelGGL((k_product8_few<XT, CT, MI, 16>), grid, dim3(1024), 0, st, f);
-  else hipLaunchKernelGGL((k_product8_few<XT, CT, MI, 8>), grid, dim3(512), 0, st, f);
+  constexpr int NJ = MI > 1 ? 2 : 1;
+  const dim3 grid((unsigned)((f.b.rows + 16 * NJ - 1) / (16 * NJ)));
+  if (MI == 1 && f.b.blocks > 32) hipLaunchKernelGGL((k_product8_few<XT, CT, MI, NJ, MI == 1 ? 16 : 8>), grid, dim3(1024), 0, st, f);
+  else hipLaunchKernelGGL((k_product8_few<XT, CT, MI, NJ, 8>), grid, dim3(512), 0, st, f);
 }
 
 Few few_of(const mtdao_matrix8& b, void* c, int64_t ldc, int32_t accumulate, int64_t m) {
@@ -1183,6 +1251,8 @@ int32_t mtdao_linear8_backward(const void* dy, const void* x, int32_t dtype, int
       for (auto& i : in)
         if (overlap(o.p, o.bytes, i.p, i.bytes)) return fail(e, MTDAO_ERR_INVALID_ARG, "dx or dw overlaps dy or x");
     if (overlap(out[0].p, out[0].bytes, out[1].p, out[1].bytes)) return fail(e, MTDAO_ERR_INVALID_ARG, "dx overlaps dw");
+    if (overlap(dw, out[1].bytes, wt->codes, wt->rows * wt->ld) || overlap(dw, out[1].bytes, wt->scales, scale_bytes(*wt)))
+      return fail(e, MTDAO_ERR_INVALID_ARG, "dw overlaps wt");
   }
   if (r != MTDAO_OK) return r;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);

@@ -134,6 +134,32 @@ def test_larger_products(m, n, k, dtype):
     assert torch.equal(c, ops.product8(a, b, dtype=DT[dtype])), "the order of the sums is fixed"
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(4200, 2200, 384), (4097, 4100, 1), (2050, 8195, 700), (8200, 2048, 129)])
+def test_products_of_many_tiles(m, n, k, dtype):
+    """More than two 128 x 128 tiles a compute unit, ragged at both ends."""
+    a, b = ops.quantize8(rand((m, k), seed=1)), ops.quantize8(rand((n, k), 0.02, seed=2))
+    wide = torch.full((m, n + 3), 7.0, device="cuda").to(DT[dtype])
+    c = wide[:, 1:1 + n]
+    ops.product8(a, b, out=c)
+    check_product(a, b, c, dtype)
+    if dtype == "f32":
+        keep = c.cpu().double()
+        ops.product8(a, b, out=c, accumulate=True)
+        check_product(a, b, c, dtype, keep)
+    c[:] = 7.0
+    assert bool((wide == 7.0).all())
+
+
+@pytest.mark.parametrize("m,n,k", [(17, 33, 260), (30, 100, 1000), (49, 31, 4224), (64, 95, 130)])
+def test_accumulate_to_few_rows(m, n, k):
+    a, b = ops.quantize8(rand((m, k), seed=1)), ops.quantize8(rand((n, k), seed=2))
+    c = torch.randn((m, n), device="cuda")
+    keep = c.cpu().double()
+    ops.product8(a, b, out=c, accumulate=True)
+    check_product(a, b, c, "f32", keep)
+
+
 @pytest.mark.parametrize("m,n,k", [(5, 7, 130), (8, 512, 4096), (300, 200, 520), (512, 520, 9000), (2100, 700, 128)])
 def test_accumulate_and_strided_output(m, n, k):
     a, b = ops.quantize8(rand((m, k), seed=1)), ops.quantize8(rand((n, k), seed=2))

@@ -205,6 +205,50 @@ def test_product8_without_rows_does_nothing():
         c.mtdao_product8_workspace_bytes(-1, 1, 1)
 
 
+LINEAR_BAD = [
+    (dict(dtype=2), -1), (dict(x=None), -1), (dict(x=(BASE << 1) + 2), -2), (dict(ld=199), -1), (dict(rows=-1), -1),
+    (dict(rows=(1 << 22) + 1), -1), (dict(y=None), -1), (dict(y_dtype=3), -1), (dict(ldy=4), -1), (dict(y=BASE << 1), -1),
+    (dict(y=BASE), -1), (dict(w=matrix(5, 200, codes=None)), -1), (dict(w=matrix(5, 200, scale_ld=8)), -1), (dict(workspace=None), -5),
+    (dict(size=-1), -5), (dict(workspace=(BASE << 3) + 4), -2),
+]
+
+
+@pytest.mark.parametrize("kw,code", LINEAR_BAD, ids=[str(i) for i in range(len(LINEAR_BAD))])
+def test_linear8_refuses(kw, code):
+    a = {"x": BASE << 1, "dtype": 0, "rows": 40, "ld": 200, "w": matrix(5, 200), "y": BASE << 2, "y_dtype": 0, "ldy": 5,
+         "workspace": BASE << 3, "size": 0, **kw}
+    need = c.mtdao_linear8_workspace_bytes(40, 5, 200)[0] + a.pop("size")
+    with pytest.raises(abi.MtdaoError) as e:
+        c.mtdao_linear8(*a.values(), need, None)
+    assert e.value.code == code
+
+
+LINEAR_BACKWARD_BAD = [
+    (dict(dtype=2), -1), (dict(dy=None), -1), (dict(x=None), -1), (dict(dy=(BASE << 1) + 2), -2), (dict(ld_dy=4), -1), (dict(ld_x=199), -1),
+    (dict(rows=-1), -1), (dict(rows=(1 << 22) + 1), -1), (dict(dx=None), -1), (dict(dw=None), -1), (dict(ld_dx=199), -1), (dict(ld_dw=199), -1),
+    (dict(dw=(BASE << 4) + 2), -2), (dict(dx=BASE << 4), -1), (dict(dx=BASE << 1), -1), (dict(dw=BASE << 2), -1), (dict(dw=BASE), -1),
+    (dict(wt=matrix(200, 5, codes=None)), -1), (dict(workspace=None), -5), (dict(size=-1), -5), (dict(workspace=(BASE << 5) + 4), -2),
+]
+
+
+@pytest.mark.parametrize("kw,code", LINEAR_BACKWARD_BAD, ids=[str(i) for i in range(len(LINEAR_BACKWARD_BAD))])
+def test_linear8_backward_refuses(kw, code):
+    a = {"dy": BASE << 1, "x": BASE << 2, "dtype": 0, "rows": 40, "ld_dy": 5, "ld_x": 200, "wt": matrix(200, 5), "dx": BASE << 3, "ld_dx": 200,
+         "dw": BASE << 4, "ld_dw": 200, "accumulate": False, "workspace": BASE << 5, "size": 0, **kw}
+    need = c.mtdao_linear8_workspace_bytes(40, 5, 200)[1] + a.pop("size")
+    with pytest.raises(abi.MtdaoError) as e:
+        c.mtdao_linear8_backward(*a.values(), need, None)
+    assert e.value.code == code
+
+
+def test_linear8_sizes():
+    assert c.mtdao_linear8_workspace_bytes(0, 5, 200)[0] == 0
+    for sizes in ((-1, 5, 200), (5, -1, 200), (5, 5, -1), ((1 << 22) + 1, 5, 5), (5, (1 << 22) + 1, 5), (5, 5, (1 << 22) + 1)):
+        with pytest.raises(abi.MtdaoError):
+            c.mtdao_linear8_workspace_bytes(*sizes)
+    c.mtdao_linear8(None, 0, 0, 200, matrix(5, 200), None, 0, 5, None, 0, None)
+
+
 # ------------------------------------------------------------- torch level
 
 
