@@ -241,6 +241,40 @@ def test_elements_past_two_to_the_32():
     assert torch.equal(opt.v_scale[0].view(torch.uint8).gt(1).nonzero().flatten(), at // 128)
 
 
+@pytest.mark.parametrize("p,g", [("f32", "f32"), ("bf16", "f32")])
+def test_large_passes_equal_small_ones(p, g):
+    """A pass over more than 2^26 elements spreads its chunks in another order:
+    the same results as passes over pieces of the same values, bit for bit."""
+    sizes = [3 * 32768 - 1, (1 << 26) - 12345, 8 * 4096, 5, 32768 + 4097]
+    params, grads, opt = make(sizes, p, g, weight_decay=0.1)
+    before = [t.clone() for t in params]
+    for _ in range(2):
+        opt.step(LR)
+    cuts = [0, 40000, 1 << 25, 1 << 26]
+    for i, n in enumerate(sizes):
+        for a, b in zip(cuts, cuts[1:]):
+            if a < n:
+                q = before[i][a:b]
+                part = ops.AdamW([q], [grads[i][a:b]], betas=(B1, B2), eps=EPS, weight_decay=0.1)
+                for _ in range(2):
+                    part.step(LR)
+                for got, want in ((params, q), (opt.m, part.m[0]), (opt.v, part.v[0])):
+                    assert torch.equal(got[i][a:b], want), (i, a)
+
+
+def test_second_moments_below_the_smallest_normal_number():
+    """v from 1e-41 on, whose products, sum and root are as exact as its 2^-149
+    steps allow, with an eps that does not hide them."""
+    p = torch.zeros(4096, device="cuda")
+    g = torch.logspace(-19.4, -15, 4096, device="cuda")
+    opt = ops.AdamW([p], [g], betas=(B1, B2), eps=1e-30)
+    opt.step(LR)
+    want, m, v = oracle.adamw(torch.zeros(4096).double(), g.cpu().double(), 0.0, 0.0, 1, LR, B1, B2, 1e-30, 0.0, 1.0)
+    verr = 12 * U * v + 2 * 2.0 ** -149
+    assert bool(((opt.v[0].cpu().double() - v).abs() <= verr).all())
+    assert bool(((p.cpu().double() - want).abs() <= want.abs() * (32 * U + verr / v)).all())
+
+
 def test_refusals():
     x = torch.zeros(8, device="cuda")
     with pytest.raises(ValueError):
