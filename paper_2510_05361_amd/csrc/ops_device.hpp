@@ -111,6 +111,43 @@ __device__ __forceinline__ void store_some(T* p, int n, const float (&o)[N]) {
   }
 }
 
+// Eight elements as they are in memory, zeros from n on (n <= 0: none).
+template <typename T, bool NT = false>
+struct Raw;
+template <bool NT>
+struct Raw<bf16_t, NT> {
+  uint32_t w[4];
+  __device__ __forceinline__ void set(int i, uint32_t dword) { w[i] = dword; }
+  __device__ __forceinline__ void load(const bf16_t* p, int n) {
+    if (n >= 8) {
+      const u32v4h v = vec_load<NT, u32v4h>(p);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) w[t] = v[t];
+    } else {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        w[t] = (2 * t < n ? (uint32_t)p[2 * t] : 0u) | (2 * t + 1 < n ? (uint32_t)p[2 * t + 1] << 16 : 0u);
+    }
+  }
+  __device__ __forceinline__ void values(float (&o)[8]) const {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      o[2 * t] = __uint_as_float(w[t] << 16);
+      o[2 * t + 1] = __uint_as_float(w[t] & 0xffff0000u);
+    }
+  }
+};
+template <bool NT>
+struct Raw<float, NT> {
+  float w[8];
+  __device__ __forceinline__ void set(int i, uint32_t dword) { w[i] = __uint_as_float(dword); }
+  __device__ __forceinline__ void load(const float* p, int n) { load_some<8, NT>(p, n, w); }
+  __device__ __forceinline__ void values(float (&o)[8]) const {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) o[t] = w[t];
+  }
+};
+
 // A wave-uniform value that no running kernel writes, through the scalar
 // cache.
 template <typename T>

@@ -671,44 +671,6 @@ struct Few {
   int64_t ldc;
 };
 
-// Eight elements of a row as they are in memory, zeros from n on.
-struct RawBf16 {
-  uint32_t w[4];
-  __device__ __forceinline__ void load(const bf16_t* p, int64_t n) {
-    if (n >= kE) {
-      const u32v4h v = vec_load<false, u32v4h>(p);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) w[t] = v[t];
-    } else {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-        w[t] = (2 * t < n ? (uint32_t)p[2 * t] : 0u) | (2 * t + 1 < n ? (uint32_t)p[2 * t + 1] << 16 : 0u);
-    }
-  }
-  __device__ __forceinline__ void values(float (&o)[kE]) const {
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      o[2 * t] = __uint_as_float(w[t] << 16);
-      o[2 * t + 1] = __uint_as_float(w[t] & 0xffff0000u);
-    }
-  }
-};
-struct RawF32 {
-  float w[kE];
-  __device__ __forceinline__ void load(const float* p, int64_t n) {
-    if (n > 0) {
-      load_some<kE>(p, n > kE ? kE : (int)n, w);
-    } else {
-#pragma unroll
-      for (int t = 0; t < kE; ++t) w[t] = 0.0f;
-    }
-  }
-  __device__ __forceinline__ void values(float (&o)[kE]) const {
-#pragma unroll
-    for (int t = 0; t < kE; ++t) o[t] = w[t];
-  }
-};
-
 // NJ: sixteens of columns of a workgroup, two from seventeen rows on, where a's
 // blocks are most of what is read; kAtOnce: blocks that a wave has in flight
 // (more of them do not fit the registers).
@@ -717,7 +679,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
   constexpr bool kCodes = sizeof(XT) == 1;
   constexpr int kAtOnce = sizeof(XT) == 4 || MI > 1 || (sizeof(XT) == 2 && WAVES > 8) ? 2 : 4;
   static_assert(kCodes || MI == 1, "sixteen rows");
-  using Raw = std::conditional_t<sizeof(XT) == 4, RawF32, RawBf16>;
+  using Rows = Raw<std::conditional_t<kCodes, bf16_t, XT>>;
   __shared__ v4f part[WAVES][MI * NJ][64];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
   const int64_t col0 = (int64_t)blockIdx.x * (16 * NJ);
@@ -745,7 +707,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
   for (int k0 = wave; k0 < p.b.blocks; k0 += kAtOnce * WAVES) {
     v8i fb[kAtOnce][NJ], fa[kAtOnce][MI];
     uint32_t eb[kAtOnce][NJ], ea[kAtOnce][MI];
-    Raw raw[kCodes ? 1 : kAtOnce][4];
+    Rows raw[kCodes ? 1 : kAtOnce][4];
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
       const int kb = k0 + u * WAVES, e = kb * kBlock8;
@@ -765,7 +727,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
         }
       } else {
 #pragma unroll
-        for (int v = 0; v < 4; ++v) raw[u][v].load(a[0] + e + v * kE, p.k - e - g * 32 - v * kE);
+        for (int v = 0; v < 4; ++v) raw[u][v].load(a[0] + e + v * kE, (int)(p.k - e) - g * 32 - v * kE);
       }
     }
 #pragma unroll
