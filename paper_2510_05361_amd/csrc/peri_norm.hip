@@ -11,7 +11,7 @@
 // stored ones: the rows pass through registers anyway.
 //
 // Measured at 16384 x 2048 in bf16, RMSNorm with a gate for each channel: forward
-// 48 us (268 MB, 5.6 TB/s), backward 74 us (403 MB, 5.4 TB/s) with the 5 us that
+// 46 us (268 MB, 5.8 TB/s), backward 74 us (403 MB, 5.4 TB/s) with the 5 us that
 // k_peri_columns takes.  Backward, rows of a workgroup lying apart by the number
 // of workgroups, so that all of them sweep one part of memory, took 80 us where
 // rows one after the other took 87 us; 768 and 1024 workgroups are slower than
@@ -205,35 +205,45 @@ __global__ __launch_bounds__(TPR > kGroup ? TPR : kGroup) void k_peri_norm(Args 
     if (a.f) load_columns<WHOLE>(reinterpret_cast<const BT*>(a.f) + row * a.ld_f + e, n[v], fa[v]);
   }
   const bool wb = a.weight_bf16 != 0;
+  // with one vector a thread, what the rows are multiplied with is on its way with them
+  constexpr bool kEarly = NV == 1;
+  const int64_t gate_row = a.gate ? row / a.rows_per_gate * a.d : 0;
+  float w_post[NV][kE], w_pre[NV][kE], gate[NV][kE];
+  auto weights = [&](const void* p, int64_t at, float (&w)[NV][kE]) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) load_weight<WHOLE>(p, wb, at + (v * TPR + lane) * kE, n[v], w[v]);
+  };
+  if (kEarly) {
+    if (a.f) weights(a.w_post, 0, w_post);
+    if (a.gate) weights(a.gate, gate_row, gate);
+    if (a.w_pre) weights(a.w_pre, 0, w_pre);
+  }
   if (a.f) {
     const float r = normalize<TPR, NV, LAYER>(fa, n, a, buf) * a.scale;
-    const int64_t gate_row = a.gate ? row / a.rows_per_gate * a.d : 0;
     ST* out = reinterpret_cast<ST*>(a.x_out) + row * a.d;
+    if (!kEarly) {
+      weights(a.w_post, 0, w_post);
+      if (a.gate) weights(a.gate, gate_row, gate);
+    }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int e = (v * TPR + lane) * kE;
-      float w[kE], g[kE];
-      load_weight<WHOLE>(a.w_post, wb, e, n[v], w);
-      if (a.gate) load_weight<WHOLE>(a.gate, wb, gate_row + e, n[v], g);
 #pragma unroll
       for (int t = 0; t < kE; ++t) {
-        const float h = fa[v][t] * r * w[t];
-        xa[v][t] += a.gate ? h * g[t] : h;
+        const float h = fa[v][t] * r * w_post[v][t];
+        xa[v][t] += a.gate ? h * gate[v][t] : h;
       }
-      if (live) store_columns<WHOLE, true>(out + e, n[v], xa[v]);
+      if (live) store_columns<WHOLE, true>(out + (v * TPR + lane) * kE, n[v], xa[v]);
     }
   }
   if (a.w_pre) {
     const float r = normalize<TPR, NV, LAYER>(xa, n, a, buf + 2 * kWaves);
     BT* out = reinterpret_cast<BT*>(a.n_out) + row * a.d;
+    if (!kEarly) weights(a.w_pre, 0, w_pre);
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const int e = (v * TPR + lane) * kE;
-      float w[kE];
-      load_weight<WHOLE>(a.w_pre, wb, e, n[v], w);
 #pragma unroll
-      for (int t = 0; t < kE; ++t) xa[v][t] = xa[v][t] * r * w[t];
-      if (live) store_columns<WHOLE, true>(out + e, n[v], xa[v]);
+      for (int t = 0; t < kE; ++t) xa[v][t] = xa[v][t] * r * w_pre[v][t];
+      if (live) store_columns<WHOLE, true>(out + (v * TPR + lane) * kE, n[v], xa[v]);
     }
   }
 }
@@ -584,6 +594,14 @@ void with_types(const mtdao_peri_norm_args& a, F&& f) {
 // registers for two rows in flight and the sums of the thread's columns.
 int backward_threads(int64_t d) { return d <= 64 * kE ? 64 : d <= 128 * kE ? 128 : d <= 256 * kE ? 256 : 512; }
 
+// Forward, a row has one vector a thread up to D = 512 and from 1025 to 2048 (one
+// wave with four: 16384 x 2048 bf16 54.0 us against 46.1 us), and else where there
+// are few elements: then the latency of one row counts, above it the work of the
+// reductions.  One vector a thread against two or four: 1024 x 768 4.7 us (5.0),
+// 2048 x 768 5.9 us (5.2), 256 x 4096 4.8 us (5.4), 1024 x 4096 6.9 us (6.4),
+// 1 x 8192 4.5 us (7.0), 512 x 8192 8.6 us (8.3).
+constexpr int64_t kFew = INT64_C(1) << 20;
+
 // How the rows go over the workgroups, backward: at most kBlocks of them, at
 // least eight rows each, none across gates unless it has them whole.
 constexpr int64_t kBlocks = 512;
@@ -646,8 +664,8 @@ int32_t mtdao_peri_norm(const mtdao_peri_norm_args* args, void* hip_stream) {
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   RoctxRange range("mtdao_peri_norm rows=%lld d=%lld", (long long)a.rows, (long long)a.d);
   const Args k = device_args(a);
-  // a wave per row up to D = 2048, else four
-  const int64_t per = a.d <= 2048 ? kGroup / 64 : 1;
+  const bool few = a.rows * a.d <= kFew;
+  const int64_t per = a.d <= 512 || (a.d <= 1024 && !few) ? 4 : 1;
   const int64_t blocks = (a.rows + per - 1) / per;
   if (blocks > 0x7fffffff) return fail(e, MTDAO_ERR_INVALID_ARG, "rows exceed the largest launch");
   with_types(a, [&](auto s, auto b, auto layer, auto whole) {
@@ -660,10 +678,12 @@ int32_t mtdao_peri_norm(const mtdao_peri_norm_args* args, void* hip_stream) {
                          dim3(T > kGroup ? T : kGroup), 0, st, k);
     };
     if (a.d <= 512) go(Int<64>{}, Int<1>{});
-    else if (a.d <= 1024) go(Int<64>{}, Int<2>{});
-    else if (a.d <= 2048) go(Int<64>{}, Int<4>{});
-    else if (a.d <= 4096) go(Int<256>{}, Int<2>{});
-    else go(Int<256>{}, Int<4>{});
+    else if (a.d <= 1024 && !few) go(Int<64>{}, Int<2>{});
+    else if (a.d <= 2048) go(Int<256>{}, Int<1>{});
+    else if (a.d <= 4096 && !few) go(Int<256>{}, Int<2>{});
+    else if (a.d <= 4096) go(Int<512>{}, Int<1>{});
+    else if (!few) go(Int<256>{}, Int<4>{});
+    else go(Int<1024>{}, Int<1>{});
   });
   return hip_check(e, hipGetLastError(), "mtdao_peri_norm launch");
 }

@@ -139,6 +139,14 @@ def test_types(stream, branch, w, kind, d):
     check_backward(s, kind, 0, -1.5)
 
 
+@pytest.mark.parametrize("stream,branch,kind", [("bf16", "bf16", "rms"), ("f32", "bf16", "layer"), ("f32", "f32", "rms")])
+@pytest.mark.parametrize("t,d", [(1500, 1000), (1100, 1021), (700, 2048), (515, 2050), (300, 4096), (260, 4100), (200, 5003), (170, 8192), (90, 8192)])
+def test_widths_of_many_rows(t, d, stream, branch, kind):
+    s = inputs(t, d, stream, branch, gate=97)
+    check_forward(s, kind, 97, 0.7)
+    check_backward(s, kind, 97, 0.7)
+
+
 @pytest.mark.parametrize("t", [1, 2, 3, 31, 600, 4099])
 @pytest.mark.parametrize("gate", [None, 1, 2, 7, 300, 5000])
 @pytest.mark.parametrize("d", [96, 1000])
@@ -201,6 +209,22 @@ def test_large_mean_constant_and_zero_rows(d):
     for kind in ("rms", "layer"):
         check_forward(s, kind, 0, 0.5)
         check_backward(s, kind, 0, 0.5)
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("d", [24, 100])
+def test_rows_whose_squares_vanish(d, kind):
+    """eps = 0 and rows of 1e-20, whose mean square lies below the smallest
+    normal number (three decades above the smallest there is: 2^-149 more in
+    every sum of squares, d of them, a relative 2^-14 of the root at most)."""
+    s = inputs(6, d, gate=None)
+    s["x"] *= 2.0 ** -66
+    s["f"] *= 2.0 ** -64
+    x, f, w, v = (s[k].cpu().double() for k in ("x", "f", "w_post", "w_pre"))
+    out, n = ops.peri_norm(s["x"], s["f"], s["w_post"], s["w_pre"], eps=0.0, kind=kind, scale=2.0 ** -66)
+    want, want_n = oracle.peri_norm(x, f, w, v, None, 6, 2.0 ** -66, 0.0, kind == "layer")
+    assert bool(((out.cpu().double() - want).abs() <= 2.0 ** -13 * (want.abs() + x.abs())).all())
+    assert bool(((n.cpu().double() - want_n).abs() <= 2.0 ** -10 * want_n.abs().amax()).all())
 
 
 @pytest.mark.parametrize("d", [100, 3000])
