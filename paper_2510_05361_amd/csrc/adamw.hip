@@ -13,8 +13,8 @@
 // are non-temporal (354 M elements of 28 bytes 1821 -> 1700 us).  With 8-bit
 // states the arithmetic is close behind: square root and quotient are the
 // hardware's, an ulp each (IEEE sequences: 1311 M elements of 10 bytes 2750 us,
-// 4.8 TB/s, against 2270 us), the clip factor, the betas and the blocks' scales
-// are folded into four factors, and what only rare values need is behind branches
+// 4.8 TB/s, against 2270 us), the betas are folded into the blocks' scales (powers
+// of two: no rounding more), and what only rare values need is behind branches
 // (2180 us, 6.0 TB/s).
 
 #include <hip/hip_runtime.h>
@@ -63,8 +63,7 @@ struct Step {
   const uint32_t* owner;   // tensor of every chunk
   const float* clip;       // the factor of the gradients (clipping)
   int64_t chunks;
-  float beta1, rest1, beta2;         // rest1 = 1 - beta1
-  float root_beta2, root_rest2;      // square roots of beta2 and 1 - beta2
+  float beta1, rest1, beta2, rest2;  // rest = 1 - beta
   float lr, step;          // step = lr / (1 - beta1^t)
   float root2, eps;        // root2 = 1 / sqrt(1 - beta2^t)
   bool spread;             // Span
@@ -232,7 +231,6 @@ __global__ __launch_bounds__(kThreads) void k_adamw_step(Step s) {
   const GT* g = reinterpret_cast<const GT*>(uniform_load(&row->g)) + span.base;
   const float keep = 1.0f - s.lr * uniform_load(&row->decay);
   const float clip = s.clip ? uniform_load(s.clip) : 1.0f;
-  const float gm = s.rest1 * clip, gv = s.root_rest2 * clip;
   // p from the new m and r = sqrt(v), each off by an ulp of v_sqrt and v_rcp
   auto moved = [&](float p, float m, float r) {
     return fmaf(-s.step * m, __builtin_amdgcn_rcpf(fmaf(r, s.root2, s.eps)), p * keep);
@@ -259,9 +257,9 @@ __global__ __launch_bounds__(kThreads) void k_adamw_step(Step s) {
     for (int k = 0; k < kSlots; ++k) {
 #pragma unroll
       for (int t = 0; t < V; ++t) {
-        const float h = gv * ga[k][t];
-        ma[k][t] = fmaf(gm, ga[k][t], s.beta1 * ma[k][t]);
-        va[k][t] = fmaf(h, h, s.beta2 * va[k][t]);
+        const float g = ga[k][t] * clip;
+        ma[k][t] = fmaf(s.rest1, g, s.beta1 * ma[k][t]);
+        va[k][t] = fmaf(s.rest2 * g, g, s.beta2 * va[k][t]);
       }
       float r[V];
       roots(va[k], r);
@@ -294,13 +292,13 @@ __global__ __launch_bounds__(kThreads) void k_adamw_step(Step s) {
       float ma[V], ra[V];
       mc[k].values(ma);
       vc[k].values(ra);
-      const float mk = s.beta1 * scale_of(mb[k]), vk = s.root_beta2 * scale_of(vb[k]);
+      const float mk = s.beta1 * scale_of(mb[k]), vk = scale_of(vb[k]), vk2 = s.beta2 * vk;
       float mm = 0.0f, vm = 0.0f;
 #pragma unroll
       for (int t = 0; t < V; ++t) {
-        const float h = gv * ga[k][t], w = vk * ra[t];
-        ma[t] = fmaf(gm, ga[k][t], mk * ma[t]);
-        ra[t] = fmaf(h, h, w * w);
+        const float g = ga[k][t] * clip;
+        ma[t] = fmaf(s.rest1, g, mk * ma[t]);
+        ra[t] = fmaf(s.rest2 * g, g, (vk2 * ra[t]) * (vk * ra[t]));
       }
       roots(ra, ra);
 #pragma unroll
@@ -592,8 +590,7 @@ int32_t mtdao_adamw_step(mtdao_adamw* h, double lr, void* hip_stream) {
     s.beta1 = (float)c.beta1;
     s.rest1 = (float)(1.0 - c.beta1);
     s.beta2 = (float)c.beta2;
-    s.root_beta2 = (float)std::sqrt(c.beta2);
-    s.root_rest2 = (float)std::sqrt(1.0 - c.beta2);
+    s.rest2 = (float)(1.0 - c.beta2);
     const Pass pass = pass_of(c, h->elements);
     s.spread = pass.spread;
     s.lr = (float)lr;
