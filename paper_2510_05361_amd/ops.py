@@ -166,6 +166,14 @@ def _rows(t: Optional[torch.Tensor], shape, what: str):
     return t, t.data_ptr(), t.stride(0) if t.shape[0] > 1 else d
 
 
+def _empty(like: torch.Tensor, shape, dtype: torch.dtype) -> torch.Tensor:
+    """A new contiguous tensor (the way through ``empty_like`` takes half the
+    host time, 1.2 us)."""
+    if like.shape == shape and like.is_contiguous():
+        return torch.empty_like(like) if like.dtype is dtype else torch.empty_like(like, dtype=dtype)
+    return torch.empty(shape, dtype=dtype, device=like.device)
+
+
 def _ptr(t: Optional[torch.Tensor]) -> int:
     return 0 if t is None else t.data_ptr()
 
@@ -218,8 +226,8 @@ def peri_norm(x: torch.Tensor, f: Optional[torch.Tensor], w_post: Optional[torch
     shape = x.shape
     x_in, px, ld_x = _rows(x, shape, "x")
     f_in, pf, ld_f = _rows(f, shape, "f")
-    out = torch.empty(shape, dtype=x.dtype, device=x.device) if f is not None else x
-    n = torch.empty(shape, dtype=branch, device=x.device) if w_pre is not None else None
+    out = _empty(x, shape, x.dtype) if f is not None else x
+    n = _empty(f if f is not None else x, shape, branch) if w_pre is not None else None
     if rows:
         c_ops.mtdao_peri_norm(
             c_ops.PACKED_ARGS.pack(rows, d, _KINDS[kind], stream, _TYPES[branch], _TYPES[weight], eps, scale, per, ld_x, ld_f, d, d,
@@ -252,16 +260,16 @@ def peri_norm_backward(d_out: Optional[torch.Tensor], dn: Optional[torch.Tensor]
         raise TypeError("d_out has the type of x_out, dn that of f")
     rows, d, weight, per = _peri_sizes(x_out, f, w_post, w_pre, gate, rows_per_gate, kind)
     stream = _type(x_out, "x_out")
-    shape, dev, f32 = x_out.shape, x_out.device, torch.float32
+    shape, f32 = x_out.shape, torch.float32
     x_in, px, ld_x = _rows(x_out, shape, "x_out")
     f_in, pf, ld_f = _rows(f, shape, "f")
     d_in, pd, ld_d = _rows(d_out, shape, "d_out")
     y_in, py, ld_y = _rows(dn, shape, "dn")
-    dx = torch.empty(shape, dtype=x_out.dtype, device=dev)
-    df = torch.empty(shape, dtype=branch, device=dev) if f is not None else None
-    dw_post = torch.empty(d, dtype=f32, device=dev) if f is not None else None
-    dw_pre = torch.empty(d, dtype=f32, device=dev) if w_pre is not None else None
-    dgate = torch.empty(gate.shape, dtype=f32, device=dev) if gate is not None else None
+    dx = _empty(x_out, shape, x_out.dtype)
+    df = _empty(f, shape, branch) if f is not None else None
+    dw_post = _empty(w_post, (d,), f32) if f is not None else None
+    dw_pre = _empty(w_pre, (d,), f32) if w_pre is not None else None
+    dgate = _empty(gate, gate.shape, f32) if gate is not None else None
     if rows == 0:
         for t in (dw_post, dw_pre, dgate):
             if t is not None:
@@ -270,7 +278,7 @@ def peri_norm_backward(d_out: Optional[torch.Tensor], dn: Optional[torch.Tensor]
     if d > c_ops.MTDAO_PERI_MAX_D:
         raise ValueError(f"rows of {d}: at most {c_ops.MTDAO_PERI_MAX_D}")
     need = _peri_workspace(rows, d, per, gate is not None)
-    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    ws = torch.empty(need, dtype=torch.uint8, device=x_out.device)
     c_ops.mtdao_peri_norm_backward(
         c_ops.PACKED_ARGS.pack(rows, d, _KINDS[kind], stream, _TYPES[branch], _TYPES[weight], eps, scale, per, ld_x, ld_f, ld_d, ld_y,
                                px, pf, _ptr(w_post), _ptr(w_pre), _ptr(gate), pd, py, dx.data_ptr(), 0, _ptr(df), _ptr(dw_post),
@@ -433,7 +441,7 @@ def linear8_backward(dy: torch.Tensor, x: torch.Tensor, w: Weight8, *, dw: Optio
     x2 = _matrix(x if x.dim() == 2 else x.reshape(-1, k))
     dy2 = _matrix(dy if dy.dim() == 2 else dy.reshape(-1, n))
     m = x2.shape[0]
-    dx = torch.empty(x.shape, dtype=dy.dtype, device=dev)
+    dx = _empty(x, x.shape, dy.dtype)
     need = _linear_workspace(m, n, k)[1]
     ws = torch.empty(need, dtype=torch.uint8, device=dev)
     c_ops.mtdao_linear8_backward(dy2.data_ptr(), x2.data_ptr(), _type(dy, "dy"), m, _ld(dy2), _ld(x2), w.qt.args, dx.data_ptr(), k,
