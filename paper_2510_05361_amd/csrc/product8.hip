@@ -666,8 +666,8 @@ __global__ __launch_bounds__(kThreads) void k_product8_join(Product p) {
 }
 
 // Products of a few rows (up to 64): what counts is to read b once, with as
-// many loads in flight as the chip takes.  A workgroup has sixteen rows of b
-// (columns of c), whose blocks its waves take in turn, straight from memory
+// many loads in flight as the chip takes.  A workgroup has sixteen or 32 rows
+// of b (columns of c), whose blocks its waves take in turn, straight from memory
 // into registers; their sums meet in LDS, in the order of the waves.  XT
 // uint8_t: a is given as 8-bit blocks; else as it is, up to sixteen rows of
 // it, which every workgroup quantizes as it reads them (one launch less).
@@ -684,8 +684,7 @@ struct Few {
   int64_t ldc;
 };
 
-// NJ: sixteens of columns of a workgroup, two from seventeen rows on, where a's
-// blocks are most of what is read; kAtOnce: blocks that a wave has in flight
+// NJ: sixteens of columns of a workgroup; kAtOnce: blocks that a wave has in flight
 // (more of them do not fit the registers).
 template <typename XT, typename CT, int MI, int NJ, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
@@ -826,7 +825,10 @@ int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 constexpr int64_t kMostCols = INT64_C(1) << 22;  // a tile's rows stay within 2^31 bytes
 
 // How a product of m x n x k goes over the chip.  Up to 64 rows the kernel for
-// few rows.  Tiles of 256 x 256 from two tiles of 128 x 128 a CU on, unless
+// few rows, with more than sixteen while the contraction is short: a workgroup
+// takes all of it (64 x 4096 x 4096 12.9 us, in parts of tiles 14.3 us; 64 x
+// 2048 x 8192 26.8 us, in parts 15.9 us; 24 x 2048 x 8192 13.4 us, in parts
+// 12.6 us).  Tiles of 256 x 256 from two tiles of 128 x 128 a CU on, unless
 // that pads more than a quarter (2000 x 4000 x 1024, 512 such tiles: 17.5 us
 // in 128 large ones, 14.4 us).  Else tiles of 128 x 128: with more than one a
 // CU two workgroups a CU of two stages each (`shared`; 1999 x 2304 x 768 12.1
@@ -839,7 +841,8 @@ struct Shape {
 };
 Shape shape_of(int64_t m, int64_t n, int64_t k) {
   const int64_t blocks = up(k, kBlock8) / kBlock8;
-  Shape s = {m <= kFew && blocks > 0, false, false, 1, (int32_t)blocks};
+  const bool few = m <= 16 || (m <= kFew && (m <= 32 ? 2 : 4) * blocks <= 128);
+  Shape s = {few && blocks > 0, false, false, 1, (int32_t)blocks};
   if (s.few) return s;
   const int64_t big = (up(m, kBig) / kBig) * (up(n, kBig) / kBig), tiles = (up(m, kMid) / kMid) * (up(n, kMid) / kMid);
   s.big = blocks > 0 && tiles > 512 && 4 * big <= tiles + tiles / 4;
@@ -953,13 +956,27 @@ int32_t launch_quantize(const void* x, int32_t dtype, int64_t ld, const mtdao_ma
   return MTDAO_OK;
 }
 
-// Waves of a workgroup of the kernel for few rows: enough that each has a few blocks.
+template <int V>
+using Int = std::integral_constant<int, V>;
+
+// Waves of a workgroup of the kernel for few rows: enough that each has a few
+// blocks.  Its columns: sixteen, or 32 where a's blocks, read by every workgroup, are
+// much and there are workgroups enough (64 x 8192 x 2048 9.2 us, 13.7 us with sixteen;
+// 64 x 4096 x 2048 8.8 us, 7.7 us with sixteen).
+constexpr int64_t kWideFrom = 4096;
 template <typename XT, typename CT, int MI>
 void launch_few(const Few& f, hipStream_t st) {
-  constexpr int NJ = MI > 1 ? 2 : 1;
-  const dim3 grid((unsigned)((f.b.rows + 16 * NJ - 1) / (16 * NJ)));
-  if (MI == 1 && f.b.blocks > 32) hipLaunchKernelGGL((k_product8_few<XT, CT, MI, NJ, MI == 1 ? 16 : 8>), grid, dim3(1024), 0, st, f);
-  else hipLaunchKernelGGL((k_product8_few<XT, CT, MI, NJ, 8>), grid, dim3(512), 0, st, f);
+  auto go = [&](auto nj, auto waves) {
+    constexpr int NJ = decltype(nj)::value, W = decltype(waves)::value;
+    hipLaunchKernelGGL((k_product8_few<XT, CT, MI, NJ, W>), dim3((unsigned)((f.b.rows + 16 * NJ - 1) / (16 * NJ))), dim3(64 * W), 0, st, f);
+  };
+  if constexpr (MI > 1) {
+    if (f.b.rows > kWideFrom) return go(Int<2>{}, Int<8>{});
+  }
+  if constexpr (MI < 4) {  // (four fragments of rows: at most 32 blocks)
+    if (f.b.blocks > 32) return go(Int<1>{}, Int<16>{});
+  }
+  go(Int<1>{}, Int<8>{});
 }
 
 Few few_of(const mtdao_matrix8& b, void* c, int64_t ldc, int32_t accumulate, int64_t m) {
