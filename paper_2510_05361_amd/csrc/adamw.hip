@@ -137,12 +137,22 @@ __global__ __launch_bounds__(kThreads) void k_adamw_norm(const Row* rows, const 
   if (threadIdx.x == 0) partial[c] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// The clip factor from the partial sums, each thread in steps of the block.
+// The clip factor from the partial sums, each thread in steps of the block with
+// several loads in flight (one by one: 36 us for 354 M elements, sixteen: 17 us).
 constexpr int kFinish = 1024;
 __global__ __launch_bounds__(kFinish) void k_adamw_clip(const double* partial, int64_t n, double max_norm, float* clip) {
   __shared__ double part[kFinish / 64];
+  constexpr int kAtOnce = 16;
   double sum = 0.0;
-  for (int64_t i = threadIdx.x; i < n; i += kFinish) sum += partial[i];
+  int64_t i = threadIdx.x;
+  for (; i + (kAtOnce - 1) * kFinish < n; i += kAtOnce * kFinish) {
+    double part_of[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) part_of[k] = partial[i + k * kFinish];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) sum += part_of[k];
+  }
+  for (; i < n; i += kFinish) sum += partial[i];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;

@@ -457,8 +457,16 @@ __global__ __launch_bounds__(kCols * 32) void k_peri_columns(Args a, int64_t blo
 #pragma unroll 8
       for (int64_t r = lane; r < count; r += 32) s = fmaf(weight_at(a.gate, wb, (int64_t)((uint32_t)r / a.parts) * a.d + c), in[r * a.d + c], s);
     } else {
-#pragma unroll 8
-      for (int64_t r = lane; r < count; r += 32) s += in[r * a.d + c];
+      int64_t r = lane;
+      for (; r + 15 * 32 < count; r += 16 * 32) {  // (512 workgroups: all of them at once)
+        float v[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = in[(r + k * 32) * a.d + c];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) s += v[k];
+      }
+#pragma unroll 4
+      for (; r < count; r += 32) s += in[r * a.d + c];
     }
   }
   part[lane][col] = s;
