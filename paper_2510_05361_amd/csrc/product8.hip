@@ -79,16 +79,27 @@ __global__ __launch_bounds__(kThreads) void k_quantize8_rows(const T* x, int64_t
 // the tile; else blocks along the rows for q, along the columns for qt.  qt
 // goes through LDS to be written in whole lines.  16384 x 8192 bf16 both ways:
 // 107 us, 5.0 TB/s; the transposed one alone 4.9 TB/s.
+// A launch takes one matrix, or two of as many rows one beside the other.
+struct Quantized {
+  const void* x;
+  int64_t ld, cols;
+  Mat q, qt;      // codes NULL: not wanted
+  int32_t tiles;  // across
+};
 constexpr int kTileThreads = 512;
 template <typename T, bool SQUARE>
-__global__ __launch_bounds__(kTileThreads) void k_quantize8_tile(const T* x, int64_t ld, int64_t cols, int64_t rows, Mat q,
-                                                                 Mat qt) {
+__global__ __launch_bounds__(kTileThreads) void k_quantize8_tile(Quantized one, Quantized two, int64_t rows) {
+  const bool first = (int)blockIdx.x < one.tiles;
+  const T* x = reinterpret_cast<const T*>(first ? one.x : two.x);
+  const int64_t ld = first ? one.ld : two.ld, cols = first ? one.cols : two.cols;
+  const Mat q = first ? one.q : two.q, qt = first ? one.qt : two.qt;
+  const int tile = first ? (int)blockIdx.x : (int)blockIdx.x - one.tiles, tiles = first ? one.tiles : two.tiles;
   constexpr int kRows = 4, kWaves = kTileThreads / 64;
   __shared__ __attribute__((aligned(16))) uint8_t turned[kBlock8 * kBlock8];
   __shared__ __attribute__((aligned(16))) float most[kWaves][kBlock8];
   __shared__ __attribute__((aligned(8))) uint8_t bytes_of[kBlock8];
   const int c8 = (int)(threadIdx.x % 16) * kE, r4 = (int)(threadIdx.x / 16) * kRows, wave = threadIdx.x / 64;
-  const int64_t row0 = (int64_t)blockIdx.y * kBlock8, col0 = (int64_t)blockIdx.x * kBlock8;
+  const int64_t row0 = (int64_t)blockIdx.y * kBlock8, col0 = (int64_t)tile * kBlock8;
   const int64_t in_cols = cols - col0 - c8, in_rows = rows - row0 - r4;
   const int nc = in_cols < 0 ? 0 : in_cols > kE ? kE : (int)in_cols;
   float a[kRows][kE];
@@ -177,15 +188,15 @@ __global__ __launch_bounds__(kTileThreads) void k_quantize8_tile(const T* x, int
       }
     }
     // (the last block's thread writes the unused bytes of its four too)
-    const int past = blockIdx.x + 1 == gridDim.x ? (blockIdx.x & ~3u) + 4 : blockIdx.x + 1;
+    const int past = tile + 1 == tiles ? (tile & ~3) + 4 : tile + 1;
     if constexpr (SQUARE) {
       if (threadIdx.x == 0)
-        for (int k = blockIdx.x; k < past; ++k) *scale_at(q, blockIdx.y, k) = k == (int)blockIdx.x ? (uint8_t)row_byte[0] : 127;
+        for (int k = tile; k < past; ++k) *scale_at(q, blockIdx.y, k) = k == tile ? (uint8_t)row_byte[0] : 127;
     } else if (threadIdx.x % 16 == 0) {
 #pragma unroll
       for (int i = 0; i < kRows; ++i)
         if (i < in_rows)
-          for (int k = blockIdx.x; k < past; ++k) *scale_at(q, row0 + r4 + i, k) = k == (int)blockIdx.x ? (uint8_t)row_byte[i] : 127;
+          for (int k = tile; k < past; ++k) *scale_at(q, row0 + r4 + i, k) = k == tile ? (uint8_t)row_byte[i] : 127;
     }
   }
   if (qt.codes) {
@@ -204,7 +215,7 @@ __global__ __launch_bounds__(kTileThreads) void k_quantize8_tile(const T* x, int
     const int past = blockIdx.y + 1 == gridDim.y ? (blockIdx.y & ~3u) + 4 : blockIdx.y + 1;
     if constexpr (SQUARE) {
       if (threadIdx.x == 0)
-        for (int k = blockIdx.y; k < past; ++k) *scale_at(qt, blockIdx.x, k) = k == (int)blockIdx.y ? (uint8_t)col_byte[0] : 127;
+        for (int k = blockIdx.y; k < past; ++k) *scale_at(qt, tile, k) = k == (int)blockIdx.y ? (uint8_t)col_byte[0] : 127;
     } else if (threadIdx.x < 16) {
 #pragma unroll
       for (int t = 0; t < kE; ++t)
@@ -929,30 +940,38 @@ int32_t check_workspace(const void* workspace, size_t given, size_t need, std::s
   return MTDAO_OK;
 }
 
+Quantized quantized_of(const void* x, int64_t ld, const mtdao_matrix8* q, const mtdao_matrix8* qt) {
+  const int64_t cols = q ? q->cols : qt->rows;
+  return {x, ld, cols, mat_of(q), mat_of(qt), (int32_t)(up(cols, kBlock8) / kBlock8)};
+}
+
+// Tiles of one matrix, or of two (`two.tiles` not 0) of as many rows.
+int32_t launch_tiles(const Quantized& one, const Quantized& two, int32_t dtype, int64_t rows, bool square, hipStream_t st, std::string* e) {
+  const int64_t ty = up(rows, kBlock8) / kBlock8;
+  if (ty > 65535) return fail(e, MTDAO_ERR_INVALID_ARG, "the matrix exceeds the largest launch");
+  const dim3 grid((unsigned)(one.tiles + two.tiles), (unsigned)ty), block(kTileThreads);
+  auto with = [&](auto t) {
+    using T = decltype(t);
+    if (square) hipLaunchKernelGGL((k_quantize8_tile<T, true>), grid, block, 0, st, one, two, rows);
+    else hipLaunchKernelGGL((k_quantize8_tile<T, false>), grid, block, 0, st, one, two, rows);
+  };
+  if (dtype == MTDAO_BF16) with(bf16_t{});
+  else with(float{});
+  return MTDAO_OK;
+}
+
 int32_t launch_quantize(const void* x, int32_t dtype, int64_t ld, const mtdao_matrix8* q, const mtdao_matrix8* qt, hipStream_t st,
                         std::string* e) {
   const int64_t rows = q ? q->rows : qt->cols, cols = q ? q->cols : qt->rows;
-  const Mat m = mat_of(q), mt = mat_of(qt);
   const bool square = (q ? q : qt)->scale_rows == kBlock8;
-  auto with = [&](auto t) {
-    using T = decltype(t);
-    const T* in = static_cast<const T*>(x);
-    if (!qt && !square) {
-      const int groups = (m.blocks + 3) / 4;
-      const int64_t wgs = (rows + 3) / 4 * groups;
-      if (wgs > INT64_C(0xffffff)) return false;  // 2^32 threads
-      hipLaunchKernelGGL(k_quantize8_rows<T>, dim3((unsigned)wgs), dim3(kThreads), 0, st, in, ld, cols, groups, m);
-      return true;
-    }
-    const int64_t ty = up(rows, kBlock8) / kBlock8;
-    if (ty > 65535) return false;
-    const dim3 grid((unsigned)(up(cols, kBlock8) / kBlock8), (unsigned)ty);
-    if (square) hipLaunchKernelGGL((k_quantize8_tile<T, true>), grid, dim3(kTileThreads), 0, st, in, ld, cols, rows, m, mt);
-    else hipLaunchKernelGGL((k_quantize8_tile<T, false>), grid, dim3(kTileThreads), 0, st, in, ld, cols, rows, m, mt);
-    return true;
-  };
-  if (!(dtype == MTDAO_BF16 ? with(bf16_t{}) : with(float{})))
-    return fail(e, MTDAO_ERR_INVALID_ARG, "the matrix exceeds the largest launch");
+  if (qt || square) return launch_tiles(quantized_of(x, ld, q, qt), Quantized{}, dtype, rows, square, st, e);
+  const Mat m = mat_of(q);
+  const int groups = (m.blocks + 3) / 4;
+  const int64_t wgs = (rows + 3) / 4 * groups;
+  if (wgs > INT64_C(0xffffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "the matrix exceeds the largest launch");  // 2^32 threads
+  const dim3 grid((unsigned)wgs), block(kThreads);
+  if (dtype == MTDAO_BF16) hipLaunchKernelGGL(k_quantize8_rows<bf16_t>, grid, block, 0, st, static_cast<const bf16_t*>(x), ld, cols, groups, m);
+  else hipLaunchKernelGGL(k_quantize8_rows<float>, grid, block, 0, st, static_cast<const float*>(x), ld, cols, groups, m);
   return MTDAO_OK;
 }
 
@@ -1250,8 +1269,7 @@ int32_t mtdao_linear8_backward(const void* dy, const void* x, int32_t dtype, int
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   RoctxRange range("mtdao_linear8_backward m=%lld n=%lld k=%lld", (long long)rows, (long long)n, (long long)k);
   if (rows > 0 && n > 0 && k > 0) {
-    r = launch_quantize(dy, dtype, ld_dy, &q, &qt, st, e);
-    if (r == MTDAO_OK) r = launch_quantize(x, dtype, ld_x, nullptr, &xt, st, e);
+    r = launch_tiles(quantized_of(dy, ld_dy, &q, &qt), quantized_of(x, ld_x, nullptr, &xt), dtype, rows, false, st, e);
   }
   char* product = static_cast<char*>(workspace) + f.product;
   if (r == MTDAO_OK && rows > 0 && k > 0) r = launch_product(q, *wt, dx, dtype, ld_dx, 0, product, st, e);
