@@ -150,8 +150,8 @@ typedef struct mtdao_peri_norm_args {
 
 int32_t mtdao_peri_norm(const mtdao_peri_norm_args* a, void* hip_stream);
 
-/* Device workspace of the backward pass (partial sums of the three
- * parameter gradients).  Reads the sizes of a and which of f, w_pre and gate
+/* Device workspace of the backward pass (partial sums for the parameter
+ * gradients).  Reads the sizes of a and which of f, w_pre and gate
  * are given.  Host-only. */
 int32_t mtdao_peri_norm_backward_workspace_bytes(const mtdao_peri_norm_args* a, size_t* bytes);
 

@@ -610,8 +610,11 @@ int backward_threads(int64_t d) { return d <= 64 * kE ? 64 : d <= 128 * kE ? 128
 // 1 x 8192 4.5 us (7.0), 512 x 8192 8.6 us (8.3).
 constexpr int64_t kFew = INT64_C(1) << 20;
 
-// How the rows go over the workgroups, backward: at most kBlocks of them, at
-// least eight rows each, none across gates unless it has them whole.
+// How the rows go over the workgroups, backward: kBlocks of them at most, one a
+// CU as long as that leaves them two to eight rows, none across gates unless it
+// has them whole.  (A workgroup for each two rows up to 512 of them, against eight
+// rows each: 64 x 2048 9.0 us (14.1), 1024 x 2048 17.3 us (16.3; with four 14.6 us),
+// 2047 x 768 14.5 us (13.0): more sums to write and read back.)
 constexpr int64_t kBlocks = 512;
 struct Plan {
   int64_t blocks, per_block, parts;
@@ -619,7 +622,8 @@ struct Plan {
 };
 Plan backward_plan(const mtdao_peri_norm_args& a) {
   Plan p;
-  const int64_t rows = std::max<int64_t>(8, (a.rows + kBlocks - 1) / kBlocks);
+  const int64_t few = std::min<int64_t>(8, std::max<int64_t>(2, (a.rows + 255) / 256));
+  const int64_t rows = std::max(few, (a.rows + kBlocks - 1) / kBlocks);
   const int64_t gates = gates_of(a);
   if (gates > 1 && a.rows_per_gate <= rows / 2) {
     p.per_block = rows / a.rows_per_gate;
@@ -773,7 +777,7 @@ int32_t mtdao_peri_norm_backward(const mtdao_peri_norm_args* args, void* workspa
   }
   const int64_t jobs = 2 + (plan.whole_gates || a.rows == 0 ? 0 : gates_of(a));
   const int64_t blocks = a.rows > 0 ? plan.blocks : 0;  // no rows: sums of nothing
-  // (gates that are not whole hold over a 1024th of the rows each, so jobs fit a launch)
+  // (gates that are not whole hold over a 1024th of the rows each, or two, so jobs fit a launch)
   hipLaunchKernelGGL(k_peri_columns, dim3((unsigned)((a.d + kCols - 1) / kCols), (unsigned)jobs), dim3(kCols * 32), 0, st, k,
                      blocks);
   return hip_check(e, hipGetLastError(), "mtdao_peri_norm_backward launch");
