@@ -440,45 +440,46 @@ __global__ __launch_bounds__(TPR > kGroup ? TPR : kGroup) void k_peri_norm_backw
 
 // Sums of the workgroups' partial rows.  Job 0: w_pre.  Job 1: w_post, of the
 // sums over its rows (whole_gates) or of t times the gate of each workgroup.
-// Job 2 + j: gate j, of t.  32 columns x 32 rows at once.
+// From job 2 on 32 / fold gates each, of t, with fold the power of two that holds
+// a gate's parts (32 at most).  32 columns x 32 rows at once.
 constexpr int kCols = 32;
-__global__ __launch_bounds__(kCols * 32) void k_peri_columns(Args a, int64_t blocks) {
+__global__ __launch_bounds__(kCols * 32) void k_peri_columns(Args a, int64_t blocks, int fold) {
   __shared__ float part[32][kCols + 1];
   const int col = threadIdx.x % kCols, lane = threadIdx.x / kCols;
   const int64_t c = (int64_t)blockIdx.x * kCols + col;
-  const int64_t job = blockIdx.y;
+  const int job = blockIdx.y, apart = job < 2 ? 32 : fold;
   if ((job == 0 && !a.w_pre) || (job == 1 && !a.f)) return;
   const bool wb = a.weight_bf16 != 0, gated = a.gate && !a.whole_gates;
-  const int64_t from = job < 2 ? 0 : (job - 2) * a.parts, count = job < 2 ? blocks : a.parts;
+  const int64_t gate = job < 2 ? 0 : (int64_t)(job - 2) * (32 / fold) + lane / fold;
+  const int64_t from = job < 2 ? 0 : gate * a.parts, count = job < 2 ? blocks : gate < a.gates ? a.parts : 0;
   const float* in = a.partial + ((job == 0 ? 0 : blocks) + from) * a.d;
   float s = 0.0f;
   if (c < a.d) {
+    int64_t r = lane % apart;
     if (job == 1 && gated) {
 #pragma unroll 8
-      for (int64_t r = lane; r < count; r += 32) s = fmaf(weight_at(a.gate, wb, (int64_t)((uint32_t)r / a.parts) * a.d + c), in[r * a.d + c], s);
+      for (; r < count; r += 32) s = fmaf(weight_at(a.gate, wb, (int64_t)((uint32_t)r / a.parts) * a.d + c), in[r * a.d + c], s);
     } else {
-      int64_t r = lane;
-      for (; r + 15 * 32 < count; r += 16 * 32) {  // (512 workgroups: all of them at once)
+      for (; r + 15 * apart < count; r += 16 * apart) {  // (512 workgroups: all of them at once)
         float v[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = in[(r + k * 32) * a.d + c];
+        for (int k = 0; k < 16; ++k) v[k] = in[(r + k * apart) * a.d + c];
 #pragma unroll
         for (int k = 0; k < 16; ++k) s += v[k];
       }
 #pragma unroll 4
-      for (; r < count; r += 32) s += in[r * a.d + c];
+      for (; r < count; r += apart) s += in[r * a.d + c];
     }
   }
   part[lane][col] = s;
   __syncthreads();
-  if (lane == 0 && c < a.d) {
-    s = 0.0f;
-#pragma unroll
-    for (int r = 0; r < 32; ++r) s += part[r][col];
-    if (job == 0) a.d_w_pre[c] = s;
-    else if (job == 1) a.d_w_post[c] = a.whole_gates ? s : s * a.scale;
-    else a.d_gate[(job - 2) * a.d + c] = s * a.scale * weight_at(a.w_post, wb, c);
-  }
+  if (lane % apart != 0 || c >= a.d) return;
+  s = 0.0f;
+#pragma unroll 8
+  for (int r = 0; r < apart; ++r) s += part[lane + r][col];
+  if (job == 0) a.d_w_pre[c] = s;
+  else if (job == 1) a.d_w_post[c] = a.whole_gates ? s : s * a.scale;
+  else if (gate < a.gates) a.d_gate[gate * a.d + c] = s * a.scale * weight_at(a.w_post, wb, c);
 }
 
 // --------------------------------------------------------------------- host
@@ -775,11 +776,13 @@ int32_t mtdao_peri_norm_backward(const mtdao_peri_norm_args* args, void* workspa
       }
     });
   }
-  const int64_t jobs = 2 + (plan.whole_gates || a.rows == 0 ? 0 : gates_of(a));
+  int fold = 1;
+  while (fold < 32 && fold < plan.parts) fold *= 2;
+  const int64_t jobs = 2 + (plan.whole_gates || a.rows == 0 ? 0 : (gates_of(a) + 32 / fold - 1) / (32 / fold));
   const int64_t blocks = a.rows > 0 ? plan.blocks : 0;  // no rows: sums of nothing
   // (gates that are not whole hold over a 1024th of the rows each, or two, so jobs fit a launch)
-  hipLaunchKernelGGL(k_peri_columns, dim3((unsigned)((a.d + kCols - 1) / kCols), (unsigned)jobs), dim3(kCols * 32), 0, st, k,
-                     blocks);
+  hipLaunchKernelGGL(k_peri_columns, dim3((unsigned)((a.d + kCols - 1) / kCols), (unsigned)jobs), dim3(kCols * 32), 0, st, k, blocks,
+                     fold);
   return hip_check(e, hipGetLastError(), "mtdao_peri_norm_backward launch");
 }
 
