@@ -626,8 +626,12 @@ Plan backward_plan(const mtdao_peri_norm_args& a) {
   const int64_t few = std::min<int64_t>(8, std::max<int64_t>(2, (a.rows + 255) / 256));
   const int64_t rows = std::max(few, (a.rows + kBlocks - 1) / kBlocks);
   const int64_t gates = gates_of(a);
-  if (gates > 1 && a.rows_per_gate <= rows / 2) {
-    p.per_block = rows / a.rows_per_gate;
+  // Whole gates up to as many rows as a workgroup has (4452 x 3968, five rows a gate
+  // of nine: 94 -> 61 us; 16384 x 2048, 32 of 32: 83 -> 74 us); where a workgroup has
+  // several row groups, which then take a gate each, up to two thirds (d = 256, 20 of
+  // 32: 37 -> 30 us, 32 of 32: 24 -> 39 us).
+  if (gates > 1 && a.rows_per_gate <= (backward_threads(a.d) < kGroup ? 2 * rows / 3 : rows)) {
+    p.per_block = (rows + a.rows_per_gate - 1) / a.rows_per_gate;
     p.parts = 1;
     p.blocks = (gates + p.per_block - 1) / p.per_block;
     p.whole_gates = true;
@@ -780,7 +784,7 @@ int32_t mtdao_peri_norm_backward(const mtdao_peri_norm_args* args, void* workspa
   while (fold < 32 && fold < plan.parts) fold *= 2;
   const int64_t jobs = 2 + (plan.whole_gates || a.rows == 0 ? 0 : (gates_of(a) + 32 / fold - 1) / (32 / fold));
   const int64_t blocks = a.rows > 0 ? plan.blocks : 0;  // no rows: sums of nothing
-  // (gates that are not whole hold over a 1024th of the rows each, or two, so jobs fit a launch)
+  // (gates that are not whole hold over a 768th of the rows each, or two, so jobs fit a launch)
   hipLaunchKernelGGL(k_peri_columns, dim3((unsigned)((a.d + kCols - 1) / kCols), (unsigned)jobs), dim3(kCols * 32), 0, st, k, blocks,
                      fold);
   return hip_check(e, hipGetLastError(), "mtdao_peri_norm_backward launch");

@@ -156,6 +156,14 @@ def test_rows_and_gates(t, gate, d):
     check_backward(s, "rms", gate or 0, 0.5)
 
 
+@pytest.mark.parametrize("t,d,gate", [(4452, 300, 5), (4452, 300, 6), (4452, 300, 7), (2500, 1500, 4), (2500, 1500, 8), (2500, 1500, 9), (600, 2056, 3),
+                                      (600, 4100, 2), (600, 4100, 4), (9000, 64, 18), (9000, 64, 11), (3000, 1021, 5), (2100, 900, 64)])
+def test_gates_of_a_few_rows(t, d, gate):
+    """Gates that a workgroup has whole, several or one, and those it has not."""
+    s = inputs(t, d, "f32", "bf16", gate=gate)
+    check_backward(s, "layer", gate, 0.5)
+
+
 @pytest.mark.parametrize("kind", ["rms", "layer"])
 @pytest.mark.parametrize("drop", [("f",), ("w_pre",), ("d_out",), ("dn",), ("f", "d_out"), ("w_pre", "gate"), ("gate",)])
 @pytest.mark.parametrize("d", [200, 2500])
