@@ -184,6 +184,7 @@ int32_t mtdao_quantize8(const void* x, int32_t dtype, int64_t ld, const mtdao_ma
 
 /* c [a->rows][b->rows] = a b^T: the sums over the common columns (a->cols ==
  * b->cols) in fp32, rounded once to c_dtype.  accumulate (fp32 c only): c +=.
+ * Without columns the sums are zero, and nothing of a or b is read.
  * The order of the sums depends on the sizes alone.
  * workspace: mtdao_product8_workspace_bytes, 256-byte aligned. */
 int32_t mtdao_product8_workspace_bytes(int64_t m, int64_t n, int64_t k, size_t* bytes);

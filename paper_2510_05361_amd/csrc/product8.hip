@@ -676,6 +676,18 @@ __global__ __launch_bounds__(kThreads) void k_product8_join(Product p) {
   store_some<4>(to, n, o);
 }
 
+// c = 0: a product over no columns, which has no block that the kernels above could
+// load.  Four columns a thread, in steps of the grid.
+template <typename CT>
+__global__ __launch_bounds__(kThreads) void k_product8_zero(CT* c, int64_t rows, int64_t cols, int64_t ldc) {
+  const int64_t quads = (cols + 3) / 4;
+  const float zeros[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x; at < rows * quads; at += (int64_t)gridDim.x * kThreads) {
+    const int64_t row = at / quads, col = (at - row * quads) * 4;
+    store_some<4>(c + row * ldc + col, cols - col > 4 ? 4 : (int)(cols - col), zeros);
+  }
+}
+
 // Products of a few rows (up to 64): what counts is to read b once, with as
 // many loads in flight as the chip takes.  A workgroup has sixteen or 32 rows
 // of b (columns of c), whose blocks its waves take in turn, straight from memory
@@ -853,10 +865,10 @@ struct Shape {
 Shape shape_of(int64_t m, int64_t n, int64_t k) {
   const int64_t blocks = up(k, kBlock8) / kBlock8;
   const bool few = m <= 16 || (m <= kFew && (m <= 32 ? 2 : 4) * blocks <= 128);
-  Shape s = {few && blocks > 0, false, false, 1, (int32_t)blocks};
+  Shape s = {few, false, false, 1, (int32_t)blocks};
   if (s.few) return s;
   const int64_t big = (up(m, kBig) / kBig) * (up(n, kBig) / kBig), tiles = (up(m, kMid) / kMid) * (up(n, kMid) / kMid);
-  s.big = blocks > 0 && tiles > 512 && 4 * big <= tiles + tiles / 4;
+  s.big = tiles > 512 && 4 * big <= tiles + tiles / 4;
   s.shared = !s.big && tiles > 256;
   if (!s.big && tiles > 0 && tiles <= 128 && blocks >= 8) {
     const int64_t parts = std::min<int64_t>(256 / tiles, blocks / 4);
@@ -1041,6 +1053,18 @@ int32_t allow_lds(const void* kernel, int bytes, std::string* e) try {
 // a, b, c: checked; c has elements.
 int32_t launch_product(const mtdao_matrix8& a, const mtdao_matrix8& b, void* c, int32_t c_dtype, int64_t ldc, int32_t accumulate,
                        void* workspace, hipStream_t st, std::string* e) {
+  if (a.cols == 0) {  // no codes, no scales: their addresses may be anything
+    if (accumulate) return MTDAO_OK;
+    const int64_t quads = a.rows * ((b.rows + 3) / 4);
+    const dim3 grid((unsigned)std::min<int64_t>((quads + kThreads - 1) / kThreads, 4096)), block(kThreads);
+    auto zero = [&](auto ct) {
+      using CT = decltype(ct);
+      hipLaunchKernelGGL(k_product8_zero<CT>, grid, block, 0, st, static_cast<CT*>(c), a.rows, b.rows, ldc);
+    };
+    if (c_dtype == MTDAO_F32) zero(float{});
+    else zero(bf16_t{});
+    return MTDAO_OK;
+  }
   const Shape shape = shape_of(a.rows, b.rows, a.cols);
   if (shape.few) {
     Few f = few_of(b, c, ldc, accumulate, a.rows);
@@ -1229,7 +1253,7 @@ int32_t mtdao_linear8(const void* x, int32_t dtype, int64_t rows, int64_t ld, co
   if (rows <= kFewWhole && w->cols > 0) {
     r = launch_few_whole(x, dtype, rows, ld, *w, y, y_dtype, ldy, st);
   } else {
-    r = launch_quantize(x, dtype, ld, &q, nullptr, st, e);
+    if (w->cols > 0) r = launch_quantize(x, dtype, ld, &q, nullptr, st, e);
     if (r == MTDAO_OK)
       r = launch_product(q, *w, y, y_dtype, ldy, 0, static_cast<char*>(workspace) + f.product, st, e);
   }

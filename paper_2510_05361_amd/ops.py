@@ -13,6 +13,7 @@ for any torch operation.  There is no CPU path.
 from __future__ import annotations
 
 import functools
+import math
 from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
@@ -333,6 +334,11 @@ def _matrix(x: torch.Tensor) -> torch.Tensor:
     return x
 
 
+def _flat(x: torch.Tensor) -> torch.Tensor:
+    """x [..., k] as a matrix [tokens, k] (k may be 0)."""
+    return _matrix(x if x.dim() == 2 else x.reshape(math.prod(x.shape[:-1]), x.shape[-1]))
+
+
 def _ld(x: torch.Tensor) -> int:
     return x.stride(0) if x.shape[0] > 1 else x.shape[1]
 
@@ -410,7 +416,7 @@ def linear8(x: torch.Tensor, w: Weight8, *, dtype: Optional[torch.dtype] = None)
     if x.shape[-1] != wq.cols:
         raise ValueError(f"x has {x.shape[-1]} columns, the weight {wq.cols}")
     dev = _on_device(x, wq._buf)
-    x2 = _matrix(x if x.dim() == 2 else x.reshape(-1, wq.cols))
+    x2 = _flat(x)
     m = x2.shape[0]
     y = torch.empty((*x.shape[:-1], wq.rows), dtype=dtype or x.dtype, device=dev)
     need = _linear_workspace(m, wq.rows, wq.cols)[0]
@@ -438,8 +444,8 @@ def linear8_backward(dy: torch.Tensor, x: torch.Tensor, w: Weight8, *, dw: Optio
     elif tuple(dw.shape) != (n, k) or k > 1 and dw.stride(1) != 1 or dw.dtype != torch.float32:
         raise ValueError(f"dw is {tuple(dw.shape)}, {dw.dtype} with strides {dw.stride()}, not float32 [{n}, {k}] with contiguous rows")
     dev = _on_device(x, dy, dw, w.qt._buf)
-    x2 = _matrix(x if x.dim() == 2 else x.reshape(-1, k))
-    dy2 = _matrix(dy if dy.dim() == 2 else dy.reshape(-1, n))
+    x2 = _flat(x)
+    dy2 = _flat(dy)
     m = x2.shape[0]
     dx = _empty(x, x.shape, dy.dtype)
     need = _linear_workspace(m, n, k)[1]

@@ -300,3 +300,31 @@ def test_refusals():
         ops.product8(q, ops.quantize8(rand((8, 130))))
     with pytest.raises(RuntimeError, match="accumulate"):
         ops.product8(q, w.q, out=torch.zeros((4, 8), device="cuda", dtype=torch.bfloat16), accumulate=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n", [(1, 3), (20, 5), (130, 259), (3000, 1030)])
+def test_empty_contractions(m, n, dtype):
+    """Sums over no columns are zero; with accumulate c stays as it is."""
+    x, w = torch.empty((m, 0), dtype=DT[dtype], device="cuda"), torch.empty((n, 0), device="cuda")
+    wide = torch.full((m + 2, n + 5), 7.0, device="cuda").to(DT[dtype])
+    out = wide[1:-1, 3:3 + n]
+    ops.product8(ops.quantize8(x), ops.quantize8(w), out=out)
+    assert bool((out == 0).all())
+    out[:] = 7.0
+    assert bool((wide == 7.0).all())
+    kept = torch.randn((m, n), device="cuda")
+    before = kept.clone()
+    ops.product8(ops.quantize8(x), ops.quantize8(w), out=kept, accumulate=True)
+    assert torch.equal(kept, before)
+    assert torch.equal(ops.linear8(x, ops.Weight8(w)), torch.zeros((m, n), dtype=DT[dtype], device="cuda"))
+    assert ops.linear8(x.view(1, m, 0), ops.Weight8(w)).shape == (1, m, n)
+
+
+@pytest.mark.parametrize("m", [3, 200])
+def test_linear_of_no_outputs(m):
+    w = ops.Weight8(torch.empty((0, 130), device="cuda"))
+    x = rand((m, 130))
+    assert ops.linear8(x, w).shape == (m, 0)
+    dx, dw = ops.linear8_backward(torch.empty((m, 0), device="cuda"), x, w)
+    assert dw.shape == (0, 130) and torch.equal(dx, torch.zeros((m, 130), device="cuda"))

@@ -1,0 +1,62 @@
+"""What the operators of include/mtdao_ops.h launch (CPU: launches are taken
+down, nothing runs; addresses are numbers)."""
+
+import pytest
+
+import launch_recorder
+
+
+@pytest.fixture(scope="module")
+def run(tmp_path_factory):
+    shim = launch_recorder.build(str(tmp_path_factory.mktemp("shim")))
+    return lambda body: launch_recorder.run(shim, body)
+
+
+def names(launches):
+    return [name for name, *_ in launches]
+
+
+# ------------------------------------------------------------ 8-bit product
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("m,n", [(1, 5), (40, 5), (600, 700), (40000, 4000)])
+def test_empty_contractions_read_no_matrix(run, m, n, dtype):
+    """Products over no columns, whose codes and scales may be NULL: zeros, or
+    nothing where c is added to."""
+    launches, _ = run(f"""
+        B = 1 << 40
+        empty = lambda rows, scale_rows=1: c.Matrix8(None, None, rows, 0, 128, 4 * -(-rows // scale_rows), scale_rows)
+        c.mtdao_product8(empty({m}), empty({n}), B, {dtype}, {n}, False, None, 0, None)
+        c.mtdao_linear8(B, {dtype}, {m}, 0, empty({n}, 128), B << 1, {dtype}, {n}, None, 0, None)
+        c.mtdao_product8(empty({m}), empty({n}), B, 0, {n}, True, None, 0, None)
+    """)
+    assert names(launches) == ["k_product8_zero"] * 2
+
+
+@pytest.mark.parametrize("tokens,outputs,inputs", [(0, 40, 256), (0, 700, 3000), (30, 0, 256), (3, 0, 40)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_linear_gradients_of_nothing(run, tokens, outputs, inputs, accumulate):
+    """No tokens: dw = 0 (or as it was).  No outputs: dx = 0.  The workspace holds
+    no scales of matrices without columns."""
+    launches, _ = run(f"""
+        B = 1 << 40
+        t, n, k = {tokens}, {outputs}, {inputs}
+        wt = c.Matrix8(B, B + (1 << 30), k, n, max(1, -(-n // 128)) * 128, 4 * -(-k // 128), 128)
+        need = c.mtdao_linear8_workspace_bytes(t, n, k)[1]
+        c.mtdao_linear8_backward(B << 1, B << 2, 0, t, n, k, wt, B << 3, k, B << 4, k, {accumulate}, B << 5, need, None)
+    """)
+    assert names(launches) == ([] if tokens == 0 and accumulate else ["k_product8_zero"])
+
+
+def test_products_with_a_contraction(run):
+    """... launch what they did."""
+    launches, _ = run("""
+        B = 1 << 40
+        def matrix(rows, cols, at, scale_rows=1):
+            return c.Matrix8(at, at + (1 << 36), rows, cols, -(-cols // 128) * 128, 4 * -(-rows // scale_rows), scale_rows)
+        for m, n, k in ((8, 512, 256), (64, 512, 1), (300, 512, 1), (2000, 512, 128), (8192, 8192, 128), (1536, 512, 8191)):
+            need = c.mtdao_product8_workspace_bytes(m, n, k)
+            c.mtdao_product8(matrix(m, k, B), matrix(n, k, B + (1 << 38)), B << 2, 0, n, False, B << 3, need, None)
+    """)
+    assert names(launches) == ["k_product8_few"] * 2 + ["k_product8_tiles"] * 4 + ["k_product8_join"]
