@@ -726,7 +726,7 @@ int32_t mtdao_peri_norm_backward(const mtdao_peri_norm_args* args, void* workspa
   if (r != MTDAO_OK) return r;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   Args k = device_args(a);
-  const Plan plan = backward_plan(a);
+  const Plan plan = a.rows > 0 ? backward_plan(a) : Plan{0, 1, 1, false};  // no rows: sums of nothing
   const size_t need = backward_bytes(a);
   if (a.rows > 0) {
     if (a.w_pre) r = check_rows(a, a.x, a.ld_x, a.stream_dtype, "x", e);
@@ -782,10 +782,9 @@ int32_t mtdao_peri_norm_backward(const mtdao_peri_norm_args* args, void* workspa
   }
   int fold = 1;
   while (fold < 32 && fold < plan.parts) fold *= 2;
-  const int64_t jobs = 2 + (plan.whole_gates || a.rows == 0 ? 0 : (gates_of(a) + 32 / fold - 1) / (32 / fold));
-  const int64_t blocks = a.rows > 0 ? plan.blocks : 0;  // no rows: sums of nothing
+  const int64_t jobs = 2 + (plan.whole_gates ? 0 : (gates_of(a) + 32 / fold - 1) / (32 / fold));
   // (gates that are not whole hold over a 768th of the rows each, or two, so jobs fit a launch)
-  hipLaunchKernelGGL(k_peri_columns, dim3((unsigned)((a.d + kCols - 1) / kCols), (unsigned)jobs), dim3(kCols * 32), 0, st, k, blocks,
+  hipLaunchKernelGGL(k_peri_columns, dim3((unsigned)((a.d + kCols - 1) / kCols), (unsigned)jobs), dim3(kCols * 32), 0, st, k, plan.blocks,
                      fold);
   return hip_check(e, hipGetLastError(), "mtdao_peri_norm_backward launch");
 }

@@ -332,3 +332,22 @@ def test_refusals():
                  lambda: ops.peri_norm(torch.zeros(2, 8193, device="cuda"), None, None, torch.ones(8193, device="cuda"))):
         with pytest.raises(RuntimeError):
             call()
+
+
+@pytest.mark.parametrize("per", [0, 3])
+def test_gradients_of_no_rows_at_the_c_entry(per):
+    """Sums over no rows are zero."""
+    from paper_2510_05361_amd import mtdao_ops as c_ops
+    d = 72
+    w = torch.ones(d, device="cuda")
+    sums = torch.full((2, d), 7.0, device="cuda")
+    a = c_ops.PeriNormArgs()
+    a.rows, a.d, a.eps, a.scale, a.rows_per_gate = 0, d, EPS, 0.5, per
+    a.ld_x = a.ld_f = a.ld_d_out = a.ld_dn = d
+    a.f = a.w_post = a.w_pre = w.data_ptr()
+    a.d_w_post, a.d_w_pre = sums[0].data_ptr(), sums[1].data_ptr()
+    if per:
+        a.gate, a.d_gate = w.data_ptr(), w.data_ptr()
+    assert c_ops.mtdao_peri_norm_backward_workspace_bytes(a) == 0
+    c_ops.mtdao_peri_norm_backward(a, None, 0, torch.cuda.current_stream().cuda_stream)
+    assert bool((sums == 0).all()) and bool((w == 1).all())

@@ -60,3 +60,29 @@ def test_products_with_a_contraction(run):
             c.mtdao_product8(matrix(m, k, B), matrix(n, k, B + (1 << 38)), B << 2, 0, n, False, B << 3, need, None)
     """)
     assert names(launches) == ["k_product8_few"] * 2 + ["k_product8_tiles"] * 4 + ["k_product8_join"]
+
+
+# -------------------------------------------------------- Peri-LN boundary
+
+PERI = """
+        B = 1 << 40
+        def peri(rows, d, per=0, drop=(), **kw):
+            a = c.PeriNormArgs()
+            a.rows, a.d, a.eps, a.scale, a.rows_per_gate = rows, d, 1e-5, 0.5, per
+            a.ld_x = a.ld_f = a.ld_d_out = a.ld_dn = d
+            for i, name in enumerate(("x", "f", "w_post", "w_pre", "d_out", "dn", "x_out", "n_out", "df", "d_w_post", "d_w_pre", "gate", "d_gate")):
+                if name not in drop and (per or "gate" not in name):
+                    setattr(a, name, B + (i << 42))
+            for k, v in kw.items():
+                setattr(a, k, v)
+            return a
+        def backward(a):
+            c.mtdao_peri_norm_backward(a, B << 8, c.mtdao_peri_norm_backward_workspace_bytes(a), None)
+"""
+
+
+@pytest.mark.parametrize("more", ["", ", drop=('w_pre', 'dn')", ", drop=('f', 'w_post', 'df', 'd_w_post')", ", 5"])
+def test_boundary_gradients_of_no_rows(run, more):
+    """Only the sums over rows are written."""
+    launches, _ = run(PERI + f"        backward(peri(0, 64{more}))\n")
+    assert launches == [("k_peri_columns", (2, 2, 1), 1024, 0)]
