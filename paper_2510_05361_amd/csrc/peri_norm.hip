@@ -356,7 +356,9 @@ __global__ __launch_bounds__(TPR > kGroup ? TPR : kGroup) void k_peri_norm_backw
           q[2] = fmaf(y[v][t] * w_pre[v][t], x[v][t], q[2]);
         }
       sum_row<TPR>(q, buf + 3 * kWaves);
-      const float sx = inverse_root(fmaf(q[0], a.inv_d, a.eps)), sf = inverse_root(fmaf(q[1], a.inv_d, a.eps));
+      // (zeros stand for what is not there, rows past the end among it: without an eps their roots would be infinite)
+      const float sx = live && a.w_pre ? inverse_root(fmaf(q[0], a.inv_d, a.eps)) : 0.0f;
+      const float sf = live && a.f ? inverse_root(fmaf(q[1], a.inv_d, a.eps)) : 0.0f;
       const float along = q[2] * sx * a.inv_d;
       float c[2] = {0.0f, 0.0f};  // a = dd u against fh, and its sum
 #pragma unroll

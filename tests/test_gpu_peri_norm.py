@@ -351,3 +351,16 @@ def test_gradients_of_no_rows_at_the_c_entry(per):
     assert c_ops.mtdao_peri_norm_backward_workspace_bytes(a) == 0
     c_ops.mtdao_peri_norm_backward(a, None, 0, torch.cuda.current_stream().cuda_stream)
     assert bool((sums == 0).all()) and bool((w == 1).all())
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("t,d,gate", [(1, 24, None), (6, 24, None), (7, 100, 2), (3, 2048, None), (11, 1000, 3), (1030, 700, 5), (5, 5000, 2)])
+@pytest.mark.parametrize("drop", [(), ("w_pre", "dn"), ("f", "gate"), ("d_out",)], ids=str)
+def test_gradients_without_eps(t, d, gate, kind, drop, monkeypatch):
+    """eps = 0, with rows that leave some of a workgroup's shares empty: finite
+    gradients, as the definition has them."""
+    monkeypatch.setitem(globals(), "EPS", 0.0)
+    s = inputs(t, d, gate=gate)
+    for k in drop:
+        s[k] = None
+    check_backward(s, kind, gate if gate and s["gate"] is not None else 0, 0.5)
