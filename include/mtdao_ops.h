@@ -117,7 +117,8 @@ void mtdao_adamw_destroy(mtdao_adamw* h);
  *   d_w_pre  = sum_t dn norm(x')    d_w_post = sum_t dh norm(f)
  *   d_gate[j] = scale sum over the rows of gate j of D' h
  * The sums over rows are fp32, in an order that sizes alone fix.
- * d_out == NULL or dn == NULL: that gradient is zero. */
+ * d_out == NULL or dn == NULL: that gradient is zero.  w_pre == NULL: there is
+ * no n, and dn is not read. */
 enum { MTDAO_NORM_RMS = 0, MTDAO_NORM_LAYER = 1 };
 
 #define MTDAO_PERI_MAX_D 8192

@@ -275,7 +275,7 @@ __global__ __launch_bounds__(TPR > kGroup ? TPR : kGroup) void k_peri_norm_backw
     for (int t = 0; t < kE; ++t) w_pre[v][t] = u[v][t] = s_pre[v][t] = s_post[v][t] = s_t[v][t] = 0.0f;
     if (a.w_pre) load_weight<WHOLE>(a.w_pre, wb, (v * TPR + lane) * kE, n[v], w_pre[v]);
   }
-  const int of_x = a.w_pre ? a.d : 0, of_f = a.f ? a.d : 0, of_d = a.d_out ? a.d : 0, of_y = a.dn ? a.d : 0;  // columns to load
+  const int of_x = a.w_pre ? a.d : 0, of_f = a.f ? a.d : 0, of_d = a.d_out ? a.d : 0, of_y = a.dn && a.w_pre ? a.d : 0;  // columns to load
   const uint32_t block = blockIdx.x;
   const int rounds = a.whole_gates ? (a.per_block + kGroups - 1) / kGroups : 1;
   for (int round = 0; round < rounds; ++round) {

@@ -364,3 +364,14 @@ def test_gradients_without_eps(t, d, gate, kind, drop, monkeypatch):
     for k in drop:
         s[k] = None
     check_backward(s, kind, gate if gate and s["gate"] is not None else 0, 0.5)
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("d", [100, 2048])
+def test_gradient_of_an_output_that_is_not_there(d, kind):
+    """Without w_pre there is no n: dn has no part in the gradients, whatever it holds."""
+    s = inputs(9, d)
+    want = ops.peri_norm_backward(s["d_out"], None, s["x"], s["f"], s["w_post"], None, kind=kind)
+    got = ops.peri_norm_backward(s["d_out"], torch.full_like(s["dn"], math.nan), s["x"], s["f"], s["w_post"], None, kind=kind)
+    for a, b in zip(got, want):
+        assert a is b is None or torch.equal(a, b)
