@@ -488,8 +488,9 @@ __global__ __launch_bounds__(kCols * 32) void k_peri_columns(Args a, int64_t blo
 
 int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
 bool is_type(int32_t dt) { return dt == MTDAO_F32 || dt == MTDAO_BF16; }
+// (rows_per_gate may be any number: nothing is added to it)
 int64_t gates_of(const mtdao_peri_norm_args& a) {
-  return a.gate ? (a.rows + a.rows_per_gate - 1) / a.rows_per_gate : 0;
+  return a.gate ? a.rows / a.rows_per_gate + (a.rows % a.rows_per_gate != 0) : 0;
 }
 
 int32_t validate_sizes(const mtdao_peri_norm_args* p, std::string* e) {

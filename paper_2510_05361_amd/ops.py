@@ -201,7 +201,7 @@ def _peri_sizes(x, f, w_post, w_pre, gate, rows_per_gate, kind):
         raise TypeError(f"weights must be float32 or bfloat16, not {weight}")
     if gate is None:
         return rows, d, weight, 1
-    per = rows_per_gate if rows_per_gate > 0 else max(1, rows)
+    per = max(1, rows) if rows_per_gate <= 0 else min(rows_per_gate, max(1, rows))
     if gate.numel() != max(1, -(-rows // per)) * d:
         raise ValueError(f"gate is {tuple(gate.shape)}: one row of {d} per {per} rows of {rows}")
     return rows, d, weight, per

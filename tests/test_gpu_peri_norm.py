@@ -375,3 +375,12 @@ def test_gradient_of_an_output_that_is_not_there(d, kind):
     got = ops.peri_norm_backward(s["d_out"], torch.full_like(s["dn"], math.nan), s["x"], s["f"], s["w_post"], None, kind=kind)
     for a, b in zip(got, want):
         assert a is b is None or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("per", [41, 2 ** 31, 2 ** 63 - 1, 2 ** 70])
+def test_one_gate_for_more_rows_than_there_are(per):
+    s = inputs(40, 96, gate=40)
+    a, b = ((ops.peri_norm(s["x"], s["f"], s["w_post"], s["w_pre"], gate=s["gate"], rows_per_gate=n) +
+             ops.peri_norm_backward(s["d_out"], s["dn"], s["x"], s["f"], s["w_post"], s["w_pre"], gate=s["gate"], rows_per_gate=n))
+            for n in (per, 40))
+    assert all(torch.equal(p, q) for p, q in zip(a, b))

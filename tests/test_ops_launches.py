@@ -86,3 +86,16 @@ def test_boundary_gradients_of_no_rows(run, more):
     """Only the sums over rows are written."""
     launches, _ = run(PERI + f"        backward(peri(0, 64{more}))\n")
     assert launches == [("k_peri_columns", (2, 2, 1), 1024, 0)]
+
+
+@pytest.mark.parametrize("rows", [1, 7, 5000])
+@pytest.mark.parametrize("per", [2 ** 63 - 1, 2 ** 62, 2 ** 31])
+def test_gates_of_more_rows_than_there_are(run, rows, per):
+    """... are one gate: their gradient is summed as that of exactly the rows."""
+    launches, _ = run(PERI + f"""
+        backward(peri({rows}, 64, {per}))
+        backward(peri({rows}, 64, {rows}))
+        c.mtdao_peri_norm(peri({rows}, 64, {per}), None)
+    """)
+    assert names(launches) == ["k_peri_norm_backward", "k_peri_columns"] * 2 + ["k_peri_norm"]
+    assert launches[:2] == launches[2:4] and launches[1][1] == (2, 3, 1)
