@@ -7,7 +7,8 @@ current HIP stream; the work runs in the library's kernels through
 ``mtdao_ops.py`` (include/mtdao_ops.h has the formulas).  Outputs and
 workspaces are allocated from torch's caching allocator on the current
 stream; inputs that belong to another stream are the caller's to order, as
-for any torch operation.  There is no CPU path.
+for any torch operation.  What ``AdamW`` allocates for itself is kept from the
+allocator until the streams of its steps are done with it.  There is no CPU path.
 """
 
 from __future__ import annotations
@@ -114,7 +115,24 @@ class AdamW:
                                 betas[1], eps, max_norm, start_step)
         need = c_ops.mtdao_adamw_workspace_bytes(cfg, rows)
         self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        self.handle = c_ops.mtdao_adamw_init(cfg, rows, self.workspace.data_ptr(), need, _stream(self.workspace))
+        self._own = [self.workspace]
+        if states is None:
+            self._own += [t for name in kinds for t in getattr(self, name)]
+        home = _stream(self.workspace)
+        self._streams = {home}
+        self.handle = c_ops.mtdao_adamw_init(cfg, rows, self.workspace.data_ptr(), need, home)
+
+    def _stream_here(self) -> int:
+        """The current stream.  On another one than that of construction the
+        allocator learns of it: freed earlier, the table of addresses in the
+        workspace would be another tensor's while a step still reads it."""
+        stream = _stream(self.workspace)
+        if stream not in self._streams:
+            current = torch.cuda.current_stream(self.workspace.device)
+            for t in self._own:
+                t.record_stream(current)
+            self._streams.add(stream)
+        return stream
 
     def _grads_ok(self, grads, dtype) -> None:
         if len(grads) != len(self.params):
@@ -127,11 +145,11 @@ class AdamW:
     def set_grads(self, grads: Sequence[torch.Tensor]) -> None:
         """Take the gradients from these tensors from here on."""
         self._grads_ok(grads, self.grads[0].dtype)
-        c_ops.mtdao_adamw_set_grads(self.handle, [g.data_ptr() for g in grads], _stream(self.workspace))
+        c_ops.mtdao_adamw_set_grads(self.handle, [g.data_ptr() for g in grads], self._stream_here())
         self.grads = list(grads)
 
     def step(self, lr: float) -> None:
-        c_ops.mtdao_adamw_step(self.handle, lr, _stream(self.workspace))
+        c_ops.mtdao_adamw_step(self.handle, lr, self._stream_here())
 
     @property
     def step_count(self) -> int:

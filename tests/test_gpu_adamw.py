@@ -299,3 +299,28 @@ def test_refusals():
     with pytest.raises(RuntimeError, match="lr"):
         opt.step(math.inf)
     assert opt.step_count == 0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_closed_with_a_step_in_flight_on_another_stream(bits):
+    """What the object allocated is not handed out before that step is done."""
+    params, grads, opt = make([300000, 70], bits=bits, max_norm=1.0)
+    p2, _, opt2 = make([300000, 70], bits=bits, max_norm=1.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        opt.step(LR)
+    held = [opt.workspace] + opt.m + opt.v + (opt.m_scale + opt.v_scale if bits == 8 else [])
+    ranges = [(t.data_ptr(), t.numel() * t.element_size()) for t in held]
+    opt.close()
+    del held, opt
+    fresh = [torch.empty(size, dtype=torch.uint8, device="cuda") for _, size in ranges for _ in range(4)]
+    busy = not side.query()
+    for t in fresh:
+        for at, size in ranges:
+            assert t.data_ptr() + t.numel() <= at or at + size <= t.data_ptr()
+    side.synchronize()
+    assert busy, "the step was to be in flight"
+    opt2.step(LR)
+    assert all(torch.equal(a, b) for a, b in zip(params, p2))

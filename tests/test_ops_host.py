@@ -258,3 +258,45 @@ def test_operators_refuse_cpu_tensors():
                  lambda: ops.quantize8(x), lambda: ops.Weight8(x)):
         with pytest.raises(ValueError, match="GPU only"):
             call()
+
+
+class Held:
+    """A tensor as far as streams go."""
+
+    device = torch.device("cuda", 0)
+
+    def __init__(self):
+        self.streams = []
+
+    def get_device(self):
+        return 0
+
+    def record_stream(self, stream):
+        self.streams.append(stream)
+
+
+@pytest.fixture
+def streams(monkeypatch):
+    """streams[0]: the handle of the current stream."""
+    now = [1]
+    monkeypatch.setattr(ops, "_stream", lambda t: now[0])
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: f"stream {now[0]}")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    return now
+
+
+@pytest.mark.parametrize("call", ["mtdao_adamw_step", "mtdao_adamw_set_grads"])
+def test_adamw_keeps_what_it_allocated_for_the_streams_of_its_calls(call, streams, monkeypatch):
+    seen = []
+    monkeypatch.setattr(c, call, lambda *a: seen.append(a[-1]))
+    opt = ops.AdamW.__new__(ops.AdamW)
+    opt.handle, opt.params, opt.grads, opt.workspace = None, [], [torch.zeros(1)], Held()
+    state = Held()
+    opt._own, opt._streams = [opt.workspace, state], {1}
+    monkeypatch.setattr(opt, "_grads_ok", lambda *a: None)
+    go = (lambda: opt.step(0.1)) if call == "mtdao_adamw_step" else (lambda: opt.set_grads([]) or setattr(opt, "grads", [torch.zeros(1)]))
+    for now in (1, 2, 2, 3, 1, 2):
+        streams[0] = now
+        go()
+    assert seen == [1, 2, 2, 3, 1, 2]
+    assert opt.workspace.streams == state.streams == ["stream 2", "stream 3"]
