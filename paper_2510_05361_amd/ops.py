@@ -123,9 +123,11 @@ class AdamW:
         self.handle = c_ops.mtdao_adamw_init(cfg, rows, self.workspace.data_ptr(), need, home)
 
     def _stream_here(self) -> int:
-        """The current stream.  On another one than that of construction the
+        """The current stream, of the tensors' device.  On another one than that of construction the
         allocator learns of it: freed earlier, the table of addresses in the
         workspace would be another tensor's while a step still reads it."""
+        if torch.cuda.current_device() != self.workspace.get_device():
+            raise ValueError(f"the tensors are on {self.workspace.device}, the current device is {torch.cuda.current_device()}")
         stream = _stream(self.workspace)
         if stream not in self._streams:
             current = torch.cuda.current_stream(self.workspace.device)

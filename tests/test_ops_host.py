@@ -300,3 +300,14 @@ def test_adamw_keeps_what_it_allocated_for_the_streams_of_its_calls(call, stream
         go()
     assert seen == [1, 2, 2, 3, 1, 2]
     assert opt.workspace.streams == state.streams == ["stream 2", "stream 3"]
+
+
+@pytest.mark.parametrize("call", ["mtdao_adamw_step", "mtdao_adamw_set_grads"])
+def test_adamw_refuses_another_current_device(call, streams, monkeypatch):
+    monkeypatch.setattr(c, call, lambda *a: pytest.fail("enqueued on another device"))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    opt = ops.AdamW.__new__(ops.AdamW)
+    opt.handle, opt.params, opt.grads, opt.workspace, opt._own, opt._streams = None, [], [torch.zeros(1)], Held(), [], {1}
+    monkeypatch.setattr(opt, "_grads_ok", lambda *a: None)
+    with pytest.raises(ValueError, match="current device"):
+        opt.step(0.1) if call == "mtdao_adamw_step" else opt.set_grads([])
