@@ -7,8 +7,9 @@ current HIP stream; the work runs in the library's kernels through
 ``mtdao_ops.py`` (include/mtdao_ops.h has the formulas).  Outputs and
 workspaces are allocated from torch's caching allocator on the current
 stream; inputs that belong to another stream are the caller's to order, as
-for any torch operation.  What ``AdamW`` allocates for itself is kept from the
-allocator until the streams of its steps are done with it.  There is no CPU path.
+for any torch operation.  What ``AdamW``, ``Matrix8`` and ``Weight8`` allocate for
+themselves is kept from the allocator until the streams of their calls are done
+with it.  There is no CPU path.
 """
 
 from __future__ import annotations
@@ -324,16 +325,26 @@ class Matrix8:
         scale_ld = 4 * -(-rows // scale_rows)
         buf = torch.empty(rows * ld + -(-blocks // 4) * scale_ld, dtype=torch.uint8, device=device)
         self._buf = buf
+        self._streams = {_stream(buf)}
         self.args = c_ops.Matrix8(buf.data_ptr(), buf.data_ptr() + rows * ld, rows, cols, ld, scale_ld, scale_rows)
+
+    def on(self, stream: int) -> "c_ops.Matrix8":
+        """The C structure, for a call on the current stream, whose handle is
+        ``stream``: on another one than that of construction the allocator learns
+        of it."""
+        if stream not in self._streams:
+            self._buf.record_stream(torch.cuda.current_stream(self._buf.device))
+            self._streams.add(stream)
+        return self.args
 
     @property
     def codes(self) -> torch.Tensor:
-        a = self.args
+        a = self.on(_stream(self._buf))
         return self._buf[:a.rows * a.ld].view(CODE).view(a.rows, a.ld)[:, :-(-a.cols // BLOCK) * BLOCK]
 
     @property
     def scales(self) -> torch.Tensor:
-        a = self.args
+        a = self.on(_stream(self._buf))
         held = self._buf[a.rows * a.ld:].view(-1, a.scale_ld // 4, 4)
         return held.permute(1, 0, 2).reshape(a.scale_ld // 4, -1).view(SCALE)
 
@@ -374,8 +385,9 @@ def _linear_workspace(m: int, n: int, k: int) -> Tuple[int, int]:
 
 
 def _quantize(x: torch.Tensor, q: Optional[Matrix8], qt: Optional[Matrix8]) -> None:
-    c_ops.mtdao_quantize8(x.data_ptr(), _type(x, "x"), _ld(x), q.args if q is not None else None,
-                          qt.args if qt is not None else None, _stream(x))
+    st = _stream(x)
+    c_ops.mtdao_quantize8(x.data_ptr(), _type(x, "x"), _ld(x), q.on(st) if q is not None else None,
+                          qt.on(st) if qt is not None else None, st)
 
 
 def quantize8(x: torch.Tensor, *, rows: bool = True, transposed: bool = False):
@@ -405,8 +417,8 @@ def product8(a: Matrix8, b: Matrix8, *, dtype: torch.dtype = torch.bfloat16, out
     _on_device(out, a._buf, b._buf)
     need = _product_workspace(a.rows, b.rows, a.cols)
     ws = torch.empty(need, dtype=torch.uint8, device=out.device) if need else None
-    c_ops.mtdao_product8(a.args, b.args, out.data_ptr(), _type(out, "out"), _ld(out), accumulate, _ptr(ws), need,
-                         _stream(out))
+    st = _stream(out)
+    c_ops.mtdao_product8(a.on(st), b.on(st), out.data_ptr(), _type(out, "out"), _ld(out), accumulate, _ptr(ws), need, st)
     return out
 
 
@@ -441,8 +453,8 @@ def linear8(x: torch.Tensor, w: Weight8, *, dtype: Optional[torch.dtype] = None)
     y = torch.empty((*x.shape[:-1], wq.rows), dtype=dtype or x.dtype, device=dev)
     need = _linear_workspace(m, wq.rows, wq.cols)[0]
     ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    c_ops.mtdao_linear8(x2.data_ptr(), _type(x, "x"), m, _ld(x2), wq.args, y.data_ptr(), _type(y, "dtype"), wq.rows, _ptr(ws), need,
-                        _stream(x))
+    st = _stream(x)
+    c_ops.mtdao_linear8(x2.data_ptr(), _type(x, "x"), m, _ld(x2), wq.on(st), y.data_ptr(), _type(y, "dtype"), wq.rows, _ptr(ws), need, st)
     return y
 
 
@@ -470,6 +482,7 @@ def linear8_backward(dy: torch.Tensor, x: torch.Tensor, w: Weight8, *, dw: Optio
     dx = _empty(x, x.shape, dy.dtype)
     need = _linear_workspace(m, n, k)[1]
     ws = torch.empty(need, dtype=torch.uint8, device=dev)
-    c_ops.mtdao_linear8_backward(dy2.data_ptr(), x2.data_ptr(), _type(dy, "dy"), m, _ld(dy2), _ld(x2), w.qt.args, dx.data_ptr(), k,
-                                 dw.data_ptr(), _ld(dw), accumulate, ws.data_ptr(), need, _stream(x))
+    st = _stream(x)
+    c_ops.mtdao_linear8_backward(dy2.data_ptr(), x2.data_ptr(), _type(dy, "dy"), m, _ld(dy2), _ld(x2), w.qt.on(st), dx.data_ptr(), k,
+                                 dw.data_ptr(), _ld(dw), accumulate, ws.data_ptr(), need, st)
     return dx, dw

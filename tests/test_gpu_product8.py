@@ -328,3 +328,27 @@ def test_linear_of_no_outputs(m):
     assert ops.linear8(x, w).shape == (m, 0)
     dx, dw = ops.linear8_backward(torch.empty((m, 0), device="cuda"), x, w)
     assert dw.shape == (0, 130) and torch.equal(dx, torch.zeros((m, 130), device="cuda"))
+
+
+def test_weight_dropped_with_a_call_in_flight_on_another_stream():
+    """A weight quantized on one stream, used on a second one that waits for it, and
+    dropped: its memory is not handed out before the call is done."""
+    x, w = rand((300, 512), dtype="bf16"), rand((384, 512), 0.02)
+    want = ops.linear8(x, ops.Weight8(w))
+    held = ops.Weight8(w)
+    ranges = [(m._buf.data_ptr(), m._buf.numel()) for m in (held.q, held.qt)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        got = ops.linear8(x, held)
+        got_dx = ops.linear8_backward(want, x, held)[0]
+    del held
+    fresh = [torch.full((size,), 127, dtype=torch.uint8, device="cuda") for _, size in ranges for _ in range(4)]
+    busy = not side.query()
+    for t in fresh:
+        for at, size in ranges:
+            assert t.data_ptr() + t.numel() <= at or at + size <= t.data_ptr()
+    side.synchronize()
+    assert busy, "the calls were to be in flight"
+    assert torch.equal(got, want) and torch.equal(got_dx, ops.linear8_backward(want, x, ops.Weight8(w))[0])

@@ -311,3 +311,27 @@ def test_adamw_refuses_another_current_device(call, streams, monkeypatch):
     monkeypatch.setattr(opt, "_grads_ok", lambda *a: None)
     with pytest.raises(ValueError, match="current device"):
         opt.step(0.1) if call == "mtdao_adamw_step" else opt.set_grads([])
+
+
+def test_matrices_of_blocks_stay_for_the_streams_of_their_calls(streams, monkeypatch):
+    seen = []
+    for call in ("mtdao_quantize8", "mtdao_product8", "mtdao_linear8", "mtdao_linear8_backward"):
+        monkeypatch.setattr(c, call, lambda *a: seen.append(a[-1]))
+    monkeypatch.setattr(ops, "_on_device", lambda *a: torch.device("cpu"))
+
+    def fake(rows, cols):
+        q = ops.Matrix8(rows, cols, "cpu", ops.BLOCK)
+        q._buf = Held()
+        return q
+
+    w = ops.Weight8.__new__(ops.Weight8)
+    w.q, w.qt, a = fake(40, 256), fake(256, 40), fake(30, 256)
+    x, y = torch.zeros(30, 256), torch.zeros(30, 40)
+    for now, go, used in ((2, lambda: ops.linear8(x, w), [w.q]), (3, lambda: ops.linear8_backward(y, x, w), [w.qt]),
+                          (4, lambda: w.update(torch.zeros(40, 256)), [w.q, w.qt]), (5, lambda: ops.product8(a, w.q, out=y), [a, w.q])):
+        before = {m: list(m._buf.streams) for m in (w.q, w.qt, a)}
+        for streams[0] in (1, now, now):
+            go()
+        for m, held in before.items():
+            assert m._buf.streams == held + ([f"stream {now}"] if m in used else [])
+    assert seen == [1, 2, 2, 1, 3, 3, 1, 4, 4, 1, 5, 5]
