@@ -82,7 +82,8 @@ int32_t mtdao_adamw_workspace_bytes(const mtdao_adamw_config* cfg, const mtdao_a
 
 /* Validate and build a handle; enqueues the kernels that write the tensor
  * table into the workspace.  m, v and the scales are taken as they are (zero
- * them for a fresh run).  No two written buffers may overlap. */
+ * them for a fresh run).  No two written buffers may overlap, nor a gradient
+ * and a written buffer, unless it is its own tensor's, element on element. */
 int32_t mtdao_adamw_init(const mtdao_adamw_config* cfg, const mtdao_adamw_tensor* tensors, void* workspace,
                          size_t workspace_bytes, void* hip_stream, mtdao_adamw** out);
 

@@ -430,17 +430,30 @@ int32_t validate(const mtdao_adamw_config* c, const mtdao_adamw_tensor* t, std::
   return MTDAO_OK;
 }
 
-int32_t check_grad(const mtdao_adamw_config& c, int i, int64_t numel, const void* g, std::string* e) {
+// Memory that steps write: [lo, hi) of a tensor.
+struct Written {
+  uintptr_t lo, hi;
+  int tensor;
+};
+
+// written: in order, none over another.  A gradient may lie on its own tensor's
+// parameters or states, element on element: a lane reads all of its elements
+// before it writes them.  Elsewhere it would be read while it changes.
+int32_t check_grad(const mtdao_adamw_config& c, int i, int64_t numel, const void* g, const std::vector<Written>& written, std::string* e) {
   if (numel == 0) return MTDAO_OK;
   if (!g) return fail(e, MTDAO_ERR_INVALID_ARG, "g of tensor %d is NULL", i);
   if (!aligned_to(g, (uintptr_t)esize(c.grad_dtype)))
     return fail(e, MTDAO_ERR_ALIGN, "g of tensor %d is not aligned to its element", i);
+  const uintptr_t lo = (uintptr_t)g, hi = lo + (uintptr_t)(numel * esize(c.grad_dtype));
+  auto w = std::upper_bound(written.begin(), written.end(), lo, [](uintptr_t at, const Written& r) { return at < r.hi; });
+  for (; w != written.end() && w->lo < hi; ++w)
+    if (w->tensor != i || w->lo != lo || w->hi != hi)
+      return fail(e, MTDAO_ERR_INVALID_ARG, "g of tensor %d overlaps parameters or states of tensor %d", i, w->tensor);
   return MTDAO_OK;
 }
 
-int32_t check_pointers(const mtdao_adamw_config& c, const mtdao_adamw_tensor* t, std::string* e) {
+int32_t check_pointers(const mtdao_adamw_config& c, const mtdao_adamw_tensor* t, std::vector<Written>& written, std::string* e) {
   const bool eight = c.state_bits == 8;
-  std::vector<std::pair<uintptr_t, uintptr_t>> written;
   for (int i = 0; i < c.n_tensors; ++i) {
     const mtdao_adamw_tensor& a = t[i];
     if (a.numel == 0) continue;
@@ -450,9 +463,7 @@ int32_t check_pointers(const mtdao_adamw_config& c, const mtdao_adamw_tensor* t,
     if (!aligned_to(a.p, (uintptr_t)esize(c.param_dtype)))
       return fail(e, MTDAO_ERR_ALIGN, "p of tensor %d is not aligned to its element", i);
     if (!aligned16(a.m) || !aligned16(a.v)) return fail(e, MTDAO_ERR_ALIGN, "m or v of tensor %d is not 16-byte aligned", i);
-    const int32_t r = check_grad(c, i, a.numel, a.g, e);
-    if (r != MTDAO_OK) return r;
-    auto add = [&](const void* p, int64_t bytes) { written.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes}); };
+    auto add = [&](const void* p, int64_t bytes) { written.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, i}); };
     const int64_t blocks = (a.numel + kBlock8 - 1) / kBlock8;
     add(a.p, a.numel * esize(c.param_dtype));
     add(a.m, a.numel * (eight ? 1 : 4));
@@ -462,10 +473,14 @@ int32_t check_pointers(const mtdao_adamw_config& c, const mtdao_adamw_tensor* t,
       add(a.v_scale, blocks);
     }
   }
-  std::sort(written.begin(), written.end());
+  std::sort(written.begin(), written.end(), [](const Written& x, const Written& y) { return x.lo < y.lo; });
   for (size_t k = 1; k < written.size(); ++k)
-    if (written[k].first < written[k - 1].second)
+    if (written[k].lo < written[k - 1].hi)
       return fail(e, MTDAO_ERR_INVALID_ARG, "parameters or states of the tensors overlap");
+  for (int i = 0; i < c.n_tensors; ++i) {
+    const int32_t r = check_grad(c, i, t[i].numel, t[i].g, written, e);
+    if (r != MTDAO_OK) return r;
+  }
   return MTDAO_OK;
 }
 
@@ -474,6 +489,7 @@ int32_t check_pointers(const mtdao_adamw_config& c, const mtdao_adamw_tensor* t,
 struct mtdao_adamw {
   mtdao_adamw_config cfg;
   std::vector<int64_t> numel;
+  std::vector<Written> written;
   Row* rows = nullptr;
   uint32_t* owner = nullptr;
   float* clip = nullptr;
@@ -500,7 +516,8 @@ int32_t mtdao_adamw_init(const mtdao_adamw_config* cfg, const mtdao_adamw_tensor
   if (r != MTDAO_OK) return r;
   if (!out) return fail(&g_err, MTDAO_ERR_INVALID_ARG, "out is NULL");
   const mtdao_adamw_config& c = *cfg;
-  r = check_pointers(c, tensors, &g_err);
+  std::vector<Written> written;
+  r = check_pointers(c, tensors, written, &g_err);
   if (r != MTDAO_OK) return r;
   const Layout l = layout_of(c, tensors);
   if (!workspace || workspace_bytes < l.bytes)
@@ -515,6 +532,7 @@ int32_t mtdao_adamw_init(const mtdao_adamw_config* cfg, const mtdao_adamw_tensor
   mtdao_adamw* h = own.h;
   char* w = static_cast<char*>(workspace);
   h->cfg = c;
+  h->written = std::move(written);
   h->rows = reinterpret_cast<Row*>(w);
   h->owner = reinterpret_cast<uint32_t*>(w + l.owner);
   if (c.max_norm > 0.0) {
@@ -560,7 +578,7 @@ int32_t mtdao_adamw_set_grads(mtdao_adamw* h, const void* const* grads, void* hi
   if (!grads) return fail(&h->err, MTDAO_ERR_INVALID_ARG, "grads is NULL");
   const int n = h->cfg.n_tensors;
   for (int i = 0; i < n; ++i) {
-    const int32_t r = check_grad(h->cfg, i, h->numel[i], grads[i], &h->err);
+    const int32_t r = check_grad(h->cfg, i, h->numel[i], grads[i], h->written, &h->err);
     if (r != MTDAO_OK) return r;
   }
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);

@@ -335,3 +335,16 @@ def test_matrices_of_blocks_stay_for_the_streams_of_their_calls(streams, monkeyp
         for m, held in before.items():
             assert m._buf.streams == held + ([f"stream {now}"] if m in used else [])
     assert seen == [1, 2, 2, 1, 3, 3, 1, 4, 4, 1, 5, 5]
+
+
+AT = 1 << 30  # from tensor to tensor in adamw_case
+
+
+@pytest.mark.parametrize("kw", [dict(g__1=BASE), dict(g__0=BASE + 4), dict(g__0=BASE + AT + 3996), dict(g__2=BASE + AT + (2 << 26) - 3996),
+                                dict(g__0=BASE + AT + (3 << 26)), dict(bits=8, g__0=BASE + (2 << 26)), dict(bits=8, g__1=BASE + (5 << 26)),
+                                dict(bits=8, g__1=BASE + 2 * AT + (4 << 26) - 3996), dict(g__1=BASE, grad_dtype=1)], ids=str)
+def test_adamw_refuses_gradients_on_what_it_writes(kw):
+    cfg, rows = adamw_case(**kw)
+    with pytest.raises(abi.MtdaoError, match="overlaps") as e:
+        c.mtdao_adamw_init(cfg, rows, BASE << 1, 1 << 30, None)
+    assert e.value.code == abi.MTDAO_ERR_INVALID_ARG

@@ -99,3 +99,41 @@ def test_gates_of_more_rows_than_there_are(run, rows, per):
     """)
     assert names(launches) == ["k_peri_norm_backward", "k_peri_columns"] * 2 + ["k_peri_norm"]
     assert launches[:2] == launches[2:4] and launches[1][1] == (2, 3, 1)
+
+
+# ------------------------------------------------------------------- AdamW
+
+ADAMW = """
+        B, AT = 1 << 40, 1 << 30
+        def adamw(numels, bits=32, **kw):
+            cfg = c.AdamwConfig(0, 0, bits, len(numels), 0.9, 0.95, 1e-8, 0.0, 0)
+            rows = (c.AdamwTensor * len(numels))()
+            for i, n in enumerate(numels):
+                at = B + i * AT
+                rows[i] = c.AdamwTensor(at, at + (1 << 26), at + (2 << 26), at + (3 << 26), at + (4 << 26), at + (5 << 26), n, 0.1)
+            for k, v in kw.items():
+                name, _, i = k.partition("__")
+                setattr(rows[int(i)] if i else cfg, name, v)
+            return c.mtdao_adamw_init(cfg, rows, B << 1, c.mtdao_adamw_workspace_bytes(cfg, rows), None)
+"""
+
+
+def test_adamw_gradients_and_what_is_written(run):
+    """On its own tensor, element on element, a gradient is taken (as before); on
+    others, or shifted, it is refused, at construction and later."""
+    launches, said = run(ADAMW + """
+        for kw in (dict(g__0=B), dict(g__1=B + AT + (2 << 26)), dict(g__1=B + AT + (3 << 26)), dict(g__0=B + 4000), dict(g__1=B + AT - 4000)):
+            c.mtdao_adamw_destroy(adamw([1000, 1000, 0], **kw))
+        h = adamw([1000, 1000, 0])
+        good = [B + (1 << 26), B + AT + (1 << 26), None]
+        for i, g in ((0, B), (1, B + AT), (0, B + AT), (1, B + 4), (0, B + AT - 3996), (1, B + (2 << 26)), (2, B)):
+            grads = list(good)
+            grads[i] = g
+            try:
+                c.mtdao_adamw_set_grads(h, grads, None)
+                say("taken")
+            except abi.MtdaoError as e:
+                say(str(e))
+    """)
+    assert names(launches) == ["k_adamw_table"] * 6 + ["k_adamw_grads"] * 3
+    assert [s if s == "taken" else "overlaps" in s for s in said] == ["taken"] * 2 + [True] * 4 + ["taken"]
