@@ -13,8 +13,9 @@
 // are non-temporal (354 M elements of 28 bytes 1821 -> 1700 us).  With 8-bit
 // states the arithmetic is close behind: square root and quotient are the
 // hardware's, an ulp each (IEEE sequences: 1311 M elements of 10 bytes 2750 us,
-// 4.8 TB/s, against 2270 us), the betas are folded into the blocks' scales (powers
-// of two: no rounding more), and what only rare values need is behind branches
+// 4.8 TB/s, against 2270 us), beta1 is folded into the blocks' scales (powers of
+// two: no rounding more; a root of v has four significant bits, so its square
+// rounds nothing either), and what only rare values need is behind branches
 // (2180 us, 6.0 TB/s).
 
 #include <hip/hip_runtime.h>
@@ -302,13 +303,13 @@ __global__ __launch_bounds__(kThreads) void k_adamw_step(Step s) {
       float ma[V], ra[V];
       mc[k].values(ma);
       vc[k].values(ra);
-      const float mk = s.beta1 * scale_of(mb[k]), vk = scale_of(vb[k]), vk2 = s.beta2 * vk;
+      const float mk = s.beta1 * scale_of(mb[k]), vk = scale_of(vb[k]);
       float mm = 0.0f, vm = 0.0f;
 #pragma unroll
       for (int t = 0; t < V; ++t) {
-        const float g = ga[k][t] * clip;
+        const float g = ga[k][t] * clip, r = vk * ra[t];
         ma[t] = fmaf(s.rest1, g, mk * ma[t]);
-        ra[t] = fmaf(s.rest2 * g, g, (vk2 * ra[t]) * (vk * ra[t]));
+        ra[t] = fmaf(s.rest2 * g, g, s.beta2 * (r * r));
       }
       roots(ra, ra);
 #pragma unroll

@@ -324,3 +324,22 @@ def test_closed_with_a_step_in_flight_on_another_stream(bits):
     assert busy, "the step was to be in flight"
     opt2.step(LR)
     assert all(torch.equal(a, b) for a, b in zip(params, p2))
+
+
+@pytest.mark.parametrize("p,g", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
+def test_8_bit_states_are_stepped_as_the_32_bit_ones_of_their_values(p, g):
+    """Codes times scales and the squares of such roots are fp32 values, so that a
+    step from them rounds where one from 32-bit states does: the same parameters,
+    bit for bit."""
+    sizes = [20000, 777]
+    params, grads, opt = make(sizes, p, g, 8, max_norm=0.5, weight_decay=0.1)
+    for seed in range(3):
+        opt.step(LR)
+        for x in grads:
+            x.normal_(0, 1e-2)
+    wide = [t.clone() for t in params]
+    states = {k: [held(c, s)[0].pow(2 if k == "v" else 1).float().cuda() for c, s in zip(getattr(opt, k), getattr(opt, k + "_scale"))] for k in ("m", "v")}
+    other = ops.AdamW(wide, grads, betas=(B1, B2), eps=EPS, weight_decay=0.1, max_norm=0.5, start_step=3, states=states)
+    opt.step(LR)
+    other.step(LR)
+    assert all(torch.equal(a, b) for a, b in zip(params, wide))
