@@ -623,9 +623,13 @@ int32_t mtdao_adamw_step(mtdao_adamw* h, double lr, void* hip_stream) {
     const Pass pass = pass_of(c, h->elements);
     s.spread = pass.spread;
     s.lr = (float)lr;
-    s.step = (float)(lr / (1.0 - std::pow(c.beta1, (double)t)));
-    s.root2 = (float)(1.0 / std::sqrt(1.0 - std::pow(c.beta2, (double)t)));
-    s.eps = (float)c.eps;
+    // m / (sqrt(v) + eps): both sides times a power of two where eps is close to the
+    // numbers that the hardware's reciprocal takes for zero, which made NaN of m = v = 0
+    const bool tiny = c.eps > 0.0 && c.eps < 0x1p-100;
+    const double both = tiny ? 0x1p40 : 1.0;
+    s.step = (float)(both * lr / (1.0 - std::pow(c.beta1, (double)t)));
+    s.root2 = (float)(both / std::sqrt(1.0 - std::pow(c.beta2, (double)t)));
+    s.eps = (float)(tiny ? std::max(both * c.eps, 0x1p-126) : c.eps);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, pass.lds, st, s); };
     auto with = [&](auto p, auto g) {
       using PT = decltype(p);

@@ -343,3 +343,26 @@ def test_8_bit_states_are_stepped_as_the_32_bit_ones_of_their_values(p, g):
     opt.step(LR)
     other.step(LR)
     assert all(torch.equal(a, b) for a, b in zip(params, wide))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [1e-25, 1e-31, 1e-37, 2e-38, 1e-38, 1e-40, 1e-44, 1e-46, 1e-300])
+def test_elements_without_gradients_under_an_eps_of_almost_nothing(eps, bits):
+    """m = v = 0 and eps > 0: the update is 0, however small eps is.  Elsewhere it
+    is nothing next to sqrt(v), and steps are those of eps = 1e-25."""
+    params, grads, opt = make([3000], bits=bits, weight_decay=0.1)
+    p2, g2, ref = make([3000], bits=bits, weight_decay=0.1)
+    for t, e in ((opt, eps), (ref, 1e-25)):
+        t.close()
+    opt = ops.AdamW(params, grads, betas=(B1, B2), eps=eps, weight_decay=0.1, state_bits=bits)
+    ref = ops.AdamW(p2, g2, betas=(B1, B2), eps=1e-25, weight_decay=0.1, state_bits=bits)
+    for g in (grads[0], g2[0]):
+        g[g.abs() < 1e-5] = 1e-5
+        g[::3] = 0
+    start = params[0].clone()
+    for _ in range(3):
+        opt.step(LR)
+        ref.step(LR)
+    assert bool(params[0].isfinite().all())
+    assert bool(((params[0][::3] - start[::3] * (1 - LR * 0.1) ** 3).abs() <= 16 * U * start[::3].abs()).all())
+    assert torch.equal(params[0], p2[0])
