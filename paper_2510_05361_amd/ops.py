@@ -10,6 +10,10 @@ stream; inputs that belong to another stream are the caller's to order, as
 for any torch operation.  What ``AdamW``, ``Matrix8`` and ``Weight8`` allocate for
 themselves is kept from the allocator until the streams of their calls are done
 with it.  There is no CPU path.
+
+``peri_norm`` and ``linear8`` take part in autograd where an input (of
+``linear8``: x, or the tensor that its weight was made from) requires a gradient;
+their backward passes are the functions of the same names, for once only.
 """
 
 from __future__ import annotations
@@ -19,6 +23,7 @@ import math
 from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import mtdao as abi
 from . import mtdao_ops as c_ops
@@ -51,6 +56,13 @@ def _on_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> torch.de
     if index != torch.cuda.current_device():
         raise ValueError(f"the tensors are on {first.device}, the current device is {torch.cuda.current_device()}")
     return first.device
+
+
+def _wants_grad(*tensors: Optional[torch.Tensor]) -> bool:
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            return True
+    return False
 
 
 # ------------------------------------------------------------------- AdamW
@@ -239,6 +251,14 @@ def peri_norm(x: torch.Tensor, f: Optional[torch.Tensor], w_post: Optional[torch
     None.  ``gate`` has one row of D per ``rows_per_gate`` rows of x (0: one
     row for all).  n has f's type (``branch_dtype``, x's by default, without
     f)."""
+    if torch.is_grad_enabled() and _wants_grad(x, f, w_post, w_pre, gate):
+        if f is None and w_pre is not None:
+            return x, _PeriNorm.apply(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype)[1]
+        return _PeriNorm.apply(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype)
+    return _peri_norm(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype)
+
+
+def _peri_norm(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype):
     _on_device(x, f, w_post, w_pre, gate)
     branch = f.dtype if f is not None else branch_dtype or x.dtype
     if branch not in _TYPES:
@@ -306,6 +326,26 @@ def peri_norm_backward(d_out: Optional[torch.Tensor], dn: Optional[torch.Tensor]
                                px, pf, _ptr(w_post), _ptr(w_pre), _ptr(gate), pd, py, dx.data_ptr(), 0, _ptr(df), _ptr(dw_post),
                                _ptr(dw_pre), _ptr(dgate)), ws.data_ptr(), need, _stream(x_out))
     return dx, df, dw_post, dw_pre, dgate
+
+
+class _PeriNorm(torch.autograd.Function):
+    """peri_norm for autograd (x' only where there is an f: else it is x itself)."""
+
+    @staticmethod
+    def forward(ctx, x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype):
+        ctx.set_materialize_grads(False)
+        out, n = _peri_norm(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype)
+        ctx.save_for_backward(out, f, w_post, w_pre, gate)
+        ctx.how = {"rows_per_gate": rows_per_gate, "scale": scale, "eps": eps, "kind": kind}
+        return out if f is not None else None, n
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_out, dn):
+        out, f, *weights = ctx.saved_tensors
+        dx, df, *sums = peri_norm_backward(d_out, dn, out, f, weights[0], weights[1], gate=weights[2], **ctx.how)
+        sums = [None if w is None else s.view(w.shape).to(w.dtype) for s, w in zip(sums, weights)]
+        return (*(g if needed else None for g, needed in zip((dx, df, *sums), ctx.needs_input_grad)), *(None,) * 5)
 
 
 # ------------------------------------------------------------ 8-bit blocks
@@ -425,10 +465,17 @@ def product8(a: Matrix8, b: Matrix8, *, dtype: torch.dtype = torch.bfloat16, out
 class Weight8:
     """The weight [out, in] of a linear layer in 8-bit blocks of 128 x 128,
     with its transpose for the gradient of the input (the same values).
-    ``update`` takes the weight again after an optimizer step, in place."""
+    ``update`` takes the weight again after an optimizer step, in place.  In
+    autograd the weight's gradient goes to the last tensor taken that required
+    one (``source``)."""
+
+    source: Optional[torch.Tensor] = None
+    version = 0
 
     def __init__(self, w: torch.Tensor):
         _on_device(w)
+        if w.requires_grad:
+            self.source = w
         w = _matrix(w)
         self.q = Matrix8(w.shape[0], w.shape[1], w.device, BLOCK)
         self.qt = Matrix8(w.shape[1], w.shape[0], w.device, BLOCK)
@@ -438,12 +485,21 @@ class Weight8:
         _on_device(w, self.q._buf)
         if tuple(w.shape) != (self.q.rows, self.q.cols):
             raise ValueError(f"the weight is [{self.q.rows}, {self.q.cols}], not {tuple(w.shape)}")
+        if w.requires_grad:
+            self.source = w
+        self.version += 1
         _quantize(_matrix(w), self.q, self.qt)
 
 
 def linear8(x: torch.Tensor, w: Weight8, *, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """x W^T over the last axis of x, x in 8-bit blocks along it; in x's type
     unless ``dtype`` is given."""
+    if torch.is_grad_enabled() and _wants_grad(x, w.source):
+        return _Linear8.apply(x, w.source, w, dtype)
+    return _linear8(x, w, dtype)
+
+
+def _linear8(x, w, dtype):
     wq = w.q
     if x.shape[-1] != wq.cols:
         raise ValueError(f"x has {x.shape[-1]} columns, the weight {wq.cols}")
@@ -486,3 +542,23 @@ def linear8_backward(dy: torch.Tensor, x: torch.Tensor, w: Weight8, *, dw: Optio
     c_ops.mtdao_linear8_backward(dy2.data_ptr(), x2.data_ptr(), _type(dy, "dy"), m, _ld(dy2), _ld(x2), w.qt.on(st), dx.data_ptr(), k,
                                  dw.data_ptr(), _ld(dw), accumulate, ws.data_ptr(), need, st)
     return dx, dw
+
+
+class _Linear8(torch.autograd.Function):
+    """linear8 for autograd; ``source`` takes the weight's gradient."""
+
+    @staticmethod
+    def forward(ctx, x, source, w, dtype):
+        ctx.save_for_backward(x)
+        ctx.w, ctx.version, ctx.type = w, w.version, source.dtype if source is not None else torch.float32
+        return _linear8(x, w, dtype)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, = ctx.saved_tensors
+        if ctx.w.version != ctx.version:
+            raise RuntimeError("the weight has been updated since the forward pass that this gradient belongs to")
+        kind = x.dtype if x.dtype == dy.dtype else torch.float32
+        dx, dw = linear8_backward(dy.to(kind), x.to(kind), ctx.w)
+        return dx.to(x.dtype) if ctx.needs_input_grad[0] else None, dw.to(ctx.type) if ctx.needs_input_grad[1] else None, None, None

@@ -384,3 +384,43 @@ def test_one_gate_for_more_rows_than_there_are(per):
              ops.peri_norm_backward(s["d_out"], s["dn"], s["x"], s["f"], s["w_post"], s["w_pre"], gate=s["gate"], rows_per_gate=n))
             for n in (per, 40))
     assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("drop", [(), ("f", "w_post", "gate"), ("w_pre",), ("gate",)], ids=str)
+@pytest.mark.parametrize("stream,branch,w", [("f32", "f32", "f32"), ("f32", "bf16", "bf16"), ("bf16", "bf16", "f32")])
+def test_autograd(stream, branch, w, drop, kind):
+    """Gradients through autograd are those of peri_norm_backward, in their tensors'
+    types; of either output alone too.  A part without requires_grad takes none."""
+    s = inputs(30, 200, stream, branch, w, gate=7)
+    names = [k for k in ("x", "f", "w_post", "w_pre", "gate") if k not in drop]
+    leaves = {k: s[k].clone().requires_grad_() if k in names else None for k in ("x", "f", "w_post", "w_pre", "gate")}
+    how = dict(rows_per_gate=0 if leaves["gate"] is None else 7, scale=0.5, kind=kind)
+
+    def forward(v):
+        return ops.peri_norm(v["x"], v["f"], v["w_post"], v["w_pre"], gate=v["gate"], branch_dtype=DT[branch], **how)
+
+    with torch.no_grad():
+        plain = forward(leaves)
+    assert not any(t is not None and t.grad_fn is not None for t in plain)
+    for given in ((True, True), (True, False), (False, True)):
+        out, n = forward(leaves)
+        assert torch.equal(out, plain[0]) and (n is plain[1] is None or torch.equal(n, plain[1]))
+        d_out, dn = (s[k] if use else None for k, use in zip(("d_out", "dn"), given))
+        dn = dn if n is not None else None
+        pairs = [(t, g) for t, g in ((out, d_out), (n, dn)) if g is not None]
+        if not pairs or leaves["f"] is None and dn is None:
+            continue
+        got = torch.autograd.grad([t for t, _ in pairs], [leaves[k] for k in names], [g for _, g in pairs], allow_unused=True)
+        want = dict(zip(("x", "f", "w_post", "w_pre", "gate"), ops.peri_norm_backward(
+            d_out if leaves["f"] is not None else None, dn, plain[0], s["f"] if leaves["f"] is not None else None,
+            *(s[k] if leaves[k] is not None else None for k in ("w_post", "w_pre")), gate=s["gate"] if leaves["gate"] is not None else None, **how)))
+        if leaves["f"] is None and d_out is not None:
+            want["x"] = want["x"] + d_out  # x' is x itself
+        for k, g in zip(names, got):
+            assert g.dtype == leaves[k].dtype and torch.equal(g, want[k].to(g.dtype)), (k, given)
+    if "f" in names:
+        some = {k: t if t is None or k == "f" else t.detach() for k, t in leaves.items()}
+        out, _ = forward(some)
+        out.float().sum().backward()
+        assert leaves["f"].grad is not None and leaves["x"].grad is None

@@ -352,3 +352,31 @@ def test_weight_dropped_with_a_call_in_flight_on_another_stream():
     side.synchronize()
     assert busy, "the calls were to be in flight"
     assert torch.equal(got, want) and torch.equal(got_dx, ops.linear8_backward(want, x, ops.Weight8(w))[0])
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("w_dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m", [5, 77])
+def test_autograd(m, w_dtype, dtype, out):
+    """Gradients through autograd are those of linear8_backward; the weight's goes
+    to the tensor that it was made from."""
+    x, w, dy = rand((m, 200), dtype=dtype), rand((90, 200), 0.02, w_dtype, seed=2), rand((m, 90), dtype=out, seed=3)
+    common = DT[dtype] if dtype == out else torch.float32
+    plain = ops.Weight8(w)
+    want = ops.linear8_backward(dy.to(common), x.to(common), plain)
+    for grads in ((True, True), (True, False), (False, True)):
+        a, b = x.clone().requires_grad_(grads[0]), w.clone().requires_grad_(grads[1])
+        held = ops.Weight8(b)
+        y = ops.linear8(a.view(1, m, 200), held, dtype=DT[out])
+        assert torch.equal(y[0], ops.linear8(x, plain, dtype=DT[out]))
+        y.backward(dy[None])
+        for t, g, needed in ((a, want[0], grads[0]), (b, want[1], grads[1])):
+            assert (t.grad is not None) == needed
+            assert not needed or t.grad.dtype == t.dtype and torch.equal(t.grad, g.to(t.dtype))
+        with torch.no_grad():
+            assert ops.linear8(a, held).grad_fn is None
+    held.update(w)
+    y = ops.linear8(a, held)
+    held.update(w)
+    with pytest.raises(RuntimeError, match="updated"):
+        y.sum().backward()
