@@ -64,6 +64,14 @@ inline bool overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes
   return a0 < b0 + (uintptr_t)bbytes && b0 < a0 + (uintptr_t)abytes;
 }
 
+// A grid of at least n workgroups of up to 1024 threads: a launch takes fewer than
+// 2^32 threads along x (and 65535 rows of workgroups along y).
+inline constexpr int64_t kGridRow = INT64_C(1) << 21, kGridMost = kGridRow * 65535;
+inline dim3 grid_of(int64_t n) {
+  const int64_t y = n > kGridRow ? (n + kGridRow - 1) / kGridRow : 1;
+  return dim3((unsigned)(y > 1 ? kGridRow : n), (unsigned)y);
+}
+
 inline int32_t hip_check(std::string* e, hipError_t r, const char* what) {
   if (r != hipSuccess) return fail(e, MTDAO_ERR_HIP, "%s: %s", what, hipGetErrorString(r));
   return MTDAO_OK;

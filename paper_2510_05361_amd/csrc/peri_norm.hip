@@ -190,7 +190,8 @@ __global__ __launch_bounds__(TPR > kGroup ? TPR : kGroup) void k_peri_norm(Args 
   constexpr int kThreads = TPR > kGroup ? TPR : kGroup, kWaves = kThreads / 64;
   __shared__ float buf[4 * kWaves];
   const int lane = threadIdx.x % TPR;
-  const int64_t row_or_past = (int64_t)blockIdx.x * (kThreads / TPR) + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+  const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  const int64_t row_or_past = block * (kThreads / TPR) + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
   const bool live = row_or_past < a.rows;
   if (TPR == 64 && !live) return;  // (wider rows fill a workgroup or meet at barriers)
   const int64_t row = live ? row_or_past : a.rows - 1;
@@ -687,15 +688,14 @@ int32_t mtdao_peri_norm(const mtdao_peri_norm_args* args, void* hip_stream) {
   const bool few = a.rows * a.d <= kFew;
   const int64_t per = a.d <= 512 || (a.d <= 1024 && !few) ? 4 : 1;
   const int64_t blocks = (a.rows + per - 1) / per;
-  if (blocks > 0x7fffffff) return fail(e, MTDAO_ERR_INVALID_ARG, "rows exceed the largest launch");
+  if (blocks > kGridMost) return fail(e, MTDAO_ERR_INVALID_ARG, "rows exceed the largest launch");
   with_types(a, [&](auto s, auto b, auto layer, auto whole) {
     using ST = decltype(s);
     using BT = decltype(b);
     constexpr bool L = decltype(layer)::value, W = decltype(whole)::value;
     auto go = [&](auto tpr, auto nv) {
       constexpr int T = decltype(tpr)::value;
-      hipLaunchKernelGGL((k_peri_norm<ST, BT, L, W, T, decltype(nv)::value>), dim3((unsigned)blocks),
-                         dim3(T > kGroup ? T : kGroup), 0, st, k);
+      hipLaunchKernelGGL((k_peri_norm<ST, BT, L, W, T, decltype(nv)::value>), grid_of(blocks), dim3(T > kGroup ? T : kGroup), 0, st, k);
     };
     if (a.d <= 512) go(Int<64>{}, Int<1>{});
     else if (a.d <= 1024 && !few) go(Int<64>{}, Int<2>{});

@@ -43,10 +43,10 @@ constexpr int kE = 8;  // elements of a thread's vector: 16 threads hold a block
 // Blocks along the rows: four of each of four rows a workgroup, a row a wave; a
 // block's largest value is found by its sixteen lanes.  16384 x 8192 bf16: 5.6 TB/s.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_quantize8_rows(const T* x, int64_t ld, int64_t cols, int groups, Mat q) {
-  const int64_t four = blockIdx.x / (unsigned)groups;
-  const int64_t row = four * 4 + threadIdx.x / 64;
-  const int kb = (int)(blockIdx.x - four * groups) * 4 + (int)threadIdx.x % 64 / 16, e = kb * kBlock8 + (int)(threadIdx.x % 16) * kE;
+__global__ __launch_bounds__(kThreads) void k_quantize8_rows(const T* x, int64_t ld, int64_t cols, int groups, int fours, Mat q) {
+  const unsigned in_x = blockIdx.x / (unsigned)groups;  // of `fours` along x
+  const int64_t row = ((int64_t)blockIdx.y * fours + in_x) * 4 + threadIdx.x / 64;
+  const int kb = (int)(blockIdx.x - in_x * groups) * 4 + (int)threadIdx.x % 64 / 16, e = kb * kBlock8 + (int)(threadIdx.x % 16) * kE;
   float a[kE], most = 0.0f;
   const bool live = row < q.rows && kb < q.blocks;
   const int64_t n = live ? cols - e : 0;
@@ -717,7 +717,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_product8_few(Few p) {
   using Rows = Raw<std::conditional_t<kCodes, bf16_t, XT>>;
   __shared__ v4f part[WAVES][MI * NJ][64];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
-  const int64_t col0 = (int64_t)blockIdx.x * (16 * NJ);
+  const int64_t col0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (16 * NJ);
   const uint8_t* b[NJ];
   int64_t bs[NJ];
 #pragma unroll
@@ -960,7 +960,7 @@ Quantized quantized_of(const void* x, int64_t ld, const mtdao_matrix8* q, const 
 // Tiles of one matrix, or of two (`two.tiles` not 0) of as many rows.
 int32_t launch_tiles(const Quantized& one, const Quantized& two, int32_t dtype, int64_t rows, bool square, hipStream_t st, std::string* e) {
   const int64_t ty = up(rows, kBlock8) / kBlock8;
-  if (ty > 65535) return fail(e, MTDAO_ERR_INVALID_ARG, "the matrix exceeds the largest launch");
+  if (ty > 65535 || (int64_t)one.tiles + two.tiles > 0x7fffff) return fail(e, MTDAO_ERR_INVALID_ARG, "the matrix exceeds the largest launch");
   const dim3 grid((unsigned)(one.tiles + two.tiles), (unsigned)ty), block(kTileThreads);
   auto with = [&](auto t) {
     using T = decltype(t);
@@ -979,11 +979,12 @@ int32_t launch_quantize(const void* x, int32_t dtype, int64_t ld, const mtdao_ma
   if (qt || square) return launch_tiles(quantized_of(x, ld, q, qt), Quantized{}, dtype, rows, square, st, e);
   const Mat m = mat_of(q);
   const int groups = (m.blocks + 3) / 4;
-  const int64_t wgs = (rows + 3) / 4 * groups;
-  if (wgs > INT64_C(0xffffff)) return fail(e, MTDAO_ERR_INVALID_ARG, "the matrix exceeds the largest launch");  // 2^32 threads
-  const dim3 grid((unsigned)wgs), block(kThreads);
-  if (dtype == MTDAO_BF16) hipLaunchKernelGGL(k_quantize8_rows<bf16_t>, grid, block, 0, st, static_cast<const bf16_t*>(x), ld, cols, groups, m);
-  else hipLaunchKernelGGL(k_quantize8_rows<float>, grid, block, 0, st, static_cast<const float*>(x), ld, cols, groups, m);
+  const int64_t all = (rows + 3) / 4, fours = std::min(all, INT64_C(0xffffff) / groups);  // fewer than 2^32 threads along x
+  const int64_t along_y = (all + fours - 1) / fours;
+  if (along_y > 65535) return fail(e, MTDAO_ERR_INVALID_ARG, "the matrix exceeds the largest launch");
+  const dim3 grid((unsigned)(fours * groups), (unsigned)along_y), block(kThreads);
+  if (dtype == MTDAO_BF16) hipLaunchKernelGGL(k_quantize8_rows<bf16_t>, grid, block, 0, st, static_cast<const bf16_t*>(x), ld, cols, groups, (int)fours, m);
+  else hipLaunchKernelGGL(k_quantize8_rows<float>, grid, block, 0, st, static_cast<const float*>(x), ld, cols, groups, (int)fours, m);
   return MTDAO_OK;
 }
 
@@ -999,7 +1000,7 @@ template <typename XT, typename CT, int MI>
 void launch_few(const Few& f, hipStream_t st) {
   auto go = [&](auto nj, auto waves) {
     constexpr int NJ = decltype(nj)::value, W = decltype(waves)::value;
-    hipLaunchKernelGGL((k_product8_few<XT, CT, MI, NJ, W>), dim3((unsigned)((f.b.rows + 16 * NJ - 1) / (16 * NJ))), dim3(64 * W), 0, st, f);
+    hipLaunchKernelGGL((k_product8_few<XT, CT, MI, NJ, W>), grid_of((f.b.rows + 16 * NJ - 1) / (16 * NJ)), dim3(64 * W), 0, st, f);
   };
   if constexpr (MI > 1) {
     if (f.b.rows > kWideFrom) return go(Int<2>{}, Int<8>{});

@@ -424,3 +424,15 @@ def test_autograd(stream, branch, w, drop, kind):
         out, _ = forward(some)
         out.float().sum().backward()
         assert leaves["f"].grad is not None and leaves["x"].grad is None
+
+
+def test_rows_past_one_row_of_workgroups():
+    """Four rows a workgroup and 2^21 workgroups along x: many narrow rows."""
+    t, d = (1 << 24) + 5, 8
+    x = torch.zeros((t, d), dtype=torch.bfloat16, device="cuda")
+    some = torch.tensor([0, 1 << 23, (1 << 23) + 3, (1 << 24) - 1, 1 << 24, t - 1], device="cuda")
+    x[some] = torch.randn((6, d), device="cuda").bfloat16()
+    w = torch.ones(d, device="cuda")
+    small, big = ops.peri_norm(x[some], x[some], w, w), ops.peri_norm(x, x, w, w)
+    for a, b in zip(small, big):
+        assert torch.equal(b[some], a) and int(b.abs().sum(1).nonzero().numel()) == 6

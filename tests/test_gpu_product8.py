@@ -380,3 +380,28 @@ def test_autograd(m, w_dtype, dtype, out):
     held.update(w)
     with pytest.raises(RuntimeError, match="updated"):
         y.sum().backward()
+
+
+def test_rows_past_one_row_of_workgroups():
+    """More four rows by four blocks than go along x."""
+    rows, k = (1 << 26) + 5, 8
+    x = torch.zeros((rows, k), dtype=torch.bfloat16, device="cuda")
+    some = torch.tensor([0, 1 << 25, (1 << 26) - 5, (1 << 26) - 4, 1 << 26, rows - 1], device="cuda")
+    x[some] = torch.randn((6, k), device="cuda").bfloat16()
+    q, small = ops.quantize8(x), ops.quantize8(x[some])
+    assert torch.equal(q.codes.view(torch.uint8)[some], small.codes.view(torch.uint8))
+    assert torch.equal(q.scales.view(torch.uint8)[some], small.scales.view(torch.uint8))
+    assert int(q.scales.view(torch.uint8)[:, 0].gt(1).sum()) == 6
+
+
+@pytest.mark.parametrize("m", [8, 40])
+def test_many_columns_and_few_rows(m):
+    """More columns than workgroups go along x take."""
+    n = (1 << 26) + 37
+    a = ops.quantize8(rand((m, 100)))
+    w = torch.zeros((n, 100), dtype=torch.bfloat16, device="cuda")
+    some = torch.tensor([0, 1 << 24, (1 << 25) - 1, 1 << 25, (1 << 26) - 1, 1 << 26, n - 1], device="cuda")
+    w[some] = torch.randn((7, 100), device="cuda").bfloat16()
+    c = ops.product8(a, ops.quantize8(w))
+    assert torch.equal(c[:, some], ops.product8(a, ops.quantize8(w[some])))
+    assert int(c.abs().sum(0).nonzero().numel()) == 7

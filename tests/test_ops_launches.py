@@ -137,3 +137,43 @@ def test_adamw_gradients_and_what_is_written(run):
     """)
     assert names(launches) == ["k_adamw_table"] * 6 + ["k_adamw_grads"] * 3
     assert [s if s == "taken" else "overlaps" in s for s in said] == ["taken"] * 2 + [True] * 4 + ["taken"]
+
+
+# -------------------------------------------------------------- largest launches
+
+
+@pytest.mark.parametrize("rows,d", [(1, 64), ((1 << 21) + 1, 2048), ((1 << 23) + 1, 64), ((1 << 26) + 5, 8), (1 << 24, 8192), (1 << 30, 512), ((1 << 38) + 1, 1)])
+def test_boundaries_of_many_rows_fit_a_launch(run, rows, d):
+    """Fewer than 2^32 threads along x, every row in a workgroup, no row of
+    workgroups without one."""
+    launches, _ = run(PERI + f"        c.mtdao_peri_norm(peri({rows}, {d}, ld_f={d}), None)\n")
+    (name, (x, y, z), threads, _), = launches
+    per = 4 if d <= 512 else 1
+    assert name == "k_peri_norm" and z == 1 and x * threads < 1 << 32 and y <= 65535
+    assert x * y * per >= rows > x * (y - 1) * per
+
+
+@pytest.mark.parametrize("rows,cols", [(5, 300), ((1 << 26) + 1, 8), (1 << 22, 8192), (3, 1 << 22), ((1 << 31) - 1, 100)])
+def test_quantized_rows_fit_a_launch(run, rows, cols):
+    launches, _ = run(f"""
+        B = 1 << 40
+        c.mtdao_quantize8(B, 1, {cols}, c.Matrix8(B << 8, B << 10, {rows}, {cols}, -(-{cols} // 128) * 128, 4 * {rows}, 1), None, None)
+    """)
+    (name, (x, y, z), threads, _), = launches
+    groups, fours = -(-cols // 512), -(-rows // 4)
+    assert name == "k_quantize8_rows" and z == 1 and x % groups == 0 and x * threads < 1 << 32 and y <= 65535
+    assert x // groups * y >= fours > x // groups * (y - 1)
+
+
+@pytest.mark.parametrize("n", [100, (1 << 25) + 3, (1 << 27) + 1, (1 << 31) - 1])
+def test_products_of_many_columns_and_few_rows_fit_a_launch(run, n):
+    launches, _ = run(f"""
+        B = 1 << 40
+        matrix = lambda rows, at: c.Matrix8(at, at + (1 << 39), rows, 128, 128, 4 * rows, 1)
+        for m in (8, 64):
+            c.mtdao_product8(matrix(m, B), matrix({n}, B << 2), B << 4, 1, {n}, False, None, 0, None)
+    """)
+    assert len(launches) == 2
+    for (name, (x, y, z), threads, _), cols in zip(launches, (16, 32 if n > 4096 else 16)):
+        assert name == "k_product8_few" and z == 1 and x * threads < 1 << 32 and y <= 65535
+        assert x * y * cols >= n > x * (y - 1) * cols
