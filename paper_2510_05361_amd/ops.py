@@ -58,13 +58,6 @@ def _on_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> torch.de
     return first.device
 
 
-def _wants_grad(*tensors: Optional[torch.Tensor]) -> bool:
-    for t in tensors:
-        if t is not None and t.requires_grad:
-            return True
-    return False
-
-
 # ------------------------------------------------------------------- AdamW
 
 
@@ -200,12 +193,18 @@ def _rows(t: Optional[torch.Tensor], shape, what: str):
     return t, t.data_ptr(), t.stride(0) if t.shape[0] > 1 else d
 
 
-def _empty(like: torch.Tensor, shape, dtype: torch.dtype) -> torch.Tensor:
-    """A new contiguous tensor (the way through ``empty_like`` takes half the
-    host time, 1.2 us)."""
-    if like.shape == shape and like.is_contiguous():
+def _empty(like: torch.Tensor, dtype: torch.dtype) -> torch.Tensor:
+    """A new contiguous tensor of like's shape (the way through ``empty_like`` takes
+    half the host time, 1.2 us)."""
+    if like.is_contiguous():
         return torch.empty_like(like) if like.dtype is dtype else torch.empty_like(like, dtype=dtype)
-    return torch.empty(shape, dtype=dtype, device=like.device)
+    return torch.empty(like.shape, dtype=dtype, device=like.device)
+
+
+def _sums(w: torch.Tensor) -> torch.Tensor:
+    """For the gradient of w: float32 along one axis."""
+    g = _empty(w, torch.float32)
+    return g if g.dim() == 1 else g.view(-1)
 
 
 def _ptr(t: Optional[torch.Tensor]) -> int:
@@ -251,14 +250,10 @@ def peri_norm(x: torch.Tensor, f: Optional[torch.Tensor], w_post: Optional[torch
     None.  ``gate`` has one row of D per ``rows_per_gate`` rows of x (0: one
     row for all).  n has f's type (``branch_dtype``, x's by default, without
     f)."""
-    if torch.is_grad_enabled() and _wants_grad(x, f, w_post, w_pre, gate):
-        if f is None and w_pre is not None:
-            return x, _PeriNorm.apply(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype)[1]
-        return _PeriNorm.apply(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype)
-    return _peri_norm(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype)
-
-
-def _peri_norm(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype):
+    if torch.is_grad_enabled() and (x.requires_grad or f is not None and f.requires_grad or w_pre is not None and w_pre.requires_grad or
+                                    w_post is not None and w_post.requires_grad or gate is not None and gate.requires_grad):
+        out, n = _PeriNorm.apply(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype)
+        return x if f is None else out, n
     _on_device(x, f, w_post, w_pre, gate)
     branch = f.dtype if f is not None else branch_dtype or x.dtype
     if branch not in _TYPES:
@@ -268,8 +263,8 @@ def _peri_norm(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branc
     shape = x.shape
     x_in, px, ld_x = _rows(x, shape, "x")
     f_in, pf, ld_f = _rows(f, shape, "f")
-    out = _empty(x, shape, x.dtype) if f is not None else x
-    n = _empty(f if f is not None else x, shape, branch) if w_pre is not None else None
+    out = _empty(x, x.dtype) if f is not None else x
+    n = _empty(f if f is not None else x, branch) if w_pre is not None else None
     if rows:
         c_ops.mtdao_peri_norm(
             c_ops.PACKED_ARGS.pack(rows, d, _KINDS[kind], stream, _TYPES[branch], _TYPES[weight], eps, scale, per, ld_x, ld_f, d, d,
@@ -307,11 +302,11 @@ def peri_norm_backward(d_out: Optional[torch.Tensor], dn: Optional[torch.Tensor]
     f_in, pf, ld_f = _rows(f, shape, "f")
     d_in, pd, ld_d = _rows(d_out, shape, "d_out")
     y_in, py, ld_y = _rows(dn, shape, "dn")
-    dx = _empty(x_out, shape, x_out.dtype)
-    df = _empty(f, shape, branch) if f is not None else None
-    dw_post = _empty(w_post, (d,), f32) if f is not None else None
-    dw_pre = _empty(w_pre, (d,), f32) if w_pre is not None else None
-    dgate = _empty(gate, gate.shape, f32) if gate is not None else None
+    dx = _empty(x_out, x_out.dtype)
+    df = _empty(f, branch) if f is not None else None
+    dw_post = _sums(w_post) if f is not None else None
+    dw_pre = _sums(w_pre) if w_pre is not None else None
+    dgate = _empty(gate, f32) if gate is not None else None
     if rows == 0:
         for t in (dw_post, dw_pre, dgate):
             if t is not None:
@@ -329,14 +324,15 @@ def peri_norm_backward(d_out: Optional[torch.Tensor], dn: Optional[torch.Tensor]
 
 
 class _PeriNorm(torch.autograd.Function):
-    """peri_norm for autograd (x' only where there is an f: else it is x itself)."""
+    """peri_norm for autograd (x' only where there is an f: else it is x itself).
+    A function's ``forward`` runs without gradients."""
 
     @staticmethod
     def forward(ctx, x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype):
         ctx.set_materialize_grads(False)
-        out, n = _peri_norm(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype)
-        ctx.save_for_backward(out, f, w_post, w_pre, gate)
         ctx.how = {"rows_per_gate": rows_per_gate, "scale": scale, "eps": eps, "kind": kind}
+        out, n = peri_norm(x, f, w_post, w_pre, gate=gate, branch_dtype=branch_dtype, **ctx.how)
+        ctx.save_for_backward(out, f, w_post, w_pre, gate)
         return out if f is not None else None, n
 
     @staticmethod
@@ -494,12 +490,8 @@ class Weight8:
 def linear8(x: torch.Tensor, w: Weight8, *, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """x W^T over the last axis of x, x in 8-bit blocks along it; in x's type
     unless ``dtype`` is given."""
-    if torch.is_grad_enabled() and _wants_grad(x, w.source):
+    if torch.is_grad_enabled() and (x.requires_grad or w.source is not None and w.source.requires_grad):
         return _Linear8.apply(x, w.source, w, dtype)
-    return _linear8(x, w, dtype)
-
-
-def _linear8(x, w, dtype):
     wq = w.q
     if x.shape[-1] != wq.cols:
         raise ValueError(f"x has {x.shape[-1]} columns, the weight {wq.cols}")
@@ -535,7 +527,7 @@ def linear8_backward(dy: torch.Tensor, x: torch.Tensor, w: Weight8, *, dw: Optio
     x2 = _flat(x)
     dy2 = _flat(dy)
     m = x2.shape[0]
-    dx = _empty(x, x.shape, dy.dtype)
+    dx = _empty(x, dy.dtype)
     need = _linear_workspace(m, n, k)[1]
     ws = torch.empty(need, dtype=torch.uint8, device=dev)
     st = _stream(x)
@@ -551,7 +543,7 @@ class _Linear8(torch.autograd.Function):
     def forward(ctx, x, source, w, dtype):
         ctx.save_for_backward(x)
         ctx.w, ctx.version, ctx.type = w, w.version, source.dtype if source is not None else torch.float32
-        return _linear8(x, w, dtype)
+        return linear8(x, w, dtype=dtype)
 
     @staticmethod
     @once_differentiable
