@@ -246,7 +246,7 @@ __global__ __launch_bounds__(kTileThreads) void k_quantize8_tile(Quantized one, 
 // 13 bits below the largest one (measured: 65536 + 4 gives 65536, in the
 // instruction with scales and the one without), which leaves sums 1.3e-5
 // (normal values) to 4e-5 (outlier columns) off in relative norm.  For a bf16
-// c that is a hundredth of its rounding.  An fp32 c is formed by bf16
+// c that is a fortieth of its rounding, 1.7e-3, and rate counts for more.  An fp32 c is formed by bf16
 // instructions instead, at half their rate: codes times scales are bf16
 // values, and their products are summed in fp32.
 

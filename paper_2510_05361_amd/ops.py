@@ -442,8 +442,11 @@ def quantize8(x: torch.Tensor, *, rows: bool = True, transposed: bool = False):
 
 def product8(a: Matrix8, b: Matrix8, *, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None,
              accumulate: bool = False) -> torch.Tensor:
-    """a b^T [a.rows, b.rows], summed in float32.  ``out``: written in place
-    of a new tensor (contiguous rows); ``accumulate``: added to (float32)."""
+    """a b^T [a.rows, b.rows].  float32 results are float32 sums of exact products;
+    bfloat16 ones, at twice the rate, leave out what lies more than 13 bits below
+    the largest product of a group: up to 4e-5 of the result's norm, next to 1.7e-3
+    for their rounding.  ``out``: written in place of a new tensor (contiguous
+    rows); ``accumulate``: added to (float32)."""
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
@@ -489,7 +492,7 @@ class Weight8:
 
 def linear8(x: torch.Tensor, w: Weight8, *, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """x W^T over the last axis of x, x in 8-bit blocks along it; in x's type
-    unless ``dtype`` is given."""
+    unless ``dtype`` is given, which also says how it is summed (``product8``)."""
     if torch.is_grad_enabled() and (x.requires_grad or w.source is not None and w.source.requires_grad):
         return _Linear8.apply(x, w.source, w, dtype)
     wq = w.q
@@ -511,7 +514,8 @@ def linear8_backward(dy: torch.Tensor, x: torch.Tensor, w: Weight8, *, dw: Optio
     """(dx, dw) of ``linear8``: dx = dy W in dy's type, with dy in 8-bit
     blocks along its rows; dw = dy^T x in float32, with dy and x in 8-bit
     blocks along the tokens.  ``dw``: written in place of a new tensor
-    (float32, contiguous rows); ``accumulate``: added to."""
+    (float32, contiguous rows); ``accumulate``: added to.  Sums are those of
+    ``product8`` for these types."""
     n, k = w.q.rows, w.q.cols
     if x.shape[-1] != k or dy.shape[-1] != n or x.shape[:-1] != dy.shape[:-1]:
         raise ValueError(f"dy is {tuple(dy.shape)}, x {tuple(x.shape)}, the weight [{n}, {k}]")

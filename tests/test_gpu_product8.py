@@ -405,3 +405,23 @@ def test_many_columns_and_few_rows(m):
     c = ops.product8(a, ops.quantize8(w))
     assert torch.equal(c[:, some], ops.product8(a, ops.quantize8(w[some])))
     assert int(c.abs().sum(0).nonzero().numel()) == 7
+
+
+@pytest.mark.parametrize("outliers", [False, True])
+@pytest.mark.parametrize("m,n,k", [(8, 8192, 2048), (48, 4096, 1000), (300, 520, 1024), (512, 1536, 4096), (2100, 2048, 700)])
+def test_what_bf16_sums_leave_out(m, n, k, outliers):
+    """bf16 results against the exact sums of the stored values, rounded.  Sums that
+    are off by e of their norm, 0.8 e in the mean, cross a midpoint of bf16's steps
+    (5.6e-3 of a value in the middle of its octave) in 0.8 e / 5.6e-3 of all cases
+    and are then one step off: 5.6e-3 sqrt(0.8 e / 5.6e-3) of the norm.  For the
+    stated e = 4e-5 that is 4.2e-4; twice that e is let pass, 6e-4.  fp32 results:
+    k sums of like sizes, half a unit each at random."""
+    gen = torch.Generator(device="cuda").manual_seed(k)
+    x, w = torch.randn((m, k), device="cuda", generator=gen), torch.randn((n, k), device="cuda", generator=gen) * 0.02
+    if outliers:
+        x *= 1 + 20 * (torch.rand(k, device="cuda", generator=gen) < 0.02)
+    a, b = ops.quantize8(x), ops.quantize8(w)
+    want = stored(a) @ stored(b).t()
+    got = ops.product8(a, b).cpu().double()
+    assert float((got - want.bfloat16().double()).norm() / want.norm()) <= 6e-4
+    assert float((ops.product8(a, b, dtype=torch.float32).cpu().double() - want).norm() / want.norm()) <= 4 * U * math.sqrt(k)
