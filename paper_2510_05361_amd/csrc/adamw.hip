@@ -371,13 +371,15 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // How a pass goes over its elements.  Workgroups of one CU and, for states of
 // 32 bits, spread pieces set how many DRAM pages are open at once.  Measured for
 // 354 M elements, all the registers allow and contiguous against the choice here:
-// 32 bits, fp32 1715 -> 1624 us (6.1 TB/s; the rest of a chunk's 64 KiB of loads
+// 32 bits, fp32 1688 -> 1643 us (6.0 TB/s; the rest of a chunk's 64 KiB of loads
 // in two workgroups covers the latency), 32 bits with bf16 parameters and
-// gradients 1292 -> 1217 us, four workgroups (two 1505 us); 8 bits with fp32
-// parameters 839 -> 803 us, four workgroups, contiguous (spread 827 us).  Below
-// 64 M elements 32-bit passes gain nothing (32 M: 151.2 and 151.2 us) or lose
-// (16 M: 76.7 and 81.1 us); with bf16 parameters 8-bit passes lose at any limit
-// (1311 M: 2081 and 2202 us).  The limit is an amount of unused LDS, of 160 KiB.
+// gradients 1283 -> 1226 us, four workgroups (two 1505 us); 8 bits with fp32
+// parameters 839 -> 803 us, four workgroups, contiguous (spread 827 us).  In
+// between, 32 bits: 256 M 1216 -> 1145 us (bf16 915 -> 880), 128 M 597 -> 577 (456
+// -> 445), 64 M 294 -> 286 (232 -> 226).  Below 64 M they gain less than their noise
+// or lose (48 M 223.5 and 223.4 us, 32 M 145.9 and 146.9, 8 M 36.3 and 40.0); with
+// bf16 parameters 8-bit passes lose at any limit (1311 M: 2081 and 2202 us).  The
+// limit is an amount of unused LDS, of 160 KiB.
 struct Pass {
   bool spread;
   size_t lds;

@@ -267,14 +267,13 @@ struct Product {
   float* partial;                // [splits][rows of a][rows of b] with more than one part
 };
 
-// A 128-byte row in LDS: its eight 16-byte chunks, each at the place that its
-// number and the row's key give.  A 16-byte read of a wave takes 16 lanes at
+// A 128-byte row in LDS: each of its eight 16-byte chunks is at the place that its
+// number and the row's key give, by an exclusive or.  A 16-byte read of a wave takes 16 lanes at
 // once, which have to lie in different ones of the 16 such places of the 64
 // banks: two rows of eight, told apart by the row's last bit, so the key has
 // the next three.  (With the last three bits as the key half of the reads'
 // cycles were conflicts.)
 __device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
-__device__ __forceinline__ int chunk_at(int row, int chunk) { return row * 128 + ((chunk ^ row_key(row)) << 4); }
 
 // The row of b's fragment that the instruction's row r takes: results of a lane
 // are rows 8 q + 4 h + t, so these are sixteen consecutive columns of c.
@@ -988,13 +987,13 @@ int32_t launch_quantize(const void* x, int32_t dtype, int64_t ld, const mtdao_ma
   return MTDAO_OK;
 }
 
-template <int V>
-using Int = std::integral_constant<int, V>;
-
 // Waves of a workgroup of the kernel for few rows: enough that each has a few
 // blocks.  Its columns: sixteen, or 32 where a's blocks, read by every workgroup, are
-// much and there are workgroups enough (64 x 8192 x 2048 9.2 us, 13.7 us with sixteen;
-// 64 x 4096 x 2048 8.8 us, 7.7 us with sixteen).
+// much (from 17 rows on) and sixteen would take more than one workgroup a CU, 4096
+// columns (with 32 against sixteen: 64 x 4096 x 2048 8.6 us (7.4), 64 x 5120 x 2048 8.6
+// us (13.0), 64 x 8192 x 2048 8.7 us (13.1); 24 x 4096 x 768 3.8 us (3.3), 24 x 5120 x 768
+// 3.8 us (4.1), 24 x 8192 x 8192 18.0 us (25.1); between 24 and 64 rows and 256 and 8192
+// columns of a the turn is at 4096 everywhere, for either c).
 constexpr int64_t kWideFrom = 4096;
 template <typename XT, typename CT, int MI>
 void launch_few(const Few& f, hipStream_t st) {
