@@ -381,8 +381,9 @@ class Matrix8:
     @property
     def scales(self) -> torch.Tensor:
         a = self.on(_stream(self._buf))
-        held = self._buf[a.rows * a.ld:].view(-1, a.scale_ld // 4, 4)
-        return held.permute(1, 0, 2).reshape(a.scale_ld // 4, -1).view(SCALE)
+        fours, rows = -(-a.cols // (4 * BLOCK)), a.scale_ld // 4
+        held = self._buf[a.rows * a.ld:].view(fours, rows, 4)
+        return held.permute(1, 0, 2).reshape(rows, 4 * fours).view(SCALE)
 
     def dequantize(self) -> torch.Tensor:
         """The values as float32 [rows, cols]."""
@@ -390,7 +391,7 @@ class Matrix8:
         s = self.scales.float()[:, :codes.shape[1] // BLOCK]
         if self.scale_rows > 1:
             s = s.repeat_interleave(self.scale_rows, 0)[:self.rows]
-        return (codes.view(self.rows, -1, BLOCK) * s[:, :, None]).view(codes.shape)[:, :self.cols]
+        return (codes.view(self.rows, codes.shape[1] // BLOCK, BLOCK) * s[:, :, None]).view(codes.shape)[:, :self.cols]
 
 
 def _matrix(x: torch.Tensor) -> torch.Tensor:

@@ -425,3 +425,14 @@ def test_what_bf16_sums_leave_out(m, n, k, outliers):
     got = ops.product8(a, b).cpu().double()
     assert float((got - want.bfloat16().double()).norm() / want.norm()) <= 6e-4
     assert float((ops.product8(a, b, dtype=torch.float32).cpu().double() - want).norm() / want.norm()) <= 4 * U * math.sqrt(k)
+
+
+@pytest.mark.parametrize("rows,cols", [(0, 0), (0, 5), (0, 700), (5, 0), (200, 0)])
+def test_matrices_without_elements_can_be_looked_at(rows, cols):
+    x = torch.empty((rows, cols), device="cuda")
+    up = lambda n, m: -(-n // m) * m  # noqa: E731
+    for q, r, c, per in ((ops.quantize8(x), rows, cols, 1), (ops.quantize8(x, rows=False, transposed=True), cols, rows, 1),
+                         (ops.Weight8(x).q, rows, cols, 128), (ops.Weight8(x).qt, cols, rows, 128)):
+        assert q.codes.shape == (r, up(c, 128))
+        assert q.scales.shape == (-(-r // per), up(c, 512) // 128)
+        assert q.dequantize().shape == (r, c)
