@@ -24,6 +24,7 @@ from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
 from torch.autograd.function import once_differentiable
+from torch.autograd.graph import increment_version
 
 from . import mtdao as abi
 from . import mtdao_ops as c_ops
@@ -121,6 +122,7 @@ class AdamW:
                                 betas[1], eps, max_norm, start_step)
         need = c_ops.mtdao_adamw_workspace_bytes(cfg, rows)
         self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        self._followed = [p for p in self.params if not p.is_inference()]  # by autograd
         self._own = [self.workspace]
         if states is None:
             self._own += [t for name in kinds for t in getattr(self, name)]
@@ -157,7 +159,10 @@ class AdamW:
         self.grads = list(grads)
 
     def step(self, lr: float) -> None:
+        """One step.  To autograd it is a change in place: a backward pass over
+        parameters from before it is refused."""
         c_ops.mtdao_adamw_step(self.handle, lr, self._stream_here())
+        increment_version(self._followed)
 
     @property
     def step_count(self) -> int:
@@ -448,7 +453,8 @@ def product8(a: Matrix8, b: Matrix8, *, dtype: torch.dtype = torch.bfloat16, out
     the largest product of a group: up to 4e-5 of the result's norm, next to 1.7e-3
     for their rounding.  ``out``: written in place of a new tensor (contiguous
     rows); ``accumulate``: added to (float32)."""
-    if out is None:
+    given = out is not None
+    if not given:
         if accumulate:
             raise ValueError("accumulate needs out")
         out = torch.empty((a.rows, b.rows), dtype=dtype, device=a._buf.device)
@@ -459,6 +465,8 @@ def product8(a: Matrix8, b: Matrix8, *, dtype: torch.dtype = torch.bfloat16, out
     ws = torch.empty(need, dtype=torch.uint8, device=out.device) if need else None
     st = _stream(out)
     c_ops.mtdao_product8(a.on(st), b.on(st), out.data_ptr(), _type(out, "out"), _ld(out), accumulate, _ptr(ws), need, st)
+    if given and not out.is_inference():
+        increment_version(out)
     return out
 
 
@@ -522,7 +530,8 @@ def linear8_backward(dy: torch.Tensor, x: torch.Tensor, w: Weight8, *, dw: Optio
         raise ValueError(f"dy is {tuple(dy.shape)}, x {tuple(x.shape)}, the weight [{n}, {k}]")
     if dy.dtype != x.dtype:
         raise TypeError(f"dy is {dy.dtype}, x {x.dtype}")
-    if dw is None:
+    given = dw is not None
+    if not given:
         if accumulate:
             raise ValueError("accumulate needs dw")
         dw = torch.empty((n, k), dtype=torch.float32, device=x.device)
@@ -538,6 +547,8 @@ def linear8_backward(dy: torch.Tensor, x: torch.Tensor, w: Weight8, *, dw: Optio
     st = _stream(x)
     c_ops.mtdao_linear8_backward(dy2.data_ptr(), x2.data_ptr(), _type(dy, "dy"), m, _ld(dy2), _ld(x2), w.qt.on(st), dx.data_ptr(), k,
                                  dw.data_ptr(), _ld(dw), accumulate, ws.data_ptr(), need, st)
+    if given and not dw.is_inference():
+        increment_version(dw)
     return dx, dw
 
 

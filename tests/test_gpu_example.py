@@ -58,3 +58,29 @@ def test_training():
     assert len(losses) == 100 and all(x == x for x in losses)
     start, warm, end = losses[0], sum(losses[50:60]) / 10, sum(losses[-10:]) / 10
     assert warm < 0.6 * start and end < warm
+
+
+def test_backward_passes_over_changed_tensors_are_refused():
+    """What the operators write in place has changed for autograd too."""
+    from paper_2510_05361_amd import ops
+
+    x, w = torch.randn((6, 64), device="cuda"), torch.ones(64, device="cuda", requires_grad=True)
+    _, n = ops.peri_norm(x, None, None, w)
+    ops.AdamW([w.detach()], [torch.ones_like(w)]).step(1e-3)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        n.sum().backward()
+    a, b = ops.quantize8(torch.randn((6, 256), device="cuda")), ops.quantize8(torch.randn((64, 256), device="cuda"))
+    for change in (lambda t: ops.product8(a, b, out=t),
+                   lambda t: ops.linear8_backward(torch.ones((3, 6), device="cuda"), torch.ones((3, 64), device="cuda"),
+                                                  ops.Weight8(torch.ones((6, 64), device="cuda")), dw=t)):
+        y = torch.ones((6, 64), device="cuda")
+        s = (y * w).sum()
+        change(y)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            s.backward()
+    with torch.inference_mode():
+        x = torch.ones((6, 64), device="cuda")
+    ops.product8(a, b, out=x)
+    opt = ops.AdamW([x], [torch.ones_like(x)])
+    opt.step(1e-3)
+    assert opt.step_count == 1

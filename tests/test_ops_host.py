@@ -290,7 +290,7 @@ def test_adamw_keeps_what_it_allocated_for_the_streams_of_its_calls(call, stream
     seen = []
     monkeypatch.setattr(c, call, lambda *a: seen.append(a[-1]))
     opt = ops.AdamW.__new__(ops.AdamW)
-    opt.handle, opt.params, opt.grads, opt.workspace = None, [], [torch.zeros(1)], Held()
+    opt.handle, opt.params, opt._followed, opt.grads, opt.workspace = None, [], [], [torch.zeros(1)], Held()
     state = Held()
     opt._own, opt._streams = [opt.workspace, state], {1}
     monkeypatch.setattr(opt, "_grads_ok", lambda *a: None)
