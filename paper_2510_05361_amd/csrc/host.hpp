@@ -45,13 +45,19 @@ struct RoctxRange {
   }
 };
 
-inline int32_t fail(std::string* sink, int32_t code, const char* fmt, ...) {
+// The code, with a message in sink; no message where there is no memory for one
+// (nothing is thrown: this runs at C entries, and in their catch blocks).
+inline int32_t fail(std::string* sink, int32_t code, const char* fmt, ...) noexcept {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
-  *sink = buf;
+  try {
+    *sink = buf;
+  } catch (...) {
+    sink->clear();
+  }
   return code;
 }
 

@@ -348,3 +348,39 @@ def test_adamw_refuses_gradients_on_what_it_writes(kw):
     with pytest.raises(abi.MtdaoError, match="overlaps") as e:
         c.mtdao_adamw_init(cfg, rows, BASE << 1, 1 << 30, None)
     assert e.value.code == abi.MTDAO_ERR_INVALID_ARG
+
+
+OUT_OF_MEMORY = r"""
+#include <cstdio>
+#include <cstdlib>
+#include <new>
+#include "host.hpp"
+static bool none = false;
+void* operator new(size_t n) {
+  if (none) throw std::bad_alloc();
+  return std::malloc(n);
+}
+void operator delete(void* p) noexcept { std::free(p); }
+void operator delete(void* p, size_t) noexcept { std::free(p); }
+int main() {
+  std::string sink = "an earlier message";
+  sink.shrink_to_fit();
+  none = true;
+  const int32_t code = mtdao::fail(&sink, MTDAO_ERR_WORKSPACE, "%s", "a message that does not fit into the string without more memory");
+  none = false;
+  std::printf("%d [%s]\n", code, sink.c_str());
+}
+"""
+
+
+def test_errors_without_memory_for_their_message(tmp_path):
+    """The code is returned; nothing is thrown through the C entry."""
+    if not os.path.exists(build.HIPCC):
+        pytest.skip("hipcc not available")
+    src, exe = tmp_path / "oom.hip", tmp_path / "oom"
+    src.write_text(OUT_OF_MEMORY)
+    flags = [f for f in build.FLAGS if f not in ("-shared", "-fPIC", "-O3")]
+    subprocess.run([build.HIPCC, *flags, "-O1", "-w", "-I", os.path.dirname(build.SRC), "-I", os.path.dirname(HEADER), "-o", str(exe), str(src)],
+                   check=True, stderr=subprocess.DEVNULL)
+    r = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60)
+    assert (r.returncode, r.stdout) == (0, f"{abi.MTDAO_ERR_WORKSPACE} []\n"), r
