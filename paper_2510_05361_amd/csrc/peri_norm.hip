@@ -583,7 +583,7 @@ using Int = std::integral_constant<int, V>;
 
 // Rows of whole vectors from dword to dword.
 bool whole_rows(const mtdao_peri_norm_args& a) {
-  auto dwords = [](const void* p, int64_t ld, int32_t dt) { return !p || (aligned_to(p, 4) && ld * esize(dt) % 4 == 0); };
+  auto dwords = [](const void* p, int64_t ld, int32_t dt) { return !p || (aligned_to(p, 4) && ld % 4 * esize(dt) % 4 == 0); };
   return a.d % kE == 0 && dwords(a.x, a.ld_x, a.stream_dtype) && dwords(a.f, a.ld_f, a.branch_dtype) &&
          dwords(a.d_out, a.ld_d_out, a.stream_dtype) && dwords(a.dn, a.ld_dn, a.branch_dtype) && dwords(a.x_out, a.d, a.stream_dtype) &&
          dwords(a.n_out, a.d, a.branch_dtype) && dwords(a.df, a.d, a.branch_dtype);

@@ -177,3 +177,75 @@ def test_products_of_many_columns_and_few_rows_fit_a_launch(run, n):
     for (name, (x, y, z), threads, _), cols in zip(launches, (16, 32 if n > 4096 else 16)):
         assert name == "k_product8_few" and z == 1 and x * threads < 1 << 32 and y <= 65535
         assert x * y * cols >= n > x * (y - 1) * cols
+
+
+ANY_SIZES = r"""
+        import random
+        rng = random.Random(5)
+        B, MOST = 1 << 40, (1 << 63) - 1
+        up = lambda n, m: -(-n // m) * m if n < 1 << 60 else 0
+
+        def size():
+            return rng.choice([0, 1, 2, 3, 7, 64, 127, 128, 129, 4096, 8192, 8193, 1 << 22, (1 << 22) + 1, (1 << 31) - 1, 1 << 31, 1 << 40, 1 << 62, MOST, -1,
+                               rng.randrange(1, 1 << 20)])
+
+        def matrix(rows, cols, at, scale_rows=1, ld=None):
+            return c.Matrix8(at, at + (1 << 52), rows, cols, max(128, up(cols, 128)) if ld is None else ld, 4 * up(rows, scale_rows) // scale_rows, scale_rows)
+
+        def boundary():
+            a = c.PeriNormArgs()
+            a.rows, a.d, a.rows_per_gate = size(), rng.choice([size(), 64, 768, 2048]), size()
+            a.kind, a.stream_dtype, a.branch_dtype, a.weight_dtype = (rng.choice([0, 1]) for _ in range(4))
+            a.eps, a.scale = 1e-5, 1.0
+            a.ld_x, a.ld_f, a.ld_d_out, a.ld_dn = (rng.choice([a.d, a.d, size()]) for _ in range(4))
+            for i, name in enumerate(("x", "f", "w_post", "w_pre", "gate", "d_out", "dn", "x_out", "n_out", "df", "d_w_post", "d_w_pre", "d_gate")):
+                if rng.random() < 0.85:
+                    setattr(a, name, B + (i << 44) + rng.choice([0, 0, 0, 0, 2, 4]))
+            if rng.random() < 0.5:
+                c.mtdao_peri_norm(a, None)
+            else:
+                c.mtdao_peri_norm_backward(a, B << 10, c.mtdao_peri_norm_backward_workspace_bytes(a), None)
+
+        def quantize():
+            r, k, s = size(), size(), rng.choice([1, 128])
+            q, qt = matrix(r, k, B, s, rng.choice([up(k, 128), size()])), matrix(k, r, B << 8, s)
+            c.mtdao_quantize8(B << 14, rng.choice([0, 1]), rng.choice([k, size()]), rng.choice([q, None]), rng.choice([qt, None]), None)
+
+        def product():
+            m, n, k = size(), size(), size()
+            need = c.mtdao_product8_workspace_bytes(m, n, k)
+            c.mtdao_product8(matrix(m, k, B), matrix(n, k, B << 13), B << 17, rng.choice([0, 1]), rng.choice([n, size()]), 0, B << 18, need, None)
+
+        def linear():
+            m, n, k = (rng.choice([0, 1, 5, 16, 17, 64, 65, 300, 4000, 1 << 22]) for _ in range(3))
+            f, b = c.mtdao_linear8_workspace_bytes(m, n, k)
+            t = rng.choice([0, 1])
+            c.mtdao_linear8(B << 14, t, m, k, matrix(n, k, B, 128), B << 15, rng.choice([0, 1]), n, B << 16, f, None)
+            c.mtdao_linear8_backward(B << 14, B << 15, t, m, n, k, matrix(k, n, B, 128), B << 16, k, B << 17, k, rng.choice([0, 1]), B << 18, b, None)
+
+        def adamw():
+            n = rng.randrange(1, 5)
+            cfg = c.AdamwConfig(rng.choice([0, 1]), rng.choice([0, 1]), rng.choice([32, 8]), n, 0.9, 0.95, rng.choice([0, 1e-8, 1e-40]), rng.choice([0, 1.0]),
+                                rng.choice([0, 5, MOST - 10]))
+            rows = (c.AdamwTensor * n)(*(c.AdamwTensor(*(B + (i << 46) + (j << 43) for j in range(6)), size(), 0.1) for i in range(n)))
+            need = c.mtdao_adamw_workspace_bytes(cfg, rows)
+            h = c.mtdao_adamw_init(cfg, rows, B << 20, need, None)
+            c.mtdao_adamw_step(h, 1e-3, None)
+            c.mtdao_adamw_destroy(h)
+
+        taken = refused = 0
+        for _ in range(6000):
+            try:
+                rng.choice([boundary, boundary, quantize, product, linear, adamw])()
+                taken += 1
+            except abi.MtdaoError:
+                refused += 1
+        say([taken, refused])
+"""
+
+
+def test_any_sizes_are_refused_or_fit_their_launches(run):
+    launches, said = run(ANY_SIZES)
+    assert min(said[0]) > 1000, said
+    for name, (x, y, z), threads, _ in launches:
+        assert x >= 1 and y >= 1 and z == 1 and x * threads < 1 << 32 and y <= 65535, (name, x, y, threads)
