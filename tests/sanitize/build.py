@@ -33,6 +33,7 @@ def _inputs_hash() -> str:
     h = hashlib.sha256()
     for f in (os.path.join(ROOT, "paper_2510_05361_amd", "csrc", "mtdao.hip"),
               os.path.join(ROOT, "paper_2510_05361_amd", "csrc", "kernels.hpp"),
+              os.path.join(ROOT, "paper_2510_05361_amd", "csrc", "host.hpp"),
               os.path.join(ROOT, "include", "mtdao.h"), os.path.join(HERE, "host_abi_check.c"), __file__):
         with open(f, "rb") as fh:
             h.update(fh.read())
