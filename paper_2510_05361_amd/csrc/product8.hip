@@ -242,9 +242,10 @@ __global__ __launch_bounds__(kTileThreads) void k_quantize8_tile(Quantized one, 
 // since they share one scale.  Rows of b go in as the instruction's rows, so
 // that a lane ends with sixteen consecutive columns of a row of c.
 //
-// Within a group of products the 8-bit instructions drop what lies more than
-// 13 bits below the largest one (measured: 65536 + 4 gives 65536, in the
-// instruction with scales and the one without), which leaves sums 1.3e-5
+// Within a group of eight products, neighbours in a row, the 8-bit instructions
+// drop what lies more than 13 bits below the largest one (measured: 65536 + 4 gives
+// 65536, 65536 + 8 does not, in the instruction with scales and the one without;
+// 4 in the next group stays), which leaves sums 1.3e-5
 // (normal values) to 4e-5 (outlier columns) off in relative norm.  For a bf16
 // c that is a fortieth of its rounding, 1.7e-3, and rate counts for more.  An fp32 c is formed by bf16
 // instructions instead, at half their rate: codes times scales are bf16

@@ -450,8 +450,8 @@ def product8(a: Matrix8, b: Matrix8, *, dtype: torch.dtype = torch.bfloat16, out
              accumulate: bool = False) -> torch.Tensor:
     """a b^T [a.rows, b.rows].  float32 results are float32 sums of exact products;
     bfloat16 ones, at twice the rate, leave out what lies more than 13 bits below
-    the largest product of a group: up to 4e-5 of the result's norm, next to 1.7e-3
-    for their rounding.  ``out``: written in place of a new tensor (contiguous
+    the largest of each eight products: up to 4e-5 of the result's norm, next to
+    1.7e-3 for their rounding.  ``out``: written in place of a new tensor (contiguous
     rows); ``accumulate``: added to (float32)."""
     given = out is not None
     if not given:
@@ -524,7 +524,8 @@ def linear8_backward(dy: torch.Tensor, x: torch.Tensor, w: Weight8, *, dw: Optio
     blocks along its rows; dw = dy^T x in float32, with dy and x in 8-bit
     blocks along the tokens.  ``dw``: written in place of a new tensor
     (float32, contiguous rows); ``accumulate``: added to.  Sums are those of
-    ``product8`` for these types."""
+    ``product8`` for these types (its float32 sums for a bfloat16 dy:
+    ``product8(quantize8(dy), w.qt, dtype=torch.float32)``)."""
     n, k = w.q.rows, w.q.cols
     if x.shape[-1] != k or dy.shape[-1] != n or x.shape[:-1] != dy.shape[:-1]:
         raise ValueError(f"dy is {tuple(dy.shape)}, x {tuple(x.shape)}, the weight [{n}, {k}]")

@@ -436,3 +436,21 @@ def test_matrices_without_elements_can_be_looked_at(rows, cols):
         assert q.codes.shape == (r, up(c, 128))
         assert q.scales.shape == (-(-r // per), up(c, 512) // 128)
         assert q.dequantize().shape == (r, c)
+
+
+@pytest.mark.parametrize("m", [8, 48, 300])
+def test_the_most_that_bf16_sums_leave_out(m):
+    """One product of 2^16 in each eight, seven below 2^-13 of it, and as much of the
+    other sign in the next block: what is left is the seven, of which each may be
+    dropped.  At most 2^-10 of the sum of magnitudes, and the rounding."""
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    a = torch.randint(1, 3, (m, 512), device="cuda", generator=gen).float()
+    b = torch.randint(1, 3, (64, 512), device="cuda", generator=gen).float()
+    a[:, ::8], b[:, :256:8], b[:, 256::8] = 256, 256, -256
+    qa, qb = ops.quantize8(a), ops.quantize8(b)
+    want = a.cpu().double() @ b.cpu().double().t()
+    size = a.cpu().double() @ b.abs().cpu().double().t()
+    assert torch.equal(qa.dequantize(), a) and torch.equal(qb.dequantize(), b)
+    got = ops.product8(qa, qb).cpu().double()
+    assert bool(((got - want).abs() <= 2.0 ** -10 * size + 2.0 ** -8 * want.abs()).all())
+    assert torch.equal(ops.product8(qa, qb, dtype=torch.float32).cpu().double(), want)
