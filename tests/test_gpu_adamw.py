@@ -309,7 +309,7 @@ def test_closed_with_a_step_in_flight_on_another_stream(bits):
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
-        torch.cuda._sleep(20_000_000)
+        torch.cuda._sleep(240_000_000)  # a tenth of a second
         opt.step(LR)
     held = [opt.workspace] + opt.m + opt.v + (opt.m_scale + opt.v_scale if bits == 8 else [])
     ranges = [(t.data_ptr(), t.numel() * t.element_size()) for t in held]

@@ -340,7 +340,7 @@ def test_weight_dropped_with_a_call_in_flight_on_another_stream():
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
-        torch.cuda._sleep(20_000_000)
+        torch.cuda._sleep(240_000_000)  # a tenth of a second
         got = ops.linear8(x, held)
         got_dx = ops.linear8_backward(want, x, held)[0]
     del held
