@@ -8,6 +8,11 @@
  *                      the next block, and their gradients
  *   mtdao_quantize8,   matrices in 8-bit floating point with a scale for
  *   mtdao_product8     each block of 128, and their product
+ *   mtdao_orthogonalize, mtdao_muon_*   updates of matrices orthogonalised by
+ *                      Newton-Schulz products, and the optimizer of a model's
+ *                      matrices that takes them
+ *   mtdao_embedding*   rows of a table by token, and the table's gradient
+ *   mtdao_cross_entropy   the loss over a vocabulary and its gradient
  *
  * Conventions are those of mtdao.h: caller-owned device memory, work that is
  * only enqueued on the HIP stream passed to each call (no allocation, no
@@ -214,6 +219,133 @@ int32_t mtdao_linear8(const void* x, int32_t dtype, int64_t rows, int64_t ld, co
 int32_t mtdao_linear8_backward(const void* dy, const void* x, int32_t dtype, int64_t rows, int64_t ld_dy, int64_t ld_x,
                                const mtdao_matrix8* wt, void* dx, int64_t ld_dx, float* dw, int64_t ld_dw, int32_t accumulate,
                                void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------ orthogonalised updates
+ *
+ * For a matrix x [rows][cols], its transpose where rows > cols:
+ *   X = x / (||x|| + eps)              ||x||: the root of the sum of squares
+ *   `steps` times:  A = X X^T,  X <- a X + (b A + c A A) X
+ *   with a, b, c = 3.4445, -4.7750, 2.0315
+ * which leaves the singular vectors of x as they are and moves its singular
+ * values towards 1 (after five steps those from 1/400 of ||x|| on lie in about
+ * 0.7 to 1.2).  ||x|| is summed in fp64; products are of the precision of fp32 (factors
+ * in 24 bits, sums in fp32), and the order of sums depends on the sizes alone.
+ * Elements of X are held to 2^-39: a matrix with ||x|| far below eps, whose X is as
+ * small, keeps fewer bits, or none.
+ * x = 0 gives 0 (eps > 0); infinities and NaN make all of their matrix NaN. */
+#define MTDAO_MUON_MAX_SIDE 16384 /* of a matrix's smaller side; the larger one: 2^20 */
+#define MTDAO_MUON_MAX_STEPS 64
+
+/* batch matrices, one after another without gaps, x (dtype) to out (out_dtype);
+ * out may be x where the types are equal.  workspace: 256-byte aligned. */
+int32_t mtdao_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, size_t* bytes);
+int32_t mtdao_orthogonalize(const void* x, int32_t dtype, int64_t batch, int64_t rows, int64_t cols, void* out, int32_t out_dtype,
+                            int32_t steps, double eps, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* One step of every matrix:
+ *   m = momentum m + g
+ *   u = g + momentum m (nesterov) or m
+ *   p = p (1 - lr weight_decay) - lr factor o,   o: u orthogonalised
+ * m is fp32; o and the new p are formed in fp32, p rounded once. */
+typedef struct mtdao_muon_matrix {
+  void* p;             /* [rows][cols], param_dtype                                    */
+  const void* g;       /* [rows][cols], grad_dtype                                     */
+  float* m;            /* [rows][cols]                                                 */
+  int64_t rows, cols;  /* >= 0                                                         */
+  double weight_decay; /* >= 0                                                         */
+  double factor;       /* of the update                                                */
+} mtdao_muon_matrix;
+
+typedef struct mtdao_muon_config {
+  int32_t param_dtype;
+  int32_t grad_dtype;
+  int32_t n_matrices;
+  int32_t nesterov;
+  int32_t steps;       /* 1..MTDAO_MUON_MAX_STEPS                                      */
+  int32_t reserved;    /* 0                                                            */
+  double momentum;     /* in [0, 1)                                                    */
+  double eps;          /* >= 0                                                         */
+} mtdao_muon_config;
+
+typedef struct mtdao_muon mtdao_muon;
+
+/* Device workspace (bytes, 256-byte aligned, caller-owned, must outlive the
+ * handle): a row per matrix, and the factors of the matrices that are worked
+ * on together (4 GiB, or what a single larger matrix takes).  Reads the sizes of matrices
+ * only.  Host-only. */
+int32_t mtdao_muon_workspace_bytes(const mtdao_muon_config* cfg, const mtdao_muon_matrix* matrices, size_t* bytes);
+
+/* Validate and build a handle; enqueues the kernels that write the table of
+ * matrices into the workspace.  m is taken as it is.  No two of all p and m may
+ * overlap, nor a gradient and one of them. */
+int32_t mtdao_muon_init(const mtdao_muon_config* cfg, const mtdao_muon_matrix* matrices, void* workspace, size_t workspace_bytes,
+                        void* hip_stream, mtdao_muon** out);
+
+/* Take the gradients of every matrix from other addresses from here on
+ * (ordered on the stream). */
+int32_t mtdao_muon_set_grads(mtdao_muon* h, const void* const* grads, void* hip_stream);
+
+/* One step of all matrices; lr is fixed at call time: a captured step replays
+ * with it. */
+int32_t mtdao_muon_step(mtdao_muon* h, double lr, void* hip_stream);
+
+const char* mtdao_muon_last_error(const mtdao_muon* h);
+void mtdao_muon_destroy(mtdao_muon* h);
+
+/* ------------------------------------------------------------- embedding
+ *
+ * out[i] = scale table[tokens[i]], for n_tokens tokens (token_bits: 32 or 64)
+ * and a table of rows x d with row stride ld, in fp32, rounded once to out_dtype.
+ * A token below 0 stands for none: its row is zero.  One that the table does not
+ * have makes its row NaN; no memory outside the table is read.
+ *
+ * Backward: dw[r] = scale sum of dy[i] over the places i with tokens[i] == r
+ * (accumulate: dw[r] +=, and rows of tokens that do not come are not touched),
+ * fp32 sums in the order of the places, in pieces of 64; tokens outside the
+ * table are left out.  Results depend on the operands alone.
+ * workspace: 256-byte aligned. */
+int32_t mtdao_embedding(const void* tokens, int32_t token_bits, int64_t n_tokens, const void* table, int32_t table_dtype, int64_t rows,
+                        int64_t d, int64_t ld, float scale, void* out, int32_t out_dtype, int64_t ld_out, void* hip_stream);
+int32_t mtdao_embedding_backward_workspace_bytes(int64_t n_tokens, int64_t rows, int64_t d, size_t* bytes);
+int32_t mtdao_embedding_backward(const void* dy, int32_t dy_dtype, int64_t ld_dy, const void* tokens, int32_t token_bits, int64_t n_tokens,
+                                 float scale, float* dw, int64_t rows, int64_t d, int64_t ld_dw, int32_t accumulate, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream);
+
+/* ---------------------------------------------------------- cross entropy
+ *
+ * For every row x of logits and its target y:
+ *   lse = log sum_j exp(x_j)
+ *   loss_i = lse - x_y + z_loss lse^2
+ *   d_i = w_i (softmax(x) (1 + 2 z_loss lse) - [j = y])
+ * in fp32.  A target below 0 stands for none: loss 0, gradient 0, whatever its
+ * logits are.  One that the row does not have makes its loss and gradient NaN, as
+ * does a row without a logit above minus infinity.  loss is the sum of the rows' losses, or their
+ * mean over the rows with a target (0 where there is none), summed in fp64.  w_i = scale d_loss, over the
+ * number of rows with a target for the mean; d_loss is one number, or for
+ * MTDAO_LOSS_NONE one for each row (NULL: 1). */
+enum { MTDAO_LOSS_NONE = 0, MTDAO_LOSS_SUM = 1, MTDAO_LOSS_MEAN = 2 };
+
+typedef struct mtdao_cross_entropy_args {
+  int64_t rows, cols;    /* 0..2^31, 1..2^31                                           */
+  int64_t ld_logits;     /* elements from row to row, >= cols                          */
+  int64_t ld_d;          /* of d_logits                                                */
+  int32_t dtype;         /* of logits and d_logits                                     */
+  int32_t target_bits;   /* 32 or 64                                                   */
+  int32_t reduction;     /* MTDAO_LOSS_*                                               */
+  float z_loss;
+  float scale;           /* of the gradient                                            */
+  int32_t reserved;      /* 0                                                          */
+  const void* logits;
+  const void* targets;
+  const float* d_loss;   /* device; NULL: 1                                            */
+  float* losses;         /* of every row, or NULL                                      */
+  float* loss;           /* their sum or mean, or NULL                                 */
+  void* d_logits;        /* or NULL; may be logits itself when the strides are equal   */
+} mtdao_cross_entropy_args;
+
+/* Reads the sizes of a.  Host-only.  workspace: 256-byte aligned. */
+int32_t mtdao_cross_entropy_workspace_bytes(const mtdao_cross_entropy_args* a, size_t* bytes);
+int32_t mtdao_cross_entropy(const mtdao_cross_entropy_args* a, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -21,8 +21,8 @@ from concurrent.futures import ThreadPoolExecutor
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 SRC = os.path.join(PKG, "csrc", "mtdao.hip")
-OPS_SRCS = [os.path.join(PKG, "csrc", f) for f in ("adamw.hip", "peri_norm.hip", "product8.hip")]
-HEADERS = [os.path.join(PKG, "csrc", f) for f in ("kernels.hpp", "host.hpp", "ops_device.hpp")] + \
+OPS_SRCS = [os.path.join(PKG, "csrc", f) for f in ("adamw.hip", "peri_norm.hip", "product8.hip", "muon.hip", "embedding.hip", "cross_entropy.hip")]
+HEADERS = [os.path.join(PKG, "csrc", f) for f in ("kernels.hpp", "host.hpp", "ops_device.hpp", "tiles.hpp")] + \
     [os.path.join(ROOT, "include", f) for f in ("mtdao.h", "mtdao_ops.h")]
 LIB = os.path.join(PKG, "libmtdao.so")
 STREAM_SRC = os.path.join(PKG, "csrc", "stream_ref.hip")
@@ -93,7 +93,7 @@ def build(out: str = LIB, extra=()) -> str:
     (libstream_ref.so).  The register, scratch and occupancy figures of every
     kernel go to RESOURCES."""
     flags = [f for f in FLAGS if f != "-shared"]
-    with tempfile.TemporaryDirectory() as d, ThreadPoolExecutor(4) as pool:
+    with tempfile.TemporaryDirectory() as d, ThreadPoolExecutor(8) as pool:
         def compile_one(src):
             obj = os.path.join(d, os.path.basename(src) + ".o")
             return obj, _run([HIPCC, *flags, *extra, "-I", os.path.join(ROOT, "include"), "-c", "-o", obj, src, _REMARK])

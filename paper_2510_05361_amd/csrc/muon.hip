@@ -1,0 +1,917 @@
+// Orthogonalised updates of matrices by Newton-Schulz products, and the
+// optimizer step that takes them (include/mtdao_ops.h).
+//
+// Numbers.  Every factor of a product is held as the sum of two fp16 numbers,
+// x 2^e = hi + lo: hi is x 2^e rounded to eleven bits, lo the rest rounded to
+// eleven bits, so that together they are off by 2^-24 |x| at most, as an fp32 number is.
+// A product is hi hi + hi lo + lo hi in the fp16 matrix instructions, each
+// term exact and summed in fp32; lo lo, 2^-24 of the product at most, is left out.
+// That is three matrix instructions for a product of fp32's precision, at a
+// sixteenth of the cost of fp32's own each.  (One fp16 or bf16 term alone would leave the directions
+// with small singular values, which the iteration raises 480-fold, to rounding:
+// errors of 2 to 40 in a hundred of the result.)
+// fp16's exponents suffice because all factors are bounded: the singular values
+// s of X are at most 1.21 from the first product on (the largest of a s + b s^3 + c s^5
+// over [0, 1.27] is 1.2016), so elements of X and A = X X^T stay below 1.21 and 1.46,
+// those of b A + c A^2 within 2.81.  e is chosen for these (kX, kA, kB); what lies
+// below 2^-24 of the stored number's unit, 2^-38 of the largest, is lost.
+//
+// A row of a factor is a row of 128-byte lines, each the 32 high and then the 32
+// low parts of 32 elements; rows are an odd number of lines apart, which spreads
+// them over the L2.  Rows and columns are padded with zeros to multiples of 128.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <numeric>
+#include <string>
+#include <utility>
+#include <vector>
+
+#include "../../include/mtdao_ops.h"
+#include "host.hpp"
+#include "ops_device.hpp"
+#include "tiles.hpp"
+
+using namespace mtdao;
+using namespace mtdao::ops;
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kChunk = 4096;   // elements of a workgroup that sums squares
+constexpr int kLine = 32;      // elements of a row in one line
+constexpr int kPad = 128;      // rows and columns of a factor are multiples of this
+constexpr int kMostParts = 12, kMostGemms = 2 * kMostParts;
+
+// X <- a X + (b A + c A^2) X with A = X X^T.
+constexpr double kCa = 3.4445, kCb = -4.7750, kCc = 2.0315;
+// Exponents of the stored factors: X, A and b A + c A^2.
+constexpr int kX = 14, kA = 14, kB = 13;
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// A matrix's row of the device table.
+struct Row {
+  void* p;
+  const void* g;
+  float* m;
+  float decay, factor;
+};
+
+// Matrices of one shape: what the passes over elements need.
+struct Part {
+  uint8_t *natural, *turned;    // X and X^T of the first one: rows as the matrix's, and as its columns
+  int64_t step;                 // bytes from one matrix's factors to the next one's
+  int64_t rows, cols;           // of the matrix
+  int32_t ld_natural, ld_turned;  // bytes
+  int32_t matrix, count;        // the first one's place in the table, how many
+  int32_t first_chunk, chunks;  // chunks of elements before these matrices, of each
+  int32_t first_tile, tiles_r, tiles_c;
+};
+struct Parts {
+  Part part[kMostParts];
+  int32_t n, items;
+};
+
+// Where the updates come from: rows of the table (Muon) or matrices one after another.
+struct Source {
+  const Row* rows;
+  const void* x;
+  double* sums;    // of every chunk
+  double* scale;   // of every matrix of this launch
+  float momentum;
+  int32_t nesterov;
+  double eps;
+};
+
+__device__ __forceinline__ int64_t item_of_launch() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
+// The update of N elements from the new momentum and the gradient.
+template <int N>
+__device__ __forceinline__ void update_of(const Source& s, const float (&g)[N], const float (&m)[N], float (&u)[N]) {
+#pragma unroll
+  for (int t = 0; t < N; ++t) u[t] = s.nesterov ? fmaf(s.momentum, m[t], g[t]) : m[t];
+}
+
+// Momentum (Muon) and the sum of the squares of a chunk of the update, in fp64.
+template <typename GT, bool MUON>
+__global__ __launch_bounds__(kThreads) void k_muon_sums(Parts parts, Source s) {
+  __shared__ double part[kThreads / 64];
+  const int64_t item = item_of_launch();
+  if (item >= parts.items) return;
+  int k = 0;
+  while (k + 1 < parts.n && item >= parts.part[k + 1].first_chunk) ++k;
+  const Part& a = parts.part[k];
+  const int in = (int)(item - a.first_chunk), which = in / a.chunks;
+  const int64_t base = (int64_t)(in - which * a.chunks) * kChunk, numel = a.rows * a.cols;
+  const GT* g;
+  float* m = nullptr;
+  if (MUON) {
+    g = reinterpret_cast<const GT*>(uniform_load(&s.rows[a.matrix + which].g));
+    m = uniform_load(&s.rows[a.matrix + which].m);
+  } else {
+    g = reinterpret_cast<const GT*>(s.x) + (int64_t)(a.matrix + which) * numel;
+  }
+  constexpr int V = 8, kSlots = kChunk / (kThreads * V);
+  double sum = 0.0;
+  float ga[kSlots][V], ma[kSlots][V];
+  int n[kSlots];
+#pragma unroll
+  for (int t = 0; t < kSlots; ++t) {
+    const int64_t e = base + (t * kThreads + (int)threadIdx.x) * V, left = numel - e;
+    n[t] = left > V ? V : (int)(left < 0 ? 0 : left);
+    load_some<V>(g + e, n[t], ga[t]);
+    if (MUON) load_some<V>(m + e, n[t], ma[t]);
+  }
+#pragma unroll
+  for (int t = 0; t < kSlots; ++t) {
+    float u[V];
+    if (MUON) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) ma[t][i] = fmaf(s.momentum, ma[t][i], ga[t][i]);
+      if (n[t] > 0) store_some<V>(m + base + (t * kThreads + (int)threadIdx.x) * V, n[t], ma[t]);
+      update_of(s, ga[t], ma[t], u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) u[i] = ga[t][i];
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum += (double)u[i] * (double)u[i];
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) s.sums[item] = (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+// A workgroup's sum of a matrix's squares, in an order that the sizes fix, and
+// what its elements are divided by.
+__global__ __launch_bounds__(kThreads) void k_muon_scales(Parts parts, Source s) {
+  __shared__ double part[kThreads / 64];
+  int k = 0, before = 0;
+  while (k + 1 < parts.n && (int)blockIdx.x >= before + parts.part[k].count) before += parts.part[k++].count;
+  const Part& a = parts.part[k];
+  const double* from = s.sums + a.first_chunk + (int64_t)((int)blockIdx.x - before) * a.chunks;
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < a.chunks; i += kThreads) sum += from[i];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) s.scale[blockIdx.x] = (double)(1 << kX) / (sqrt((part[0] + part[1]) + (part[2] + part[3])) + s.eps);
+}
+
+// v as hi (low half of the word) and lo.
+__device__ __forceinline__ uint32_t split_of(float v) {
+  const _Float16 hi = (_Float16)v;
+  const _Float16 lo = (_Float16)(v - (float)hi);
+  return (uint32_t)__builtin_bit_cast(uint16_t, hi) | (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
+}
+// Sixteen elements of a line from its element 0 or 16 on.
+__device__ __forceinline__ void store_split(uint8_t* line, int half, const uint32_t (&w)[16]) {
+  u32x4 hi[2], lo[2];
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    hi[t / 4][t % 4] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x05040100u);
+    lo[t / 4][t % 4] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x07060302u);
+  }
+  u32x4* at = reinterpret_cast<u32x4*>(line + half * 32);
+  at[0] = hi[0];
+  at[1] = hi[1];
+  at[4] = lo[0];
+  at[5] = lo[1];
+}
+__device__ __forceinline__ void load_split(const uint8_t* line, int half, float (&v)[16]) {
+  const v8h* at = reinterpret_cast<const v8h*>(line + half * 32);
+  const v8h hi[2] = {at[0], at[1]}, lo[2] = {at[4], at[5]};
+#pragma unroll
+  for (int t = 0; t < 16; ++t) v[t] = (float)hi[t / 8][t % 8] + (float)lo[t / 8][t % 8];
+}
+
+// X and its transpose from the update: a tile of 64 x 64, whose transpose goes
+// through LDS.  A thread has sixteen elements of a row, then of a column.
+constexpr int kSplit = 64;
+template <typename GT, bool MUON>
+__global__ __launch_bounds__(kThreads) void k_muon_split(Parts parts, Source s) {
+  __shared__ uint32_t tile[kSplit][kSplit + 1];
+  const int64_t item = item_of_launch();
+  if (item >= parts.items) return;
+  int k = 0, before = 0;
+  while (k + 1 < parts.n && item >= parts.part[k + 1].first_tile) before += parts.part[k++].count;
+  const Part& a = parts.part[k];
+  const int in = (int)(item - a.first_tile), tiles = a.tiles_r * a.tiles_c, which = in / tiles, at = in - which * tiles;
+  const int64_t row0 = (int64_t)(at / a.tiles_c) * kSplit, col0 = (int64_t)(at % a.tiles_c) * kSplit;
+  const int line = threadIdx.x / 4, part = threadIdx.x % 4;
+  const double scale = uniform_load(s.scale + before + which);
+  const int64_t row = row0 + line, col = col0 + part * 16, left = row < a.rows ? a.cols - col : 0;
+  const int n = left < 0 ? 0 : left > 16 ? 16 : (int)left;
+  uint32_t w[16];
+  const GT* g;
+  const float* m = nullptr;
+  if (MUON) {
+    g = reinterpret_cast<const GT*>(uniform_load(&s.rows[a.matrix + which].g));
+    m = uniform_load(&s.rows[a.matrix + which].m);
+  } else {
+    g = reinterpret_cast<const GT*>(s.x) + (int64_t)(a.matrix + which) * a.rows * a.cols;
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float ga[8], ma[8], u[8];
+    const int64_t e = row * a.cols + col + h * 8;
+    load_some<8>(g + e, n - h * 8, ga);
+    if (MUON) {
+      load_some<8>(m + e, n - h * 8, ma);
+      update_of(s, ga, ma, u);
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) w[h * 8 + t] = h * 8 + t < n ? split_of((float)((double)(MUON ? u[t] : ga[t]) * scale)) : 0u;
+  }
+  const int64_t own = (int64_t)which * a.step;
+  store_split(a.natural + own + row * a.ld_natural + col / kLine * 128, part % 2, w);
+#pragma unroll
+  for (int t = 0; t < 16; ++t) tile[line][part * 16 + t] = w[t];
+  __syncthreads();
+#pragma unroll
+  for (int t = 0; t < 16; ++t) w[t] = tile[part * 16 + t][line];
+  store_split(a.turned + own + (col0 + line) * a.ld_turned + (row0 + part * 16) / kLine * 128, part % 2, w);
+}
+
+// ------------------------------------------------------------------ products
+
+// c = k0 a b^T + k1 d1 + k2 d2 of `count` matrices: as a factor (out, and its transpose in
+// turned), or as the result of the last product.
+struct Gemm {
+  const uint8_t *a, *b, *d1, *d2;
+  uint8_t *out, *turned;
+  int64_t step;               // bytes from one matrix's factors to the next one's
+  int64_t rows, cols;         // of the result, without padding (last product)
+  int32_t rows_a, rows_b, blocks;  // padded rows, lines of the contraction
+  int32_t lda, ldb, ldo, ldt;      // bytes; d1 and d2 have out's rows
+  int32_t symmetric;          // tiles on and above the diagonal only, out is turned
+  int32_t tiles_a, tiles_b, tiles;
+  int32_t first, count;       // tiles before these matrices, matrices
+  int32_t matrix;             // the first one's place in the table
+  int32_t last;
+  float k0, k1, k2;
+};
+struct Gemms {
+  Gemm gemm[kMostGemms];
+  int32_t n, items;
+};
+struct Last {
+  const Row* rows;   // Muon's table
+  void* out;         // or matrices one after another
+  float lr;
+};
+
+// Tile (i, j) of the tiles on and above the diagonal of n x n, row by row.
+__device__ __forceinline__ void triangle_place(int t, int n, int& i, int& j) {
+  i = 0;
+  while (t >= n - i) t -= n - i++;
+  j = i + t;
+}
+
+// Sixteen consecutive elements of a row of the last result.
+template <typename PT>
+__device__ __forceinline__ void store_last(const Gemm& q, const Last& last, int which, int64_t row, int64_t col, const float (&v)[16]) {
+  if (row >= q.rows || col >= q.cols) return;
+  const int n = q.cols - col > 16 ? 16 : (int)(q.cols - col);
+  const int64_t e = row * q.cols + col;
+  if (last.rows) {
+    const Row& r = last.rows[q.matrix + which];
+    PT* p = reinterpret_cast<PT*>(r.p) + e;
+    const float keep = 1.0f - last.lr * r.decay, step = -last.lr * r.factor;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float o[8];
+      load_some<8>(p + h * 8, n - h * 8, o);
+#pragma unroll
+      for (int t = 0; t < 8; ++t) o[t] = fmaf(step, v[h * 8 + t], o[t] * keep);
+      if (n > h * 8) store_some<8>(p + h * 8, n - h * 8, o);
+    }
+  } else {
+    PT* p = reinterpret_cast<PT*>(last.out) + (int64_t)(q.matrix + which) * q.rows * q.cols + e;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float o[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) o[t] = v[h * 8 + t];
+      if (n > h * 8) store_some<8>(p + h * 8, n - h * 8, o);
+    }
+  }
+}
+
+// The products of a launch in tiles of B x B over WR x WC waves, a tile a workgroup.
+// Rows of b go in as the instruction's rows, so that a lane ends with sixteen
+// consecutive columns of a row of c.
+template <int B, int WR, int WC, typename PT>
+__global__ __launch_bounds__(64 * WR * WC) void k_muon_product(Gemms all, Last last) {
+  constexpr int kWaves = WR * WC, kGroup = 64 * kWaves, kMI = B / WR / 32, kNI = B / WC / 32;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * B * 128 > kWaves * 32 * 33 * 4 ? 2 * B * 128 : kWaves * 32 * 33 * 4];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const int per = (all.items + 7) / 8, item = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
+  if (item >= all.items || (int)(blockIdx.x / 8) >= per) return;
+  int k = 0;
+  while (k + 1 < all.n && item >= all.gemm[k + 1].first) ++k;
+  const Gemm& q = all.gemm[k];
+  const int in = item - q.first, which = in / q.tiles, tile = in - which * q.tiles;
+  int ti, tj;
+  if (q.symmetric) {
+    triangle_place(tile, q.tiles_a, ti, tj);
+  } else {
+    ti = tile % q.tiles_a;
+    tj = tile / q.tiles_a;
+  }
+  const int row0 = ti * B, col0 = tj * B;
+  const int64_t own = (int64_t)which * q.step;
+  const uint8_t *a = q.a + own, *b = q.b + own;
+  const int wm = wave / WC * (32 * kMI), wn = wave % WC * (32 * kNI), fr = lane % 32, fg = lane / 32;
+  v16f acc[kMI][kNI];
+#pragma unroll
+  for (int i = 0; i < kMI; ++i)
+#pragma unroll
+    for (int j = 0; j < kNI; ++j)
+#pragma unroll
+      for (int t = 0; t < 16; ++t) acc[i][j][t] = 0.0f;
+  constexpr int kLoads = 2 * B * 8 / kGroup;
+  for (int block = 0; block < q.blocks; ++block) {
+    u32x4 got[kLoads];
+#pragma unroll
+    for (int t = 0; t < kLoads; ++t) {
+      const int c = t * kGroup + (int)threadIdx.x, r = c / 8 % B;
+      const bool of_b = c / 8 >= B;
+      const int most = (of_b ? q.rows_b : q.rows_a) - 1, at = (of_b ? col0 : row0) + r;
+      const uint8_t* from = (of_b ? b : a) + (int64_t)(at < most ? at : most) * (of_b ? q.ldb : q.lda) + (int64_t)block * 128;
+      got[t] = *reinterpret_cast<const u32x4*>(from + c % 8 * 16);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kLoads; ++t) {
+      const int c = t * kGroup + (int)threadIdx.x, r = c / 8;
+      *reinterpret_cast<u32x4*>(lds + r * 128 + (c % 8 ^ row_key(r)) * 16) = got[t];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      v8h ha[kMI], la[kMI], hb[kNI], lb[kNI];
+#pragma unroll
+      for (int i = 0; i < kMI; ++i) {
+        const int r = wm + i * 32 + fr;
+        ha[i] = *reinterpret_cast<const v8h*>(lds + r * 128 + ((2 * s + fg) ^ row_key(r)) * 16);
+        la[i] = *reinterpret_cast<const v8h*>(lds + r * 128 + ((4 + 2 * s + fg) ^ row_key(r)) * 16);
+      }
+#pragma unroll
+      for (int j = 0; j < kNI; ++j) {
+        const int r = B + wn + j * 32 + row_of_b(fr);
+        hb[j] = *reinterpret_cast<const v8h*>(lds + r * 128 + ((2 * s + fg) ^ row_key(r)) * 16);
+        lb[j] = *reinterpret_cast<const v8h*>(lds + r * 128 + ((4 + 2 * s + fg) ^ row_key(r)) * 16);
+      }
+#pragma unroll
+      for (int i = 0; i < kMI; ++i)
+#pragma unroll
+        for (int j = 0; j < kNI; ++j) {
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hb[j], ha[i], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lb[j], ha[i], acc[i][j], 0, 0, 0);
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hb[j], la[i], acc[i][j], 0, 0, 0);
+        }
+    }
+  }
+  __syncthreads();
+  uint32_t* words = reinterpret_cast<uint32_t*>(lds) + wave * (32 * 33);
+  uint8_t* turned = q.symmetric ? (ti == tj ? nullptr : q.out) : q.turned;
+  const int ldt = q.symmetric ? q.ldo : q.ldt;
+#pragma unroll
+  for (int i = 0; i < kMI; ++i)
+#pragma unroll
+    for (int j = 0; j < kNI; ++j) {
+      const int r0 = row0 + wm + i * 32, c0 = col0 + wn + j * 32;
+      if (r0 >= q.rows_a || c0 >= q.rows_b) continue;
+      const int64_t line = own + (int64_t)(r0 + fr) * q.ldo + c0 / kLine * 128;
+      float v[16], d[16];
+#pragma unroll
+      for (int t = 0; t < 16; ++t) v[t] = q.k0 * acc[i][j][t];
+      if (q.d1) {
+        load_split(q.d1 + line, fg, d);
+#pragma unroll
+        for (int t = 0; t < 16; ++t) v[t] = fmaf(q.k1, d[t], v[t]);
+      }
+      if (q.d2) {
+        load_split(q.d2 + line, fg, d);
+#pragma unroll
+        for (int t = 0; t < 16; ++t) v[t] = fmaf(q.k2, d[t], v[t]);
+      }
+      if (q.last) {
+        store_last<PT>(q, last, which, r0 + fr, c0 + fg * 16, v);
+        continue;
+      }
+      uint32_t w[16];
+#pragma unroll
+      for (int t = 0; t < 16; ++t) w[t] = split_of(v[t]);
+      store_split(q.out + line, fg, w);
+      if (turned) {
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int t = 0; t < 16; ++t) words[fr * 33 + fg * 16 + t] = w[t];
+        __builtin_amdgcn_wave_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int t = 0; t < 16; ++t) w[t] = words[(fg * 16 + t) * 33 + fr];
+        asm volatile("" ::: "memory");
+        store_split(turned + own + (int64_t)(c0 + fr) * ldt + r0 / kLine * 128, fg, w);
+      }
+    }
+}
+
+// Writes rows `at`.. of the table.
+constexpr int kRowsAtOnce = 64;
+struct Rows {
+  Row row[kRowsAtOnce];
+};
+__global__ __launch_bounds__(kRowsAtOnce) void k_muon_table(Rows in, int at, int n, Row* rows) {
+  if ((int)threadIdx.x < n) rows[at + threadIdx.x] = in.row[threadIdx.x];
+}
+
+// --------------------------------------------------------------------- host
+
+int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
+
+// A matrix's factors: X [m][n] and X^T [n][m] with m <= n, X^T's next value,
+// and the products of X with itself.
+struct Shape {
+  int64_t rows, cols;
+  int64_t m, n, ldm, ldn;  // padded; bytes of rows of m and n elements
+  int64_t x, xt[2], square[2], bytes;
+  bool tall;
+};
+Shape shape_of(int64_t rows, int64_t cols) {
+  Shape s = {};
+  s.rows = rows;
+  s.cols = cols;
+  s.tall = rows > cols;
+  s.m = up(std::min(rows, cols), kPad);
+  s.n = up(std::max(rows, cols), kPad);
+  s.ldm = (s.m / kLine | 1) * 128;
+  s.ldn = (s.n / kLine | 1) * 128;
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t here = at;
+    at += up(bytes, 256);
+    return here;
+  };
+  s.x = take(s.m * s.ldn);
+  for (int64_t& t : s.xt) t = take(s.n * s.ldm);
+  for (int64_t& t : s.square) t = take(s.m * s.ldm);
+  s.bytes = at;
+  return s;
+}
+
+// Matrices that go through the products together: runs of one shape in the
+// table's order.
+struct Run {
+  Shape shape;
+  int32_t matrix, count;
+  int64_t at;  // of the first one's factors in the group's memory
+};
+struct Group {
+  std::vector<Run> runs;
+  int64_t bytes = 0, chunks = 0;
+  int32_t matrices = 0;
+};
+// Memory that a group's factors may take, unless a single matrix needs more.
+constexpr int64_t kGroupBytes = INT64_C(4) << 30;
+
+int64_t chunks_of(const Shape& s) { return (s.rows * s.cols + kChunk - 1) / kChunk; }
+
+// shapes: in the table's order, equal ones together, none empty.
+std::vector<Group> groups_of(const std::vector<std::pair<int64_t, int64_t>>& shapes) {
+  std::vector<Group> groups;
+  for (size_t i = 0; i < shapes.size(); ++i) {
+    const Shape s = shape_of(shapes[i].first, shapes[i].second);
+    const bool same = i > 0 && shapes[i] == shapes[i - 1];
+    if (groups.empty() || groups.back().bytes + s.bytes > kGroupBytes || (!same && groups.back().runs.size() == kMostParts) ||
+        groups.back().chunks + chunks_of(s) > (1 << 30))
+      groups.emplace_back();
+    Group& g = groups.back();
+    if (!same || g.runs.empty()) g.runs.push_back({s, (int32_t)i, 0, g.bytes});
+    g.runs.back().count++;
+    g.bytes += s.bytes;
+    g.chunks += chunks_of(s);
+    g.matrices++;
+  }
+  return groups;
+}
+
+struct Layout {
+  size_t scales, sums, factors, bytes;
+};
+Layout layout_of(const std::vector<Group>& groups, size_t table_rows) {
+  int64_t bytes = 0, chunks = 0, matrices = 0;
+  for (const Group& g : groups) {
+    bytes = std::max(bytes, g.bytes);
+    chunks = std::max(chunks, g.chunks);
+    matrices = std::max<int64_t>(matrices, g.matrices);
+  }
+  Layout l;
+  l.scales = up256(table_rows * sizeof(Row));
+  l.sums = l.scales + up256((size_t)matrices * sizeof(double));
+  l.factors = l.sums + up256((size_t)chunks * sizeof(double));
+  l.bytes = l.factors + (size_t)bytes;
+  return l;
+}
+
+// The products of a run, one entry per launch.
+std::vector<Gemm> products_of(const Run& run, uint8_t* base, int steps) {
+  const Shape& s = run.shape;
+  uint8_t* at = base + run.at;
+  uint8_t *x = at + s.x, *xt[2] = {at + s.xt[0], at + s.xt[1]}, *sq[2] = {at + s.square[0], at + s.square[1]};
+  Gemm zero;
+  std::memset(&zero, 0, sizeof zero);
+  zero.step = s.bytes;
+  zero.count = run.count;
+  zero.matrix = run.matrix;
+  std::vector<Gemm> list;
+  auto pow2 = [](int e) { return std::ldexp(1.0, e); };
+  auto square = [&](const uint8_t* a, const uint8_t* b, int64_t ld, int64_t cols, uint8_t* out) {
+    Gemm g = zero;
+    g.a = a;
+    g.b = b;
+    g.out = out;
+    g.rows_a = g.rows_b = (int32_t)s.m;
+    g.blocks = (int32_t)(cols / kLine);
+    g.lda = g.ldb = (int32_t)ld;
+    g.ldo = (int32_t)s.ldm;
+    g.symmetric = 1;
+    return g;
+  };
+  for (int i = 0; i < steps; ++i) {
+    Gemm gram = square(x, x, s.ldn, s.n, sq[0]);
+    gram.k0 = (float)pow2(kA - 2 * kX);
+    list.push_back(gram);
+    Gemm poly = square(sq[0], sq[0], s.ldm, s.m, sq[1]);  // b A + c A A
+    poly.d1 = sq[0];
+    poly.k0 = (float)(kCc * pow2(kB - 2 * kA));
+    poly.k1 = (float)(kCb * pow2(kB - kA));
+    list.push_back(poly);
+    const bool last = i + 1 == steps, flip = last && s.tall;
+    Gemm apply = zero;  // X <- a X + (b A + c A A) X
+    apply.a = flip ? xt[i & 1] : sq[1];
+    apply.b = flip ? sq[1] : xt[i & 1];
+    apply.d1 = flip ? xt[i & 1] : x;
+    apply.lda = apply.ldb = (int32_t)s.ldm;
+    apply.ldo = (int32_t)(flip ? s.ldm : s.ldn);
+    apply.rows_a = (int32_t)(flip ? s.n : s.m);
+    apply.rows_b = (int32_t)(flip ? s.m : s.n);
+    apply.blocks = (int32_t)(s.m / kLine);
+    const int e = last ? 0 : kX;
+    apply.k0 = (float)pow2(e - kB - kX);
+    apply.k1 = (float)(kCa * pow2(e - kX));
+    if (last) {
+      apply.last = 1;
+      apply.rows = s.rows;
+      apply.cols = s.cols;
+    } else {
+      apply.out = x;
+      apply.turned = xt[(i & 1) ^ 1];
+      apply.ldt = (int32_t)s.ldm;
+    }
+    list.push_back(apply);
+  }
+  return list;
+}
+
+constexpr int kTile = 128;
+
+template <typename PT>
+void launch_products(Gemms& all, const Last& last, hipStream_t st) {
+  int64_t items = 0;
+  for (int i = 0; i < all.n; ++i) {
+    Gemm& g = all.gemm[i];
+    g.tiles_a = (g.rows_a + kTile - 1) / kTile;
+    g.tiles_b = (g.rows_b + kTile - 1) / kTile;
+    g.tiles = g.symmetric ? g.tiles_a * (g.tiles_a + 1) / 2 : g.tiles_a * g.tiles_b;
+    g.first = (int32_t)items;
+    items += (int64_t)g.tiles * g.count;
+  }
+  all.items = (int32_t)items;
+  hipLaunchKernelGGL((k_muon_product<kTile, 2, 2, PT>), dim3((unsigned)((items + 7) / 8 * 8)), dim3(256), 0, st, all, last);
+}
+
+// All the work of a group's matrices.
+template <typename GT, typename PT, bool MUON>
+void launch_group(const Group& group, Source s, const Last& last, uint8_t* factors, int steps, hipStream_t st) {
+  Parts parts;
+  std::memset(&parts, 0, sizeof parts);
+  int64_t chunks = 0, tiles = 0;
+  for (const Run& r : group.runs) {
+    const Shape& h = r.shape;
+    Part& a = parts.part[parts.n++];
+    a.natural = factors + r.at + (h.tall ? h.xt[0] : h.x);
+    a.turned = factors + r.at + (h.tall ? h.x : h.xt[0]);
+    a.ld_natural = (int32_t)(h.tall ? h.ldm : h.ldn);
+    a.ld_turned = (int32_t)(h.tall ? h.ldn : h.ldm);
+    a.step = h.bytes;
+    a.rows = h.rows;
+    a.cols = h.cols;
+    a.matrix = r.matrix;
+    a.count = r.count;
+    a.first_chunk = (int32_t)chunks;
+    a.chunks = (int32_t)chunks_of(h);
+    chunks += (int64_t)a.chunks * r.count;
+    a.first_tile = (int32_t)tiles;
+    a.tiles_r = (int32_t)((h.tall ? h.n : h.m) / kSplit);
+    a.tiles_c = (int32_t)((h.tall ? h.m : h.n) / kSplit);
+    tiles += (int64_t)a.tiles_r * a.tiles_c * r.count;
+  }
+  parts.items = (int32_t)chunks;
+  hipLaunchKernelGGL((k_muon_sums<GT, MUON>), grid_of(chunks), dim3(kThreads), 0, st, parts, s);
+  hipLaunchKernelGGL(k_muon_scales, dim3((unsigned)group.matrices), dim3(kThreads), 0, st, parts, s);
+  parts.items = (int32_t)tiles;
+  hipLaunchKernelGGL((k_muon_split<GT, MUON>), grid_of(tiles), dim3(kThreads), 0, st, parts, s);
+  std::vector<std::vector<Gemm>> lists;
+  size_t most = 0;
+  for (const Run& r : group.runs) {
+    lists.push_back(products_of(r, factors, steps));
+    most = std::max(most, lists.back().size());
+  }
+  for (size_t i = 0; i < most; ++i) {
+    Gemms all;
+    std::memset(&all, 0, sizeof all);
+    for (const auto& list : lists)
+      if (i < list.size()) all.gemm[all.n++] = list[i];
+    launch_products<PT>(all, last, st);
+  }
+}
+
+int32_t check_numbers(int32_t steps, double eps, std::string* e) {
+  if (steps < 1 || steps > MTDAO_MUON_MAX_STEPS) return fail(e, MTDAO_ERR_INVALID_ARG, "steps %d: 1..%d", steps, MTDAO_MUON_MAX_STEPS);
+  if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(e, MTDAO_ERR_INVALID_ARG, "eps=%g must be finite and >= 0", eps);
+  return MTDAO_OK;
+}
+int32_t check_sides(int64_t rows, int64_t cols, int i, std::string* e) {
+  if (rows < 0 || cols < 0) return fail(e, MTDAO_ERR_INVALID_ARG, "rows or cols of matrix %d < 0", i);
+  if (std::min(rows, cols) > MTDAO_MUON_MAX_SIDE || std::max(rows, cols) > (INT64_C(1) << 20))
+    return fail(e, MTDAO_ERR_INVALID_ARG, "matrix %d is %lld x %lld: its smaller side is at most %d, its larger one 2^20", i, (long long)rows, (long long)cols,
+                MTDAO_MUON_MAX_SIDE);
+  return MTDAO_OK;
+}
+int32_t check_type(int32_t dtype, const char* name, std::string* e) {
+  if (dtype != MTDAO_F32 && dtype != MTDAO_BF16) return fail(e, MTDAO_ERR_INVALID_ARG, "%s must be F32(0) or BF16(1)", name);
+  return MTDAO_OK;
+}
+int32_t check_workspace(const void* workspace, size_t given, size_t need, std::string* e) {
+  if (!workspace || given < need)
+    return fail(e, MTDAO_ERR_WORKSPACE, "workspace of %zu bytes required, %zu given", need, workspace ? given : (size_t)0);
+  if (!aligned_to(workspace, 256)) return fail(e, MTDAO_ERR_ALIGN, "workspace is not 256-byte aligned");
+  return MTDAO_OK;
+}
+
+int32_t validate(const mtdao_muon_config* c, const mtdao_muon_matrix* t, std::string* e) {
+  if (!c || !t) return fail(e, MTDAO_ERR_INVALID_ARG, "config or matrices is NULL");
+  int32_t r = check_type(c->param_dtype, "param_dtype", e);
+  if (r == MTDAO_OK) r = check_type(c->grad_dtype, "grad_dtype", e);
+  if (r == MTDAO_OK) r = check_numbers(c->steps, c->eps, e);
+  if (r != MTDAO_OK) return r;
+  if (c->n_matrices < 1 || c->n_matrices > (1 << 20)) return fail(e, MTDAO_ERR_INVALID_ARG, "n_matrices %d: 1..2^20", c->n_matrices);
+  if (!(c->momentum >= 0.0 && c->momentum < 1.0)) return fail(e, MTDAO_ERR_INVALID_ARG, "momentum=%g: in [0,1)", c->momentum);
+  for (int i = 0; i < c->n_matrices; ++i) {
+    r = check_sides(t[i].rows, t[i].cols, i, e);
+    if (r != MTDAO_OK) return r;
+    if (!(t[i].weight_decay >= 0.0) || !std::isfinite((float)t[i].weight_decay))
+      return fail(e, MTDAO_ERR_INVALID_ARG, "weight_decay of matrix %d must be finite and >= 0", i);
+    if (!std::isfinite((float)t[i].factor)) return fail(e, MTDAO_ERR_INVALID_ARG, "factor of matrix %d is not finite", i);
+  }
+  return MTDAO_OK;
+}
+
+struct Written {
+  uintptr_t lo, hi;
+};
+
+// Gradients are read after the momenta are written.
+int32_t check_grad(const mtdao_muon_config& c, int i, int64_t numel, const void* g, const std::vector<Written>& written, std::string* e) {
+  if (numel == 0) return MTDAO_OK;
+  if (!g) return fail(e, MTDAO_ERR_INVALID_ARG, "g of matrix %d is NULL", i);
+  if (!aligned_to(g, (uintptr_t)esize(c.grad_dtype))) return fail(e, MTDAO_ERR_ALIGN, "g of matrix %d is not aligned to its element", i);
+  const uintptr_t lo = (uintptr_t)g, hi = lo + (uintptr_t)(numel * esize(c.grad_dtype));
+  auto w = std::upper_bound(written.begin(), written.end(), lo, [](uintptr_t at, const Written& r) { return at < r.hi; });
+  if (w != written.end() && w->lo < hi) return fail(e, MTDAO_ERR_INVALID_ARG, "g of matrix %d overlaps parameters or momenta", i);
+  return MTDAO_OK;
+}
+
+int32_t check_pointers(const mtdao_muon_config& c, const mtdao_muon_matrix* t, std::vector<Written>& written, std::string* e) {
+  for (int i = 0; i < c.n_matrices; ++i) {
+    const int64_t numel = t[i].rows * t[i].cols;
+    if (numel == 0) continue;
+    if (!t[i].p || !t[i].m) return fail(e, MTDAO_ERR_INVALID_ARG, "p or m of matrix %d is NULL", i);
+    if (!aligned_to(t[i].p, (uintptr_t)esize(c.param_dtype)) || !aligned_to(t[i].m, 4))
+      return fail(e, MTDAO_ERR_ALIGN, "p or m of matrix %d is not aligned to its element", i);
+    written.push_back({(uintptr_t)t[i].p, (uintptr_t)t[i].p + (uintptr_t)(numel * esize(c.param_dtype))});
+    written.push_back({(uintptr_t)t[i].m, (uintptr_t)t[i].m + (uintptr_t)(numel * 4)});
+  }
+  std::sort(written.begin(), written.end(), [](const Written& x, const Written& y) { return x.lo < y.lo; });
+  for (size_t k = 1; k < written.size(); ++k)
+    if (written[k].lo < written[k - 1].hi) return fail(e, MTDAO_ERR_INVALID_ARG, "parameters or momenta of the matrices overlap");
+  for (int i = 0; i < c.n_matrices; ++i) {
+    const int32_t r = check_grad(c, i, t[i].rows * t[i].cols, t[i].g, written, e);
+    if (r != MTDAO_OK) return r;
+  }
+  return MTDAO_OK;
+}
+
+// Matrices in the table's order (shapes together, none empty): their numbers.
+std::vector<int> order_of(const mtdao_muon_config& c, const mtdao_muon_matrix* t) {
+  std::vector<int> order;
+  for (int i = 0; i < c.n_matrices; ++i)
+    if (t[i].rows > 0 && t[i].cols > 0) order.push_back(i);
+  std::stable_sort(order.begin(), order.end(), [&](int a, int b) {
+    return std::make_pair(t[a].rows * t[a].cols, t[a].rows) > std::make_pair(t[b].rows * t[b].cols, t[b].rows);
+  });
+  return order;
+}
+std::vector<Group> groups_of(const std::vector<int>& order, const mtdao_muon_matrix* t) {
+  std::vector<std::pair<int64_t, int64_t>> shapes;
+  for (int i : order) shapes.push_back({t[i].rows, t[i].cols});
+  return groups_of(shapes);
+}
+std::vector<Group> groups_of(int64_t batch, int64_t rows, int64_t cols) {
+  return groups_of(std::vector<std::pair<int64_t, int64_t>>((size_t)(rows > 0 && cols > 0 ? batch : 0), {rows, cols}));
+}
+
+int32_t check_batch(int64_t batch, int64_t rows, int64_t cols, std::string* e) {
+  if (batch < 0 || batch > (1 << 20)) return fail(e, MTDAO_ERR_INVALID_ARG, "batch %lld: 0..2^20", (long long)batch);
+  return check_sides(rows, cols, 0, e);
+}
+
+}  // namespace
+
+struct mtdao_muon {
+  mtdao_muon_config cfg;
+  std::vector<int64_t> numel;       // of every matrix
+  std::vector<int> order;
+  std::vector<Row> rows;            // the table
+  std::vector<Written> written;
+  std::vector<Group> groups;
+  Layout layout;
+  char* workspace = nullptr;
+  std::string err;
+};
+
+namespace {
+int32_t write_table(mtdao_muon* h, std::string* e, hipStream_t st) {
+  for (size_t at = 0; at < h->rows.size(); at += kRowsAtOnce) {
+    Rows in;
+    std::memset(&in, 0, sizeof in);
+    const int n = (int)std::min<size_t>(kRowsAtOnce, h->rows.size() - at);
+    std::copy_n(h->rows.begin() + at, n, in.row);
+    hipLaunchKernelGGL(k_muon_table, dim3(1), dim3(kRowsAtOnce), 0, st, in, (int)at, n, reinterpret_cast<Row*>(h->workspace));
+  }
+  return hip_check(e, hipGetLastError(), "mtdao_muon table launch");
+}
+}  // namespace
+
+extern "C" {
+
+int32_t mtdao_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t cols, size_t* bytes) try {
+  const int32_t r = check_batch(batch, rows, cols, &g_err);
+  if (r != MTDAO_OK) return r;
+  if (!bytes) return fail(&g_err, MTDAO_ERR_INVALID_ARG, "bytes is NULL");
+  const std::vector<Group> groups = groups_of(batch, rows, cols);
+  *bytes = groups.empty() ? 0 : layout_of(groups, 0).bytes;
+  return MTDAO_OK;
+} catch (const std::bad_alloc&) {
+  return fail(&g_err, MTDAO_ERR_WORKSPACE, "out of host memory");
+}
+
+int32_t mtdao_orthogonalize(const void* x, int32_t dtype, int64_t batch, int64_t rows, int64_t cols, void* out, int32_t out_dtype,
+                            int32_t steps, double eps, void* workspace, size_t workspace_bytes, void* hip_stream) try {
+  std::string* e = &g_err;
+  int32_t r = check_batch(batch, rows, cols, e);
+  if (r == MTDAO_OK) r = check_type(dtype, "dtype", e);
+  if (r == MTDAO_OK) r = check_type(out_dtype, "out_dtype", e);
+  if (r == MTDAO_OK) r = check_numbers(steps, eps, e);
+  if (r != MTDAO_OK) return r;
+  const std::vector<Group> groups = groups_of(batch, rows, cols);
+  if (groups.empty()) return MTDAO_OK;
+  if (!x || !out) return fail(e, MTDAO_ERR_INVALID_ARG, "x or out is NULL");
+  if (!aligned_to(x, (uintptr_t)esize(dtype)) || !aligned_to(out, (uintptr_t)esize(out_dtype)))
+    return fail(e, MTDAO_ERR_ALIGN, "x or out is not aligned to its element");
+  const int64_t numel = batch * rows * cols;
+  // (matrices go group by group, so a later one's x may not lie under an earlier one's result)
+  if (overlap(x, numel * esize(dtype), out, numel * esize(out_dtype)) && (x != out || dtype != out_dtype))
+    return fail(e, MTDAO_ERR_INVALID_ARG, "out overlaps x");
+  const Layout l = layout_of(groups, 0);
+  r = check_workspace(workspace, workspace_bytes, l.bytes, e);
+  if (r != MTDAO_OK) return r;
+  char* w = static_cast<char*>(workspace);
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  RoctxRange range("mtdao_orthogonalize %lld x %lld x %lld", (long long)batch, (long long)rows, (long long)cols);
+  Source s = {nullptr, x, reinterpret_cast<double*>(w + l.sums), reinterpret_cast<double*>(w + l.scales), 0.0f, 0, eps};
+  const Last last = {nullptr, out, 0.0f};
+  for (const Group& g : groups) {
+    uint8_t* factors = reinterpret_cast<uint8_t*>(w + l.factors);
+    if (dtype == MTDAO_F32 && out_dtype == MTDAO_F32) launch_group<float, float, false>(g, s, last, factors, steps, st);
+    else if (dtype == MTDAO_F32) launch_group<float, bf16_t, false>(g, s, last, factors, steps, st);
+    else if (out_dtype == MTDAO_F32) launch_group<bf16_t, float, false>(g, s, last, factors, steps, st);
+    else launch_group<bf16_t, bf16_t, false>(g, s, last, factors, steps, st);
+  }
+  return hip_check(e, hipGetLastError(), "mtdao_orthogonalize launch");
+} catch (const std::bad_alloc&) {
+  return fail(&g_err, MTDAO_ERR_WORKSPACE, "out of host memory");
+}
+
+int32_t mtdao_muon_workspace_bytes(const mtdao_muon_config* cfg, const mtdao_muon_matrix* matrices, size_t* bytes) try {
+  const int32_t r = validate(cfg, matrices, &g_err);
+  if (r != MTDAO_OK) return r;
+  if (!bytes) return fail(&g_err, MTDAO_ERR_INVALID_ARG, "bytes is NULL");
+  const std::vector<int> order = order_of(*cfg, matrices);
+  *bytes = layout_of(groups_of(order, matrices), order.size()).bytes;
+  return MTDAO_OK;
+} catch (const std::bad_alloc&) {
+  return fail(&g_err, MTDAO_ERR_WORKSPACE, "out of host memory");
+}
+
+int32_t mtdao_muon_init(const mtdao_muon_config* cfg, const mtdao_muon_matrix* matrices, void* workspace, size_t workspace_bytes,
+                        void* hip_stream, mtdao_muon** out) try {
+  int32_t r = validate(cfg, matrices, &g_err);
+  if (r != MTDAO_OK) return r;
+  if (!out) return fail(&g_err, MTDAO_ERR_INVALID_ARG, "out is NULL");
+  std::vector<Written> written;
+  r = check_pointers(*cfg, matrices, written, &g_err);
+  if (r != MTDAO_OK) return r;
+  struct Owned {
+    mtdao_muon* h = new mtdao_muon();
+    ~Owned() { delete h; }
+  } own;
+  mtdao_muon* h = own.h;
+  h->cfg = *cfg;
+  h->order = order_of(*cfg, matrices);
+  h->groups = groups_of(h->order, matrices);
+  h->layout = layout_of(h->groups, h->order.size());
+  if (h->layout.bytes > 0) {
+    r = check_workspace(workspace, workspace_bytes, h->layout.bytes, &g_err);
+    if (r != MTDAO_OK) return r;
+  }
+  h->workspace = static_cast<char*>(workspace);
+  h->written = std::move(written);
+  for (int i = 0; i < cfg->n_matrices; ++i) h->numel.push_back(matrices[i].rows * matrices[i].cols);
+  for (int i : h->order)
+    h->rows.push_back({matrices[i].p, matrices[i].g, matrices[i].m, (float)matrices[i].weight_decay, (float)matrices[i].factor});
+  RoctxRange range("mtdao_muon_init matrices=%d", cfg->n_matrices);
+  r = write_table(h, &g_err, reinterpret_cast<hipStream_t>(hip_stream));
+  if (r != MTDAO_OK) return r;
+  g_err.clear();
+  *out = h;
+  own.h = nullptr;
+  return MTDAO_OK;
+} catch (const std::bad_alloc&) {
+  return fail(&g_err, MTDAO_ERR_WORKSPACE, "out of host memory");
+}
+
+int32_t mtdao_muon_set_grads(mtdao_muon* h, const void* const* grads, void* hip_stream) {
+  if (!h) return fail(&g_err, MTDAO_ERR_INVALID_ARG, "handle is NULL");
+  if (!grads) return fail(&h->err, MTDAO_ERR_INVALID_ARG, "grads is NULL");
+  for (int i = 0; i < h->cfg.n_matrices; ++i) {
+    const int32_t r = check_grad(h->cfg, i, h->numel[i], grads[i], h->written, &h->err);
+    if (r != MTDAO_OK) return r;
+  }
+  RoctxRange range("mtdao_muon_set_grads matrices=%d", h->cfg.n_matrices);
+  for (size_t k = 0; k < h->order.size(); ++k) h->rows[k].g = grads[h->order[k]];
+  return write_table(h, &h->err, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+int32_t mtdao_muon_step(mtdao_muon* h, double lr, void* hip_stream) try {
+  if (!h) return fail(&g_err, MTDAO_ERR_INVALID_ARG, "handle is NULL");
+  if (!std::isfinite((float)lr)) return fail(&h->err, MTDAO_ERR_INVALID_ARG, "lr is not finite");
+  const mtdao_muon_config& c = h->cfg;
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  RoctxRange range("mtdao_muon_step matrices=%d", c.n_matrices);
+  char* w = h->workspace;
+  const Row* rows = reinterpret_cast<const Row*>(w);
+  const Source s = {rows, nullptr, reinterpret_cast<double*>(w + h->layout.sums), reinterpret_cast<double*>(w + h->layout.scales),
+                    (float)c.momentum, c.nesterov != 0, c.eps};
+  const Last last = {rows, nullptr, (float)lr};
+  uint8_t* factors = reinterpret_cast<uint8_t*>(w + h->layout.factors);
+  for (const Group& g : h->groups) {
+    if (c.param_dtype == MTDAO_F32 && c.grad_dtype == MTDAO_F32) launch_group<float, float, true>(g, s, last, factors, c.steps, st);
+    else if (c.param_dtype == MTDAO_F32) launch_group<bf16_t, float, true>(g, s, last, factors, c.steps, st);
+    else if (c.grad_dtype == MTDAO_F32) launch_group<float, bf16_t, true>(g, s, last, factors, c.steps, st);
+    else launch_group<bf16_t, bf16_t, true>(g, s, last, factors, c.steps, st);
+  }
+  return hip_check(&h->err, hipGetLastError(), "mtdao_muon_step launch");
+} catch (const std::bad_alloc&) {
+  return fail(h ? &h->err : &g_err, MTDAO_ERR_WORKSPACE, "out of host memory");
+}
+
+const char* mtdao_muon_last_error(const mtdao_muon* h) { return h ? h->err.c_str() : g_err.c_str(); }
+
+void mtdao_muon_destroy(mtdao_muon* h) { delete h; }
+
+}  // extern "C"

@@ -14,6 +14,7 @@
 #include "../../include/mtdao_ops.h"
 #include "host.hpp"
 #include "ops_device.hpp"
+#include "tiles.hpp"
 
 using namespace mtdao;
 using namespace mtdao::ops;
@@ -251,13 +252,6 @@ __global__ __launch_bounds__(kTileThreads) void k_quantize8_tile(Quantized one, 
 // instructions instead, at half their rate: codes times scales are bf16
 // values, and their products are summed in fp32.
 
-typedef int v8i __attribute__((ext_vector_type(8)));
-typedef int v4i __attribute__((ext_vector_type(4)));
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef float v16f __attribute__((ext_vector_type(16)));
-typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-
 struct Product {
   Mat a, b;
   void* c;
@@ -267,18 +261,6 @@ struct Product {
   int32_t splits, split_blocks;  // parts of the contraction, and their blocks
   float* partial;                // [splits][rows of a][rows of b] with more than one part
 };
-
-// A 128-byte row in LDS: each of its eight 16-byte chunks is at the place that its
-// number and the row's key give, by an exclusive or.  A 16-byte read of a wave takes 16 lanes at
-// once, which have to lie in different ones of the 16 such places of the 64
-// banks: two rows of eight, told apart by the row's last bit, so the key has
-// the next three.  (With the last three bits as the key half of the reads'
-// cycles were conflicts.)
-__device__ __forceinline__ int row_key(int row) { return (row >> 1) & 7; }
-
-// The row of b's fragment that the instruction's row r takes: results of a lane
-// are rows 8 q + 4 h + t, so these are sixteen consecutive columns of c.
-__device__ __forceinline__ int row_of_b(int r) { return ((r >> 2) & 1) * 16 + (r >> 3) * 4 + (r & 3); }
 
 // Eight codes times their scale, as bf16: exact down to bf16's smallest values.
 __device__ __forceinline__ v8bf widened(int w0, int w1, float scale) {
@@ -295,29 +277,6 @@ __device__ __forceinline__ v8bf widened(int w0, int w1, float scale) {
   }
   return o;
 }
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t* p, int64_t bytes) {
-  const int64_t most = INT64_C(0x7fffffff);
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, (int)(bytes < most ? bytes : most), 0x00027000);
-}
-
-// Every wave of the workgroup has come here; nothing is moved across.
-__device__ __forceinline__ void meet() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_sched_barrier(0);
-  asm volatile("" ::: "memory");
-}
-// This wave's loads (global memory to registers or LDS; LDS to registers)
-// have arrived, but for the last LEFT of them.
-template <int LEFT = 0>
-__device__ __forceinline__ void loads_landed() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x0f70 | (LEFT & 15) | (LEFT >> 4) << 14);  // vmcnt(LEFT)
-  asm volatile("" ::: "memory");
-}
-__device__ __forceinline__ void reads_landed() { __builtin_amdgcn_s_waitcnt(0xc07f); }  // lgkmcnt(0)
 
 // Tile t of c's tiles in the order in which they are worked on: groups of
 // p.group tile rows, down the rows first, so that tiles in work at one time

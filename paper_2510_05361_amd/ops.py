@@ -1,20 +1,21 @@
 """Operators of a Peri-LN training step next to the optimizer, on torch
 tensors: AdamW over many tensors, the boundary of a Peri-LN block, linear
-layers in 8-bit floating point.
+layers in 8-bit floating point, orthogonalised updates of matrices and their
+optimizer, the embedding of tokens, the cross entropy over a vocabulary.
 
 As in ``optimizer.py``, torch only allocates device memory and supplies the
 current HIP stream; the work runs in the library's kernels through
 ``mtdao_ops.py`` (include/mtdao_ops.h has the formulas).  Outputs and
 workspaces are allocated from torch's caching allocator on the current
 stream; inputs that belong to another stream are the caller's to order, as
-for any torch operation.  What ``AdamW``, ``Matrix8`` and ``Weight8`` allocate for
+for any torch operation.  What ``AdamW``, ``Muon``, ``Matrix8`` and ``Weight8`` allocate for
 themselves is kept from the allocator until the streams of their calls are done
 with it.  There is no CPU path.
 
-``peri_norm`` and ``linear8`` take part in autograd where an input (of
-``linear8``: x, or the tensor that its weight was made from) requires a gradient;
-their backward passes are the functions of the same names and not
-differentiable themselves.
+``peri_norm``, ``linear8``, ``embedding`` and ``cross_entropy`` take part in autograd
+where an input (of ``linear8``: x, or the tensor that its weight was made from)
+requires a gradient; their backward passes are the functions of the same names
+and not differentiable themselves.
 """
 
 from __future__ import annotations
@@ -60,10 +61,53 @@ def _on_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> torch.de
     return first.device
 
 
-# ------------------------------------------------------------------- AdamW
+# -------------------------------------------------------------- optimizers
 
 
-class AdamW:
+class _Stepper:
+    """What the optimizers share: a C handle over device memory that steps on
+    any stream read."""
+
+    handle: Optional[int] = None
+    workspace: torch.Tensor
+
+    def _stream_here(self) -> int:
+        """The current stream, of the tensors' device.  On another one than that of construction the
+        allocator learns of it: freed earlier, the table of addresses in the
+        workspace would be another tensor's while a step still reads it."""
+        if torch.cuda.current_device() != self.workspace.get_device():
+            raise ValueError(f"the tensors are on {self.workspace.device}, the current device is {torch.cuda.current_device()}")
+        stream = _stream(self.workspace)
+        if stream not in self._streams:
+            current = torch.cuda.current_stream(self.workspace.device)
+            for t in self._own:
+                t.record_stream(current)
+            self._streams.add(stream)
+        return stream
+
+    def _grads_ok(self, grads, dtype) -> None:
+        if len(grads) != len(self.params):
+            raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
+        _on_device(self.params[0], *grads)
+        for i, (p, g) in enumerate(zip(self.params, grads)):
+            if g.dtype != dtype or g.numel() != p.numel() or not g.is_contiguous():
+                raise ValueError(f"grads[{i}]: gradients are contiguous, of one type and as large as their parameters")
+
+    def _keep(self, own: List[torch.Tensor]) -> int:
+        """Tensors allocated on the current stream, whose handle it returns, that steps use."""
+        self._own = own
+        home = _stream(self.workspace)
+        self._streams = {home}
+        return home
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class AdamW(_Stepper):
     """AdamW over a list of tensors, one launch for all of them (three with
     clipping); states in 32 or 8 bits (``state_bits``).
 
@@ -124,34 +168,8 @@ class AdamW:
         need = c_ops.mtdao_adamw_workspace_bytes(cfg, rows)
         self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
         self._followed = [p for p in self.params if not p.is_inference()]  # by autograd
-        self._own = [self.workspace]
-        if states is None:
-            self._own += [t for name in kinds for t in getattr(self, name)]
-        home = _stream(self.workspace)
-        self._streams = {home}
+        home = self._keep([self.workspace] + ([t for name in kinds for t in getattr(self, name)] if states is None else []))
         self.handle = c_ops.mtdao_adamw_init(cfg, rows, self.workspace.data_ptr(), need, home)
-
-    def _stream_here(self) -> int:
-        """The current stream, of the tensors' device.  On another one than that of construction the
-        allocator learns of it: freed earlier, the table of addresses in the
-        workspace would be another tensor's while a step still reads it."""
-        if torch.cuda.current_device() != self.workspace.get_device():
-            raise ValueError(f"the tensors are on {self.workspace.device}, the current device is {torch.cuda.current_device()}")
-        stream = _stream(self.workspace)
-        if stream not in self._streams:
-            current = torch.cuda.current_stream(self.workspace.device)
-            for t in self._own:
-                t.record_stream(current)
-            self._streams.add(stream)
-        return stream
-
-    def _grads_ok(self, grads, dtype) -> None:
-        if len(grads) != len(self.params):
-            raise ValueError(f"{len(grads)} gradients for {len(self.params)} parameters")
-        _on_device(self.params[0], *grads)
-        for i, (p, g) in enumerate(zip(self.params, grads)):
-            if g.dtype != dtype or g.numel() != p.numel() or not g.is_contiguous():
-                raise ValueError(f"grads[{i}]: gradients are contiguous, of one type and as large as their parameters")
 
     def set_grads(self, grads: Sequence[torch.Tensor]) -> None:
         """Take the gradients from these tensors from here on."""
@@ -174,11 +192,114 @@ class AdamW:
             c_ops.mtdao_adamw_destroy(self.handle)
             self.handle = None
 
-    def __del__(self):
-        try:
-            self.close()
-        except Exception:
-            pass
+
+def orthogonalize(x: torch.Tensor, *, steps: int = 5, eps: float = 1e-7, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """x [..., r, c] with the singular values of each matrix moved to about 1 by
+    ``steps`` Newton-Schulz products (include/mtdao_ops.h), in x's type unless
+    ``dtype`` is given.  It is not differentiable."""
+    if x.dim() < 2:
+        raise ValueError(f"matrices are wanted, not {tuple(x.shape)}")
+    if torch.is_grad_enabled() and x.requires_grad:
+        raise ValueError("x requires a gradient, which orthogonalize does not give: call it on x.detach() or under no_grad")
+    _on_device(x)
+    x = x.contiguous()
+    r, c = x.shape[-2:]
+    batch = math.prod(x.shape[:-2])
+    out = _empty(x, dtype or x.dtype)
+    need = _orthogonalize_workspace(batch, r, c)
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    c_ops.mtdao_orthogonalize(x.data_ptr(), _type(x, "x"), batch, r, c, out.data_ptr(), _type(out, "dtype"), steps, eps, _ptr(ws), need,
+                              _stream(x))
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def _orthogonalize_workspace(batch: int, r: int, c: int) -> int:
+    return c_ops.mtdao_orthogonalize_workspace_bytes(batch, r, c)
+
+
+class Muon(_Stepper):
+    """Momentum steps with orthogonalised updates, over a list of matrices at
+    once:  m = momentum m + g,  u = g + momentum m (``nesterov``) or m,
+    p = p (1 - lr weight_decay) - lr factor orthogonalize(u).
+
+    ``params`` and ``grads`` are lists of contiguous matrices (with more than two
+    axes: one for each index of the first ones), each list of one type (float32 or
+    bfloat16); the gradients are read from these tensors at every step until
+    ``set_grads`` names others.  ``weight_decay`` is one value or one per tensor;
+    ``factor`` likewise, or "shape", max(1, rows / cols)^(1/2), or "rms", 0.2
+    max(rows, cols)^(1/2), with which the root mean square of an update is about
+    AdamW's.  ``states`` takes momenta to go on from (the list "m", float32), zeros otherwise.
+    Embeddings, norms and other vectors are ``AdamW``'s.
+    """
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], *, momentum: float = 0.95, nesterov: bool = True,
+                 weight_decay: Union[float, Sequence[float]] = 0.0, factor: Union[str, float, Sequence[float]] = "shape", steps: int = 5,
+                 eps: float = 1e-7, states: Optional[Dict[str, List[torch.Tensor]]] = None):
+        self.handle = None
+        self.params = list(params)
+        n = len(self.params)
+        if n == 0:
+            raise ValueError("no parameters")
+        device = _on_device(*self.params)
+        for i, p in enumerate(self.params):
+            if p.dtype != self.params[0].dtype or not p.is_contiguous() or p.dim() < 2:
+                raise ValueError(f"params[{i}]: parameters are contiguous matrices and of one type")
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [float(weight_decay)] * n
+        if isinstance(factor, str):
+            if factor not in ("shape", "rms"):
+                raise ValueError(f"factor {factor!r} is not 'shape' or 'rms'")
+            each = [math.sqrt(max(1.0, p.shape[-2] / max(1, p.shape[-1]))) if factor == "shape" else 0.2 * math.sqrt(max(p.shape[-2:]))
+                    for p in self.params]
+        else:
+            each = list(factor) if isinstance(factor, (list, tuple)) else [float(factor)] * n
+        if len(decay) != n or len(each) != n:
+            raise ValueError(f"{len(decay)} values of weight_decay and {len(each)} of factor for {n} tensors")
+        self._grads_ok(grads, torch.float32 if len(grads) == 0 else grads[0].dtype)
+        self.grads = list(grads)
+        if states is None:
+            self.m = [torch.zeros(p.shape, dtype=torch.float32, device=device) for p in self.params]
+        else:
+            self.m = list(states["m"])
+            _on_device(self.params[0], *self.m)
+            if len(self.m) != n or any(m.dtype != torch.float32 or m.numel() != p.numel() or not m.is_contiguous()
+                                       for m, p in zip(self.m, self.params)):
+                raise ValueError(f"states['m']: {n} contiguous tensors of float32, as large as their parameters")
+        self._batch = [math.prod(p.shape[:-2]) for p in self.params]
+        rows = (c_ops.MuonMatrix * max(1, sum(self._batch)))()
+        at = 0
+        for i, p in enumerate(self.params):
+            r, c = p.shape[-2:]
+            for k in range(self._batch[i]):
+                a = rows[at]
+                a.p, a.g, a.m = (t.data_ptr() + k * r * c * t.element_size() for t in (p, self.grads[i], self.m[i]))
+                a.rows, a.cols, a.weight_decay, a.factor = r, c, decay[i], each[i]
+                at += 1
+        cfg = c_ops.MuonConfig(_type(self.params[0], "params"), _type(self.grads[0], "grads"), max(1, at), bool(nesterov), steps, 0, momentum,
+                               eps)
+        need = c_ops.mtdao_muon_workspace_bytes(cfg, rows)
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        self._followed = [p for p in self.params if not p.is_inference()]  # by autograd
+        home = self._keep([self.workspace] + (self.m if states is None else []))
+        self.handle = c_ops.mtdao_muon_init(cfg, rows, self.workspace.data_ptr(), need, home)
+
+    def set_grads(self, grads: Sequence[torch.Tensor]) -> None:
+        """Take the gradients from these tensors from here on."""
+        self._grads_ok(grads, self.grads[0].dtype)
+        at = [g.data_ptr() + k * (g.numel() // b) * g.element_size() for g, b in zip(grads, self._batch) for k in range(b)]
+        c_ops.mtdao_muon_set_grads(self.handle, at or [None], self._stream_here())
+        self.grads = list(grads)
+
+    def step(self, lr: float) -> None:
+        """One step.  To autograd it is a change in place: a backward pass over
+        parameters from before it is refused."""
+        c_ops.mtdao_muon_step(self.handle, lr, self._stream_here())
+        increment_version(self._followed)
+
+    def close(self) -> None:
+        if self.handle:
+            c_ops.mtdao_muon_destroy(self.handle)
+            self.handle = None
 
 
 # -------------------------------------------------------- Peri-LN boundary
@@ -572,3 +693,165 @@ class _Linear8(torch.autograd.Function):
         kind = x.dtype if x.dtype == dy.dtype else torch.float32
         dx, dw = linear8_backward(dy.to(kind), x.to(kind), ctx.w)
         return dx.to(x.dtype) if ctx.needs_input_grad[0] else None, dw.to(ctx.type) if ctx.needs_input_grad[1] else None, None, None
+
+
+# -------------------------------------------------------------- embedding
+
+
+def _ids(t: torch.Tensor, what: str) -> Tuple[torch.Tensor, int]:
+    """t contiguous, and its bits."""
+    bits = {torch.int32: 32, torch.int64: 64}.get(t.dtype)
+    if bits is None:
+        raise TypeError(f"{what} must be int32 or int64, not {t.dtype}")
+    return t.contiguous(), bits
+
+
+def embedding(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """scale table[tokens]: tokens (int32 or int64) of any shape, a table [rows, d];
+    in the table's type unless ``dtype`` is given.  A token below 0 stands for none:
+    its row is zero.  One that the table does not have makes its row NaN."""
+    if torch.is_grad_enabled() and table.requires_grad:
+        return _Embedding.apply(tokens, table, scale, dtype)
+    dev = _on_device(tokens, table)
+    ids, bits = _ids(tokens, "tokens")
+    w = _matrix(table)
+    rows, d = w.shape
+    out = torch.empty((*tokens.shape, d), dtype=dtype or table.dtype, device=dev)
+    if out.numel():
+        c_ops.mtdao_embedding(ids.data_ptr(), bits, ids.numel(), w.data_ptr(), _type(w, "table"), rows, d, _ld(w), scale, out.data_ptr(),
+                              _type(out, "dtype"), d, _stream(out))
+    return out
+
+
+@functools.lru_cache(maxsize=256)
+def _embedding_workspace(n: int, rows: int, d: int) -> int:
+    return c_ops.mtdao_embedding_backward_workspace_bytes(n, rows, d)
+
+
+def embedding_backward(dy: torch.Tensor, tokens: torch.Tensor, rows: int, *, scale: float = 1.0, dw: Optional[torch.Tensor] = None,
+                       accumulate: bool = False) -> torch.Tensor:
+    """The gradient of ``embedding``'s table of ``rows`` rows, in float32, from that
+    of its output: scale times the sum of each token's rows of dy, in their order.  ``dw``: written in place
+    of a new tensor (contiguous rows); ``accumulate``: added to, and rows whose token does not come are not touched."""
+    d = dy.shape[-1]
+    if dy.shape[:-1] != tokens.shape:
+        raise ValueError(f"dy is {tuple(dy.shape)}, tokens {tuple(tokens.shape)}")
+    given = dw is not None
+    if not given:
+        if accumulate:
+            raise ValueError("accumulate needs dw")
+        dw = torch.empty((rows, d), dtype=torch.float32, device=dy.device)
+    elif tuple(dw.shape) != (rows, d) or d > 1 and dw.stride(1) != 1 or dw.dtype != torch.float32:
+        raise ValueError(f"dw is {tuple(dw.shape)}, {dw.dtype} with strides {dw.stride()}, not float32 [{rows}, {d}] with contiguous rows")
+    dev = _on_device(dy, tokens, dw)
+    ids, bits = _ids(tokens, "tokens")
+    kind = _type(dy, "dy")
+    dy2 = _flat(dy)
+    if dw.numel():
+        need = _embedding_workspace(ids.numel(), rows, d)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        c_ops.mtdao_embedding_backward(dy2.data_ptr(), kind, _ld(dy2), ids.data_ptr(), bits, ids.numel(), scale, dw.data_ptr(), rows, d,
+                                       _ld(dw), accumulate, ws.data_ptr(), need, _stream(dy))
+    if given and not dw.is_inference():
+        increment_version(dw)
+    return dw
+
+
+class _Embedding(torch.autograd.Function):
+    """embedding for autograd."""
+
+    @staticmethod
+    def forward(ctx, tokens, table, scale, dtype):
+        ctx.save_for_backward(tokens)
+        ctx.rows, ctx.scale, ctx.type = table.shape[0], scale, table.dtype
+        return embedding(tokens, table, scale=scale, dtype=dtype)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        tokens, = ctx.saved_tensors
+        return None, embedding_backward(dy, tokens, ctx.rows, scale=ctx.scale).to(ctx.type), None, None
+
+
+# ---------------------------------------------------------- cross entropy
+
+_REDUCTIONS = {"none": c_ops.MTDAO_LOSS_NONE, "sum": c_ops.MTDAO_LOSS_SUM, "mean": c_ops.MTDAO_LOSS_MEAN}
+
+
+@functools.lru_cache(maxsize=256)
+def _loss_workspace(rows: int, cols: int) -> int:
+    return c_ops.mtdao_cross_entropy_workspace_bytes(c_ops.PACKED_LOSS.pack(rows, cols, cols, cols, 0, 32, 0, 0.0, 1.0, 0, *(0,) * 6))
+
+
+def _loss(logits, targets, z_loss, reduction, *, loss=False, gradient=False, d_loss=None, scale=1.0, in_place=False):
+    """The loss and/or the gradient of the logits, None for what is not asked for."""
+    if reduction not in _REDUCTIONS:
+        raise ValueError(f"reduction {reduction!r} is not 'none', 'sum' or 'mean'")
+    if logits.shape[:-1] != targets.shape or logits.shape[-1] == 0:
+        raise ValueError(f"logits are {tuple(logits.shape)}, targets {tuple(targets.shape)}: a row of at least one logit for each target")
+    dev = _on_device(logits, targets, d_loss)
+    ids, bits = _ids(targets, "targets")
+    kind = _type(logits, "logits")
+    x = _flat(logits)
+    rows, cols = x.shape
+    each = reduction == "none"
+    made = torch.empty(targets.shape if each else (), dtype=torch.float32, device=dev) if loss else None
+    d = None
+    if gradient:
+        d = logits if in_place else _empty(logits, logits.dtype)
+        if in_place and x.data_ptr() != logits.data_ptr():
+            raise ValueError(f"logits with strides {logits.stride()} cannot be written in place")
+    if rows or made is not None and not each:
+        need = _loss_workspace(rows, cols)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        c_ops.mtdao_cross_entropy(
+            c_ops.PACKED_LOSS.pack(rows, cols, _ld(x), _ld(x) if in_place else cols, kind, bits, _REDUCTIONS[reduction], z_loss, scale, 0,
+                                   x.data_ptr(), ids.data_ptr(), _ptr(d_loss), made.data_ptr() if loss and each else 0,
+                                   made.data_ptr() if loss and not each else 0, _ptr(d)), ws.data_ptr(), need, _stream(logits))
+    if in_place and not logits.is_inference():
+        increment_version(logits)
+    return made, d
+
+
+def cross_entropy(logits: torch.Tensor, targets: torch.Tensor, *, z_loss: float = 0.0, reduction: str = "mean") -> torch.Tensor:
+    """lse - x_target + z_loss lse^2 of every row x of the logits [..., vocabulary],
+    lse = log sum exp x, in float32: for each ("none"), their sum or their mean over
+    the rows with a target.  A target (int32 or int64) below 0 stands for none:
+    no loss, no gradient.  One that the row does not have gives NaN."""
+    if torch.is_grad_enabled() and logits.requires_grad:
+        return _CrossEntropy.apply(logits, targets, z_loss, reduction)
+    return _loss(logits, targets, z_loss, reduction, loss=True)[0]
+
+
+def cross_entropy_backward(d_loss: Optional[torch.Tensor], logits: torch.Tensor, targets: torch.Tensor, *, z_loss: float = 0.0,
+                           reduction: str = "mean") -> torch.Tensor:
+    """The gradient of the logits, in their type, from that of ``cross_entropy``'s
+    result (float32; None: 1)."""
+    if d_loss is not None:
+        if d_loss.dtype != torch.float32 or d_loss.shape != (targets.shape if reduction == "none" else ()):
+            raise ValueError(f"d_loss is {tuple(d_loss.shape)}, {d_loss.dtype}, not float32 of the loss's shape")
+        d_loss = d_loss.contiguous()
+    return _loss(logits, targets, z_loss, reduction, gradient=True, d_loss=d_loss)[1]
+
+
+def cross_entropy_step(logits: torch.Tensor, targets: torch.Tensor, *, z_loss: float = 0.0, reduction: str = "mean", scale: float = 1.0,
+                       in_place: bool = False) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(loss, gradient of the logits) of ``cross_entropy`` in one pass over the
+    logits; the gradient is that of ``scale`` times the loss, with ``in_place``
+    written over the logits.  Neither takes part in autograd."""
+    return _loss(logits.detach(), targets, z_loss, reduction, loss=True, gradient=True, scale=scale, in_place=in_place)
+
+
+class _CrossEntropy(torch.autograd.Function):
+    """cross_entropy for autograd."""
+
+    @staticmethod
+    def forward(ctx, logits, targets, z_loss, reduction):
+        ctx.save_for_backward(logits, targets)
+        ctx.how = {"z_loss": z_loss, "reduction": reduction}
+        return cross_entropy(logits, targets, **ctx.how)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_loss):
+        return cross_entropy_backward(d_loss, *ctx.saved_tensors, **ctx.how), None, None, None

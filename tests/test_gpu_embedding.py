@@ -1,0 +1,175 @@
+"""Embedding and its gradient (paper_2510_05361_amd.ops) against the definition
+in 64 bits.  A row is one fp32 product of rounded factors, 2 U, and one rounding;
+sums are those of lm_oracle.embedding_backward."""
+
+import math
+
+import pytest
+import torch
+
+import lm_oracle as oracle
+from paper_2510_05361_amd import ops
+
+pytestmark = pytest.mark.gpu
+
+U = oracle.U
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def tokens_of(shape, rows, seed=0, none=0.1, ids=torch.int64, kind="log"):
+    gen = torch.Generator().manual_seed(seed)
+    if kind == "log":
+        t = ((rows + 1) ** torch.rand(shape, generator=gen, dtype=torch.float64) - 1).long().clamp(0, rows - 1)
+    elif kind == "one":
+        t = torch.full(shape, rows // 2, dtype=torch.int64)
+    else:
+        t = torch.randint(0, rows, shape, generator=gen)
+    t[torch.rand(shape, generator=gen) < none] = -1
+    return t.to(ids)
+
+
+def check_rows(got, tokens, table, scale):
+    want = oracle.embedding(tokens.long(), table.double(), scale)
+    oracle.close(got, want, want.abs().nan_to_num() * (2 * U + oracle.half_step(got.dtype)))
+
+
+@pytest.mark.parametrize("w,y", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("n,rows,d", [(1, 1, 1), (1, 100, 2048), (3, 7, 5), (8, 1000, 64), (130, 50, 130), (2000, 300, 96), (5, 40, 8200), (257, 5000, 33)])
+def test_lookup(n, rows, d, w, y):
+    table = torch.randn((rows, d), generator=torch.Generator().manual_seed(1)).to(DT[w])
+    for ids in (torch.int32, torch.int64):
+        tokens = tokens_of((n,), rows, ids=ids)
+        out = ops.embedding(tokens.cuda(), table.cuda(), scale=1.7, dtype=DT[y])
+        assert out.dtype == DT[y] and out.shape == (n, d)
+        check_rows(out, tokens, table, 1.7)
+
+
+def test_lookup_shapes_strides_and_unknown_tokens():
+    table = torch.randn((50, 40))
+    tokens = tokens_of((4, 6), 50)
+    tokens[0, 0], tokens[1, 1], tokens[2, 2], tokens[3, 3] = 50, 2 ** 40, -2 ** 40, -1
+    wide = torch.randn((50, 64))
+    wide[:, 7:47] = table
+    for t, w in ((tokens.cuda(), table.cuda()), (tokens.t().contiguous().t().cuda(), wide.cuda()[:, 7:47]), (tokens.cuda(), table.t().contiguous().cuda().t())):
+        out = ops.embedding(t, w)
+        check_rows(out, tokens, table, 1.0)
+        assert out[0, 0].isnan().all() and out[1, 1].isnan().all() and bool((out[2, 2] == 0).all()) and bool((out[3, 3] == 0).all())
+    assert ops.embedding(torch.empty((0, 3), dtype=torch.int32, device="cuda"), table.cuda()).shape == (0, 3, 40)
+
+
+def check_sums(got, dy, tokens, rows, scale, before=None):
+    want, err = oracle.embedding_backward(dy.double(), tokens.long(), rows, scale)
+    if before is not None:
+        want = want + before.double()
+        err = err + 2 * U * want.abs()
+    oracle.close(got, want, err * (1 + 1e-6) + 1e-42)
+
+
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["log", "even", "one"])
+@pytest.mark.parametrize("n,rows,d", [(1, 1, 1), (1, 70000, 8), (2, 3, 130), (63, 9, 16), (65, 2, 16), (129, 1, 40), (1000, 300, 72), (4096, 256, 24), (4097, 257, 8),
+                                      (9000, 66000, 16), (20011, 17, 33), (300, 40, 2048)])
+def test_sums(n, rows, d, kind, y):
+    tokens = tokens_of((n,), rows, kind=kind, ids=torch.int32 if n % 2 else torch.int64)
+    dy = torch.randn((n, d), generator=torch.Generator().manual_seed(2)).to(DT[y])
+    dw = ops.embedding_backward(dy.cuda(), tokens.cuda(), rows, scale=0.3)
+    assert dw.dtype == torch.float32
+    check_sums(dw, dy, tokens, rows, 0.3)
+    before = torch.randn((rows, d), generator=torch.Generator().manual_seed(3))
+    onto = before.cuda()
+    version = onto._version
+    assert ops.embedding_backward(dy.cuda(), tokens.cuda(), rows, scale=0.3, dw=onto, accumulate=True) is onto and onto._version > version
+    check_sums(onto, dy, tokens, rows, 0.3, before)
+    idle = torch.ones(rows, dtype=torch.bool)
+    idle[tokens[tokens >= 0].long()] = False
+    assert torch.equal(onto.cpu()[idle], before[idle]) and bool((dw.cpu()[idle] == 0).all())
+
+
+def test_sums_into_rows_with_gaps():
+    """Rows of dw and dy apart; what lies between is left alone."""
+    tokens = tokens_of((5, 60), 100, none=0.3)
+    tokens[0, :3] = torch.tensor([100, 2 ** 35, -7])
+    dy = torch.randn((5, 60, 48))
+    wide = torch.full((100, 60), 5.0, device="cuda")
+    gaps = torch.randn((5, 60, 50), device="cuda")
+    gaps[..., 1:49] = dy.cuda()
+    ops.embedding_backward(gaps[..., 1:49], tokens.cuda(), 100, dw=wide[:, 6:54])
+    check_sums(wide[:, 6:54], dy.view(-1, 48), tokens.view(-1), 100, 1.0)
+    assert bool((wide[:, :6] == 5).all()) and bool((wide[:, 54:] == 5).all())
+
+
+def test_nothing_to_sum():
+    none = torch.full((40,), -1, dtype=torch.int64, device="cuda")
+    dy = torch.full((40, 16), math.nan, device="cuda")
+    assert bool((ops.embedding_backward(dy, none, 30) == 0).all())
+    held = torch.randn((30, 16), device="cuda")
+    assert torch.equal(ops.embedding_backward(dy, none, 30, dw=held.clone(), accumulate=True), held)
+    empty = torch.empty((0, 16), device="cuda")
+    assert bool((ops.embedding_backward(empty, none[:0], 30) == 0).all())
+    assert ops.embedding_backward(dy, none, 0).shape == (0, 16)
+
+
+def test_order_is_fixed_by_the_places():
+    """Equal sums again, replayed and with other tokens around: no atomics."""
+    tokens = tokens_of((6000,), 50, none=0.0).cuda()
+    dy = torch.randn((6000, 64), device="cuda")
+    first = ops.embedding_backward(dy, tokens, 50)
+    assert all(torch.equal(first, ops.embedding_backward(dy, tokens, 50)) for _ in range(3))
+    # the same places with row 7 alone
+    alone = torch.where(tokens == 7, tokens, -1)
+    assert torch.equal(ops.embedding_backward(dy, alone, 50)[7], first[7])
+
+
+def test_autograd_and_tied_tables():
+    table = torch.randn((90, 24), device="cuda", requires_grad=True)
+    tokens = tokens_of((7, 11), 90)
+    up = torch.randn((7, 11, 24))
+    out = ops.embedding(tokens.cuda(), table, scale=2.0)
+    (out * up.cuda()).sum().backward()
+    check_sums(table.grad, up.view(-1, 24), tokens.view(-1), 90, 2.0)
+    half = table.detach().bfloat16().requires_grad_()
+    ops.embedding(tokens.cuda(), half, scale=2.0, dtype=torch.float32).backward(up.cuda())
+    assert half.grad.dtype == torch.bfloat16
+    want, err = oracle.embedding_backward(up.view(-1, 24).double(), tokens.view(-1), 90, 2.0)
+    oracle.close(half.grad, want, err * 1.01 + want.abs() * 2.0 ** -8)
+
+
+def test_gradient_against_differences():
+    table, tokens = torch.randn((12, 6)), tokens_of((20,), 12)
+    up = torch.randn((20, 6))
+    dw = ops.embedding_backward(up.cuda(), tokens.cuda(), 12, scale=1.5).cpu()
+    f = lambda w: float((ops.embedding(tokens.cuda(), w.cuda(), scale=1.5).cpu().double() * up.double()).sum())  # noqa: E731
+    for r, c in ((0, 0), (int(tokens[tokens >= 0][3]), 2), (11, 5)):
+        more, less = table.clone(), table.clone()
+        more[r, c] += 0.5
+        less[r, c] -= 0.5
+        # (linear: only roundings of rows and of the difference itself)
+        assert abs(f(more) - f(less) - float(dw[r, c])) < 1e-5 * (1 + abs(float(dw[r, c])))
+
+
+def test_in_a_graph():
+    tokens, dy = tokens_of((500,), 1000).cuda(), torch.randn((500, 128), device="cuda")
+    table = torch.randn((1000, 128), device="cuda")
+    for _ in range(2):
+        ops.embedding(tokens, table), ops.embedding_backward(dy, tokens, 1000)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, dw = ops.embedding(tokens, table), ops.embedding_backward(dy, tokens, 1000)
+    for seed in (4, 5, 6):
+        tokens.copy_(tokens_of((500,), 1000, seed))
+        dy.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ops.embedding(tokens, table)) and torch.equal(dw, ops.embedding_backward(dy, tokens, 1000))
+
+
+def test_a_table_past_32_bits_of_elements():
+    rows, d = 550_000, 4096  # 4.5 GB in bf16
+    table = torch.zeros((rows, d), dtype=torch.bfloat16, device="cuda")
+    table[-2:] = torch.randn((2, d), device="cuda").bfloat16()
+    tokens = torch.tensor([rows - 1, 0, rows - 2, rows], device="cuda")
+    out = ops.embedding(tokens, table)
+    assert torch.equal(out[0], table[-1]) and torch.equal(out[2], table[-2]) and bool((out[1] == 0).all()) and out[3].isnan().all()
+    del table
+    dw = ops.embedding_backward(out, tokens, rows)
+    assert torch.equal(dw[-1], out[0].float()) and torch.equal(dw[-2], out[2].float()) and bool((dw[:-2] == 0).all())

@@ -1,0 +1,267 @@
+"""Orthogonalised updates (paper_2510_05361_amd.ops) against the definition in
+64 bits.
+
+The header promises products of fp32's precision, so the tolerance is what the same
+formulas in fp32 (torch on the CPU) are off by, four times over: both are sums of
+rounded products whose errors the iteration raises alike, and the kernels have up to
+twice the roundings of each (two parts of a factor, its storage).  Where fp32 happens to
+be lucky (tiny matrices) 64 U of the norm stands in its place: five steps of four products or sums each, whose
+errors of about 2 U add up as their roots and grow by at most 3.5 a step in the
+directions that are far below 1, but by less than 1 where they have arrived.
+Results are rounded once to their type."""
+
+import pytest
+import torch
+
+import lm_oracle as oracle
+from paper_2510_05361_amd import ops
+
+pytestmark = pytest.mark.gpu
+
+U = oracle.U
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def matrix(r, c, seed=0, kind="noise"):
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn((r, c), generator=gen)
+    if kind == "low":    # a few strong directions in weak noise
+        k = min(8, r, c)
+        x = 0.05 * x + torch.randn((r, k), generator=gen) @ torch.randn((k, c), generator=gen)
+    if kind == "steep":  # singular values over four decades
+        u, _, v = torch.linalg.svd(x.double(), full_matrices=False)
+        x = ((u * torch.logspace(0, -4, min(r, c), dtype=torch.float64)) @ v).float()
+    return x
+
+
+def allowed(u, steps, eps):
+    """(result in 64 bits, norm of the error allowed): u is what is orthogonalised, in fp32."""
+    want = oracle.newton_schulz(u.double(), steps, eps)
+    off = (oracle.newton_schulz(u, steps, eps).double() - want).norm()
+    return want, max(4 * off, 64 * U * want.norm())
+
+
+def check(got, x, steps=5, eps=1e-7):
+    got, x = got.cpu(), x.float()
+    for g, m in zip(got.view(-1, *got.shape[-2:]), x.view(-1, *x.shape[-2:])):
+        want, err = allowed(m, steps, eps)
+        rounding = oracle.half_step(got.dtype) * want.norm() if got.dtype != torch.float32 else U * want.norm()
+        off = (g.double() - want).norm()
+        assert off <= err + rounding, f"{float(off / want.norm()):.2e} off, {float((err + rounding) / want.norm()):.2e} allowed"
+
+
+SIZES = [(1, 1), (1, 9), (9, 1), (2, 3), (37, 100), (100, 37), (64, 64), (128, 128), (129, 127), (127, 400), (128, 129), (256, 256), (300, 301), (511, 130),
+         (96, 1000), (640, 520), (257, 1030), (1030, 257)]
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("r,c", SIZES)
+def test_sizes(r, c, t):
+    x = matrix(r, c).to(DT[t])
+    out = ops.orthogonalize(x.cuda())
+    assert out.dtype == x.dtype and out.shape == x.shape
+    check(out, x)
+
+
+@pytest.mark.parametrize("kind", ["noise", "low", "steep"])
+@pytest.mark.parametrize("r,c", [(60, 90), (200, 150), (384, 384), (256, 1024), (1100, 260)])
+def test_spectra(r, c, kind):
+    x = matrix(r, c, 3, kind)
+    check(ops.orthogonalize(x.cuda()), x)
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 6, 7, 10])
+@pytest.mark.parametrize("r,c", [(70, 200), (130, 140), (256, 800)])
+def test_steps(steps, r, c):
+    x = matrix(r, c, 4)
+    check(ops.orthogonalize(x.cuda(), steps=steps), x, steps)
+
+
+def test_singular_values_arrive():
+    """Those from 1/400 of the norm on come to lie between 0.67 and 1.21."""
+    x = matrix(200, 260, 5).cuda()
+    s = torch.linalg.svdvals(ops.orthogonalize(x).double().cpu())
+    assert 0.67 < float(s.min()) and float(s.max()) < 1.21
+    u, _, v = torch.linalg.svd(x.double().cpu(), full_matrices=False)
+    turned = u.t() @ ops.orthogonalize(x).double().cpu() @ v.t()
+    assert float((turned - torch.diag(turned.diagonal())).norm()) < 1e-4
+
+
+@pytest.mark.parametrize("magnitude", [1e-30, 1e-6, 1e30])
+def test_scale_of_the_input(magnitude):
+    """Norms whose squares fp32 does not hold; eps counts where the norm is small.
+    X is held to 2^-39 (half of fp16's smallest step, 2^-24, over 2^14) whatever its size: the start and
+    each of the five results round that much, and a step raises it at most 3.4445-fold, so with
+    3.4445^5 = 485 an element is off by 485 (1 + 1/3.4 + ...) 2^-39 < 700 2^-39 at most."""
+    x = matrix(50, 80, 6) * magnitude
+    want = oracle.newton_schulz(x.double(), 5, 1e-7)
+    got = ops.orthogonalize(x.cuda()).double().cpu()
+    assert float((got - want).norm()) <= 256 * U * float(want.norm()) + 700 * 2.0 ** -39 * x.numel() ** 0.5
+    sharp = ops.orthogonalize(x.cuda(), eps=0.0).double().cpu()
+    want = oracle.newton_schulz(x.double(), 5, 0.0)
+    assert float((sharp - want).norm()) <= 256 * U * float(want.norm())
+
+
+def test_zeros_and_what_is_not_finite():
+    x = torch.zeros((3, 40, 30))
+    x[1] = matrix(40, 30)
+    x[2] = x[1]
+    x[2, 5, 7] = float("nan")
+    out = ops.orthogonalize(x.cuda())
+    assert bool((out[0] == 0).all()) and bool(out[2].isnan().all())
+    check(out[1:2], x[1:2])
+    x[2, 5, 7] = float("inf")
+    assert bool(ops.orthogonalize(x.cuda())[2].isnan().all())
+
+
+@pytest.mark.parametrize("t,o", [("f32", "bf16"), ("bf16", "f32")])
+def test_batches_strides_and_types(t, o):
+    x = torch.stack([matrix(90, 50, s) for s in range(6)]).view(2, 3, 90, 50).to(DT[t])
+    out = ops.orthogonalize(x.cuda(), dtype=DT[o])
+    assert out.shape == x.shape and out.dtype == DT[o]
+    check(out, x)
+    for view in (x.cuda().transpose(0, 1).contiguous().transpose(0, 1), x.cuda().transpose(2, 3).contiguous().transpose(2, 3)):
+        assert torch.equal(ops.orthogonalize(view, dtype=DT[o]), out)
+    one = ops.orthogonalize(x[1, 2].cuda(), dtype=DT[o])
+    assert torch.equal(one, out[1, 2]), "a matrix alone gives what it gives among others"
+    assert ops.orthogonalize(x[:0].cuda()).shape == (0, 3, 90, 50)
+    assert ops.orthogonalize(x[:, :, :0].cuda()).shape == (2, 3, 0, 50)
+
+
+# ------------------------------------------------------------------------ steps
+
+
+def make(shapes, p="f32", g="f32", seed=0, **kw):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    new = lambda std, dtype: [torch.empty(s, device="cuda").normal_(0, std, generator=gen).to(dtype) for s in shapes]  # noqa: E731
+    params, grads = new(0.05, DT[p]), new(0.01, DT[g])
+    return params, grads, ops.Muon(params, grads, **kw)
+
+
+def step_and_check(params, grads, opt, lr=0.02, momentum=0.95, nesterov=True, decay=0.0, factor=None, steps=5, eps=1e-7):
+    before = [[t.detach().cpu() for t in ts] for ts in (params, grads, opt.m)]
+    opt.step(lr)
+    torch.cuda.synchronize()
+    for i, (p, g, m) in enumerate(zip(*before)):
+        r, c = p.shape[-2:]
+        if p.numel() == 0:
+            continue
+        f = factor[i] if factor is not None else max(1.0, r / c) ** 0.5
+        for k, (p0, g0, m0) in enumerate(zip(p.reshape(-1, r, c), g.reshape(-1, r, c), m.reshape(-1, r, c))):
+            how = (lr, momentum, nesterov, decay, f, steps, eps)
+            want, wm = oracle.muon(p0.double(), g0.double(), m0.double(), *how)
+            gm = opt.m[i].view(-1, r, c)[k].cpu().double()
+            assert bool(((gm - wm).abs() <= 3 * U * (momentum * m0.double().abs() + g0.double().abs()) + 1e-45).all())
+            # the update of the same formulas in fp32, from the same momentum and gradient
+            u64 = g0.double() + momentum * wm if nesterov else wm
+            u32 = g0.float() + momentum * (momentum * m0 + g0.float()) if nesterov else momentum * m0 + g0.float()
+            o = oracle.newton_schulz(u64, steps, eps)
+            err = lr * abs(f) * max(4 * float((oracle.newton_schulz(u32, steps, eps).double() - o).norm()), 64 * U * float(o.norm()))
+            err += 4 * U * float(p0.double().norm()) + (oracle.half_step(p0.dtype) * float(want.norm()) if p0.dtype != torch.float32 else 0)
+            off = float((params[i].detach().view(-1, r, c)[k].cpu().double() - want).norm())
+            assert off <= err, (i, k, off / err)
+
+
+MODEL = [(192, 64), (64, 64), (256, 64), (64, 256)]
+
+
+@pytest.mark.parametrize("p,g", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("nesterov", [True, False])
+def test_steps_of_a_model(p, g, nesterov):
+    shapes = MODEL + [(5, 3), (1, 1), (300, 7), (0, 4), (3, 20, 30), (130, 129)] + MODEL
+    params, grads, opt = make(shapes, p, g, nesterov=nesterov, weight_decay=0.1)
+    for _ in range(3):
+        step_and_check(params, grads, opt, nesterov=nesterov, decay=0.1)
+
+
+def test_factors_and_decay_of_each():
+    shapes = [(40, 60), (60, 40), (60, 40)]
+    params, grads, opt = make(shapes, factor="rms", weight_decay=[0.0, 0.5, 0.1])
+    before = [p.clone() for p in params]
+    opt.step(0.01)
+    for p, b, (r, c), d in zip(params, before, shapes, (0.0, 0.5, 0.1)):
+        rms = float(((p - b * (1 - 0.01 * d)) / 0.01).square().mean().sqrt())
+        assert 0.12 < rms < 0.25, "about AdamW's"
+    params, grads, opt = make(shapes, factor=[0.0, -1.0, 3.0], momentum=0.0)
+    step_and_check(params, grads, opt, momentum=0.0, factor=[0.0, -1.0, 3.0])
+
+
+def test_shapes_of_many_kinds_in_one_step():
+    """More shapes than one launch describes."""
+    shapes = [(10 + i, 200 - 3 * i) for i in range(30)] + [(150, 20), (20, 150)] * 3
+    params, grads, opt = make(shapes)
+    for _ in range(2):
+        step_and_check(params, grads, opt)
+
+
+def test_other_gradients_and_states():
+    params, grads, opt = make(MODEL)
+    opt.step(0.02)
+    new = [torch.randn_like(g) for g in grads]
+    opt.set_grads(new)
+    step_and_check(params, new, opt)
+    again = ops.Muon([p.clone() for p in params], new, states={"m": [m.clone() for m in opt.m]})
+    opt.step(0.01)
+    again.step(0.01)
+    assert all(torch.equal(a, b) for a, b in zip(params, again.params)) and all(torch.equal(a, b) for a, b in zip(opt.m, again.m))
+
+
+def test_unaligned_parts_of_one_allocation():
+    """Matrices one after another at odd places: neighbours are left alone."""
+    flat = {k: torch.randn(4000, device="cuda") for k in "pgm"}
+    cut = lambda t: [t[1:1 + 35].view(5, 7), t[40:40 + 33 * 50].view(33, 50), t[1701:1701 + 1100].view(100, 11)]  # noqa: E731
+    params, grads, m = (cut(flat[k]) for k in "pgm")
+    kept = {k: v.clone() for k, v in flat.items()}
+    opt = ops.Muon(params, grads, states={"m": m})
+    step_and_check(params, grads, opt)
+    for k in "pm":
+        for t in cut(kept[k]):
+            t.zero_()
+        now = flat[k].clone()
+        for t in cut(now):
+            t.zero_()
+        assert torch.equal(now, kept[k])
+    assert torch.equal(flat["g"][:1], kept["g"][:1])
+
+
+def test_captured_steps_and_other_streams():
+    params, grads, opt = make(MODEL + [(300, 140)])
+    twin_p = [p.clone() for p in params]
+    twin = ops.Muon(twin_p, grads)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        opt.step(0.01)
+    torch.cuda.current_stream().wait_stream(side)
+    twin.step(0.01)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step(0.02)
+    for i in range(3):
+        for g in grads:
+            g.normal_(0, 0.01)
+        graph.replay()
+        twin.step(0.02)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(params, twin_p)), i
+    assert all(torch.equal(a, b) for a, b in zip(opt.m, twin.m))
+
+
+def test_a_step_is_a_change_in_place():
+    w = torch.randn((20, 30), device="cuda", requires_grad=True)
+    g = torch.randn((20, 30), device="cuda")
+    y = (w * w).sum()
+    opt = ops.Muon([w], [g])
+    opt.step(0.1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+
+
+def test_large_matrices():
+    """Tiles of the largest size, and wide ones; 64 bits on the GPU."""
+    for r, c in ((1024, 1024), (2304, 768), (1100, 3000)):
+        x = matrix(r, c, 8)
+        want = oracle.newton_schulz(x.cuda().double(), 5, 1e-7)
+        off = (oracle.newton_schulz(x.cuda(), 5, 1e-7).double() - want).norm() / want.norm()
+        got = (ops.orthogonalize(x.cuda()).double() - want).norm() / want.norm()
+        assert float(got) <= max(4 * float(off), 64 * U), (r, c, float(got), float(off))
