@@ -9,7 +9,11 @@
 #include <cstdint>
 #include <cstdio>
 #include <cstdlib>
+#include <mutex>
+#include <new>
+#include <set>
 #include <string>
+#include <utility>
 
 #include "../../include/mtdao.h"
 
@@ -81,6 +85,22 @@ inline dim3 grid_of(int64_t n) {
 inline int32_t hip_check(std::string* e, hipError_t r, const char* what) {
   if (r != hipSuccess) return fail(e, MTDAO_ERR_HIP, "%s: %s", what, hipGetErrorString(r));
   return MTDAO_OK;
+}
+
+// More than 64 KiB of LDS for a kernel, asked for once per kernel and device.
+inline int32_t allow_lds(const void* kernel, int bytes, std::string* e) try {
+  static std::mutex lock;
+  static std::set<std::pair<const void*, int>> done;
+  int device = 0;
+  int32_t r = hip_check(e, hipGetDevice(&device), "device");
+  if (r != MTDAO_OK) return r;
+  std::lock_guard<std::mutex> held(lock);
+  if (done.count({kernel, device})) return MTDAO_OK;
+  r = hip_check(e, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes), "LDS of a kernel");
+  if (r == MTDAO_OK) done.insert({kernel, device});
+  return r;
+} catch (const std::bad_alloc&) {
+  return fail(e, MTDAO_ERR_WORKSPACE, "out of host memory");
 }
 
 }  // namespace mtdao

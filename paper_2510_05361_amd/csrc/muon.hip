@@ -49,8 +49,9 @@ constexpr int kMostParts = 12, kMostGemms = 2 * kMostParts;
 
 // X <- a X + (b A + c A^2) X with A = X X^T.
 constexpr double kCa = 3.4445, kCb = -4.7750, kCc = 2.0315;
-// Exponents of the stored factors: X, A and b A + c A^2.
-constexpr int kX = 14, kA = 14, kB = 13;
+// Exponents of the stored factors: X, A and A P, b A + c A^2, and Q - alpha I.
+constexpr int kX = 14, kA = 14, kB = 13, kR = 10;
+constexpr int kMostAtOnce = 3;  // steps that Q may stand for: kR suits Q up to a^3 = 40.9
 
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -255,14 +256,14 @@ struct Gemm {
   int32_t lda, ldb, ldo, ldt;      // bytes; d1 and d2 have out's rows
   int32_t symmetric;          // tiles on and above the diagonal only, out is turned
   int32_t tiles_a, tiles_b, tiles;
-  int32_t first, count;       // tiles before these matrices, matrices
-  int32_t matrix;             // the first one's place in the table
+  int32_t count, matrix;      // matrices, the first one's place in the table
+  int32_t first, share;       // an XCD's tiles before its share of these matrices' tiles, that share
   int32_t last;
   float k0, k1, k2;
 };
 struct Gemms {
   Gemm gemm[kMostGemms];
-  int32_t n, items;
+  int32_t n;
 };
 struct Last {
   const Row* rows;   // Muon's table
@@ -310,17 +311,26 @@ __device__ __forceinline__ void store_last(const Gemm& q, const Last& last, int 
 // The products of a launch in tiles of B x B over WR x WC waves, a tile a workgroup.
 // Rows of b go in as the instruction's rows, so that a lane ends with sixteen
 // consecutive columns of a row of c.
-template <int B, int WR, int WC, typename PT>
-__global__ __launch_bounds__(64 * WR * WC) void k_muon_product(Gemms all, Last last) {
-  constexpr int kWaves = WR * WC, kGroup = 64 * kWaves, kMI = B / WR / 32, kNI = B / WC / 32;
-  __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * B * 128 > kWaves * 32 * 33 * 4 ? 2 * B * 128 : kWaves * 32 * 33 * 4];
+//
+// LDS holds STAGES lines of each row of both sides, loaded straight into it.  A line is
+// two steps of sixteen elements; a wave reads a step's fragments while the matrix
+// cores work on the step before, so it needs others only once a line: before the last step, when the line's last
+// fragments are in registers, all meet; then its place is free to be loaded, and the next line is there.
+template <int B, int WR, int WC, int STAGES, typename PT>
+__global__ __launch_bounds__(64 * WR * WC, 2) void k_muon_product(Gemms all, Last last) {
+  constexpr int kWaves = WR * WC, kMI = B / WR / 32, kNI = B / WC / 32, kLoads = B / (8 * kWaves), kStage = 2 * B * 128;
+  constexpr int kFragments = 2 * (kMI + kNI), kCalls = 3 * kMI * kNI, kSums = kMI * kNI == 1 ? 3 : 1;
+  static_assert((STAGES & (STAGES - 1)) == 0 && STAGES >= 2 && STAGES * 2 * kLoads <= 63, "stages are told by bits, loads in flight counted");
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  const int per = (all.items + 7) / 8, item = (int)(blockIdx.x % 8) * per + (int)(blockIdx.x / 8);
-  if (item >= all.items || (int)(blockIdx.x / 8) >= per) return;
+  // Workgroups go to the eight XCDs in turn.  Each takes its eighth of the tiles of every
+  // shape, so that all have as much to do, in neighbouring tiles, which share rows in its L2.
+  const int turn = (int)(blockIdx.x / 8);
   int k = 0;
-  while (k + 1 < all.n && item >= all.gemm[k + 1].first) ++k;
+  while (k + 1 < all.n && turn >= all.gemm[k + 1].first) ++k;
   const Gemm& q = all.gemm[k];
-  const int in = item - q.first, which = in / q.tiles, tile = in - which * q.tiles;
+  const int in = (int)(blockIdx.x % 8) * q.share + turn - q.first, which = in / q.tiles, tile = in - which * q.tiles;
+  if (which >= q.count) return;
   int ti, tj;
   if (q.symmetric) {
     triangle_place(tile, q.tiles_a, ti, tj);
@@ -328,61 +338,90 @@ __global__ __launch_bounds__(64 * WR * WC) void k_muon_product(Gemms all, Last l
     ti = tile % q.tiles_a;
     tj = tile / q.tiles_a;
   }
-  const int row0 = ti * B, col0 = tj * B;
+  const int row0 = ti * B, col0 = tj * B, blocks = q.blocks;
   const int64_t own = (int64_t)which * q.step;
-  const uint8_t *a = q.a + own, *b = q.b + own;
+
+  // A wave loads eight rows at once: lane l the chunk that belongs at place l % 8 of row l / 8.
+  const int lr = wave * 8 + lane / 8, lda = q.lda, ldb = q.ldb;
+  const auto ra = buffer_of(q.a + own + (int64_t)row0 * lda, (int64_t)(q.rows_a - row0) * lda);
+  const auto rb = buffer_of(q.b + own + (int64_t)col0 * ldb, (int64_t)(q.rows_b - col0) * ldb);
+  int va = lr * lda + ((lane % 8) ^ row_key(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key(lr)) * 16;
+  auto load_part = [&](int t, int block) {  // 0 .. 2 kLoads - 1: those of a, then those of b
+    const bool of_b = t >= kLoads;
+    const int line = block < blocks ? block : blocks - 1;  // (past the last line it is loaded again, and not used)
+    asm("" : "+v"(va), "+v"(vb));  // (offsets of further rows are formed anew: they would each hold a register)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        of_b ? rb : ra, (__attribute__((address_space(3))) void*)(lds + (block & (STAGES - 1)) * kStage + wave * 1024 + t * kWaves * 1024), 16,
+        of_b ? vb + (t - kLoads) * 8 * kWaves * ldb : va + t * 8 * kWaves * lda, line * 128, 0, 0);
+  };
+
   const int wm = wave / WC * (32 * kMI), wn = wave % WC * (32 * kNI), fr = lane % 32, fg = lane / 32;
-  v16f acc[kMI][kNI];
+  const int key_a = row_key(wm + fr), key_b = row_key(wn + row_of_b(fr));
+  const int a0 = (wm + fr) * 128 + ((fg ^ key_a) << 4), b0 = (B + wn + row_of_b(fr)) * 128 + ((fg ^ key_b) << 4);
+  // Fragments of a step: of b high, of a high, of b low, of a low, in the order of their use.
+  v8h f[2][kFragments];
+  auto read_part = [&](int t, int stage, int step, int to) {
+    const bool low = t >= kMI + kNI;
+    const int r = low ? t - kMI - kNI : t, chunk = (low ? 64 : 0) ^ step * 32;
+    f[to][t] = *reinterpret_cast<const v8h*>(lds + stage * kStage + (r < kNI ? (b0 ^ chunk) + r * 4096 : (a0 ^ chunk) + (r - kNI) * 4096));
+  };
+  v16f acc[kSums][kMI][kNI];
 #pragma unroll
-  for (int i = 0; i < kMI; ++i)
+  for (int k = 0; k < kSums; ++k)
 #pragma unroll
-    for (int j = 0; j < kNI; ++j)
+    for (int i = 0; i < kMI; ++i)
 #pragma unroll
-      for (int t = 0; t < 16; ++t) acc[i][j][t] = 0.0f;
-  constexpr int kLoads = 2 * B * 8 / kGroup;
-  for (int block = 0; block < q.blocks; ++block) {
-    u32x4 got[kLoads];
+      for (int j = 0; j < kNI; ++j)
 #pragma unroll
-    for (int t = 0; t < kLoads; ++t) {
-      const int c = t * kGroup + (int)threadIdx.x, r = c / 8 % B;
-      const bool of_b = c / 8 >= B;
-      const int most = (of_b ? q.rows_b : q.rows_a) - 1, at = (of_b ? col0 : row0) + r;
-      const uint8_t* from = (of_b ? b : a) + (int64_t)(at < most ? at : most) * (of_b ? q.ldb : q.lda) + (int64_t)block * 128;
-      got[t] = *reinterpret_cast<const u32x4*>(from + c % 8 * 16);
-    }
-    __syncthreads();
+        for (int t = 0; t < 16; ++t) acc[k][i][j][t] = 0.0f;
 #pragma unroll
-    for (int t = 0; t < kLoads; ++t) {
-      const int c = t * kGroup + (int)threadIdx.x, r = c / 8;
-      *reinterpret_cast<u32x4*>(lds + r * 128 + (c % 8 ^ row_key(r)) * 16) = got[t];
-    }
-    __syncthreads();
+  for (int s = 0; s < STAGES; ++s)
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      v8h ha[kMI], la[kMI], hb[kNI], lb[kNI];
+    for (int t = 0; t < 2 * kLoads; ++t) load_part(t, s);
+  loads_landed<(STAGES - 1) * 2 * kLoads>();
+  meet();
 #pragma unroll
-      for (int i = 0; i < kMI; ++i) {
-        const int r = wm + i * 32 + fr;
-        ha[i] = *reinterpret_cast<const v8h*>(lds + r * 128 + ((2 * s + fg) ^ row_key(r)) * 16);
-        la[i] = *reinterpret_cast<const v8h*>(lds + r * 128 + ((4 + 2 * s + fg) ^ row_key(r)) * 16);
+  for (int t = 0; t < kFragments; ++t) read_part(t, 0, 0, 0);
+  for (int block = 0; block < blocks; ++block) {
+    const int stage = block & (STAGES - 1), after = (block + 1) & (STAGES - 1);
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+      if (step == 1) {
+        reads_landed();
+        loads_landed<(STAGES - 2) * 2 * kLoads>();
+        meet();
       }
 #pragma unroll
-      for (int j = 0; j < kNI; ++j) {
-        const int r = B + wn + j * 32 + row_of_b(fr);
-        hb[j] = *reinterpret_cast<const v8h*>(lds + r * 128 + ((2 * s + fg) ^ row_key(r)) * 16);
-        lb[j] = *reinterpret_cast<const v8h*>(lds + r * 128 + ((4 + 2 * s + fg) ^ row_key(r)) * 16);
-      }
+      for (int c = 0; c < kCalls; ++c) {
+        // high high, low high, high low: the same sums come up again after kMI kNI instructions (a single one has one for each)
+        const int kind = c / (kMI * kNI), i = c % (kMI * kNI) / kNI, j = c % kNI;
+        const v8h& fb = f[step][(kind == 1 ? kMI + kNI : 0) + j];
+        const v8h& fa = f[step][(kind == 2 ? kMI + kNI : 0) + kNI + i];
+        v16f& sum = acc[kSums == 3 ? kind : 0][i][j];
+        sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(fb, fa, sum, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < kMI; ++i)
+        for (int t = 0; t < kFragments; ++t)
+          if (t * kCalls / kFragments == c) read_part(t, step == 0 ? stage : after, step ^ 1, step ^ 1);
+        if (step == 1) {
 #pragma unroll
-        for (int j = 0; j < kNI; ++j) {
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hb[j], ha[i], acc[i][j], 0, 0, 0);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lb[j], ha[i], acc[i][j], 0, 0, 0);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hb[j], la[i], acc[i][j], 0, 0, 0);
+          for (int t = 0; t < 2 * kLoads; ++t)
+            if (t * kCalls / (2 * kLoads) == c) load_part(t, block + STAGES);
         }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int k = 0; k < kSums; ++k)
+#pragma unroll
+        for (int i = 0; i < kMI; ++i)
+#pragma unroll
+          for (int j = 0; j < kNI; ++j) asm volatile("" : "+v"(acc[k][i][j]));  // (without a use here the instructions would be moved past the next barrier)
     }
   }
-  __syncthreads();
+  // (past the last line its fragments are read again, and not used)
+  reads_landed();
+  loads_landed();
+  meet();
   uint32_t* words = reinterpret_cast<uint32_t*>(lds) + wave * (32 * 33);
   uint8_t* turned = q.symmetric ? (ti == tj ? nullptr : q.out) : q.turned;
   const int ldt = q.symmetric ? q.ldo : q.ldt;
@@ -395,7 +434,7 @@ __global__ __launch_bounds__(64 * WR * WC) void k_muon_product(Gemms all, Last l
       const int64_t line = own + (int64_t)(r0 + fr) * q.ldo + c0 / kLine * 128;
       float v[16], d[16];
 #pragma unroll
-      for (int t = 0; t < 16; ++t) v[t] = q.k0 * acc[i][j][t];
+      for (int t = 0; t < 16; ++t) v[t] = q.k0 * (kSums == 3 ? acc[0][i][j][t] + (acc[kSums / 2][i][j][t] + acc[kSums - 1][i][j][t]) : acc[0][i][j][t]);
       if (q.d1) {
         load_split(q.d1 + line, fg, d);
 #pragma unroll
@@ -448,9 +487,16 @@ int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
 struct Shape {
   int64_t rows, cols;
   int64_t m, n, ldm, ldn;  // padded; bytes of rows of m and n elements
-  int64_t x, xt[2], square[2], bytes;
-  bool tall;
+  int64_t x, xt[2], square[5], bytes;
+  bool tall, wide;  // wide: several steps at once
 };
+
+// How many steps go at once.  One step takes 3 m^2 n + m^3 operations (symmetric results half), k at once
+// 3 m^2 n + (4 k - 3) m^3: five as 3 + 2 instead take 38 in place of 65 m^3 for n = 4 m (2048 x 8192,
+// one matrix: 2.1 ms, one by one 3.0).  Errors of A grow in P A P, where those of X X^T do not: of five steps from 2.2e-6 of the
+// result's norm to 3.1e-6 at 512 x 2048 (fp32 arithmetic throughout: 2.8e-6), but from 1.2e-6 to 5.3e-6 at
+// 37 x 100, and below 512 latency counts, not operations.
+int at_once(int64_t m, int64_t n) { return m >= 512 && 2 * n >= 3 * m ? kMostAtOnce : 1; }
 Shape shape_of(int64_t rows, int64_t cols) {
   Shape s = {};
   s.rows = rows;
@@ -468,7 +514,8 @@ Shape shape_of(int64_t rows, int64_t cols) {
   };
   s.x = take(s.m * s.ldn);
   for (int64_t& t : s.xt) t = take(s.n * s.ldm);
-  for (int64_t& t : s.square) t = take(s.m * s.ldm);
+  s.wide = at_once(s.m, s.n) > 1;
+  for (int i = 0; i < (s.wide ? 5 : 2); ++i) s.square[i] = take(s.m * s.ldm);
   s.bytes = at;
   return s;
 }
@@ -528,85 +575,140 @@ Layout layout_of(const std::vector<Group>& groups, size_t table_rows) {
 }
 
 // The products of a run, one entry per launch.
-std::vector<Gemm> products_of(const Run& run, uint8_t* base, int steps) {
+//
+// A step is X <- P X with P = a I + B, B = b A + c A A.  Steps may be taken several at
+// once: X <- Q X with Q = P_k .. P_1, and A = X X^T of the next step from that of the one before as
+// P A P, all products of m x m matrices that commute and are symmetric, so that half of
+// each is formed.  Q is held as alpha I + R, alpha = a^k: the part that acts on
+// the directions far below 1 has no rounding.
+std::vector<std::vector<Gemm>> products_of(const Run& run, uint8_t* base, int steps) {
   const Shape& s = run.shape;
   uint8_t* at = base + run.at;
-  uint8_t *x = at + s.x, *xt[2] = {at + s.xt[0], at + s.xt[1]}, *sq[2] = {at + s.square[0], at + s.square[1]};
+  uint8_t *x = at + s.x, *xt[2] = {at + s.xt[0], at + s.xt[1]}, *gram = at + s.square[0];
   Gemm zero;
   std::memset(&zero, 0, sizeof zero);
   zero.step = s.bytes;
   zero.count = run.count;
   zero.matrix = run.matrix;
-  std::vector<Gemm> list;
-  auto pow2 = [](int e) { return std::ldexp(1.0, e); };
-  auto square = [&](const uint8_t* a, const uint8_t* b, int64_t ld, int64_t cols, uint8_t* out) {
+  std::vector<std::vector<Gemm>> list;
+  // out 2^e = k 2^e a b^T, of factors held with ea and eb; plus() adds k 2^e d.
+  auto square = [&](const uint8_t* a, int ea, const uint8_t* b, int eb, uint8_t* out, int e, double k) {
     Gemm g = zero;
     g.a = a;
     g.b = b;
     g.out = out;
     g.rows_a = g.rows_b = (int32_t)s.m;
-    g.blocks = (int32_t)(cols / kLine);
-    g.lda = g.ldb = (int32_t)ld;
-    g.ldo = (int32_t)s.ldm;
+    g.blocks = (int32_t)(s.m / kLine);
+    g.lda = g.ldb = g.ldo = (int32_t)s.ldm;
     g.symmetric = 1;
+    g.k0 = (float)std::ldexp(k, e - ea - eb);
     return g;
   };
-  for (int i = 0; i < steps; ++i) {
-    Gemm gram = square(x, x, s.ldn, s.n, sq[0]);
-    gram.k0 = (float)pow2(kA - 2 * kX);
-    list.push_back(gram);
-    Gemm poly = square(sq[0], sq[0], s.ldm, s.m, sq[1]);  // b A + c A A
-    poly.d1 = sq[0];
-    poly.k0 = (float)(kCc * pow2(kB - 2 * kA));
-    poly.k1 = (float)(kCb * pow2(kB - kA));
-    list.push_back(poly);
-    const bool last = i + 1 == steps, flip = last && s.tall;
-    Gemm apply = zero;  // X <- a X + (b A + c A A) X
-    apply.a = flip ? xt[i & 1] : sq[1];
-    apply.b = flip ? sq[1] : xt[i & 1];
-    apply.d1 = flip ? xt[i & 1] : x;
+  auto plus = [](Gemm g, int e, const uint8_t* d, int ed, double k) {
+    (g.d1 ? g.k2 : g.k1) = (float)std::ldexp(k, e - ed);
+    (g.d1 ? g.d2 : g.d1) = d;
+    return g;
+  };
+  for (int done = 0, turn = 0; done < steps; turn ^= 1) {
+    const int now = std::min(s.wide ? at_once(s.m, s.n) : 1, steps - done);
+    Gemm g = square(x, kX, x, kX, gram, kA, 1.0);
+    g.blocks = (int32_t)(s.n / kLine);
+    g.lda = g.ldb = (int32_t)s.ldn;
+    list.push_back({g});
+    uint8_t *poly = at + s.square[1], *r = nullptr, *spare = nullptr, *ap = nullptr;
+    if (now > 1) {
+      ap = at + s.square[2];
+      r = at + s.square[3];
+      spare = at + s.square[4];
+    }
+    double alpha = kCa;
+    int er = kB;
+    for (int i = 0; i < now; ++i) {
+      list.push_back({plus(square(gram, kA, gram, kA, poly, kB, kCc), kB, gram, kA, kCb)});
+      if (i == 0) {
+        std::swap(poly, r);  // Q = a I + B
+        if (now > 1) {
+          list.push_back({plus(square(gram, kA, r, kB, ap, kA, 1.0), kA, gram, kA, kCa)});
+          list.push_back({plus(square(ap, kA, r, kB, gram, kA, 1.0), kA, ap, kA, kCa)});
+        }
+        continue;
+      }
+      // alpha a I + (a R + alpha B + B R)
+      list.push_back({plus(plus(square(poly, kB, r, er, spare, kR, 1.0), kR, r, er, kCa), kR, poly, kB, alpha)});
+      if (i + 1 < now) {
+        list.back().push_back(plus(square(gram, kA, poly, kB, ap, kA, 1.0), kA, gram, kA, kCa));
+        list.push_back({plus(square(ap, kA, poly, kB, gram, kA, 1.0), kA, ap, kA, kCa)});
+      }
+      std::swap(r, spare);
+      er = kR;
+      alpha *= kCa;
+    }
+    done += now;
+    const bool last = done == steps, flip = last && s.tall;
+    Gemm apply = zero;  // X <- alpha X + R X
+    apply.a = flip ? xt[turn] : r;
+    apply.b = flip ? r : xt[turn];
     apply.lda = apply.ldb = (int32_t)s.ldm;
     apply.ldo = (int32_t)(flip ? s.ldm : s.ldn);
     apply.rows_a = (int32_t)(flip ? s.n : s.m);
     apply.rows_b = (int32_t)(flip ? s.m : s.n);
     apply.blocks = (int32_t)(s.m / kLine);
     const int e = last ? 0 : kX;
-    apply.k0 = (float)pow2(e - kB - kX);
-    apply.k1 = (float)(kCa * pow2(e - kX));
+    apply.k0 = (float)std::ldexp(1.0, e - er - kX);
+    apply = plus(apply, e, flip ? xt[turn] : x, kX, alpha);
     if (last) {
       apply.last = 1;
       apply.rows = s.rows;
       apply.cols = s.cols;
     } else {
       apply.out = x;
-      apply.turned = xt[(i & 1) ^ 1];
+      apply.turned = xt[turn ^ 1];
       apply.ldt = (int32_t)s.ldm;
     }
-    list.push_back(apply);
+    list.push_back({apply});
   }
   return list;
 }
 
-constexpr int kTile = 128;
+// Tiles of a launch.  Large ones read less of the L2 for each product, small ones keep more
+// CUs at work; of those of 64 and 128 two workgroups share a CU.  16 matrices of 512 x 512 to
+// 2048 (a step's products, us, with tiles of 64 / 128 / 256): squares 20 / 22 / 51, A = X X^T 34 / 52 / 110,
+// with X (2960 / 744 / 192 tiles) 87 / 69 / 72; four of 2048 x 512 9 / 18 / 48, 18 / 41 / 106, 26 / 22 / 50.
+// 14 matrices of 2048 x 8192: squares 504 / 372 / 360, A 2916 / 1310 / 1189, with X 4822 / 2856 / 2712.
+constexpr int kBig = 256, kMid = 128, kLittle = 64;
+constexpr int64_t kMostLittle = 2048, kMostMid = 1024;
 
 template <typename PT>
-void launch_products(Gemms& all, const Last& last, hipStream_t st) {
-  int64_t items = 0;
-  for (int i = 0; i < all.n; ++i) {
-    Gemm& g = all.gemm[i];
-    g.tiles_a = (g.rows_a + kTile - 1) / kTile;
-    g.tiles_b = (g.rows_b + kTile - 1) / kTile;
-    g.tiles = g.symmetric ? g.tiles_a * (g.tiles_a + 1) / 2 : g.tiles_a * g.tiles_b;
-    g.first = (int32_t)items;
-    items += (int64_t)g.tiles * g.count;
-  }
-  all.items = (int32_t)items;
-  hipLaunchKernelGGL((k_muon_product<kTile, 2, 2, PT>), dim3((unsigned)((items + 7) / 8 * 8)), dim3(256), 0, st, all, last);
+int32_t launch_products(Gemms& all, const Last& last, hipStream_t st, std::string* e) {
+  auto count = [&](int tile) {
+    int64_t items = 0, turns = 0;
+    for (int i = 0; i < all.n; ++i) {
+      Gemm& g = all.gemm[i];
+      g.tiles_a = (g.rows_a + tile - 1) / tile;
+      g.tiles_b = (g.rows_b + tile - 1) / tile;
+      g.tiles = g.symmetric ? g.tiles_a * (g.tiles_a + 1) / 2 : g.tiles_a * g.tiles_b;
+      g.share = (int32_t)(((int64_t)g.tiles * g.count + 7) / 8);
+      g.first = (int32_t)turns;
+      turns += g.share;
+      items += (int64_t)g.tiles * g.count;
+    }
+    return std::make_pair(items, turns);
+  };
+  auto go = [&](auto kernel, int tile, int threads, int stages) {
+    const int bytes = stages * 2 * tile * 128;
+    const int32_t r = allow_lds(reinterpret_cast<const void*>(kernel), bytes, e);
+    if (r != MTDAO_OK) return r;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(8 * count(tile).second)), dim3((unsigned)threads), (size_t)bytes, st, all, last);
+    return (int32_t)MTDAO_OK;
+  };
+  if (count(kLittle).first <= kMostLittle) return go(k_muon_product<kLittle, 2, 2, 4, PT>, kLittle, 256, 4);
+  if (count(kMid).first <= kMostMid) return go(k_muon_product<kMid, 2, 2, 2, PT>, kMid, 256, 2);
+  return go(k_muon_product<kBig, 2, 4, 2, PT>, kBig, 512, 2);
 }
 
 // All the work of a group's matrices.
 template <typename GT, typename PT, bool MUON>
-void launch_group(const Group& group, Source s, const Last& last, uint8_t* factors, int steps, hipStream_t st) {
+int32_t launch_group(const Group& group, Source s, const Last& last, uint8_t* factors, int steps, hipStream_t st, std::string* e) {
   Parts parts;
   std::memset(&parts, 0, sizeof parts);
   int64_t chunks = 0, tiles = 0;
@@ -635,7 +737,7 @@ void launch_group(const Group& group, Source s, const Last& last, uint8_t* facto
   hipLaunchKernelGGL(k_muon_scales, dim3((unsigned)group.matrices), dim3(kThreads), 0, st, parts, s);
   parts.items = (int32_t)tiles;
   hipLaunchKernelGGL((k_muon_split<GT, MUON>), grid_of(tiles), dim3(kThreads), 0, st, parts, s);
-  std::vector<std::vector<Gemm>> lists;
+  std::vector<std::vector<std::vector<Gemm>>> lists;
   size_t most = 0;
   for (const Run& r : group.runs) {
     lists.push_back(products_of(r, factors, steps));
@@ -645,9 +747,12 @@ void launch_group(const Group& group, Source s, const Last& last, uint8_t* facto
     Gemms all;
     std::memset(&all, 0, sizeof all);
     for (const auto& list : lists)
-      if (i < list.size()) all.gemm[all.n++] = list[i];
-    launch_products<PT>(all, last, st);
+      if (i < list.size())
+        for (const Gemm& g : list[i]) all.gemm[all.n++] = g;
+    const int32_t r = launch_products<PT>(all, last, st, e);
+    if (r != MTDAO_OK) return r;
   }
+  return MTDAO_OK;
 }
 
 int32_t check_numbers(int32_t steps, double eps, std::string* e) {
@@ -817,10 +922,11 @@ int32_t mtdao_orthogonalize(const void* x, int32_t dtype, int64_t batch, int64_t
   const Last last = {nullptr, out, 0.0f};
   for (const Group& g : groups) {
     uint8_t* factors = reinterpret_cast<uint8_t*>(w + l.factors);
-    if (dtype == MTDAO_F32 && out_dtype == MTDAO_F32) launch_group<float, float, false>(g, s, last, factors, steps, st);
-    else if (dtype == MTDAO_F32) launch_group<float, bf16_t, false>(g, s, last, factors, steps, st);
-    else if (out_dtype == MTDAO_F32) launch_group<bf16_t, float, false>(g, s, last, factors, steps, st);
-    else launch_group<bf16_t, bf16_t, false>(g, s, last, factors, steps, st);
+    if (dtype == MTDAO_F32 && out_dtype == MTDAO_F32) r = launch_group<float, float, false>(g, s, last, factors, steps, st, e);
+    else if (dtype == MTDAO_F32) r = launch_group<float, bf16_t, false>(g, s, last, factors, steps, st, e);
+    else if (out_dtype == MTDAO_F32) r = launch_group<bf16_t, float, false>(g, s, last, factors, steps, st, e);
+    else r = launch_group<bf16_t, bf16_t, false>(g, s, last, factors, steps, st, e);
+    if (r != MTDAO_OK) return r;
   }
   return hip_check(e, hipGetLastError(), "mtdao_orthogonalize launch");
 } catch (const std::bad_alloc&) {
@@ -899,11 +1005,13 @@ int32_t mtdao_muon_step(mtdao_muon* h, double lr, void* hip_stream) try {
                     (float)c.momentum, c.nesterov != 0, c.eps};
   const Last last = {rows, nullptr, (float)lr};
   uint8_t* factors = reinterpret_cast<uint8_t*>(w + h->layout.factors);
+  int32_t r = MTDAO_OK;
   for (const Group& g : h->groups) {
-    if (c.param_dtype == MTDAO_F32 && c.grad_dtype == MTDAO_F32) launch_group<float, float, true>(g, s, last, factors, c.steps, st);
-    else if (c.param_dtype == MTDAO_F32) launch_group<bf16_t, float, true>(g, s, last, factors, c.steps, st);
-    else if (c.grad_dtype == MTDAO_F32) launch_group<float, bf16_t, true>(g, s, last, factors, c.steps, st);
-    else launch_group<bf16_t, bf16_t, true>(g, s, last, factors, c.steps, st);
+    if (c.param_dtype == MTDAO_F32 && c.grad_dtype == MTDAO_F32) r = launch_group<float, float, true>(g, s, last, factors, c.steps, st, &h->err);
+    else if (c.param_dtype == MTDAO_F32) r = launch_group<bf16_t, float, true>(g, s, last, factors, c.steps, st, &h->err);
+    else if (c.grad_dtype == MTDAO_F32) r = launch_group<float, bf16_t, true>(g, s, last, factors, c.steps, st, &h->err);
+    else r = launch_group<bf16_t, bf16_t, true>(g, s, last, factors, c.steps, st, &h->err);
+    if (r != MTDAO_OK) return r;
   }
   return hip_check(&h->err, hipGetLastError(), "mtdao_muon_step launch");
 } catch (const std::bad_alloc&) {

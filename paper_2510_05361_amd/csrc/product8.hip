@@ -4,9 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <mutex>
 #include <new>
-#include <set>
 #include <string>
 #include <type_traits>
 #include <utility>
@@ -993,22 +991,6 @@ int32_t launch_few_whole(const void* x, int32_t dtype, int64_t rows, int64_t ld,
   else if (y_dtype == MTDAO_BF16) launch_few<float, bf16_t, 1>(f, st);
   else launch_few<float, float, 1>(f, st);
   return MTDAO_OK;
-}
-
-// More than 64 KiB of LDS for a kernel, asked for once per kernel and device.
-int32_t allow_lds(const void* kernel, int bytes, std::string* e) try {
-  static std::mutex lock;
-  static std::set<std::pair<const void*, int>> done;
-  int device = 0;
-  int32_t r = hip_check(e, hipGetDevice(&device), "mtdao_product8 device");
-  if (r != MTDAO_OK) return r;
-  std::lock_guard<std::mutex> held(lock);
-  if (done.count({kernel, device})) return MTDAO_OK;
-  r = hip_check(e, hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes), "mtdao_product8 LDS");
-  if (r == MTDAO_OK) done.insert({kernel, device});
-  return r;
-} catch (const std::bad_alloc&) {
-  return fail(e, MTDAO_ERR_WORKSPACE, "out of host memory");
 }
 
 // a, b, c: checked; c has elements.

@@ -64,14 +64,14 @@ def test_sizes(r, c, t):
 
 
 @pytest.mark.parametrize("kind", ["noise", "low", "steep"])
-@pytest.mark.parametrize("r,c", [(60, 90), (200, 150), (384, 384), (256, 1024), (1100, 260)])
+@pytest.mark.parametrize("r,c", [(60, 90), (200, 150), (384, 384), (256, 1024), (1100, 260), (1600, 513)])
 def test_spectra(r, c, kind):
     x = matrix(r, c, 3, kind)
     check(ops.orthogonalize(x.cuda()), x)
 
 
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 6, 7, 10])
-@pytest.mark.parametrize("r,c", [(70, 200), (130, 140), (256, 800)])
+@pytest.mark.parametrize("r,c", [(70, 200), (130, 140), (256, 800), (520, 900)])
 def test_steps(steps, r, c):
     x = matrix(r, c, 4)
     check(ops.orthogonalize(x.cuda(), steps=steps), x, steps)
