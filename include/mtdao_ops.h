@@ -301,7 +301,7 @@ void mtdao_muon_destroy(mtdao_muon* h);
  *
  * Backward: dw[r] = scale sum of dy[i] over the places i with tokens[i] == r
  * (accumulate: dw[r] +=, and rows of tokens that do not come are not touched),
- * fp32 sums in the order of the places, in pieces of 64; tokens outside the
+ * fp32 sums in the order of the places, in pieces of 32; tokens outside the
  * table are left out.  Results depend on the operands alone.
  * workspace: 256-byte aligned. */
 int32_t mtdao_embedding(const void* tokens, int32_t token_bits, int64_t n_tokens, const void* table, int32_t table_dtype, int64_t rows,
@@ -343,7 +343,7 @@ typedef struct mtdao_cross_entropy_args {
   void* d_logits;        /* or NULL; may be logits itself when the strides are equal   */
 } mtdao_cross_entropy_args;
 
-/* Reads the sizes of a.  Host-only.  workspace: 256-byte aligned. */
+/* Reads the sizes and the reduction of a.  Host-only.  workspace: 256-byte aligned. */
 int32_t mtdao_cross_entropy_workspace_bytes(const mtdao_cross_entropy_args* a, size_t* bytes);
 int32_t mtdao_cross_entropy(const mtdao_cross_entropy_args* a, void* workspace, size_t workspace_bytes, void* hip_stream);
 

@@ -1,7 +1,10 @@
 // Cross entropy of rows of logits and its gradient (include/mtdao_ops.h).
 //
-// A workgroup takes a row: its largest logit m, the sum s of exp(x - m), then the
-// gradient.  The loss is log s - (x_target - m), which loses nothing where the
+// For the gradient a row of up to 65536 logits (bf16: 131072) lies in the registers of a wave or a workgroup,
+// as it is in memory, and is read once: its largest logit m, the sum s of exp(x - m), then the
+// gradient.  The loss alone is formed as the row streams by, with a running maximum; so
+// is that of longer rows, which are read again for their gradient.
+// The loss is log s - (x_target - m), which loses nothing where the
 // target is all but certain, as lse - x_target would.
 
 #include <hip/hip_runtime.h>
@@ -19,8 +22,8 @@ using namespace mtdao::ops;
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kE = 8;          // elements of a thread's vector
+template <typename T>
+constexpr int kE = 16 / (int)sizeof(T);  // elements of a thread's vector: 16 bytes
 constexpr int kFinish = 1024;  // threads of the kernels over all rows
 
 struct Args {
@@ -39,81 +42,215 @@ __device__ __forceinline__ int64_t id_of(const void* ids, int32_t wide, int64_t 
   return wide ? reinterpret_cast<const int64_t*>(ids)[i] : (int64_t) reinterpret_cast<const int32_t*>(ids)[i];
 }
 
-// Largest and sum over the workgroup, in every thread.
-template <int WAVES>
-__device__ __forceinline__ float group_max(float x, float* part) {
+// Largest and sum over the THREADS threads of a row (a wave, or the workgroup), in each.
+template <int THREADS>
+__device__ __forceinline__ float row_max(float x, float* part) {
   x = max_with32(max32(x));
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = x;
-  __syncthreads();
+  if constexpr (THREADS > 64) {
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = x;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) x = fmaxf(x, part[w]);
+    for (int w = 0; w < THREADS / 64; ++w) x = fmaxf(x, part[w]);
+  }
   return x;
 }
-template <int WAVES>
-__device__ __forceinline__ float group_sum(float x, float* part) {
+template <int THREADS>
+__device__ __forceinline__ float row_sum(float x, float* part) {
   x = sum64(x);
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = x;
-  __syncthreads();
-  x = 0.0f;
+  if constexpr (THREADS > 64) {
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = x;
+    __syncthreads();
+    x = 0.0f;
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) x += part[w];
+    for (int w = 0; w < THREADS / 64; ++w) x += part[w];
+  }
   return x;
 }
 
 constexpr float kLog2e = 1.44269504f;
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
+// A vector as it is in memory.  (Of fp32 four: with eight, two loads apart by a lane's 32
+// bytes, 2047 x 32003 took 139 us.)
+template <typename T, bool NT>
+struct Vector : Raw<T, NT> {};
+template <bool NT>
+struct Vector<float, NT> {
+  float w[4];
+  __device__ __forceinline__ void load(const float* p, int n) { load_some<4, NT>(p, n, w); }
+  __device__ __forceinline__ void values(float (&o)[4]) const {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] = w[t];
+  }
+};
+
+// A vector's logits, minus infinity from n on.
+template <typename R, int N>
+__device__ __forceinline__ void logits_of(const R& raw, int n, float (&v)[N]) {
+  raw.values(v);
+  if (n < N) {
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+      if (t >= n) v[t] = -INFINITY;
+  }
+}
+
+// What a row's target asks for.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_cross_entropy(Args a) {
-  __shared__ float part[kThreads / 64];
+struct Target {
+  int64_t at;   // < 0: nothing
+  bool known;
+  float x;      // its logit
+  __device__ __forceinline__ Target(const Args& a, const T* x, int64_t row) : at(id_of(a.targets, a.wide, row)) {
+    known = at < a.cols;
+    this->x = at < 0 ? 0.0f : known ? to_f32(x[at]) : NAN;
+  }
+};
+
+// The row's loss from m and s (one thread stores it), and the factors of its gradient: of exp(x - m) and of the target.
+struct Weights {
+  float each, target;
+};
+template <typename T>
+__device__ __forceinline__ Weights weights_of(const Args& a, const Target<T>& target, int64_t row, float m, float s, bool stores) {
+  const float log_s = logf(s), lse = m + log_s;
+  if (a.losses && stores) a.losses[row] = log_s - (target.x - m) + (a.z != 0.0f ? a.z * lse * lse : 0.0f);
+  float w = a.scale;
+  if (a.weight) w *= *a.weight;
+  if (a.d_loss) w *= a.d_loss[a.each ? row : 0];
+  if (!target.known) w = NAN;
+  return {w * (a.z != 0.0f ? 1.0f + 2.0f * a.z * lse : 1.0f) / s, w};
+}
+
+// A vector of the gradient (the first n elements), the target's counted from the first.
+template <bool NT, typename T, int N>
+__device__ __forceinline__ void store_gradient(T* d, int n, float (&v)[N], float m, const Weights& w, int64_t target) {
+#pragma unroll
+  for (int t = 0; t < N; ++t) v[t] = w.each * exp_of(v[t] - m);
+  if (target >= 0 && target < N) {
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+      if (t == target) v[t] -= w.target;
+  }
+  store_some<N, NT>(d, n, v);
+}
+
+// Nothing is asked of the row, and nothing of it is read.
+template <int THREADS, typename T>
+__device__ __forceinline__ void store_nothing(const Args& a, T* d, int64_t row, int tid) {
+  if (a.losses && tid == 0) a.losses[row] = 0.0f;
+  constexpr int N = kE<T>;
+  const float none[N] = {};
+  if (d)
+    for (int64_t e = tid * N; e < a.cols; e += THREADS * N) store_some<N>(d + e, a.cols - e > N ? N : (int)(a.cols - e), none);
+}
+
+// Rows in registers: THREADS threads (64: four rows a workgroup) with NV vectors each.  Where
+// they fit 64 registers two workgroups share a CU, and one's loads fill the other's sums and stores.
+template <typename T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS > 64 ? THREADS : 4 * THREADS, NV <= (sizeof(T) == 2 ? 7 : 8) ? 8 : 4) void k_cross_entropy_held(Args a) {
+  __shared__ float part[THREADS / 64];
+  constexpr int N = kE<T>, kRows = THREADS > 64 ? 1 : 4, kApart = THREADS * N;
+  const int tid = (int)threadIdx.x % THREADS;
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRows + (int)threadIdx.x / THREADS;
+  if (row >= a.rows) return;
+  const T* x = reinterpret_cast<const T*>(a.logits) + row * a.ld;
+  T* d = a.d_logits ? reinterpret_cast<T*>(a.d_logits) + row * a.ld_d : nullptr;
+  const Target<T> target(a, x, row);
+  if (target.at < 0) return store_nothing<THREADS>(a, d, row, tid);
+  const int left = (int)a.cols - tid * N;  // elements from the thread's first vector on
+  x += tid * N;
+  Vector<T, true> raw[NV];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) raw[k].load(x + k * kApart, left - k * kApart);
+  float m = -INFINITY, v[N];
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    if (left > k * kApart) {
+      logits_of(raw[k], left - k * kApart, v);
+#pragma unroll
+      for (int t = 0; t < N; ++t) m = fmaxf(m, v[t]);
+    }
+  }
+  m = row_max<THREADS>(m, part);
+  float s = 0.0f;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    if (left > k * kApart) {
+      logits_of(raw[k], left - k * kApart, v);
+#pragma unroll
+      for (int t = 0; t < N; ++t) s += exp_of(v[t] - m);
+    }
+  }
+  s = row_sum<THREADS>(s, part);
+  const Weights w = weights_of(a, target, row, m, s, tid == 0);
+  if (!d) return;
+  d += tid * N;
+  const int at = target.known ? (int)target.at - tid * N : -1;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int n = left - k * kApart;
+    if (n > 0) {
+      logits_of(raw[k], n, v);
+      store_gradient<true>(d + k * kApart, n, v, m, w, at - k * kApart);
+    }
+  }
+}
+
+// Rows that stream by.  Each thread keeps the largest of its logits so far and the sum of exp(x - it).
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_cross_entropy(Args a) {
+  __shared__ float part[THREADS / 64];
+  constexpr int N = kE<T>, kAtOnce = 16 / N * 2;
+  const int tid = (int)threadIdx.x;
   const int64_t row = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   if (row >= a.rows) return;
   const T* x = reinterpret_cast<const T*>(a.logits) + row * a.ld;
   T* d = a.d_logits ? reinterpret_cast<T*>(a.d_logits) + row * a.ld_d : nullptr;
-  const int64_t target = id_of(a.targets, a.wide, row);
-  const float none[kE] = {};
-  if (target < 0) {  // nothing is asked of this row, and nothing of it is read
-    if (a.losses && threadIdx.x == 0) a.losses[row] = 0.0f;
-    if (d)
-      for (int64_t e = threadIdx.x * kE; e < a.cols; e += kThreads * kE) store_some<kE>(d + e, a.cols - e > kE ? kE : (int)(a.cols - e), none);
-    return;
-  }
-  const bool known = target < a.cols;
-  const float at_target = known ? to_f32(x[target]) : NAN;
-  float m = -INFINITY, v[kE];
-  for (int64_t e = threadIdx.x * kE; e < a.cols; e += kThreads * kE) {
-    const int n = a.cols - e > kE ? kE : (int)(a.cols - e);
-    load_some<kE>(x + e, n, v);
+  const Target<T> target(a, x, row);
+  if (target.at < 0) return store_nothing<THREADS>(a, d, row, tid);
+  float mine = -INFINITY, s = 0.0f, v[N];
+  for (int64_t from = 0; from < a.cols; from += kAtOnce * THREADS * N) {
+    Vector<T, false> raw[kAtOnce];
+    int n[kAtOnce];
 #pragma unroll
-    for (int t = 0; t < kE; ++t)
-      if (t < n) m = fmaxf(m, v[t]);
-  }
-  m = group_max<kThreads / 64>(m, part);
-  float s = 0.0f;
-  for (int64_t e = threadIdx.x * kE; e < a.cols; e += kThreads * kE) {
-    const int n = a.cols - e > kE ? kE : (int)(a.cols - e);
-    load_some<kE>(x + e, n, v);
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int64_t e = from + (k * THREADS + tid) * N, left = a.cols - e;
+      n[k] = left > N ? N : left < 0 ? 0 : (int)left;
+      raw[k].load(x + e, n[k]);
+    }
+    float most = mine;
 #pragma unroll
-    for (int t = 0; t < kE; ++t)
-      if (t < n) s += exp_of(v[t] - m);
+    for (int k = 0; k < kAtOnce; ++k) {
+      logits_of(raw[k], n[k], v);
+#pragma unroll
+      for (int t = 0; t < N; ++t) most = fmaxf(most, v[t]);
+    }
+    if (most > mine) {
+      s *= exp_of(mine - most);
+      mine = most;
+    }
+    const float base = mine == -INFINITY ? 0.0f : mine;  // (nothing above minus infinity so far: terms of 0, not NaN)
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      logits_of(raw[k], n[k], v);
+#pragma unroll
+      for (int t = 0; t < N; ++t) s += exp_of(v[t] - base);
+    }
   }
-  s = group_sum<kThreads / 64>(s, part);
-  const float log_s = logf(s), lse = m + log_s;
-  if (a.losses && threadIdx.x == 0) a.losses[row] = log_s - (at_target - m) + (a.z != 0.0f ? a.z * lse * lse : 0.0f);
+  const float m = row_max<THREADS>(mine, part);
+  // (of a thread without a logit, or with none above minus infinity, s is 0; where no thread has one it is NaN)
+  s = row_sum<THREADS>(mine > -INFINITY ? s * exp_of(mine - m) : m > -INFINITY ? s : NAN, part);
+  const Weights w = weights_of(a, target, row, m, s, tid == 0);
   if (!d) return;
-  float weight = a.scale;
-  if (a.weight) weight *= *a.weight;
-  if (a.d_loss) weight *= a.d_loss[a.each ? row : 0];
-  if (!known) weight = NAN;
-  const float of_each = weight * (1.0f + 2.0f * a.z * lse) / s;
-  for (int64_t e = threadIdx.x * kE; e < a.cols; e += kThreads * kE) {
-    const int n = a.cols - e > kE ? kE : (int)(a.cols - e);
-    load_some<kE>(x + e, n, v);
-#pragma unroll
-    for (int t = 0; t < kE; ++t) v[t] = of_each * exp_of(v[t] - m) - (e + t == target ? weight : 0.0f);
-    store_some<kE>(d + e, n, v);
+  for (int64_t e = tid * N; e < a.cols; e += THREADS * N) {
+    const int n = a.cols - e > N ? N : (int)(a.cols - e);
+    Vector<T, false> raw;
+    raw.load(x + e, n);
+    logits_of(raw, n, v);
+    store_gradient<false>(d + e, n, v, m, w, target.at - e);
   }
 }
 
@@ -121,6 +258,7 @@ __global__ __launch_bounds__(kThreads) void k_cross_entropy(Args a) {
 __global__ __launch_bounds__(kFinish) void k_cross_entropy_count(const void* targets, int32_t wide, int64_t rows, float* weight) {
   __shared__ int64_t part[kFinish / 64];
   int64_t n = 0;
+#pragma unroll 8
   for (int64_t i = threadIdx.x; i < rows; i += kFinish) n += id_of(targets, wide, i) >= 0;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
@@ -140,6 +278,7 @@ __global__ __launch_bounds__(kFinish) void k_cross_entropy_sum(const float* loss
   __shared__ int64_t counted[kFinish / 64];
   double sum = 0.0;
   int64_t n = 0;
+#pragma unroll 8
   for (int64_t i = threadIdx.x; i < rows; i += kFinish) {
     sum += losses[i];
     n += id_of(targets, wide, i) >= 0;
@@ -203,10 +342,38 @@ int32_t check_pointers(const mtdao_cross_entropy_args& a, std::string* e) {
   return MTDAO_OK;
 }
 
+template <typename T, int THREADS, int NV>
+void launch_held(const Args& k, hipStream_t st) {
+  constexpr int rows = THREADS > 64 ? 1 : 4;
+  hipLaunchKernelGGL((k_cross_entropy_held<T, THREADS, NV>), grid_of((k.rows + rows - 1) / rows), dim3(THREADS * rows), 0, st, k);
+}
+template <typename T>
+void launch_rows(const Args& k, hipStream_t st) {
+  const int64_t c = k.cols;
+  constexpr int W = 8 / kE<T>;  // vectors of eight elements
+  if (c <= 512) return launch_held<T, 64, W>(k, st);
+  if (c <= 1024) return launch_held<T, 64, 2 * W>(k, st);
+  if (c <= 2048) return launch_held<T, 64, 4 * W>(k, st);
+  if (c <= 4096) return launch_held<T, 256, 2 * W>(k, st);
+  if (c <= 8192) return launch_held<T, 256, 4 * W>(k, st);
+  if (k.d_logits) {
+    if (c <= 16384) return launch_held<T, 512, 4 * W>(k, st);
+    if (c <= 32768) return launch_held<T, 1024, 4 * W>(k, st);
+    if (c <= 57344) return launch_held<T, 1024, 7 * W>(k, st);
+    if (c <= 65536) return launch_held<T, 1024, 8 * W>(k, st);
+    if constexpr (sizeof(T) == 2) {
+      if (c <= 131072) return launch_held<T, 1024, 16>(k, st);
+    }
+  }
+  if (k.rows < 512 || k.d_logits) hipLaunchKernelGGL((k_cross_entropy<T, 1024>), grid_of(k.rows), dim3(1024), 0, st, k);
+  else hipLaunchKernelGGL((k_cross_entropy<T, 256>), grid_of(k.rows), dim3(256), 0, st, k);
+}
+
 struct Layout {
   size_t losses, weight, bytes;
 };
 Layout layout_of(const mtdao_cross_entropy_args& a) {
+  if (a.reduction == MTDAO_LOSS_NONE) return {0, 0, 0};
   return {0, up256((size_t)a.rows * sizeof(float)), up256((size_t)a.rows * sizeof(float)) + 256};
 }
 
@@ -229,9 +396,9 @@ int32_t mtdao_cross_entropy(const mtdao_cross_entropy_args* args, void* workspac
   if (r != MTDAO_OK) return r;
   const mtdao_cross_entropy_args& a = *args;
   const Layout l = layout_of(a);
-  if (!workspace || workspace_bytes < l.bytes)
+  if (l.bytes > 0 && (!workspace || workspace_bytes < l.bytes))
     return fail(e, MTDAO_ERR_WORKSPACE, "workspace of %zu bytes required, %zu given", l.bytes, workspace ? workspace_bytes : (size_t)0);
-  if (!aligned_to(workspace, 256)) return fail(e, MTDAO_ERR_ALIGN, "workspace is not 256-byte aligned");
+  if (l.bytes > 0 && !aligned_to(workspace, 256)) return fail(e, MTDAO_ERR_ALIGN, "workspace is not 256-byte aligned");
   char* w = static_cast<char*>(workspace);
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   RoctxRange range("mtdao_cross_entropy %lld x %lld", (long long)a.rows, (long long)a.cols);
@@ -244,8 +411,8 @@ int32_t mtdao_cross_entropy(const mtdao_cross_entropy_args* args, void* workspac
       hipLaunchKernelGGL(k_cross_entropy_count, dim3(1), dim3(kFinish), 0, st, a.targets, k.wide, a.rows, weight);
       k.weight = weight;
     }
-    if (a.dtype == MTDAO_BF16) hipLaunchKernelGGL(k_cross_entropy<bf16_t>, grid_of(a.rows), dim3(kThreads), 0, st, k);
-    else hipLaunchKernelGGL(k_cross_entropy<float>, grid_of(a.rows), dim3(kThreads), 0, st, k);
+    if (a.dtype == MTDAO_BF16) launch_rows<bf16_t>(k, st);
+    else launch_rows<float>(k, st);
   }
   if (a.loss)
     hipLaunchKernelGGL(k_cross_entropy_sum, dim3(1), dim3(kFinish), 0, st, k.losses, a.targets, k.wide, a.rows, (int32_t)(a.reduction == MTDAO_LOSS_MEAN),

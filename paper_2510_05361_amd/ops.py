@@ -698,9 +698,12 @@ class _Linear8(torch.autograd.Function):
 # -------------------------------------------------------------- embedding
 
 
+_BITS = {torch.int32: 32, torch.int64: 64}
+
+
 def _ids(t: torch.Tensor, what: str) -> Tuple[torch.Tensor, int]:
     """t contiguous, and its bits."""
-    bits = {torch.int32: 32, torch.int64: 64}.get(t.dtype)
+    bits = _BITS.get(t.dtype)
     if bits is None:
         raise TypeError(f"{what} must be int32 or int64, not {t.dtype}")
     return t.contiguous(), bits
@@ -779,8 +782,8 @@ _REDUCTIONS = {"none": c_ops.MTDAO_LOSS_NONE, "sum": c_ops.MTDAO_LOSS_SUM, "mean
 
 
 @functools.lru_cache(maxsize=256)
-def _loss_workspace(rows: int, cols: int) -> int:
-    return c_ops.mtdao_cross_entropy_workspace_bytes(c_ops.PACKED_LOSS.pack(rows, cols, cols, cols, 0, 32, 0, 0.0, 1.0, 0, *(0,) * 6))
+def _loss_workspace(rows: int, cols: int, reduction: int) -> int:
+    return c_ops.mtdao_cross_entropy_workspace_bytes(c_ops.PACKED_LOSS.pack(rows, cols, cols, cols, 0, 32, reduction, 0.0, 1.0, 0, *(0,) * 6))
 
 
 def _loss(logits, targets, z_loss, reduction, *, loss=False, gradient=False, d_loss=None, scale=1.0, in_place=False):
@@ -802,12 +805,13 @@ def _loss(logits, targets, z_loss, reduction, *, loss=False, gradient=False, d_l
         if in_place and x.data_ptr() != logits.data_ptr():
             raise ValueError(f"logits with strides {logits.stride()} cannot be written in place")
     if rows or made is not None and not each:
-        need = _loss_workspace(rows, cols)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        how = _REDUCTIONS[reduction]
+        need = _loss_workspace(rows, cols, how)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+        ld, at = _ld(x), _ptr(made)
         c_ops.mtdao_cross_entropy(
-            c_ops.PACKED_LOSS.pack(rows, cols, _ld(x), _ld(x) if in_place else cols, kind, bits, _REDUCTIONS[reduction], z_loss, scale, 0,
-                                   x.data_ptr(), ids.data_ptr(), _ptr(d_loss), made.data_ptr() if loss and each else 0,
-                                   made.data_ptr() if loss and not each else 0, _ptr(d)), ws.data_ptr(), need, _stream(logits))
+            c_ops.PACKED_LOSS.pack(rows, cols, ld, ld if in_place else cols, kind, bits, how, z_loss, scale, 0, x.data_ptr(), ids.data_ptr(),
+                                   _ptr(d_loss), at if each else 0, 0 if each else at, _ptr(d)), _ptr(ws), need, _stream(logits))
     if in_place and not logits.is_inference():
         increment_version(logits)
     return made, d

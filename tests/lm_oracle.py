@@ -45,14 +45,14 @@ def embedding(tokens, table, scale):
 
 
 def embedding_backward(dy, tokens, rows, scale):
-    """(dw, bound): fp32 sums of pieces of 64 rows, and of the pieces."""
+    """(dw, bound): fp32 sums of pieces of 32 rows, and of the pieces."""
     dw, mag = torch.zeros((rows, dy.shape[-1]), dtype=torch.float64), torch.zeros((rows, dy.shape[-1]), dtype=torch.float64)
     ids, dy = tokens.reshape(-1), dy.reshape(-1, dy.shape[-1])
     use = (ids >= 0) & (ids < rows)
     dw.index_add_(0, ids[use], dy[use])
     mag.index_add_(0, ids[use], dy[use].abs())
     count = torch.bincount(ids[use], minlength=rows).double()
-    adds = count.clamp(max=64) + (count / 64).ceil() + 3
+    adds = count.clamp(max=32) + (count / 32).ceil() + 3
     return dw * scale, adds[:, None] * U * mag * abs(scale)
 
 

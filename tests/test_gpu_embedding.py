@@ -67,7 +67,7 @@ def check_sums(got, dy, tokens, rows, scale, before=None):
 
 @pytest.mark.parametrize("y", ["f32", "bf16"])
 @pytest.mark.parametrize("kind", ["log", "even", "one"])
-@pytest.mark.parametrize("n,rows,d", [(1, 1, 1), (1, 70000, 8), (2, 3, 130), (63, 9, 16), (65, 2, 16), (129, 1, 40), (1000, 300, 72), (4096, 256, 24), (4097, 257, 8),
+@pytest.mark.parametrize("n,rows,d", [(16384, 65535, 8), (16384, 65536, 8), (16384, 262143, 4), (16384, 262144, 4), (16385, 1000, 8), (300000, 3000, 4), (1025, 70000, 8), (2048, 65535, 8), (2048, 262143, 4), (2048, 262144, 4), (2049, 300, 4), (65536, 500000, 4), (65537, 260, 4), (1, 1, 1), (1, 70000, 8), (2, 3, 130), (63, 9, 16), (65, 2, 16), (129, 1, 40), (1000, 300, 72), (4096, 256, 24), (4097, 257, 8),
                                       (9000, 66000, 16), (20011, 17, 33), (300, 40, 2048)])
 def test_sums(n, rows, d, kind, y):
     tokens = tokens_of((n,), rows, kind=kind, ids=torch.int32 if n % 2 else torch.int64)
