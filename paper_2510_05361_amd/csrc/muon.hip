@@ -62,6 +62,7 @@ struct Row {
   const void* g;
   float* m;
   float decay, factor;
+  int32_t rows, cols;
 };
 
 // Matrices of one shape: what the passes over elements need.
@@ -467,6 +468,222 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_muon_product(Gemms all, Las
     }
 }
 
+// ------------------------------------------------------------ small matrices
+
+// Matrices of up to 64 x 256 (or 256 x 64), all of whose work one workgroup does: X and its transpose
+// lie in LDS, lines as in memory, A and then b A + c A A in a third place; X, to which each step adds,
+// also in registers, as the fp32 it is formed in.  Wave w has the w-th 32 columns of X, the first one
+// to three waves the blocks of A on and above the diagonal.  MB: blocks of X's rows.
+// Bound by latency, of the steps' five meetings and chains of matrix instructions: 100 x 37 through
+// the launches that large matrices take 85 us.
+constexpr int kTinyM = 64, kTinyN = 256, kTinyThreads = 512;
+
+struct Tiny {
+  int32_t first, lines;   // of the table; lines of X's rows
+  int64_t rows, cols;     // matrices one after another (no table)
+  int32_t steps;
+};
+
+// Chunk `chunk` (16 bytes) of line `line` in a row of LINES lines.  Rows lie 256 bytes, all banks, or a multiple
+// apart where there are more than one: then the row's last bit swaps neighbouring lines.
+template <bool ONE>
+__device__ __forceinline__ int chunk_at(int row, int line, int chunk, int stride) {
+  return row * stride + (ONE ? line : line ^ (row & 1)) * 128 + ((chunk ^ row_key(row)) << 4);
+}
+
+template <typename GT, typename PT, bool MUON, int MB>
+__global__ __launch_bounds__(kTinyThreads) void k_muon_tiny(Tiny t, Source s, Last last) {
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  __shared__ double part[kTinyThreads / 64];
+  constexpr int kM = 32 * MB, kBlocks = MB * (MB + 1) / 2;
+  const int tid = (int)threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), fr = lane % 32, fg = lane / 32;
+  const int xs = t.lines * 128, ts = MB * 128;      // bytes of a row of X, and of X^T and A
+  uint8_t *X = lds, *T = X + kM * xs, *A = T + t.lines * kLine * ts;
+  const int which = t.first + (int)blockIdx.x;
+  const Row* entry = MUON ? s.rows + which : nullptr;
+  const int r = MUON ? entry->rows : (int)t.rows, c = MUON ? entry->cols : (int)t.cols;
+  const bool tall = r > c;
+  const int n = tall ? r : c, blocks = (n + kLine - 1) / kLine;  // columns of X
+  const GT* g;
+  float* mom = nullptr;
+  if (MUON) {
+    g = reinterpret_cast<const GT*>(entry->g);
+    mom = entry->m;
+  } else {
+    g = reinterpret_cast<const GT*>(s.x) + (int64_t)which * r * c;
+  }
+  auto at_x = [&](int row, int line, int chunk) { return X + chunk_at<false>(row, line, chunk, xs); };
+  auto at_t = [&](int row, int line, int chunk) { return T + chunk_at<MB == 1>(row, line, chunk, ts); };
+  auto at_a = [&](int row, int line, int chunk) { return A + chunk_at<MB == 1>(row, line, chunk, ts); };
+  // one element of a row, hi and lo
+  auto put = [&](auto at, int row, int col, uint32_t w) {
+    *reinterpret_cast<uint16_t*>(at(row, col / kLine, col % kLine / 8) + col % 8 * 2) = (uint16_t)w;
+    *reinterpret_cast<uint16_t*>(at(row, col / kLine, 4 + col % kLine / 8) + col % 8 * 2) = (uint16_t)(w >> 16);
+  };
+
+  for (int i = tid; i < (kM * xs + t.lines * kLine * ts) / 16; i += kTinyThreads) reinterpret_cast<u32x4*>(lds)[i] = u32x4{0, 0, 0, 0};
+  constexpr int kSlots = kTinyM * kTinyN / 8 / kTinyThreads;
+  const int vectors = (c + 7) / 8, all = r * vectors;
+  float u[kSlots][8];
+  double sum = 0.0;
+#pragma unroll
+  for (int q = 0; q < kSlots; ++q) {
+    const int v = q * kTinyThreads + tid, row = v / vectors, col = (v - row * vectors) * 8, e = row * c + col;
+    const int live = v < all ? (c - col > 8 ? 8 : c - col) : 0;
+    load_some<8>(g + e, live, u[q]);
+    if (MUON) {
+      float m[8];
+      load_some<8>(mom + e, live, m);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[i] = fmaf(s.momentum, m[i], u[q][i]);
+      if (live > 0) store_some<8>(mom + e, live, m);
+      update_of(s, u[q], m, u[q]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += (double)u[q][i] * (double)u[q][i];
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if (lane == 0) part[wave] = sum;
+  __syncthreads();
+  sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < kTinyThreads / 64; ++w) sum += part[w];
+  const double scale = (double)(1 << kX) / (sqrt(sum) + s.eps);
+#pragma unroll
+  for (int q = 0; q < kSlots; ++q) {
+    const int v = q * kTinyThreads + tid, row = v / vectors, col = (v - row * vectors) * 8;
+    if (v >= all) continue;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (col + i < c) {
+        const uint32_t w = split_of((float)((double)u[q][i] * scale));
+        if (tall) {
+          put(at_t, row, col + i, w);
+          put(at_x, col + i, row, w);
+        } else {
+          put(at_x, row, col + i, w);
+          put(at_t, col + i, row, w);
+        }
+      }
+    }
+  }
+  __syncthreads();
+
+  // sums of hi hi, lo hi and hi lo of 32 rows of a and of b over `lines` lines
+  auto product = [&](auto at_rows, int row0, auto at_cols, int col0, int lines, float (&v)[16]) {
+    v16f acc[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[k][i] = 0.0f;
+    for (int line = 0; line < lines; ++line) {
+#pragma unroll
+      for (int step = 0; step < 2; ++step) {
+        const int ra = row0 + fr, rb = col0 + row_of_b(fr);
+        const v8h ha = *reinterpret_cast<const v8h*>(at_rows(ra, line, 2 * step + fg)), la = *reinterpret_cast<const v8h*>(at_rows(ra, line, 4 + 2 * step + fg));
+        const v8h hb = *reinterpret_cast<const v8h*>(at_cols(rb, line, 2 * step + fg)), lb = *reinterpret_cast<const v8h*>(at_cols(rb, line, 4 + 2 * step + fg));
+        acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hb, ha, acc[0], 0, 0, 0);
+        acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lb, ha, acc[1], 0, 0, 0);
+        acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hb, la, acc[2], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = acc[0][i] + (acc[1][i] + acc[2][i]);
+  };
+  // a block's values as a factor (row fr, sixteen columns), and, turned, in another place
+  auto store_block = [&](auto at, int row0, int col0, const uint32_t (&w)[16]) {
+    u32x4 hi[2], lo[2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      hi[i / 4][i % 4] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x05040100u);
+      lo[i / 4][i % 4] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      *reinterpret_cast<u32x4*>(at(row0 + fr, col0 / kLine, 2 * fg + h)) = hi[h];
+      *reinterpret_cast<u32x4*>(at(row0 + fr, col0 / kLine, 4 + 2 * fg + h)) = lo[h];
+    }
+  };
+  auto store_turned = [&](auto at, int row0, int col0, const uint32_t (&w)[16]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) put(at, col0 + fg * 16 + i, row0 + fr, w[i]);
+  };
+  const int bi = wave == 2 ? 32 : 0, bj = wave == 0 ? 0 : 32;  // of A, for the first kBlocks waves
+  auto store_square = [&](const float (&v)[16]) {
+    uint32_t w[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w[i] = split_of(v[i]);
+    store_block(at_a, bi, bj, w);
+    if (bi != bj) store_turned(at_a, bi, bj, w);
+  };
+
+  float x[MB][16];
+  if (wave < blocks) {
+#pragma unroll
+    for (int b = 0; b < MB; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const v8h hi = *reinterpret_cast<const v8h*>(at_x(32 * b + fr, wave, 2 * fg + h)), lo = *reinterpret_cast<const v8h*>(at_x(32 * b + fr, wave, 4 + 2 * fg + h));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[b][8 * h + i] = (float)hi[i] + (float)lo[i];
+      }
+  }
+  for (int step = 0; step < t.steps; ++step) {
+    float gram[16], poly[16];
+    if (wave < kBlocks) {
+      product(at_x, bi, at_x, bj, blocks, gram);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) gram[i] *= __builtin_ldexpf(1.0f, kA - 2 * kX);
+      store_square(gram);
+    }
+    __syncthreads();
+    if (wave < kBlocks) {
+      product(at_a, bi, at_a, bj, MB, poly);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        poly[i] = fmaf((float)kCb * __builtin_ldexpf(1.0f, kB - kA), gram[i], (float)kCc * __builtin_ldexpf(1.0f, kB - 2 * kA) * poly[i]);
+    }
+    __syncthreads();
+    if (wave < kBlocks) store_square(poly);
+    __syncthreads();
+    if (wave < blocks) {
+#pragma unroll
+      for (int b = 0; b < MB; ++b) {
+        float v[16];
+        product(at_a, 32 * b, at_t, 32 * wave, MB, v);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[b][i] = fmaf((float)kCa, x[b][i], __builtin_ldexpf(1.0f, -kB) * v[i]);
+      }
+      if (step + 1 < t.steps) {  // (X^T is read by this wave alone, and all of X's blocks are formed)
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+          uint32_t w[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) w[i] = split_of(x[b][i]);
+          store_block(at_x, 32 * b, 32 * wave, w);
+          store_turned(at_t, 32 * b, 32 * wave, w);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  if (wave >= blocks) return;
+  PT* out = MUON ? reinterpret_cast<PT*>(entry->p) : reinterpret_cast<PT*>(last.out) + (int64_t)which * r * c;
+  const float keep = MUON ? 1.0f - last.lr * entry->decay : 0.0f, move = MUON ? -last.lr * entry->factor : 0.0f;
+#pragma unroll
+  for (int b = 0; b < MB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int row = tall ? 32 * wave + fg * 16 + i : 32 * b + fr, col = tall ? 32 * b + fr : 32 * wave + fg * 16 + i;
+      if (row < r && col < c) {
+        PT* at = out + row * c + col;
+        const float o = __builtin_ldexpf(1.0f, -kX) * x[b][i];
+        store_one(at, MUON ? fmaf(move, o, to_f32(*at) * keep) : o);
+      }
+    }
+}
+
 // Writes rows `at`.. of the table.
 constexpr int kRowsAtOnce = 64;
 struct Rows {
@@ -495,8 +712,9 @@ struct Shape {
 // 3 m^2 n + (4 k - 3) m^3: five as 3 + 2 instead take 38 in place of 65 m^3 for n = 4 m (2048 x 8192,
 // one matrix: 2.1 ms, one by one 3.0).  Errors of A grow in P A P, where those of X X^T do not: of five steps from 2.2e-6 of the
 // result's norm to 3.1e-6 at 512 x 2048 (fp32 arithmetic throughout: 2.8e-6), but from 1.2e-6 to 5.3e-6 at
-// 37 x 100, and below 512 latency counts, not operations.
-int at_once(int64_t m, int64_t n) { return m >= 512 && 2 * n >= 3 * m ? kMostAtOnce : 1; }
+// 37 x 100, and below 512 latency counts, not operations.  Three come first, then two, then one at a
+// time: once singular values have arrived near 1 errors grow faster (six steps as 3 + 3 1.4e-5).
+bool several_at_once(int64_t m, int64_t n) { return m >= 512 && 2 * n >= 3 * m; }
 Shape shape_of(int64_t rows, int64_t cols) {
   Shape s = {};
   s.rows = rows;
@@ -514,10 +732,26 @@ Shape shape_of(int64_t rows, int64_t cols) {
   };
   s.x = take(s.m * s.ldn);
   for (int64_t& t : s.xt) t = take(s.n * s.ldm);
-  s.wide = at_once(s.m, s.n) > 1;
+  s.wide = several_at_once(s.m, s.n);
   for (int i = 0; i < (s.wide ? 5 : 2); ++i) s.square[i] = take(s.m * s.ldm);
   s.bytes = at;
   return s;
+}
+
+bool is_tiny(int64_t rows, int64_t cols) { return std::min(rows, cols) <= kTinyM && std::max(rows, cols) <= kTinyN; }
+
+// Small matrices, of these sizes at most.
+template <typename GT, typename PT, bool MUON>
+int32_t launch_tiny(Tiny t, int64_t count, int64_t m, int64_t n, const Source& s, const Last& last, hipStream_t st, std::string* e) {
+  t.lines = (int32_t)((n + 2 * kLine - 1) / (2 * kLine) * 2);
+  auto go = [&](auto kernel, int mb) {
+    const int bytes = 32 * mb * t.lines * 128 + t.lines * kLine * mb * 128 + 32 * mb * mb * 128;
+    const int32_t r = allow_lds(reinterpret_cast<const void*>(kernel), 64 * 8 * 128 + 256 * 2 * 128 + 64 * 2 * 128, e);
+    if (r != MTDAO_OK) return r;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kTinyThreads), (size_t)bytes, st, t, s, last);
+    return (int32_t)MTDAO_OK;
+  };
+  return m <= 32 ? go(k_muon_tiny<GT, PT, MUON, 1>, 1) : go(k_muon_tiny<GT, PT, MUON, 2>, 2);
 }
 
 // Matrices that go through the products together: runs of one shape in the
@@ -538,9 +772,10 @@ constexpr int64_t kGroupBytes = INT64_C(4) << 30;
 int64_t chunks_of(const Shape& s) { return (s.rows * s.cols + kChunk - 1) / kChunk; }
 
 // shapes: in the table's order, equal ones together, none empty.
+// (small ones, at the end, are in no group)
 std::vector<Group> groups_of(const std::vector<std::pair<int64_t, int64_t>>& shapes) {
   std::vector<Group> groups;
-  for (size_t i = 0; i < shapes.size(); ++i) {
+  for (size_t i = 0; i < shapes.size() && !is_tiny(shapes[i].first, shapes[i].second); ++i) {
     const Shape s = shape_of(shapes[i].first, shapes[i].second);
     const bool same = i > 0 && shapes[i] == shapes[i - 1];
     if (groups.empty() || groups.back().bytes + s.bytes > kGroupBytes || (!same && groups.back().runs.size() == kMostParts) ||
@@ -610,7 +845,7 @@ std::vector<std::vector<Gemm>> products_of(const Run& run, uint8_t* base, int st
     return g;
   };
   for (int done = 0, turn = 0; done < steps; turn ^= 1) {
-    const int now = std::min(s.wide ? at_once(s.m, s.n) : 1, steps - done);
+    const int now = std::min(!s.wide || done > kMostAtOnce ? 1 : done > 0 ? 2 : kMostAtOnce, steps - done);
     Gemm g = square(x, kX, x, kX, gram, kA, 1.0);
     g.blocks = (int32_t)(s.n / kLine);
     g.lda = g.ldb = (int32_t)s.ldn;
@@ -831,13 +1066,14 @@ int32_t check_pointers(const mtdao_muon_config& c, const mtdao_muon_matrix* t, s
   return MTDAO_OK;
 }
 
-// Matrices in the table's order (shapes together, none empty): their numbers.
+// Matrices in the table's order (shapes together, small ones at the end, none empty): their numbers.
 std::vector<int> order_of(const mtdao_muon_config& c, const mtdao_muon_matrix* t) {
   std::vector<int> order;
   for (int i = 0; i < c.n_matrices; ++i)
     if (t[i].rows > 0 && t[i].cols > 0) order.push_back(i);
   std::stable_sort(order.begin(), order.end(), [&](int a, int b) {
-    return std::make_pair(t[a].rows * t[a].cols, t[a].rows) > std::make_pair(t[b].rows * t[b].cols, t[b].rows);
+    const bool ta = is_tiny(t[a].rows, t[a].cols), tb = is_tiny(t[b].rows, t[b].cols);
+    return ta != tb ? tb : std::make_pair(t[a].rows * t[a].cols, t[a].rows) > std::make_pair(t[b].rows * t[b].cols, t[b].rows);
   });
   return order;
 }
@@ -864,6 +1100,8 @@ struct mtdao_muon {
   std::vector<Row> rows;            // the table
   std::vector<Written> written;
   std::vector<Group> groups;
+  size_t tiny = 0;                  // small matrices, and their largest sides
+  int64_t tiny_m = 0, tiny_n = 0;
   Layout layout;
   char* workspace = nullptr;
   std::string err;
@@ -889,7 +1127,7 @@ int32_t mtdao_orthogonalize_workspace_bytes(int64_t batch, int64_t rows, int64_t
   if (r != MTDAO_OK) return r;
   if (!bytes) return fail(&g_err, MTDAO_ERR_INVALID_ARG, "bytes is NULL");
   const std::vector<Group> groups = groups_of(batch, rows, cols);
-  *bytes = groups.empty() ? 0 : layout_of(groups, 0).bytes;
+  *bytes = groups.empty() ? 0 : layout_of(groups, 0).bytes;  // (small matrices need none)
   return MTDAO_OK;
 } catch (const std::bad_alloc&) {
   return fail(&g_err, MTDAO_ERR_WORKSPACE, "out of host memory");
@@ -903,8 +1141,7 @@ int32_t mtdao_orthogonalize(const void* x, int32_t dtype, int64_t batch, int64_t
   if (r == MTDAO_OK) r = check_type(out_dtype, "out_dtype", e);
   if (r == MTDAO_OK) r = check_numbers(steps, eps, e);
   if (r != MTDAO_OK) return r;
-  const std::vector<Group> groups = groups_of(batch, rows, cols);
-  if (groups.empty()) return MTDAO_OK;
+  if (batch == 0 || rows == 0 || cols == 0) return MTDAO_OK;
   if (!x || !out) return fail(e, MTDAO_ERR_INVALID_ARG, "x or out is NULL");
   if (!aligned_to(x, (uintptr_t)esize(dtype)) || !aligned_to(out, (uintptr_t)esize(out_dtype)))
     return fail(e, MTDAO_ERR_ALIGN, "x or out is not aligned to its element");
@@ -912,20 +1149,33 @@ int32_t mtdao_orthogonalize(const void* x, int32_t dtype, int64_t batch, int64_t
   // (matrices go group by group, so a later one's x may not lie under an earlier one's result)
   if (overlap(x, numel * esize(dtype), out, numel * esize(out_dtype)) && (x != out || dtype != out_dtype))
     return fail(e, MTDAO_ERR_INVALID_ARG, "out overlaps x");
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  const Last last = {nullptr, out, 0.0f};
+  auto with = [&](auto go) {
+    if (dtype == MTDAO_F32 && out_dtype == MTDAO_F32) return go(float{}, float{});
+    if (dtype == MTDAO_F32) return go(float{}, bf16_t{});
+    if (out_dtype == MTDAO_F32) return go(bf16_t{}, float{});
+    return go(bf16_t{}, bf16_t{});
+  };
+  if (is_tiny(rows, cols)) {
+    RoctxRange range("mtdao_orthogonalize %lld x %lld x %lld", (long long)batch, (long long)rows, (long long)cols);
+    const Source s = {nullptr, x, nullptr, nullptr, 0.0f, 0, eps};
+    r = with([&](auto g, auto p) {
+      return launch_tiny<decltype(g), decltype(p), false>({0, 0, rows, cols, steps}, batch, std::min(rows, cols), std::max(rows, cols), s, last, st, e);
+    });
+    return r != MTDAO_OK ? r : hip_check(e, hipGetLastError(), "mtdao_orthogonalize launch");
+  }
+  const std::vector<Group> groups = groups_of(batch, rows, cols);
   const Layout l = layout_of(groups, 0);
   r = check_workspace(workspace, workspace_bytes, l.bytes, e);
   if (r != MTDAO_OK) return r;
   char* w = static_cast<char*>(workspace);
-  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   RoctxRange range("mtdao_orthogonalize %lld x %lld x %lld", (long long)batch, (long long)rows, (long long)cols);
-  Source s = {nullptr, x, reinterpret_cast<double*>(w + l.sums), reinterpret_cast<double*>(w + l.scales), 0.0f, 0, eps};
-  const Last last = {nullptr, out, 0.0f};
+  const Source s = {nullptr, x, reinterpret_cast<double*>(w + l.sums), reinterpret_cast<double*>(w + l.scales), 0.0f, 0, eps};
   for (const Group& g : groups) {
-    uint8_t* factors = reinterpret_cast<uint8_t*>(w + l.factors);
-    if (dtype == MTDAO_F32 && out_dtype == MTDAO_F32) r = launch_group<float, float, false>(g, s, last, factors, steps, st, e);
-    else if (dtype == MTDAO_F32) r = launch_group<float, bf16_t, false>(g, s, last, factors, steps, st, e);
-    else if (out_dtype == MTDAO_F32) r = launch_group<bf16_t, float, false>(g, s, last, factors, steps, st, e);
-    else r = launch_group<bf16_t, bf16_t, false>(g, s, last, factors, steps, st, e);
+    r = with([&](auto gt, auto pt) {
+      return launch_group<decltype(gt), decltype(pt), false>(g, s, last, reinterpret_cast<uint8_t*>(w + l.factors), steps, st, e);
+    });
     if (r != MTDAO_OK) return r;
   }
   return hip_check(e, hipGetLastError(), "mtdao_orthogonalize launch");
@@ -968,8 +1218,15 @@ int32_t mtdao_muon_init(const mtdao_muon_config* cfg, const mtdao_muon_matrix* m
   h->workspace = static_cast<char*>(workspace);
   h->written = std::move(written);
   for (int i = 0; i < cfg->n_matrices; ++i) h->numel.push_back(matrices[i].rows * matrices[i].cols);
-  for (int i : h->order)
-    h->rows.push_back({matrices[i].p, matrices[i].g, matrices[i].m, (float)matrices[i].weight_decay, (float)matrices[i].factor});
+  for (int i : h->order) {
+    const mtdao_muon_matrix& a = matrices[i];
+    h->rows.push_back({a.p, a.g, a.m, (float)a.weight_decay, (float)a.factor, (int32_t)a.rows, (int32_t)a.cols});
+    if (is_tiny(a.rows, a.cols)) {
+      h->tiny++;
+      h->tiny_m = std::max(h->tiny_m, std::min(a.rows, a.cols));
+      h->tiny_n = std::max(h->tiny_n, std::max(a.rows, a.cols));
+    }
+  }
   RoctxRange range("mtdao_muon_init matrices=%d", cfg->n_matrices);
   r = write_table(h, &g_err, reinterpret_cast<hipStream_t>(hip_stream));
   if (r != MTDAO_OK) return r;
@@ -1005,12 +1262,22 @@ int32_t mtdao_muon_step(mtdao_muon* h, double lr, void* hip_stream) try {
                     (float)c.momentum, c.nesterov != 0, c.eps};
   const Last last = {rows, nullptr, (float)lr};
   uint8_t* factors = reinterpret_cast<uint8_t*>(w + h->layout.factors);
+  auto with = [&](auto go) {
+    if (c.param_dtype == MTDAO_F32 && c.grad_dtype == MTDAO_F32) return go(float{}, float{});
+    if (c.param_dtype == MTDAO_F32) return go(bf16_t{}, float{});
+    if (c.grad_dtype == MTDAO_F32) return go(float{}, bf16_t{});
+    return go(bf16_t{}, bf16_t{});
+  };
   int32_t r = MTDAO_OK;
   for (const Group& g : h->groups) {
-    if (c.param_dtype == MTDAO_F32 && c.grad_dtype == MTDAO_F32) r = launch_group<float, float, true>(g, s, last, factors, c.steps, st, &h->err);
-    else if (c.param_dtype == MTDAO_F32) r = launch_group<bf16_t, float, true>(g, s, last, factors, c.steps, st, &h->err);
-    else if (c.grad_dtype == MTDAO_F32) r = launch_group<float, bf16_t, true>(g, s, last, factors, c.steps, st, &h->err);
-    else r = launch_group<bf16_t, bf16_t, true>(g, s, last, factors, c.steps, st, &h->err);
+    r = with([&](auto gt, auto pt) { return launch_group<decltype(gt), decltype(pt), true>(g, s, last, factors, c.steps, st, &h->err); });
+    if (r != MTDAO_OK) return r;
+  }
+  if (h->tiny > 0) {
+    r = with([&](auto gt, auto pt) {
+      return launch_tiny<decltype(gt), decltype(pt), true>({(int32_t)(h->rows.size() - h->tiny), 0, 0, 0, c.steps}, (int64_t)h->tiny, h->tiny_m, h->tiny_n, s, last,
+                                                           st, &h->err);
+    });
     if (r != MTDAO_OK) return r;
   }
   return hip_check(&h->err, hipGetLastError(), "mtdao_muon_step launch");

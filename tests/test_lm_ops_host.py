@@ -60,15 +60,17 @@ def test_orthogonalize_refuses_sizes(batch, rows, cols, code):
     (dict(eps=-1e-9), -1), (dict(eps=NAN), -1), (dict(eps=INF), -1), (dict(x=BASE + 2), -2), (dict(out=(BASE << 1) + 1), -2), (dict(ws=None), -5),
     (dict(need=100), -5), (dict(ws=(BASE << 2) + 128), -2), (dict(out=BASE + 400), -1), (dict(out=BASE, out_dtype=1), -1)])
 def test_orthogonalize_refuses(kw, code):
-    a = dict(x=BASE, dtype=0, out=BASE << 1, out_dtype=0, steps=5, eps=1e-7, ws=BASE << 2, need=c.mtdao_orthogonalize_workspace_bytes(2, 30, 40))
+    a = dict(x=BASE, dtype=0, out=BASE << 1, out_dtype=0, steps=5, eps=1e-7, ws=BASE << 2, need=c.mtdao_orthogonalize_workspace_bytes(2, 130, 140))
     a.update(kw)
-    refused(code, c.mtdao_orthogonalize, a["x"], a["dtype"], 2, 30, 40, a["out"], a["out_dtype"], a["steps"], a["eps"], a["ws"], a["need"], None)
+    refused(code, c.mtdao_orthogonalize, a["x"], a["dtype"], 2, 130, 140, a["out"], a["out_dtype"], a["steps"], a["eps"], a["ws"], a["need"], None)
 
 
 def test_nothing_to_orthogonalize():
     for batch, rows, cols in ((0, 5, 5), (3, 0, 5), (3, 5, 0)):
         assert c.mtdao_orthogonalize_workspace_bytes(batch, rows, cols) == 0
         c.mtdao_orthogonalize(None, 0, batch, rows, cols, None, 0, 5, 1e-7, None, 0, None)
+    assert c.mtdao_orthogonalize_workspace_bytes(1000, 64, 256) == c.mtdao_orthogonalize_workspace_bytes(1, 256, 64) == 0  # one workgroup each
+    assert c.mtdao_orthogonalize_workspace_bytes(1, 65, 65) > 0 and c.mtdao_orthogonalize_workspace_bytes(1, 1, 257) > 0
 
 
 def muon_case(n=3, **kw):
