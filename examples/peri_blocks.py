@@ -58,29 +58,38 @@ class PeriBlocks:
             held.update(w)
         return held
 
-    def loss_and_gradients(self, flat: torch.Tensor, grads: torch.Tensor, x: torch.Tensor, target: torch.Tensor) -> torch.Tensor:
-        """Mean square of norm(x of the last block) - target; the gradients of
-        ``flat`` go into ``grads`` (both [numel], float32)."""
-        p, g = self.views(flat), self.views(grads)
-        w = {k: self._weight(k, v) for k, v in p.items() if v.dim() == 2}
-        norm = {"kind": self.kind, "scale": self.scale}
+    def forward(self, p: Dict[str, torch.Tensor], x: torch.Tensor) -> Tuple[torch.Tensor, List[Tuple[torch.Tensor, ...]]]:
+        """norm(x of the last block) in bfloat16, and what the backward pass needs."""
+        w = {k: self._weight(k, p[k]) for k in self.shapes if len(self.shapes[k]) == 2}
         x, n = ops.peri_norm(x, None, None, p["pre0"], kind=self.kind, branch_dtype=torch.bfloat16)
-        kept: List[Tuple[torch.Tensor, ...]] = []
-        first = x
+        kept: List[Tuple[torch.Tensor, ...]] = [(x,)]
         for i in range(self.blocks):
             a = torch.relu(ops.linear8(n, w[f"up{i}"]))
             f = ops.linear8(a, w[f"down{i}"])
-            x, after = ops.peri_norm(x, f, p[f"post{i}"], p[f"pre{i + 1}"], **norm)
+            x, after = ops.peri_norm(x, f, p[f"post{i}"], p[f"pre{i + 1}"], kind=self.kind, scale=self.scale)
             kept.append((n, a, f, x))
             n = after
-        off = n.float() - target
-        dx, dn = None, (off * (2.0 / off.numel())).bfloat16()
+        return n, kept
+
+    def backward(self, p: Dict[str, torch.Tensor], g: Dict[str, torch.Tensor], dn: torch.Tensor, kept: List[Tuple[torch.Tensor, ...]]) -> torch.Tensor:
+        """The gradients of the parameters into ``g``; returns that of x."""
+        w, dx = self.weights, None
         for i in reversed(range(self.blocks)):
             n, a, f, x = kept.pop()
-            dx, df, g[f"post{i}"][:], g[f"pre{i + 1}"][:], _ = ops.peri_norm_backward(dx, dn, x, f, p[f"post{i}"], p[f"pre{i + 1}"], **norm)
+            dx, df, g[f"post{i}"][:], g[f"pre{i + 1}"][:], _ = ops.peri_norm_backward(dx, dn, x, f, p[f"post{i}"], p[f"pre{i + 1}"], kind=self.kind,
+                                                                                     scale=self.scale)
             da, _ = ops.linear8_backward(df, a, w[f"down{i}"], dw=g[f"down{i}"])
             dn, _ = ops.linear8_backward(da * (a > 0), n, w[f"up{i}"], dw=g[f"up{i}"])
-        g["pre0"][:] = ops.peri_norm_backward(dx, dn, first, None, None, p["pre0"], kind=self.kind)[3]
+        dx, _, _, g["pre0"][:], _ = ops.peri_norm_backward(dx, dn, kept.pop()[0], None, None, p["pre0"], kind=self.kind)
+        return dx
+
+    def loss_and_gradients(self, flat: torch.Tensor, grads: torch.Tensor, x: torch.Tensor, target: torch.Tensor) -> torch.Tensor:
+        """Mean square of norm(x of the last block) - target; the gradients of
+        ``flat`` go into ``grads`` (both [numel], float32)."""
+        p = self.views(flat)
+        n, kept = self.forward(p, x)
+        off = n.float() - target
+        self.backward(p, self.views(grads), (off * (2.0 / off.numel())).bfloat16(), kept)
         return off.square().mean()
 
 
