@@ -42,7 +42,8 @@ using namespace mtdao::ops;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 4096;   // elements of a workgroup that sums squares
+constexpr int kChunk = 4096;   // elements that a workgroup sums the squares of at once
+constexpr int kMostChunks = 1024;  // of a matrix, which every workgroup that splits it adds up
 constexpr int kLine = 32;      // elements of a row in one line
 constexpr int kPad = 128;      // rows and columns of a factor are multiples of this
 constexpr int kMostParts = 12, kMostGemms = 2 * kMostParts;
@@ -73,6 +74,7 @@ struct Part {
   int32_t ld_natural, ld_turned;  // bytes
   int32_t matrix, count;        // the first one's place in the table, how many
   int32_t first_chunk, chunks;  // chunks of elements before these matrices, of each
+  int32_t per_chunk;            // times kChunk elements
   int32_t first_tile, tiles_r, tiles_c;
 };
 struct Parts {
@@ -85,7 +87,6 @@ struct Source {
   const Row* rows;
   const void* x;
   double* sums;    // of every chunk
-  double* scale;   // of every matrix of this launch
   float momentum;
   int32_t nesterov;
   double eps;
@@ -100,6 +101,7 @@ __device__ __forceinline__ void update_of(const Source& s, const float (&g)[N], 
   for (int t = 0; t < N; ++t) u[t] = s.nesterov ? fmaf(s.momentum, m[t], g[t]) : m[t];
 }
 
+constexpr int kSumV = 4;  // elements of a lane's vector: 16 bytes of momentum
 // Momentum (Muon) and the sum of the squares of a chunk of the update, in fp64.
 template <typename GT, bool MUON>
 __global__ __launch_bounds__(kThreads) void k_muon_sums(Parts parts, Source s) {
@@ -110,7 +112,7 @@ __global__ __launch_bounds__(kThreads) void k_muon_sums(Parts parts, Source s) {
   while (k + 1 < parts.n && item >= parts.part[k + 1].first_chunk) ++k;
   const Part& a = parts.part[k];
   const int in = (int)(item - a.first_chunk), which = in / a.chunks;
-  const int64_t base = (int64_t)(in - which * a.chunks) * kChunk, numel = a.rows * a.cols;
+  const int64_t numel = a.rows * a.cols, first = (int64_t)(in - which * a.chunks) * a.per_chunk * kChunk;
   const GT* g;
   float* m = nullptr;
   if (MUON) {
@@ -119,31 +121,33 @@ __global__ __launch_bounds__(kThreads) void k_muon_sums(Parts parts, Source s) {
   } else {
     g = reinterpret_cast<const GT*>(s.x) + (int64_t)(a.matrix + which) * numel;
   }
-  constexpr int V = 8, kSlots = kChunk / (kThreads * V);
+  constexpr int V = kSumV, kSlots = kChunk / (kThreads * V);
   double sum = 0.0;
-  float ga[kSlots][V], ma[kSlots][V];
-  int n[kSlots];
+  for (int64_t base = first; base < first + (int64_t)a.per_chunk * kChunk && base < numel; base += kChunk) {
+    float ga[kSlots][V], ma[kSlots][V];
+    int n[kSlots];
 #pragma unroll
-  for (int t = 0; t < kSlots; ++t) {
-    const int64_t e = base + (t * kThreads + (int)threadIdx.x) * V, left = numel - e;
-    n[t] = left > V ? V : (int)(left < 0 ? 0 : left);
-    load_some<V>(g + e, n[t], ga[t]);
-    if (MUON) load_some<V>(m + e, n[t], ma[t]);
-  }
-#pragma unroll
-  for (int t = 0; t < kSlots; ++t) {
-    float u[V];
-    if (MUON) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) ma[t][i] = fmaf(s.momentum, ma[t][i], ga[t][i]);
-      if (n[t] > 0) store_some<V>(m + base + (t * kThreads + (int)threadIdx.x) * V, n[t], ma[t]);
-      update_of(s, ga[t], ma[t], u);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) u[i] = ga[t][i];
+    for (int t = 0; t < kSlots; ++t) {
+      const int64_t e = base + (t * kThreads + (int)threadIdx.x) * V, left = numel - e;
+      n[t] = left > V ? V : (int)(left < 0 ? 0 : left);
+      load_some<V>(g + e, n[t], ga[t]);
+      if (MUON) load_some<V>(m + e, n[t], ma[t]);
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum += (double)u[i] * (double)u[i];
+    for (int t = 0; t < kSlots; ++t) {
+      float u[V];
+      if (MUON) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) ma[t][i] = fmaf(s.momentum, ma[t][i], ga[t][i]);
+        if (n[t] > 0) store_some<V>(m + base + (t * kThreads + (int)threadIdx.x) * V, n[t], ma[t]);
+        update_of(s, ga[t], ma[t], u);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) u[i] = ga[t][i];
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum += (double)u[i] * (double)u[i];
+    }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
@@ -152,68 +156,40 @@ __global__ __launch_bounds__(kThreads) void k_muon_sums(Parts parts, Source s) {
   if (threadIdx.x == 0) s.sums[item] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-// A workgroup's sum of a matrix's squares, in an order that the sizes fix, and
-// what its elements are divided by.
-__global__ __launch_bounds__(kThreads) void k_muon_scales(Parts parts, Source s) {
-  __shared__ double part[kThreads / 64];
-  int k = 0, before = 0;
-  while (k + 1 < parts.n && (int)blockIdx.x >= before + parts.part[k].count) before += parts.part[k++].count;
-  const Part& a = parts.part[k];
-  const double* from = s.sums + a.first_chunk + (int64_t)((int)blockIdx.x - before) * a.chunks;
-  double sum = 0.0;
-  for (int i = threadIdx.x; i < a.chunks; i += kThreads) sum += from[i];
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) s.scale[blockIdx.x] = (double)(1 << kX) / (sqrt((part[0] + part[1]) + (part[2] + part[3])) + s.eps);
-}
-
 // v as hi (low half of the word) and lo.
 __device__ __forceinline__ uint32_t split_of(float v) {
   const _Float16 hi = (_Float16)v;
   const _Float16 lo = (_Float16)(v - (float)hi);
   return (uint32_t)__builtin_bit_cast(uint16_t, hi) | (uint32_t)__builtin_bit_cast(uint16_t, lo) << 16;
 }
-// Sixteen elements of a line from its element 0 or 16 on.
-__device__ __forceinline__ void store_split(uint8_t* line, int half, const uint32_t (&w)[16]) {
-  u32x4 hi[2], lo[2];
+// Eight elements of a line, its chunk-th.
+__device__ __forceinline__ void store_chunk(uint8_t* line, int chunk, const uint32_t (&w)[8]) {
+  u32x4 hi, lo;
 #pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    hi[t / 4][t % 4] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x05040100u);
-    lo[t / 4][t % 4] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x07060302u);
+  for (int t = 0; t < 4; ++t) {
+    hi[t] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x05040100u);
+    lo[t] = __builtin_amdgcn_perm(w[2 * t + 1], w[2 * t], 0x07060302u);
   }
-  u32x4* at = reinterpret_cast<u32x4*>(line + half * 32);
-  at[0] = hi[0];
-  at[1] = hi[1];
-  at[4] = lo[0];
-  at[5] = lo[1];
-}
-__device__ __forceinline__ void load_split(const uint8_t* line, int half, float (&v)[16]) {
-  const v8h* at = reinterpret_cast<const v8h*>(line + half * 32);
-  const v8h hi[2] = {at[0], at[1]}, lo[2] = {at[4], at[5]};
-#pragma unroll
-  for (int t = 0; t < 16; ++t) v[t] = (float)hi[t / 8][t % 8] + (float)lo[t / 8][t % 8];
+  *reinterpret_cast<u32x4*>(line + chunk * 16) = hi;
+  *reinterpret_cast<u32x4*>(line + 64 + chunk * 16) = lo;
 }
 
 // X and its transpose from the update: a tile of 64 x 64, whose transpose goes
-// through LDS.  A thread has sixteen elements of a row, then of a column.
+// through LDS.  A thread has eight elements, a chunk of 16 bytes high and one low, of two rows, then of two columns.
+// Every workgroup adds up the matrix's sums of squares, in an order that the sizes fix.
 constexpr int kSplit = 64;
 template <typename GT, bool MUON>
 __global__ __launch_bounds__(kThreads) void k_muon_split(Parts parts, Source s) {
   __shared__ uint32_t tile[kSplit][kSplit + 1];
+  __shared__ double part[kThreads / 64];
   const int64_t item = item_of_launch();
   if (item >= parts.items) return;
-  int k = 0, before = 0;
-  while (k + 1 < parts.n && item >= parts.part[k + 1].first_tile) before += parts.part[k++].count;
+  int k = 0;
+  while (k + 1 < parts.n && item >= parts.part[k + 1].first_tile) ++k;
   const Part& a = parts.part[k];
   const int in = (int)(item - a.first_tile), tiles = a.tiles_r * a.tiles_c, which = in / tiles, at = in - which * tiles;
   const int64_t row0 = (int64_t)(at / a.tiles_c) * kSplit, col0 = (int64_t)(at % a.tiles_c) * kSplit;
-  const int line = threadIdx.x / 4, part = threadIdx.x % 4;
-  const double scale = uniform_load(s.scale + before + which);
-  const int64_t row = row0 + line, col = col0 + part * 16, left = row < a.rows ? a.cols - col : 0;
-  const int n = left < 0 ? 0 : left > 16 ? 16 : (int)left;
-  uint32_t w[16];
+  const int line = threadIdx.x / 8, chunk = threadIdx.x % 8;
   const GT* g;
   const float* m = nullptr;
   if (MUON) {
@@ -222,26 +198,46 @@ __global__ __launch_bounds__(kThreads) void k_muon_split(Parts parts, Source s) 
   } else {
     g = reinterpret_cast<const GT*>(s.x) + (int64_t)(a.matrix + which) * a.rows * a.cols;
   }
+  float u[2][8];
+  int n[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    float ga[8], ma[8], u[8];
-    const int64_t e = row * a.cols + col + h * 8;
-    load_some<8>(g + e, n - h * 8, ga);
+    const int64_t row = row0 + h * 32 + line, col = col0 + chunk * 8, e = row * a.cols + col, left = row < a.rows ? a.cols - col : 0;
+    n[h] = left < 0 ? 0 : left > 8 ? 8 : (int)left;
+    load_some<8>(g + e, n[h], u[h]);
     if (MUON) {
-      load_some<8>(m + e, n - h * 8, ma);
-      update_of(s, ga, ma, u);
+      float ma[8];
+      load_some<8>(m + e, n[h], ma);
+      update_of(s, u[h], ma, u[h]);
     }
-#pragma unroll
-    for (int t = 0; t < 8; ++t) w[h * 8 + t] = h * 8 + t < n ? split_of((float)((double)(MUON ? u[t] : ga[t]) * scale)) : 0u;
   }
-  const int64_t own = (int64_t)which * a.step;
-  store_split(a.natural + own + row * a.ld_natural + col / kLine * 128, part % 2, w);
+  const double* from = s.sums + a.first_chunk + (int64_t)which * a.chunks;
+  double sum = 0.0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < a.chunks; i += kThreads) sum += from[i];
 #pragma unroll
-  for (int t = 0; t < 16; ++t) tile[line][part * 16 + t] = w[t];
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  const double scale = (double)(1 << kX) / (sqrt((part[0] + part[1]) + (part[2] + part[3])) + s.eps);
+  const int64_t own = (int64_t)which * a.step;
+  uint32_t w[8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      w[t] = t < n[h] ? split_of((float)((double)u[h][t] * scale)) : 0u;
+      tile[h * 32 + line][chunk * 8 + t] = w[t];
+    }
+    store_chunk(a.natural + own + (row0 + h * 32 + line) * a.ld_natural + (col0 + chunk * 8) / kLine * 128, chunk % 4, w);
+  }
   __syncthreads();
 #pragma unroll
-  for (int t = 0; t < 16; ++t) w[t] = tile[part * 16 + t][line];
-  store_split(a.turned + own + (col0 + line) * a.ld_turned + (row0 + part * 16) / kLine * 128, part % 2, w);
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) w[t] = tile[chunk * 8 + t][h * 32 + line];
+    store_chunk(a.turned + own + (col0 + h * 32 + line) * a.ld_turned + (row0 + chunk * 8) / kLine * 128, chunk % 4, w);
+  }
 }
 
 // ------------------------------------------------------------------ products
@@ -272,6 +268,62 @@ struct Last {
   float lr;
 };
 
+// Fragments of 32 x 32 go between lanes, each with sixteen elements of a row, and memory, in whole lines, by way of
+// LDS of the wave's own: 32 lines, then 32 rows of 33 words to turn a fragment.  (Pieces of 16 bytes straight from the
+// lanes take four times as many cycles of the CU's path to memory.)
+constexpr int kStaged = 32 * 128, kOwn = kStaged + 32 * 33 * 4;
+__device__ __forceinline__ void lanes_done() {  // (LDS serves a wave in order; only the compiler has to keep it)
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ u32x4* staged_at(uint8_t* mine, int row, int chunk) {
+  return reinterpret_cast<u32x4*>(mine + row * 128 + ((chunk ^ row_key(row)) << 4));
+}
+__device__ __forceinline__ void load_lines(const uint8_t* from, int ld, int lane, u32x4 (&w)[4]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = *reinterpret_cast<const u32x4*>(from + (int64_t)(k * 8 + lane / 8) * ld + lane % 8 * 16);
+}
+__device__ __forceinline__ void staged_in(uint8_t* mine, int lane, const u32x4 (&w)[4], float (&v)[16]) {
+  const int fr = lane % 32, fg = lane / 32;
+  lanes_done();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) *staged_at(mine, k * 8 + lane / 8, lane % 8) = w[k];
+  lanes_done();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const v8h hi = __builtin_bit_cast(v8h, *staged_at(mine, fr, 2 * fg + h)), lo = __builtin_bit_cast(v8h, *staged_at(mine, fr, 4 + 2 * fg + h));
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[8 * h + t] = (float)hi[t] + (float)lo[t];
+  }
+}
+__device__ __forceinline__ void staged_out(uint8_t* mine, int lane, const uint32_t (&w)[16], uint8_t* to, int ld) {
+  const int fr = lane % 32, fg = lane / 32;
+  lanes_done();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    u32x4 hi, lo;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      hi[t] = __builtin_amdgcn_perm(w[8 * h + 2 * t + 1], w[8 * h + 2 * t], 0x05040100u);
+      lo[t] = __builtin_amdgcn_perm(w[8 * h + 2 * t + 1], w[8 * h + 2 * t], 0x07060302u);
+    }
+    *staged_at(mine, fr, 2 * fg + h) = hi;
+    *staged_at(mine, fr, 4 + 2 * fg + h) = lo;
+  }
+  lanes_done();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) *reinterpret_cast<u32x4*>(to + (int64_t)(k * 8 + lane / 8) * ld + lane % 8 * 16) = *staged_at(mine, k * 8 + lane / 8, lane % 8);
+}
+__device__ __forceinline__ void turn_fragment(uint32_t* words, int lane, uint32_t (&w)[16]) {
+  const int fr = lane % 32, fg = lane / 32;
+  lanes_done();
+#pragma unroll
+  for (int t = 0; t < 16; ++t) words[fr * 33 + fg * 16 + t] = w[t];
+  lanes_done();
+#pragma unroll
+  for (int t = 0; t < 16; ++t) w[t] = words[(fg * 16 + t) * 33 + fr];
+}
+
 // Tile (i, j) of the tiles on and above the diagonal of n x n, row by row.
 __device__ __forceinline__ void triangle_place(int t, int n, int& i, int& j) {
   i = 0;
@@ -279,33 +331,37 @@ __device__ __forceinline__ void triangle_place(int t, int n, int& i, int& j) {
   j = i + t;
 }
 
-// Sixteen consecutive elements of a row of the last result.
+// A fragment of the last result, by way of LDS as above: four consecutive elements of a row a lane,
+// in four rows.
+struct Spot {
+  int64_t at;   // of the first row's four elements
+  int n, rows;  // of these that there are; rows from the first one on
+};
+__device__ __forceinline__ Spot spot_of(const Gemm& q, int lane, int r0, int c0) {
+  const int64_t row = r0 + lane / 8, col = c0 + lane % 8 * 4, left = q.cols - col, rows = q.rows - row;
+  return {row * q.cols + col, left > 4 ? 4 : left < 0 ? 0 : (int)left, rows > 32 ? 32 : rows < 0 ? 0 : (int)rows};
+}
 template <typename PT>
-__device__ __forceinline__ void store_last(const Gemm& q, const Last& last, int which, int64_t row, int64_t col, const float (&v)[16]) {
-  if (row >= q.rows || col >= q.cols) return;
-  const int n = q.cols - col > 16 ? 16 : (int)(q.cols - col);
-  const int64_t e = row * q.cols + col;
-  if (last.rows) {
-    const Row& r = last.rows[q.matrix + which];
-    PT* p = reinterpret_cast<PT*>(r.p) + e;
-    const float keep = 1.0f - last.lr * r.decay, step = -last.lr * r.factor;
+__device__ __forceinline__ void load_last(const Gemm& q, const PT* p, const Spot& spot, float (&v)[4][4]) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float o[8];
-      load_some<8>(p + h * 8, n - h * 8, o);
+  for (int k = 0; k < 4; ++k) load_some<4>(p + spot.at + k * 8 * q.cols, k * 8 < spot.rows ? spot.n : 0, v[k]);
+}
+// keep p + step v; keep and step are not looked at without `onto`: then v
+template <typename PT>
+__device__ __forceinline__ void store_last(const Gemm& q, PT* p, const Spot& spot, uint8_t* mine, int lane, const float (&v)[16], const float (&before)[4][4], bool onto,
+                                           float keep, float step) {
+  const int fr = lane % 32, fg = lane / 32;
+  lanes_done();
 #pragma unroll
-      for (int t = 0; t < 8; ++t) o[t] = fmaf(step, v[h * 8 + t], o[t] * keep);
-      if (n > h * 8) store_some<8>(p + h * 8, n - h * 8, o);
-    }
-  } else {
-    PT* p = reinterpret_cast<PT*>(last.out) + (int64_t)(q.matrix + which) * q.rows * q.cols + e;
+  for (int k = 0; k < 4; ++k) *staged_at(mine, fr, 4 * fg + k) = __builtin_bit_cast(u32x4, v4f{v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]});
+  lanes_done();
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float o[8];
+  for (int k = 0; k < 4; ++k) {
+    const v4f made = __builtin_bit_cast(v4f, *staged_at(mine, k * 8 + lane / 8, lane % 8));
+    float o[4];
 #pragma unroll
-      for (int t = 0; t < 8; ++t) o[t] = v[h * 8 + t];
-      if (n > h * 8) store_some<8>(p + h * 8, n - h * 8, o);
-    }
+    for (int t = 0; t < 4; ++t) o[t] = onto ? fmaf(step, made[t], before[k][t] * keep) : made[t];
+    if (k * 8 < spot.rows && spot.n > 0) store_some<4>(p + spot.at + k * 8 * q.cols, spot.n, o);
   }
 }
 
@@ -423,49 +479,82 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_muon_product(Gemms all, Las
   reads_landed();
   loads_landed();
   meet();
-  uint32_t* words = reinterpret_cast<uint32_t*>(lds) + wave * (32 * 33);
+  uint8_t* mine = lds + wave * kOwn;
   uint8_t* turned = q.symmetric ? (ti == tj ? nullptr : q.out) : q.turned;
   const int ldt = q.symmetric ? q.ldo : q.ldt;
-#pragma unroll
-  for (int i = 0; i < kMI; ++i)
-#pragma unroll
-    for (int j = 0; j < kNI; ++j) {
-      const int r0 = row0 + wm + i * 32, c0 = col0 + wn + j * 32;
-      if (r0 >= q.rows_a || c0 >= q.rows_b) continue;
-      const int64_t line = own + (int64_t)(r0 + fr) * q.ldo + c0 / kLine * 128;
-      float v[16], d[16];
-#pragma unroll
-      for (int t = 0; t < 16; ++t) v[t] = q.k0 * (kSums == 3 ? acc[0][i][j][t] + (acc[kSums / 2][i][j][t] + acc[kSums - 1][i][j][t]) : acc[0][i][j][t]);
-      if (q.d1) {
-        load_split(q.d1 + line, fg, d);
-#pragma unroll
-        for (int t = 0; t < 16; ++t) v[t] = fmaf(q.k1, d[t], v[t]);
-      }
-      if (q.d2) {
-        load_split(q.d2 + line, fg, d);
-#pragma unroll
-        for (int t = 0; t < 16; ++t) v[t] = fmaf(q.k2, d[t], v[t]);
-      }
-      if (q.last) {
-        store_last<PT>(q, last, which, r0 + fr, c0 + fg * 16, v);
-        continue;
-      }
-      uint32_t w[16];
-#pragma unroll
-      for (int t = 0; t < 16; ++t) w[t] = split_of(v[t]);
-      store_split(q.out + line, fg, w);
-      if (turned) {
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int t = 0; t < 16; ++t) words[fr * 33 + fg * 16 + t] = w[t];
-        __builtin_amdgcn_wave_barrier();
-        asm volatile("" ::: "memory");
-#pragma unroll
-        for (int t = 0; t < 16; ++t) w[t] = words[(fg * 16 + t) * 33 + fr];
-        asm volatile("" ::: "memory");
-        store_split(turned + own + (int64_t)(c0 + fr) * ldt + r0 / kLine * 128, fg, w);
-      }
+  auto place = [&](int f, int& r0, int& c0) {
+    r0 = row0 + wm + f / kNI * 32;
+    c0 = col0 + wn + f % kNI * 32;
+    return r0 < q.rows_a && c0 < q.rows_b;
+  };
+  // (what the next fragment adds to is on its way while one is worked on)
+  u32x4 ahead[4];
+  float before[4][4];
+  const bool onto = last.rows != nullptr;
+  PT* p = nullptr;
+  float keep = 0.0f, step = 0.0f;
+  if (q.last) {
+    if (onto) {
+      const Row& r = last.rows[q.matrix + which];
+      p = reinterpret_cast<PT*>(r.p);
+      keep = 1.0f - last.lr * r.decay;
+      step = -last.lr * r.factor;
+    } else {
+      p = reinterpret_cast<PT*>(last.out) + (int64_t)(q.matrix + which) * q.rows * q.cols;
     }
+  }
+  auto fetch = [&](int f) {
+    int r0, c0;
+    if (!place(f, r0, c0)) return;
+    if (q.d1) load_lines(q.d1 + own + (int64_t)r0 * q.ldo + c0 / kLine * 128, q.ldo, lane, ahead);
+  };
+  auto fetch_last = [&](int f) {
+    int r0, c0;
+    if (q.last && onto && place(f, r0, c0)) load_last(q, p, spot_of(q, lane, r0, c0), before);
+  };
+  fetch(0);
+  fetch_last(0);
+#pragma unroll
+  for (int f = 0; f < kMI * kNI; ++f) {
+    const int i = f / kNI, j = f % kNI;
+    int r0, c0;
+    if (!place(f, r0, c0)) continue;
+    const int64_t line = own + (int64_t)r0 * q.ldo + c0 / kLine * 128;
+    float v[16], d[16];
+#pragma unroll
+    for (int t = 0; t < 16; ++t) v[t] = q.k0 * (kSums == 3 ? acc[0][i][j][t] + (acc[kSums / 2][i][j][t] + acc[kSums - 1][i][j][t]) : acc[0][i][j][t]);
+    if (q.d1) {
+      staged_in(mine, lane, ahead, d);
+      if (f + 1 < kMI * kNI) fetch(f + 1);
+#pragma unroll
+      for (int t = 0; t < 16; ++t) v[t] = fmaf(q.k1, d[t], v[t]);
+    }
+    if (q.d2) {
+      u32x4 now[4];
+      load_lines(q.d2 + line, q.ldo, lane, now);
+      staged_in(mine, lane, now, d);
+#pragma unroll
+      for (int t = 0; t < 16; ++t) v[t] = fmaf(q.k2, d[t], v[t]);
+    }
+    if (q.last) {
+      float now[4][4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) now[k][t] = before[k][t];
+      if (f + 1 < kMI * kNI) fetch_last(f + 1);
+      store_last(q, p, spot_of(q, lane, r0, c0), mine, lane, v, now, onto, keep, step);
+      continue;
+    }
+    uint32_t w[16];
+#pragma unroll
+    for (int t = 0; t < 16; ++t) w[t] = split_of(v[t]);
+    staged_out(mine, lane, w, q.out + line, q.ldo);
+    if (turned) {
+      turn_fragment(reinterpret_cast<uint32_t*>(mine + kStaged), lane, w);
+      staged_out(mine, lane, w, turned + own + (int64_t)c0 * ldt + r0 / kLine * 128, ldt);
+    }
+  }
 }
 
 // ------------------------------------------------------------ small matrices
@@ -764,12 +853,16 @@ struct Run {
 struct Group {
   std::vector<Run> runs;
   int64_t bytes = 0, chunks = 0;
-  int32_t matrices = 0;
 };
 // Memory that a group's factors may take, unless a single matrix needs more.
 constexpr int64_t kGroupBytes = INT64_C(4) << 30;
 
-int64_t chunks_of(const Shape& s) { return (s.rows * s.cols + kChunk - 1) / kChunk; }
+// Chunks of a matrix's elements, and how many times kChunk they are.
+int64_t per_chunk(const Shape& s) { return (s.rows * s.cols + (int64_t)kChunk * kMostChunks - 1) / ((int64_t)kChunk * kMostChunks); }
+int64_t chunks_of(const Shape& s) {
+  const int64_t each = per_chunk(s) * kChunk;
+  return (s.rows * s.cols + each - 1) / each;
+}
 
 // shapes: in the table's order, equal ones together, none empty.
 // (small ones, at the end, are in no group)
@@ -786,24 +879,21 @@ std::vector<Group> groups_of(const std::vector<std::pair<int64_t, int64_t>>& sha
     g.runs.back().count++;
     g.bytes += s.bytes;
     g.chunks += chunks_of(s);
-    g.matrices++;
   }
   return groups;
 }
 
 struct Layout {
-  size_t scales, sums, factors, bytes;
+  size_t sums, factors, bytes;
 };
 Layout layout_of(const std::vector<Group>& groups, size_t table_rows) {
-  int64_t bytes = 0, chunks = 0, matrices = 0;
+  int64_t bytes = 0, chunks = 0;
   for (const Group& g : groups) {
     bytes = std::max(bytes, g.bytes);
     chunks = std::max(chunks, g.chunks);
-    matrices = std::max<int64_t>(matrices, g.matrices);
   }
   Layout l;
-  l.scales = up256(table_rows * sizeof(Row));
-  l.sums = l.scales + up256((size_t)matrices * sizeof(double));
+  l.sums = up256(table_rows * sizeof(Row));
   l.factors = l.sums + up256((size_t)chunks * sizeof(double));
   l.bytes = l.factors + (size_t)bytes;
   return l;
@@ -911,7 +1001,7 @@ std::vector<std::vector<Gemm>> products_of(const Run& run, uint8_t* base, int st
 // with X (2960 / 744 / 192 tiles) 87 / 69 / 72; four of 2048 x 512 9 / 18 / 48, 18 / 41 / 106, 26 / 22 / 50.
 // 14 matrices of 2048 x 8192: squares 504 / 372 / 360, A 2916 / 1310 / 1189, with X 4822 / 2856 / 2712.
 constexpr int kBig = 256, kMid = 128, kLittle = 64;
-constexpr int64_t kMostLittle = 2048, kMostMid = 1024;
+constexpr int64_t kMostLittle = 1000, kMostMid = 1024;
 
 template <typename PT>
 int32_t launch_products(Gemms& all, const Last& last, hipStream_t st, std::string* e) {
@@ -961,6 +1051,7 @@ int32_t launch_group(const Group& group, Source s, const Last& last, uint8_t* fa
     a.count = r.count;
     a.first_chunk = (int32_t)chunks;
     a.chunks = (int32_t)chunks_of(h);
+    a.per_chunk = (int32_t)per_chunk(h);
     chunks += (int64_t)a.chunks * r.count;
     a.first_tile = (int32_t)tiles;
     a.tiles_r = (int32_t)((h.tall ? h.n : h.m) / kSplit);
@@ -969,7 +1060,6 @@ int32_t launch_group(const Group& group, Source s, const Last& last, uint8_t* fa
   }
   parts.items = (int32_t)chunks;
   hipLaunchKernelGGL((k_muon_sums<GT, MUON>), grid_of(chunks), dim3(kThreads), 0, st, parts, s);
-  hipLaunchKernelGGL(k_muon_scales, dim3((unsigned)group.matrices), dim3(kThreads), 0, st, parts, s);
   parts.items = (int32_t)tiles;
   hipLaunchKernelGGL((k_muon_split<GT, MUON>), grid_of(tiles), dim3(kThreads), 0, st, parts, s);
   std::vector<std::vector<std::vector<Gemm>>> lists;
@@ -1159,7 +1249,7 @@ int32_t mtdao_orthogonalize(const void* x, int32_t dtype, int64_t batch, int64_t
   };
   if (is_tiny(rows, cols)) {
     RoctxRange range("mtdao_orthogonalize %lld x %lld x %lld", (long long)batch, (long long)rows, (long long)cols);
-    const Source s = {nullptr, x, nullptr, nullptr, 0.0f, 0, eps};
+    const Source s = {nullptr, x, nullptr, 0.0f, 0, eps};
     r = with([&](auto g, auto p) {
       return launch_tiny<decltype(g), decltype(p), false>({0, 0, rows, cols, steps}, batch, std::min(rows, cols), std::max(rows, cols), s, last, st, e);
     });
@@ -1171,7 +1261,7 @@ int32_t mtdao_orthogonalize(const void* x, int32_t dtype, int64_t batch, int64_t
   if (r != MTDAO_OK) return r;
   char* w = static_cast<char*>(workspace);
   RoctxRange range("mtdao_orthogonalize %lld x %lld x %lld", (long long)batch, (long long)rows, (long long)cols);
-  const Source s = {nullptr, x, reinterpret_cast<double*>(w + l.sums), reinterpret_cast<double*>(w + l.scales), 0.0f, 0, eps};
+  const Source s = {nullptr, x, reinterpret_cast<double*>(w + l.sums), 0.0f, 0, eps};
   for (const Group& g : groups) {
     r = with([&](auto gt, auto pt) {
       return launch_group<decltype(gt), decltype(pt), false>(g, s, last, reinterpret_cast<uint8_t*>(w + l.factors), steps, st, e);
@@ -1258,8 +1348,7 @@ int32_t mtdao_muon_step(mtdao_muon* h, double lr, void* hip_stream) try {
   RoctxRange range("mtdao_muon_step matrices=%d", c.n_matrices);
   char* w = h->workspace;
   const Row* rows = reinterpret_cast<const Row*>(w);
-  const Source s = {rows, nullptr, reinterpret_cast<double*>(w + h->layout.sums), reinterpret_cast<double*>(w + h->layout.scales),
-                    (float)c.momentum, c.nesterov != 0, c.eps};
+  const Source s = {rows, nullptr, reinterpret_cast<double*>(w + h->layout.sums), (float)c.momentum, c.nesterov != 0, c.eps};
   const Last last = {rows, nullptr, (float)lr};
   uint8_t* factors = reinterpret_cast<uint8_t*>(w + h->layout.factors);
   auto with = [&](auto go) {
