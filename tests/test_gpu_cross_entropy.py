@@ -128,6 +128,25 @@ def test_strides_and_in_place(cols, dtype):
     check(x, y, got=loss)
 
 
+def test_one_row_and_views_that_cannot_be_written():
+    x, y = make(1, 70, none=0.0)
+    loss, d = ops.cross_entropy_step(x[0].cuda(), y[0].cuda())
+    check(x, y, got=loss, grad=d[None])
+    wide = torch.randn((70, 9), device="cuda")
+    for bad in (wide.t(), x.cuda().expand(9, 70)):
+        with pytest.raises(ValueError, match="in place"):
+            ops.cross_entropy_step(bad, torch.zeros(9, dtype=torch.int64, device="cuda"), in_place=True)
+    check(wide.t().cpu(), torch.zeros(9, dtype=torch.int64), grad=ops.cross_entropy_step(wide.t(), torch.zeros(9, dtype=torch.int64, device="cuda"))[1])
+
+
+def test_gradients_that_are_broadcast():
+    """The sum of single losses: one number for all of them, strides of zero."""
+    x, y = make(9, 300)
+    leaf = x.cuda().requires_grad_()
+    ops.cross_entropy(leaf, y.cuda(), reduction="none").sum().backward()
+    check(x, y, reduction="sum", grad=leaf.grad)
+
+
 def test_batches_of_sequences():
     x, y = make(24, 300, "bf16")
     loss, d = ops.cross_entropy_step(x.view(4, 6, 300).cuda(), y.view(4, 6).cuda(), reduction="none")

@@ -134,6 +134,29 @@ def test_autograd_and_tied_tables():
     oracle.close(half.grad, want, err * 1.01 + want.abs() * 2.0 ** -8)
 
 
+def test_gradients_that_are_broadcast():
+    """The sum of all outputs: a gradient with strides of zero."""
+    table = torch.randn((20, 24), device="cuda", requires_grad=True)
+    tokens = tokens_of((50,), 20)
+    ops.embedding(tokens.cuda(), table).sum().backward()
+    check_sums(table.grad, torch.ones((50, 24)), tokens, 20, 1.0)
+    one = torch.randn((20, 1), device="cuda", requires_grad=True)
+    ops.embedding(tokens.cuda(), one).sum().backward()
+    check_sums(one.grad, torch.ones((50, 1)), tokens, 20, 1.0)
+
+
+def test_tables_and_tokens_that_do_not_fit():
+    table, ids = torch.randn((20, 24), device="cuda"), torch.zeros(5, dtype=torch.int64, device="cuda")
+    with pytest.raises(TypeError, match="tokens"):
+        ops.embedding(ids.float(), table)
+    with pytest.raises(TypeError, match="table"):
+        ops.embedding(ids, table.half())
+    with pytest.raises(ValueError, match="matrix"):
+        ops.embedding(ids, table[0])
+    with pytest.raises(TypeError, match="dy"):
+        ops.embedding_backward(torch.randn((5, 24), device="cuda").half(), ids, 20)
+
+
 def test_gradient_against_differences():
     table, tokens = torch.randn((12, 6)), tokens_of((20,), 12)
     up = torch.randn((20, 6))

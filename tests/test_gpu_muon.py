@@ -15,6 +15,7 @@ import torch
 
 import lm_oracle as oracle
 from paper_2510_05361_amd import ops
+from paper_2510_05361_amd.mtdao import MtdaoError
 
 pytestmark = pytest.mark.gpu
 
@@ -102,9 +103,10 @@ def test_scale_of_the_input(magnitude):
     assert float((sharp - want).norm()) <= 256 * U * float(want.norm())
 
 
-def test_zeros_and_what_is_not_finite():
-    x = torch.zeros((3, 40, 30))
-    x[1] = matrix(40, 30)
+@pytest.mark.parametrize("r,c", [(40, 30), (150, 140), (900, 530)])
+def test_zeros_and_what_is_not_finite(r, c):
+    x = torch.zeros((3, r, c))
+    x[1] = matrix(r, c)
     x[2] = x[1]
     x[2, 5, 7] = float("nan")
     out = ops.orthogonalize(x.cuda())
@@ -124,6 +126,8 @@ def test_batches_strides_and_types(t, o):
         assert torch.equal(ops.orthogonalize(view, dtype=DT[o]), out)
     one = ops.orthogonalize(x[1, 2].cuda(), dtype=DT[o])
     assert torch.equal(one, out[1, 2]), "a matrix alone gives what it gives among others"
+    small = ops.orthogonalize(x[..., :20, :].cuda(), dtype=DT[o])
+    assert torch.equal(ops.orthogonalize(x[0, 1, :20].cuda(), dtype=DT[o]), small[0, 1])
     assert ops.orthogonalize(x[:0].cuda()).shape == (0, 3, 90, 50)
     assert ops.orthogonalize(x[:, :, :0].cuda()).shape == (2, 3, 0, 50)
 
@@ -245,6 +249,49 @@ def test_captured_steps_and_other_streams():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(params, twin_p)), i
     assert all(torch.equal(a, b) for a, b in zip(opt.m, twin.m))
+
+
+def test_an_update_is_not_differentiable():
+    x = torch.randn((20, 30), device="cuda", requires_grad=True)
+    with pytest.raises(ValueError, match="requires a gradient"):
+        ops.orthogonalize(x)
+    with torch.no_grad():
+        check(ops.orthogonalize(x), x.detach().cpu())
+
+
+def test_matrices_and_gradients_that_do_not_fit():
+    w, g = torch.randn((20, 30), device="cuda"), torch.randn((20, 30), device="cuda")
+    for params, grads, kw, what in (([w[0]], [g[0]], {}, "matrices"), ([w.t()], [g], {}, "contiguous"), ([w, w.bfloat16()], [g, g], {}, "one type"),
+                                    ([w], [g.t()], {}, "gradients"), ([w], [g, g], {}, "gradients"), ([w], [g], {"factor": "norm"}, "factor"),
+                                    ([w], [g], {"weight_decay": [0.0, 0.0]}, "weight_decay"), ([w], [g], {"states": {"m": [w.double()]}}, "states")):
+        with pytest.raises(ValueError, match=what):
+            ops.Muon(params, grads, **kw)
+    for params, grads in (([w, w], [g, g]), ([w], [w])):
+        with pytest.raises(MtdaoError, match="overlap"):
+            ops.Muon(params, grads)
+    opt = ops.Muon([w], [g])
+    with pytest.raises(MtdaoError, match="overlap"):
+        opt.set_grads([opt.m[0]])
+    with pytest.raises(MtdaoError, match="lr"):
+        opt.step(float("nan"))
+
+
+def test_two_handles_on_two_streams():
+    """Workspaces of their own: steps at once give what they give one after the other."""
+    pairs = [make([(300, 200), (200, 300), (50, 60)] * 4, seed=s) for s in (1, 2)]
+    twins = [[p.clone() for p in params] for params, _, _ in pairs]
+    single = [ops.Muon(t, grads) for t, (_, grads, _) in zip(twins, pairs)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in pairs]
+    for _ in range(5):
+        for stream, (_, _, opt) in zip(streams, pairs):
+            with torch.cuda.stream(stream):
+                opt.step(0.01)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for opt in single:
+            opt.step(0.01)
+    assert all(torch.equal(a, b) for t, (params, _, _) in zip(twins, pairs) for a, b in zip(t, params))
 
 
 def test_a_step_is_a_change_in_place():
