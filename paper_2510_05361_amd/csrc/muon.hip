@@ -26,7 +26,6 @@
 #include <cmath>
 #include <cstring>
 #include <new>
-#include <numeric>
 #include <string>
 #include <utility>
 #include <vector>
@@ -101,8 +100,9 @@ __device__ __forceinline__ void update_of(const Source& s, const float (&g)[N], 
   for (int t = 0; t < N; ++t) u[t] = s.nesterov ? fmaf(s.momentum, m[t], g[t]) : m[t];
 }
 
+// Momentum (Muon) and the sum of the squares of a chunk of the update, in fp64.  Bound by HBM: 14 matrices
+// of 2048 x 8192 with bf16 gradients 434 us, 5.4 TB/s.
 constexpr int kSumV = 4;  // elements of a lane's vector: 16 bytes of momentum
-// Momentum (Muon) and the sum of the squares of a chunk of the update, in fp64.
 template <typename GT, bool MUON>
 __global__ __launch_bounds__(kThreads) void k_muon_sums(Parts parts, Source s) {
   __shared__ double part[kThreads / 64];
@@ -177,6 +177,8 @@ __device__ __forceinline__ void store_chunk(uint8_t* line, int chunk, const uint
 // X and its transpose from the update: a tile of 64 x 64, whose transpose goes
 // through LDS.  A thread has eight elements, a chunk of 16 bytes high and one low, of two rows, then of two columns.
 // Every workgroup adds up the matrix's sums of squares, in an order that the sizes fix.
+// Bound by HBM: the same 14 matrices 661 us, 5.0 TB/s (sixteen elements a thread, in pieces of 16 bytes
+// 32 apart, 715 us).
 constexpr int kSplit = 64;
 template <typename GT, bool MUON>
 __global__ __launch_bounds__(kThreads) void k_muon_split(Parts parts, Source s) {
@@ -373,6 +375,12 @@ __device__ __forceinline__ void store_last(const Gemm& q, PT* p, const Spot& spo
 // two steps of sixteen elements; a wave reads a step's fragments while the matrix
 // cores work on the step before, so it needs others only once a line: before the last step, when the line's last
 // fragments are in registers, all meet; then its place is free to be loaded, and the next line is there.
+//
+// Bound, with tiles of 256, by the matrix cores and the power they draw: A = X X^T of 14 matrices of 2048 x 8192
+// 1.2 ms, 1.35 PFLOP/s of the three instructions (a library's plain fp16 product of 8192^3: 1.06); squares 355 us, 1.14, and
+// products with X 2.6 ms, 1.11, as what a tile adds to and writes, 512 KB in some 30 us, goes by with
+// nothing behind it (one workgroup a CU).  Small products are bound by latency: 5 us a launch of one tile a CU, and
+// 0.2 us a line.
 template <int B, int WR, int WC, int STAGES, typename PT>
 __global__ __launch_bounds__(64 * WR * WC, 2) void k_muon_product(Gemms all, Last last) {
   constexpr int kWaves = WR * WC, kMI = B / WR / 32, kNI = B / WC / 32, kLoads = B / (8 * kWaves), kStage = 2 * B * 128;
@@ -563,7 +571,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_muon_product(Gemms all, Las
 // lie in LDS, lines as in memory, A and then b A + c A A in a third place; X, to which each step adds,
 // also in registers, as the fp32 it is formed in.  Wave w has the w-th 32 columns of X, the first one
 // to three waves the blocks of A on and above the diagonal.  MB: blocks of X's rows.
-// Bound by latency, of the steps' five meetings and chains of matrix instructions: 100 x 37 through
+// Bound by latency, of the steps' four meetings and chains of matrix instructions: 100 x 37 26 us, through
 // the launches that large matrices take 85 us.
 constexpr int kTinyM = 64, kTinyN = 256, kTinyThreads = 512;
 
@@ -996,10 +1004,11 @@ std::vector<std::vector<Gemm>> products_of(const Run& run, uint8_t* base, int st
 }
 
 // Tiles of a launch.  Large ones read less of the L2 for each product, small ones keep more
-// CUs at work; of those of 64 and 128 two workgroups share a CU.  16 matrices of 512 x 512 to
-// 2048 (a step's products, us, with tiles of 64 / 128 / 256): squares 20 / 22 / 51, A = X X^T 34 / 52 / 110,
-// with X (2960 / 744 / 192 tiles) 87 / 69 / 72; four of 2048 x 512 9 / 18 / 48, 18 / 41 / 106, 26 / 22 / 50.
-// 14 matrices of 2048 x 8192: squares 504 / 372 / 360, A 2916 / 1310 / 1189, with X 4822 / 2856 / 2712.
+// CUs at work; of those of 64 and 128 two workgroups share a CU.  us with tiles of 64 / 128 / 256:
+// 16 matrices of 512 x 512 to 512 x 2048: squares (576 / 160 / 48 tiles) 20 / 22 / 51, A = X X^T (as many) 34 / 52 / 110,
+// with X (2960 / 744 / 192) 87 / 67 / 72; four of 2048 x 512: squares (144 / 40 / 16) 9 / 18 / 48,
+// A 18 / 41 / 106, with X (1024 / 256 / 64) 29 / 23 / 50; 14 of 2048 x 8192: squares (7392 / 1904 / 504) 504 / 372 / 360,
+// A 2916 / 1310 / 1189, with X (57344 / 14336 / 3584) 4822 / 2856 / 2712.
 constexpr int kBig = 256, kMid = 128, kLittle = 64;
 constexpr int64_t kMostLittle = 1000, kMostMid = 1024;
 
