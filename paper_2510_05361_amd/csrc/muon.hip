@@ -255,6 +255,8 @@ struct Gemm {
   int32_t lda, ldb, ldo, ldt;      // bytes; d1 and d2 have out's rows
   int32_t symmetric;          // tiles on and above the diagonal only, out is turned
   int32_t tiles_a, tiles_b, tiles;
+  int32_t parts, part_blocks; // of the contraction, and their lines
+  float* partial;             // with more than one part: their sums, a tile after another, its parts together
   int32_t count, matrix;      // matrices, the first one's place in the table
   int32_t first, share;       // an XCD's tiles before its share of these matrices' tiles, that share
   int32_t last;
@@ -394,7 +396,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_muon_product(Gemms all, Las
   int k = 0;
   while (k + 1 < all.n && turn >= all.gemm[k + 1].first) ++k;
   const Gemm& q = all.gemm[k];
-  const int in = (int)(blockIdx.x % 8) * q.share + turn - q.first, which = in / q.tiles, tile = in - which * q.tiles;
+  const int in = (int)(blockIdx.x % 8) * q.share + turn - q.first, of_all = in / q.parts, part = in - of_all * q.parts;
+  const int which = of_all / q.tiles, tile = of_all - which * q.tiles;
   if (which >= q.count) return;
   int ti, tj;
   if (q.symmetric) {
@@ -403,7 +406,8 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_muon_product(Gemms all, Las
     ti = tile % q.tiles_a;
     tj = tile / q.tiles_a;
   }
-  const int row0 = ti * B, col0 = tj * B, blocks = q.blocks;
+  const int row0 = ti * B, col0 = tj * B, from = part * q.part_blocks;
+  const int blocks = q.blocks - from < q.part_blocks ? q.blocks - from : q.part_blocks;
   const int64_t own = (int64_t)which * q.step;
 
   // A wave loads eight rows at once: lane l the chunk that belongs at place l % 8 of row l / 8.
@@ -413,7 +417,7 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_muon_product(Gemms all, Las
   int va = lr * lda + ((lane % 8) ^ row_key(lr)) * 16, vb = lr * ldb + ((lane % 8) ^ row_key(lr)) * 16;
   auto load_part = [&](int t, int block) {  // 0 .. 2 kLoads - 1: those of a, then those of b
     const bool of_b = t >= kLoads;
-    const int line = block < blocks ? block : blocks - 1;  // (past the last line it is loaded again, and not used)
+    const int line = from + (block < blocks ? block : blocks - 1);  // (past the last line it is loaded again, and not used)
     asm("" : "+v"(va), "+v"(vb));  // (offsets of further rows are formed anew: they would each hold a register)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
         of_b ? rb : ra, (__attribute__((address_space(3))) void*)(lds + (block & (STAGES - 1)) * kStage + wave * 1024 + t * kWaves * 1024), 16,
@@ -487,6 +491,14 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_muon_product(Gemms all, Las
   reads_landed();
   loads_landed();
   meet();
+  if constexpr (kSums == 3) {
+    if (q.parts > 1) {
+      float* to = q.partial + (int64_t)in * (B * B) + wave * 1024 + lane;
+#pragma unroll
+      for (int t = 0; t < 16; ++t) to[t * 64] = acc[0][0][0][t] + (acc[1][0][0][t] + acc[2][0][0][t]);
+      return;
+    }
+  }
   uint8_t* mine = lds + wave * kOwn;
   uint8_t* turned = q.symmetric ? (ti == tj ? nullptr : q.out) : q.turned;
   const int ldt = q.symmetric ? q.ldo : q.ldt;
@@ -563,6 +575,40 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void k_muon_product(Gemms all, Las
       staged_out(mine, lane, w, turned + own + (int64_t)c0 * ldt + r0 / kLine * 128, ldt);
     }
   }
+}
+
+// A = X X^T from the sums of its parts, added in their order: a tile of 64 x 64 a workgroup.
+__global__ __launch_bounds__(256) void k_muon_join(Gemms all) {
+  constexpr int B = 64;
+  __shared__ __attribute__((aligned(128))) uint8_t lds[4 * kOwn];
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  int in = blockIdx.x, k = 0;
+  for (; k < all.n; ++k) {
+    const int here = all.gemm[k].parts > 1 ? all.gemm[k].tiles * all.gemm[k].count : 0;
+    if (in < here) break;
+    in -= here;
+  }
+  if (k == all.n) return;
+  const Gemm& q = all.gemm[k];
+  const int which = in / q.tiles;
+  int ti, tj;
+  triangle_place(in - which * q.tiles, q.tiles_a, ti, tj);
+  const float* from = q.partial + (int64_t)in * q.parts * (B * B) + wave * 1024 + lane;
+  float v[16] = {};
+#pragma unroll 4
+  for (int part = 0; part < q.parts; ++part) {
+#pragma unroll
+    for (int t = 0; t < 16; ++t) v[t] += from[part * (B * B) + t * 64];
+  }
+  uint32_t w[16];
+#pragma unroll
+  for (int t = 0; t < 16; ++t) w[t] = split_of(q.k0 * v[t]);
+  uint8_t *mine = lds + wave * kOwn, *out = q.out + (int64_t)which * q.step;
+  const int r0 = ti * B + wave / 2 * 32, c0 = tj * B + wave % 2 * 32;
+  staged_out(mine, lane, w, out + (int64_t)r0 * q.ldo + c0 / kLine * 128, q.ldo);
+  if (ti == tj) return;
+  turn_fragment(reinterpret_cast<uint32_t*>(mine + kStaged), lane, w);
+  staged_out(mine, lane, w, out + (int64_t)c0 * q.ldo + r0 / kLine * 128, q.ldo);
 }
 
 // ------------------------------------------------------------ small matrices
@@ -891,8 +937,22 @@ std::vector<Group> groups_of(const std::vector<std::pair<int64_t, int64_t>>& sha
   return groups;
 }
 
+// Tiles of a launch.  Large ones read less of the L2 for each product, small ones keep more
+// CUs at work; of those of 64 and 128 two workgroups share a CU.  us with tiles of 64 / 128 / 256:
+// 16 matrices of 512 x 512 to 512 x 2048: squares (576 / 160 / 48 tiles) 20 / 22 / 51, A = X X^T (as many) 34 / 52 / 110,
+// with X (2960 / 744 / 192) 87 / 67 / 72; four of 2048 x 512: squares (144 / 40 / 16) 9 / 18 / 48,
+// A 18 / 41 / 106, with X (1024 / 256 / 64) 29 / 23 / 50; 14 of 2048 x 8192: squares (7392 / 1904 / 504) 504 / 372 / 360,
+// A 2916 / 1310 / 1189, with X (57344 / 14336 / 3584) 4822 / 2856 / 2712.
+constexpr int kBig = 256, kMid = 128, kLittle = 64;
+constexpr int64_t kMostLittle = 1000, kMostMid = 1024;
+
+// A = X X^T of few tiles, up to kFewTiles, and many lines is formed in parts of at least kLeastPart lines, as many as
+// occupy the CUs once, and joined: 300 x 8000 396 -> 244 us, 1 x 8192 332 -> 153 us.
+constexpr int64_t kFewTiles = 128, kParts = 256, kLeastPart = 8, kManyLines = 32;
+constexpr int64_t kPartialBytes = kParts * kLittle * kLittle * 4;
+
 struct Layout {
-  size_t sums, factors, bytes;
+  size_t sums, partial, factors, bytes;
 };
 Layout layout_of(const std::vector<Group>& groups, size_t table_rows) {
   int64_t bytes = 0, chunks = 0;
@@ -902,7 +962,8 @@ Layout layout_of(const std::vector<Group>& groups, size_t table_rows) {
   }
   Layout l;
   l.sums = up256(table_rows * sizeof(Row));
-  l.factors = l.sums + up256((size_t)chunks * sizeof(double));
+  l.partial = l.sums + up256((size_t)chunks * sizeof(double));
+  l.factors = l.partial + (groups.empty() ? 0 : (size_t)kPartialBytes);
   l.bytes = l.factors + (size_t)bytes;
   return l;
 }
@@ -1003,17 +1064,12 @@ std::vector<std::vector<Gemm>> products_of(const Run& run, uint8_t* base, int st
   return list;
 }
 
-// Tiles of a launch.  Large ones read less of the L2 for each product, small ones keep more
-// CUs at work; of those of 64 and 128 two workgroups share a CU.  us with tiles of 64 / 128 / 256:
-// 16 matrices of 512 x 512 to 512 x 2048: squares (576 / 160 / 48 tiles) 20 / 22 / 51, A = X X^T (as many) 34 / 52 / 110,
-// with X (2960 / 744 / 192) 87 / 67 / 72; four of 2048 x 512: squares (144 / 40 / 16) 9 / 18 / 48,
-// A 18 / 41 / 106, with X (1024 / 256 / 64) 29 / 23 / 50; 14 of 2048 x 8192: squares (7392 / 1904 / 504) 504 / 372 / 360,
-// A 2916 / 1310 / 1189, with X (57344 / 14336 / 3584) 4822 / 2856 / 2712.
-constexpr int kBig = 256, kMid = 128, kLittle = 64;
-constexpr int64_t kMostLittle = 1000, kMostMid = 1024;
-
 template <typename PT>
-int32_t launch_products(Gemms& all, const Last& last, hipStream_t st, std::string* e) {
+int32_t launch_products(Gemms& all, const Last& last, float* partial, hipStream_t st, std::string* e) {
+  for (int i = 0; i < all.n; ++i) {
+    all.gemm[i].parts = 1;
+    all.gemm[i].part_blocks = all.gemm[i].blocks;
+  }
   auto count = [&](int tile) {
     int64_t items = 0, turns = 0;
     for (int i = 0; i < all.n; ++i) {
@@ -1021,7 +1077,7 @@ int32_t launch_products(Gemms& all, const Last& last, hipStream_t st, std::strin
       g.tiles_a = (g.rows_a + tile - 1) / tile;
       g.tiles_b = (g.rows_b + tile - 1) / tile;
       g.tiles = g.symmetric ? g.tiles_a * (g.tiles_a + 1) / 2 : g.tiles_a * g.tiles_b;
-      g.share = (int32_t)(((int64_t)g.tiles * g.count + 7) / 8);
+      g.share = (int32_t)(((int64_t)g.tiles * g.count * g.parts + 7) / 8);
       g.first = (int32_t)turns;
       turns += g.share;
       items += (int64_t)g.tiles * g.count;
@@ -1035,14 +1091,34 @@ int32_t launch_products(Gemms& all, const Last& last, hipStream_t st, std::strin
     hipLaunchKernelGGL(kernel, dim3((unsigned)(8 * count(tile).second)), dim3((unsigned)threads), (size_t)bytes, st, all, last);
     return (int32_t)MTDAO_OK;
   };
-  if (count(kLittle).first <= kMostLittle) return go(k_muon_product<kLittle, 2, 2, 4, PT>, kLittle, 256, 4);
+  const int64_t little = count(kLittle).first;
+  int64_t joined = 0;
+  if (little <= kFewTiles) {
+    float* to = partial;
+    for (int i = 0; i < all.n; ++i) {
+      Gemm& g = all.gemm[i];
+      if (!g.symmetric || g.d1 || g.blocks < kManyLines) continue;
+      const int64_t parts = std::min(kParts / little, g.blocks / kLeastPart);
+      g.part_blocks = (int32_t)((g.blocks + parts - 1) / parts);
+      g.parts = (g.blocks + g.part_blocks - 1) / g.part_blocks;
+      if (g.parts == 1) continue;
+      g.partial = to;
+      to += (int64_t)g.tiles * g.count * g.parts * (kLittle * kLittle);
+      joined += (int64_t)g.tiles * g.count;
+    }
+  }
+  if (little <= kMostLittle) {
+    const int32_t r = go(k_muon_product<kLittle, 2, 2, 4, PT>, kLittle, 256, 4);
+    if (r == MTDAO_OK && joined > 0) hipLaunchKernelGGL(k_muon_join, dim3((unsigned)joined), dim3(256), 0, st, all);
+    return r;
+  }
   if (count(kMid).first <= kMostMid) return go(k_muon_product<kMid, 2, 2, 2, PT>, kMid, 256, 2);
   return go(k_muon_product<kBig, 2, 4, 2, PT>, kBig, 512, 2);
 }
 
 // All the work of a group's matrices.
 template <typename GT, typename PT, bool MUON>
-int32_t launch_group(const Group& group, Source s, const Last& last, uint8_t* factors, int steps, hipStream_t st, std::string* e) {
+int32_t launch_group(const Group& group, Source s, const Last& last, uint8_t* factors, float* partial, int steps, hipStream_t st, std::string* e) {
   Parts parts;
   std::memset(&parts, 0, sizeof parts);
   int64_t chunks = 0, tiles = 0;
@@ -1083,7 +1159,7 @@ int32_t launch_group(const Group& group, Source s, const Last& last, uint8_t* fa
     for (const auto& list : lists)
       if (i < list.size())
         for (const Gemm& g : list[i]) all.gemm[all.n++] = g;
-    const int32_t r = launch_products<PT>(all, last, st, e);
+    const int32_t r = launch_products<PT>(all, last, partial, st, e);
     if (r != MTDAO_OK) return r;
   }
   return MTDAO_OK;
@@ -1273,7 +1349,7 @@ int32_t mtdao_orthogonalize(const void* x, int32_t dtype, int64_t batch, int64_t
   const Source s = {nullptr, x, reinterpret_cast<double*>(w + l.sums), 0.0f, 0, eps};
   for (const Group& g : groups) {
     r = with([&](auto gt, auto pt) {
-      return launch_group<decltype(gt), decltype(pt), false>(g, s, last, reinterpret_cast<uint8_t*>(w + l.factors), steps, st, e);
+      return launch_group<decltype(gt), decltype(pt), false>(g, s, last, reinterpret_cast<uint8_t*>(w + l.factors), reinterpret_cast<float*>(w + l.partial), steps, st, e);
     });
     if (r != MTDAO_OK) return r;
   }
@@ -1360,6 +1436,7 @@ int32_t mtdao_muon_step(mtdao_muon* h, double lr, void* hip_stream) try {
   const Source s = {rows, nullptr, reinterpret_cast<double*>(w + h->layout.sums), (float)c.momentum, c.nesterov != 0, c.eps};
   const Last last = {rows, nullptr, (float)lr};
   uint8_t* factors = reinterpret_cast<uint8_t*>(w + h->layout.factors);
+  float* partial = reinterpret_cast<float*>(w + h->layout.partial);
   auto with = [&](auto go) {
     if (c.param_dtype == MTDAO_F32 && c.grad_dtype == MTDAO_F32) return go(float{}, float{});
     if (c.param_dtype == MTDAO_F32) return go(bf16_t{}, float{});
@@ -1368,7 +1445,7 @@ int32_t mtdao_muon_step(mtdao_muon* h, double lr, void* hip_stream) try {
   };
   int32_t r = MTDAO_OK;
   for (const Group& g : h->groups) {
-    r = with([&](auto gt, auto pt) { return launch_group<decltype(gt), decltype(pt), true>(g, s, last, factors, c.steps, st, &h->err); });
+    r = with([&](auto gt, auto pt) { return launch_group<decltype(gt), decltype(pt), true>(g, s, last, factors, partial, c.steps, st, &h->err); });
     if (r != MTDAO_OK) return r;
   }
   if (h->tiny > 0) {

@@ -52,7 +52,7 @@ def check(got, x, steps=5, eps=1e-7):
 
 
 SIZES = [(32, 32), (33, 31), (32, 256), (33, 256), (256, 33), (64, 255), (65, 64), (20, 257), (31, 224), (64, 129), (1, 1), (1, 9), (9, 1), (2, 3), (37, 100), (100, 37), (64, 64), (128, 128), (129, 127), (127, 400), (128, 129), (256, 256), (300, 301), (511, 130),
-         (96, 1000), (640, 520), (257, 1030), (1030, 257)]
+         (96, 1000), (640, 520), (257, 1030), (1030, 257), (1, 8192), (3000, 2), (100, 5000), (1500, 300), (129, 2047)]
 
 
 @pytest.mark.parametrize("t", ["f32", "bf16"])
