@@ -617,9 +617,13 @@ __global__ __launch_bounds__(256) void k_muon_join(Gemms all) {
 // lie in LDS, lines as in memory, A and then b A + c A A in a third place; X, to which each step adds,
 // also in registers, as the fp32 it is formed in.  Wave w has the w-th 32 columns of X, the first one
 // to three waves the blocks of A on and above the diagonal.  MB: blocks of X's rows.
-// Bound by latency, of the steps' four meetings and chains of matrix instructions: 100 x 37 26 us, through
-// the launches that large matrices take 85 us.
+// Bound by latency, of the steps' four or five meetings, chains of matrix instructions and what is written both ways: 64 x 64
+// 24 us, 64 x 256 38 us; 100 x 37 25 us, through the launches that large matrices take 85 us.
 constexpr int kTinyM = 64, kTinyN = 256, kTinyThreads = 512;
+
+// Parts of X's lines in which A = X X^T is formed: eight waves among its one or three blocks.
+template <int MB>
+constexpr int kTinyParts = MB == 1 ? 8 : 2;
 
 struct Tiny {
   int32_t first, lines;   // of the table; lines of X's rows
@@ -638,10 +642,11 @@ template <typename GT, typename PT, bool MUON, int MB>
 __global__ __launch_bounds__(kTinyThreads) void k_muon_tiny(Tiny t, Source s, Last last) {
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   __shared__ double part[kTinyThreads / 64];
-  constexpr int kM = 32 * MB, kBlocks = MB * (MB + 1) / 2;
+  constexpr int kM = 32 * MB, kBlocks = MB * (MB + 1) / 2, kParts = kTinyParts<MB>;
   const int tid = (int)threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), fr = lane % 32, fg = lane / 32;
   const int xs = t.lines * 128, ts = MB * 128;      // bytes of a row of X, and of X^T and A
   uint8_t *X = lds, *T = X + kM * xs, *A = T + t.lines * kLine * ts;
+  float* sums = reinterpret_cast<float*>(A + kM * ts);  // of A's parts but the first
   const int which = t.first + (int)blockIdx.x;
   const Row* entry = MUON ? s.rows + which : nullptr;
   const int r = MUON ? entry->rows : (int)t.rows, c = MUON ? entry->cols : (int)t.cols;
@@ -697,39 +702,59 @@ __global__ __launch_bounds__(kTinyThreads) void k_muon_tiny(Tiny t, Source s, La
   for (int q = 0; q < kSlots; ++q) {
     const int v = q * kTinyThreads + tid, row = v / vectors, col = (v - row * vectors) * 8;
     if (v >= all) continue;
+    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (col + i < c) {
-        const uint32_t w = split_of((float)((double)u[q][i] * scale));
-        if (tall) {
-          put(at_t, row, col + i, w);
-          put(at_x, col + i, row, w);
-        } else {
-          put(at_x, row, col + i, w);
-          put(at_t, col + i, row, w);
-        }
+    for (int i = 0; i < 8; ++i) w[i] = split_of((float)((double)u[q][i] * scale));  // (zeros past the row's end)
+    // a chunk in the row's place, an element in each of eight rows of the transpose
+    auto both = [&](auto at_own, auto at_turned) {
+      u32x4 hi, lo;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        hi[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x05040100u);
+        lo[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
       }
-    }
+      *reinterpret_cast<u32x4*>(at_own(row, col / kLine, col % kLine / 8)) = hi;
+      *reinterpret_cast<u32x4*>(at_own(row, col / kLine, 4 + col % kLine / 8)) = lo;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) put(at_turned, col + i, row, w[i]);  // (rows there are for whole chunks)
+    };
+    if (tall) both(at_t, at_x);
+    else both(at_x, at_t);
   }
   __syncthreads();
 
-  // sums of hi hi, lo hi and hi lo of 32 rows of a and of b over `lines` lines
-  auto product = [&](auto at_rows, int row0, auto at_cols, int col0, int lines, float (&v)[16]) {
+  // sums of hi hi, lo hi and hi lo of 32 rows of a and of b over lines from .. to; a line's eight
+  // fragments are read while the one before is multiplied
+  auto product = [&](auto at_rows, int row0, auto at_cols, int col0, int from, int to, float (&v)[16]) {
     v16f acc[3];
 #pragma unroll
     for (int k = 0; k < 3; ++k)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[k][i] = 0.0f;
-    for (int line = 0; line < lines; ++line) {
+    const int ra = row0 + fr, rb = col0 + row_of_b(fr);
+    v8h now[2][4], next[2][4];
+    auto read = [&](int line, v8h (&f)[2][4]) {
+#pragma unroll
+      for (int step = 0; step < 2; ++step)
+#pragma unroll
+        for (int low = 0; low < 2; ++low) {
+          f[step][low] = *reinterpret_cast<const v8h*>(at_rows(ra, line, 4 * low + 2 * step + fg));
+          f[step][2 + low] = *reinterpret_cast<const v8h*>(at_cols(rb, line, 4 * low + 2 * step + fg));
+        }
+    };
+    if (from < to) read(from, now);
+    for (int line = from; line < to; ++line) {
+      if (line + 1 < to) read(line + 1, next);
 #pragma unroll
       for (int step = 0; step < 2; ++step) {
-        const int ra = row0 + fr, rb = col0 + row_of_b(fr);
-        const v8h ha = *reinterpret_cast<const v8h*>(at_rows(ra, line, 2 * step + fg)), la = *reinterpret_cast<const v8h*>(at_rows(ra, line, 4 + 2 * step + fg));
-        const v8h hb = *reinterpret_cast<const v8h*>(at_cols(rb, line, 2 * step + fg)), lb = *reinterpret_cast<const v8h*>(at_cols(rb, line, 4 + 2 * step + fg));
-        acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hb, ha, acc[0], 0, 0, 0);
-        acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lb, ha, acc[1], 0, 0, 0);
-        acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(hb, la, acc[2], 0, 0, 0);
+        acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[step][2], now[step][0], acc[0], 0, 0, 0);
+        acc[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[step][3], now[step][0], acc[1], 0, 0, 0);
+        acc[2] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[step][2], now[step][1], acc[2], 0, 0, 0);
       }
+#pragma unroll
+      for (int step = 0; step < 2; ++step)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) now[step][k] = next[step][k];
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = acc[0][i] + (acc[1][i] + acc[2][i]);
@@ -748,11 +773,24 @@ __global__ __launch_bounds__(kTinyThreads) void k_muon_tiny(Tiny t, Source s, La
       *reinterpret_cast<u32x4*>(at(row0 + fr, col0 / kLine, 4 + 2 * fg + h)) = lo[h];
     }
   };
+  // (two lanes share what they hold of two rows, so that each stores pairs in one of them: halves of words cost
+  // LDS as much as words, and twice where both halves come at once)
   auto store_turned = [&](auto at, int row0, int col0, const uint32_t (&w)[16]) {
+    const bool odd = fr & 1;
+    const int col = row0 + (fr & ~1);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) put(at, col0 + fg * 16 + i, row0 + fr, w[i]);
+    for (int i = 0; i < 16; i += 2) {
+      const uint32_t own = odd ? w[i + 1] : w[i];
+      const uint32_t other = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(odd ? w[i] : w[i + 1]), 0xb1, 0xf, 0xf, true);  // of the neighbour
+      const uint32_t first = odd ? other : own, second = odd ? own : other;
+      const int row = col0 + fg * 16 + i + odd;
+      *reinterpret_cast<uint32_t*>(at(row, col / kLine, col % kLine / 8) + col % 8 * 2) = __builtin_amdgcn_perm(second, first, 0x05040100u);
+      *reinterpret_cast<uint32_t*>(at(row, col / kLine, 4 + col % kLine / 8) + col % 8 * 2) = __builtin_amdgcn_perm(second, first, 0x07060302u);
+    }
   };
-  const int bi = wave == 2 ? 32 : 0, bj = wave == 0 ? 0 : 32;  // of A, for the first kBlocks waves
+  // the block of A of a wave, and its part of X's lines where there are many
+  const int block = wave % kBlocks, mine = wave / kBlocks, parts = blocks > 2 ? kParts : 1, part_lines = (blocks + parts - 1) / parts;
+  const int bi = block == 2 ? 32 : 0, bj = MB == 1 || block == 0 ? 0 : 32;
   auto store_square = [&](const float (&v)[16]) {
     uint32_t w[16];
 #pragma unroll
@@ -774,15 +812,26 @@ __global__ __launch_bounds__(kTinyThreads) void k_muon_tiny(Tiny t, Source s, La
   }
   for (int step = 0; step < t.steps; ++step) {
     float gram[16], poly[16];
+    if (mine < parts) {
+      const int from = mine * part_lines, to = from + part_lines < blocks ? from + part_lines : blocks;
+      product(at_x, bi, at_x, bj, from, to, gram);
+      if (mine > 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sums[((mine - 1) * kBlocks + block) * 1024 + i * 64 + lane] = gram[i];
+      }
+    }
+    if (parts > 1) __syncthreads();
     if (wave < kBlocks) {
-      product(at_x, bi, at_x, bj, blocks, gram);
+      for (int part = 1; part < parts; ++part)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) gram[i] += sums[((part - 1) * kBlocks + block) * 1024 + i * 64 + lane];
 #pragma unroll
       for (int i = 0; i < 16; ++i) gram[i] *= __builtin_ldexpf(1.0f, kA - 2 * kX);
       store_square(gram);
     }
     __syncthreads();
     if (wave < kBlocks) {
-      product(at_a, bi, at_a, bj, MB, poly);
+      product(at_a, bi, at_a, bj, 0, MB, poly);
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         poly[i] = fmaf((float)kCb * __builtin_ldexpf(1.0f, kB - kA), gram[i], (float)kCc * __builtin_ldexpf(1.0f, kB - 2 * kA) * poly[i]);
@@ -794,7 +843,7 @@ __global__ __launch_bounds__(kTinyThreads) void k_muon_tiny(Tiny t, Source s, La
 #pragma unroll
       for (int b = 0; b < MB; ++b) {
         float v[16];
-        product(at_a, 32 * b, at_t, 32 * wave, MB, v);
+        product(at_a, 32 * b, at_t, 32 * wave, 0, MB, v);
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[b][i] = fmaf((float)kCa, x[b][i], __builtin_ldexpf(1.0f, -kB) * v[i]);
       }
@@ -815,16 +864,35 @@ __global__ __launch_bounds__(kTinyThreads) void k_muon_tiny(Tiny t, Source s, La
   PT* out = MUON ? reinterpret_cast<PT*>(entry->p) : reinterpret_cast<PT*>(last.out) + (int64_t)which * r * c;
   const float keep = MUON ? 1.0f - last.lr * entry->decay : 0.0f, move = MUON ? -last.lr * entry->factor : 0.0f;
 #pragma unroll
-  for (int b = 0; b < MB; ++b)
+  for (int b = 0; b < MB; ++b) {
+    if (tall) {  // a column's sixteen rows a lane, neighbouring columns in neighbouring lanes
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int row = tall ? 32 * wave + fg * 16 + i : 32 * b + fr, col = tall ? 32 * b + fr : 32 * wave + fg * 16 + i;
-      if (row < r && col < c) {
+      for (int i = 0; i < 16; ++i) {
+        const int row = 32 * wave + fg * 16 + i, col = 32 * b + fr;
+        if (row < r && col < c) {
+          PT* at = out + row * c + col;
+          const float o = __builtin_ldexpf(1.0f, -kX) * x[b][i];
+          store_one(at, MUON ? fmaf(move, o, to_f32(*at) * keep) : o);
+        }
+      }
+    } else {
+      const int row = 32 * b + fr;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int col = 32 * wave + fg * 16 + 8 * h, n = row < r ? c - col : 0;
+        if (n <= 0) continue;
         PT* at = out + row * c + col;
-        const float o = __builtin_ldexpf(1.0f, -kX) * x[b][i];
-        store_one(at, MUON ? fmaf(move, o, to_f32(*at) * keep) : o);
+        float o[8];
+        if (MUON) load_some<8>(at, n, o);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float made = __builtin_ldexpf(1.0f, -kX) * x[b][8 * h + i];
+          o[i] = MUON ? fmaf(move, made, o[i] * keep) : made;
+        }
+        store_some<8>(at, n, o);
       }
     }
+  }
 }
 
 // Writes rows `at`.. of the table.
@@ -888,8 +956,12 @@ template <typename GT, typename PT, bool MUON>
 int32_t launch_tiny(Tiny t, int64_t count, int64_t m, int64_t n, const Source& s, const Last& last, hipStream_t st, std::string* e) {
   t.lines = (int32_t)((n + 2 * kLine - 1) / (2 * kLine) * 2);
   auto go = [&](auto kernel, int mb) {
-    const int bytes = 32 * mb * t.lines * 128 + t.lines * kLine * mb * 128 + 32 * mb * mb * 128;
-    const int32_t r = allow_lds(reinterpret_cast<const void*>(kernel), 64 * 8 * 128 + 256 * 2 * 128 + 64 * 2 * 128, e);
+    auto need = [&](int lines) {
+      const int sums = mb == 1 ? kTinyParts<1> - 1 : 3 * (kTinyParts<2> - 1);
+      return 32 * mb * lines * 128 + lines * kLine * mb * 128 + 32 * mb * mb * 128 + sums * 4096;
+    };
+    const int bytes = need(t.lines);
+    const int32_t r = allow_lds(reinterpret_cast<const void*>(kernel), need(kTinyN / kLine), e);
     if (r != MTDAO_OK) return r;
     hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(kTinyThreads), (size_t)bytes, st, t, s, last);
     return (int32_t)MTDAO_OK;

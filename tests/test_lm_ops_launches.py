@@ -93,4 +93,4 @@ def test_matrices_of_a_step_share_their_launches(run):
             c.mtdao_muon_destroy(h)
         """)
         counts.append(len([1 for name, *_ in launches if name != "k_muon_table"]))
-    assert counts[1] <= counts[0] <= counts[1] + 2  # (few matrices' A is formed in parts and joined)
+    assert counts[1] <= counts[0] <= counts[1] + 5  # (few matrices' A, five times, is formed in parts and joined)
