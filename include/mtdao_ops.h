@@ -18,8 +18,8 @@
  * only enqueued on the HIP stream passed to each call (no allocation, no
  * host wait, no memset, so calls can be captured into a HIP graph), negative
  * MTDAO_ERR_* codes from host-side validation before anything is enqueued,
- * messages from mtdao_last_error(NULL) (calls without a handle) or
- * mtdao_adamw_last_error.  Types are MTDAO_F32 / MTDAO_BF16.  Device pointers
+ * messages from mtdao_last_error(NULL) (calls without a handle),
+ * mtdao_adamw_last_error or mtdao_muon_last_error.  Types are MTDAO_F32 / MTDAO_BF16.  Device pointers
  * are aligned to their element unless stated otherwise.
  *
  * 8-bit blocks.  A block holds e4m3 codes c_i (4 exponent bits of bias 7, 3

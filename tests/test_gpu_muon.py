@@ -198,6 +198,15 @@ def test_shapes_of_many_kinds_in_one_step():
         step_and_check(params, grads, opt)
 
 
+def test_large_shapes_of_many_kinds_in_one_step():
+    """... each with tiles of its own, some with several steps at once, and small ones among them."""
+    shapes = [(66 + i, 300 - 3 * i) for i in range(14)] + [(300 - 5 * i, 70 + i) for i in range(5)]
+    shapes += [(520 + 8 * i, 900 - 10 * i) for i in range(7)] + [(800, 515), (20, 30), (64, 256), (600, 600), (3, 700), (700, 3), (257, 1)]
+    params, grads, opt = make(shapes, weight_decay=0.1)
+    for _ in range(2):
+        step_and_check(params, grads, opt, decay=0.1)
+
+
 def test_other_gradients_and_states():
     params, grads, opt = make(MODEL)
     opt.step(0.02)
