@@ -7,9 +7,9 @@
 // A product is hi hi + hi lo + lo hi in the fp16 matrix instructions, each
 // term exact and summed in fp32; lo lo, 2^-24 of the product at most, is left out.
 // That is three matrix instructions for a product of fp32's precision, at a
-// sixteenth of the cost of fp32's own each.  (One fp16 or bf16 term alone would leave the directions
+// sixteenth of the cost of fp32's own each.  (One bf16 term alone leaves the directions
 // with small singular values, which the iteration raises 480-fold, to rounding:
-// errors of 2 to 40 in a hundred of the result.)
+// errors of 2 (Gaussian) to 40 (low rank and noise) in a hundred of the result.)
 // fp16's exponents suffice because all factors are bounded: the singular values
 // s of X are at most 1.21 from the first product on (the largest of a s + b s^3 + c s^5
 // over [0, 1.27] is 1.2016), so elements of X and A = X X^T stay below 1.21 and 1.46,
