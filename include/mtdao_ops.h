@@ -343,6 +343,7 @@ typedef struct mtdao_cross_entropy_args {
   void* d_logits;        /* or NULL; may be logits itself when the strides are equal   */
 } mtdao_cross_entropy_args;
 
+/* What is written overlaps no other operand, but for d_logits in place of logits. */
 /* Reads the sizes and the reduction of a.  Host-only.  workspace: 256-byte aligned. */
 int32_t mtdao_cross_entropy_workspace_bytes(const mtdao_cross_entropy_args* a, size_t* bytes);
 int32_t mtdao_cross_entropy(const mtdao_cross_entropy_args* a, void* workspace, size_t workspace_bytes, void* hip_stream);

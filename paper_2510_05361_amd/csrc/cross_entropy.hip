@@ -341,8 +341,16 @@ int32_t check_pointers(const mtdao_cross_entropy_args& a, std::string* e) {
     const int64_t in = ((a.rows - 1) * a.ld_logits + a.cols) * es, out = ((a.rows - 1) * a.ld_d + a.cols) * es;
     if (overlap(a.logits, in, a.d_logits, out) && (a.logits != a.d_logits || a.ld_logits != a.ld_d))
       return fail(e, MTDAO_ERR_INVALID_ARG, "d_logits overlaps logits other than element on element");
-    if (overlap(a.targets, a.rows * a.target_bits / 8, a.d_logits, out)) return fail(e, MTDAO_ERR_INVALID_ARG, "d_logits overlaps targets");
   }
+  // (the losses are written while other rows are read)
+  struct { const void* p; int64_t bytes; bool written; } all[] = {
+      {a.losses, a.rows * 4, true}, {a.loss, 4, true}, {a.d_logits, ((a.rows - 1) * a.ld_d + a.cols) * es, true},
+      {a.logits, ((a.rows - 1) * a.ld_logits + a.cols) * es, false}, {a.targets, a.rows * a.target_bits / 8, false},
+      {a.d_loss, a.reduction == MTDAO_LOSS_NONE ? a.rows * 4 : 4, false}};
+  for (int i = 0; i < 6; ++i)
+    for (int j = i + 1; j < 6; ++j)
+      if (all[i].p && all[j].p && all[i].written && !(i == 2 && j == 3) && overlap(all[i].p, all[i].bytes, all[j].p, all[j].bytes))
+        return fail(e, MTDAO_ERR_INVALID_ARG, "losses, loss or d_logits overlaps another operand");
   return MTDAO_OK;
 }
 

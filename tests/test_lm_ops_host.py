@@ -167,6 +167,17 @@ def test_cross_entropy_refuses(kw, code):
     refused(code, c.mtdao_cross_entropy, a, BASE << 4, 1 << 40, None)
 
 
+@pytest.mark.parametrize("kw", [
+    dict(losses=BASE + 4), dict(losses=(BASE << 1) + 8), dict(losses=(BASE << 2) + 1396), dict(losses=BASE << 5), dict(losses=(BASE << 5) - 24),
+    dict(loss=BASE), dict(loss=(BASE << 1) + 52), dict(loss=(BASE << 2) + 8), dict(loss=BASE << 5), dict(losses=BASE << 3, loss=(BASE << 3) + 24),
+    dict(d_loss=(BASE << 2) + 1396), dict(reduction=0, loss=None, losses=(BASE << 5) + 24), dict(reduction=0, loss=None, d_loss=(BASE << 2) - 24)])
+def test_cross_entropy_refuses_losses_that_overlap(kw):
+    a = c.CrossEntropyArgs(7, 50, 50, 50, 0, 64, 2, 0.0, 1.0, 0, BASE, BASE << 1, BASE << 5, None, BASE << 3, BASE << 2)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    refused(-1, c.mtdao_cross_entropy, a, BASE << 4, 1 << 40, None)
+
+
 def test_cross_entropy_refuses_workspaces():
     a = c.CrossEntropyArgs(7, 50, 50, 50, 0, 64, 2, 0.0, 1.0, 0, BASE, BASE << 1, None, None, BASE << 3, BASE << 2)
     need = c.mtdao_cross_entropy_workspace_bytes(a)
