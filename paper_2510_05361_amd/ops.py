@@ -15,7 +15,8 @@ with it.  There is no CPU path.
 ``peri_norm``, ``linear8``, ``embedding`` and ``cross_entropy`` take part in autograd
 where an input (of ``linear8``: x, or the tensor that its weight was made from)
 requires a gradient; their backward passes are the functions of the same names
-and not differentiable themselves.
+and not differentiable themselves.  Derivatives in forward mode are not given: a
+tensor with a tangent is refused by these, ``orthogonalize`` and ``Weight8``.
 """
 
 from __future__ import annotations
@@ -25,6 +26,7 @@ import math
 from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 from torch.autograd.graph import increment_version
 
@@ -46,6 +48,15 @@ def _type(t: torch.Tensor, what: str) -> int:
     if code is None:
         raise TypeError(f"{what} must be float32 or bfloat16, not {t.dtype}")
     return code
+
+
+def _no_tangent(**tensors: Optional[torch.Tensor]) -> None:
+    """Refuses tensors that carry a derivative in forward mode: the results would be
+    without it.  (Called where there is a level of such derivatives: to look at a tensor
+    takes 0.6 us, at the level 0.1 us.)"""
+    for name, t in tensors.items():
+        if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError(f"{name} has a tangent: derivatives in forward mode are not given; call with its detach()")
 
 
 def _on_device(first: torch.Tensor, *others: Optional[torch.Tensor]) -> torch.device:
@@ -201,6 +212,8 @@ def orthogonalize(x: torch.Tensor, *, steps: int = 5, eps: float = 1e-7, dtype: 
         raise ValueError(f"matrices are wanted, not {tuple(x.shape)}")
     if torch.is_grad_enabled() and x.requires_grad:
         raise ValueError("x requires a gradient, which orthogonalize does not give: call it on x.detach() or under no_grad")
+    if forward_ad._current_level >= 0:
+        _no_tangent(x=x)
     _on_device(x)
     x = x.contiguous()
     r, c = x.shape[-2:]
@@ -377,6 +390,8 @@ def peri_norm(x: torch.Tensor, f: Optional[torch.Tensor], w_post: Optional[torch
     None.  ``gate`` has one row of D per ``rows_per_gate`` rows of x (0: one
     row for all).  n has f's type (``branch_dtype``, x's by default, without
     f)."""
+    if forward_ad._current_level >= 0:
+        _no_tangent(x=x, f=f, w_post=w_post, w_pre=w_pre, gate=gate)
     if torch.is_grad_enabled() and (x.requires_grad or f is not None and f.requires_grad or w_pre is not None and w_pre.requires_grad or
                                     w_post is not None and w_post.requires_grad or gate is not None and gate.requires_grad):
         out, n = _PeriNorm.apply(x, f, w_post, w_pre, gate, rows_per_gate, scale, eps, kind, branch_dtype)
@@ -603,6 +618,8 @@ class Weight8:
     version = 0
 
     def __init__(self, w: torch.Tensor):
+        if forward_ad._current_level >= 0:
+            _no_tangent(w=w)
         _on_device(w)
         if w.requires_grad:
             self.source = w
@@ -612,6 +629,8 @@ class Weight8:
         _quantize(w, self.q, self.qt)
 
     def update(self, w: torch.Tensor) -> None:
+        if forward_ad._current_level >= 0:
+            _no_tangent(w=w)
         _on_device(w, self.q._buf)
         if tuple(w.shape) != (self.q.rows, self.q.cols):
             raise ValueError(f"the weight is [{self.q.rows}, {self.q.cols}], not {tuple(w.shape)}")
@@ -624,6 +643,8 @@ class Weight8:
 def linear8(x: torch.Tensor, w: Weight8, *, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """x W^T over the last axis of x, x in 8-bit blocks along it; in x's type
     unless ``dtype`` is given, which also says how it is summed (``product8``)."""
+    if forward_ad._current_level >= 0:
+        _no_tangent(x=x)
     if torch.is_grad_enabled() and (x.requires_grad or w.source is not None and w.source.requires_grad):
         return _Linear8.apply(x, w.source, w, dtype)
     wq = w.q
@@ -713,6 +734,8 @@ def embedding(tokens: torch.Tensor, table: torch.Tensor, *, scale: float = 1.0, 
     """scale table[tokens]: tokens (int32 or int64) of any shape, a table [rows, d];
     in the table's type unless ``dtype`` is given.  A token below 0 stands for none:
     its row is zero.  One that the table does not have makes its row NaN."""
+    if forward_ad._current_level >= 0:
+        _no_tangent(table=table)
     if torch.is_grad_enabled() and table.requires_grad:
         return _Embedding.apply(tokens, table, scale, dtype)
     dev = _on_device(tokens, table)
@@ -822,6 +845,8 @@ def cross_entropy(logits: torch.Tensor, targets: torch.Tensor, *, z_loss: float 
     lse = log sum exp x, in float32: for each ("none"), their sum or their mean over
     the rows with a target.  A target (int32 or int64) below 0 stands for none:
     no loss, no gradient.  One that the row does not have gives NaN."""
+    if forward_ad._current_level >= 0:
+        _no_tangent(logits=logits)
     if torch.is_grad_enabled() and logits.requires_grad:
         return _CrossEntropy.apply(logits, targets, z_loss, reduction)
     return _loss(logits, targets, z_loss, reduction, loss=True)[0]
