@@ -63,11 +63,8 @@ def build(folder) -> str:
     return lib
 
 
-def run(shim: str, body: str):
-    """Run the Python lines ``body`` (``c``: mtdao_ops, ``abi``: mtdao) over the
-    shim.  Returns (launches, printed): launches as (kernel's name without
-    template arguments, grid, threads of a workgroup, bytes of dynamic LDS), printed as the JSON
-    values that ``say(value)`` was given, both in order."""
+def _lines(shim: str, body: str):
+    """What the Python lines ``body`` (``c``: mtdao_ops, ``abi``: mtdao) print and launch over the shim."""
     head = f"""
         import ctypes, json, sys
         sys.path.insert(0, {ROOT!r})
@@ -78,12 +75,38 @@ def run(shim: str, body: str):
     """
     r = subprocess.run([sys.executable, "-c", textwrap.dedent(head) + textwrap.dedent(body)], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, (r.returncode, r.stdout[-2000:], r.stderr[-2000:])
+    return r.stdout.splitlines()
+
+
+_KERNEL = re.compile(r"(?:12_GLOBAL__N_1|^_Z)\d+(k_[a-z0-9_]+?)(?:I|E)")
+
+
+def run(shim: str, body: str):
+    """Run the Python lines ``body`` (``c``: mtdao_ops, ``abi``: mtdao) over the
+    shim.  Returns (launches, printed): launches as (kernel's name without
+    template arguments, grid, threads of a workgroup, bytes of dynamic LDS), printed as the JSON
+    values that ``say(value)`` was given, both in order."""
     launches, said = [], []
-    for line in r.stdout.splitlines():
+    for line in _lines(shim, body):
         if line.startswith("say "):
             said.append(json.loads(line[4:]))
         elif line.startswith("launch "):
             _, what, gx, gy, gz, threads, lds = line.split()
-            launches.append((re.search(r"(?:12_GLOBAL__N_1|^_Z)\d+(k_[a-z0-9_]+?)(?:I|E)", what).group(1), (int(gx), int(gy), int(gz)),
-                             int(threads), int(lds)))
+            launches.append((_KERNEL.search(what).group(1), (int(gx), int(gy), int(gz)), int(threads), int(lds)))
     return launches, said
+
+
+def instances(shim: str, body: str):
+    """The kernels that ``body`` launches, in order, with their template arguments: "k_name<128, 2, float>"
+    (bf16 is its storage type)."""
+    out = []
+    for line in _lines(shim, body):
+        if line.startswith("launch "):
+            what = line.split()[1]
+            name = _KERNEL.search(what).group(1)
+            args = what[what.index(name) + len(name):]
+            args = args[1:args.index("EEv")] + "E" if args.startswith("I") else ""
+            args = [number or {"0": "false", "1": "true", "f": "float", "t": "bf16"}[truth or kind]
+                    for number, truth, kind in re.findall(r"Li(\d+)E|Lb([01])E|([ft])", args)]
+            out.append(name + ("<" + ", ".join(args) + ">" if args else ""))
+    return out
