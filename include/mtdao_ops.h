@@ -228,8 +228,10 @@ int32_t mtdao_linear8_backward(const void* dy, const void* x, int32_t dtype, int
  *   with a, b, c = 3.4445, -4.7750, 2.0315
  * which leaves the singular vectors of x as they are and moves its singular
  * values towards 1 (after five steps those from 1/400 of ||x|| on lie in about
- * 0.7 to 1.2).  ||x|| is summed in fp64; products are of the precision of fp32 (factors
- * in 24 bits, sums in fp32), and the order of sums depends on the sizes alone.
+ * 0.7 to 1.2).  ||x|| is summed in fp64; products are of about the precision of fp32 (factors
+ * in 23 bits, sums in fp32).  The order of sums depends on the sizes of all matrices of the
+ * call (of the batch, or of the handle) alone: equal calls give equal bits, but a
+ * matrix may give other last bits among others than alone.
  * Elements of X are held to 2^-39: a matrix with ||x|| far below eps, whose X is as
  * small, keeps fewer bits, or none.
  * x = 0 gives 0 (eps > 0); infinities and NaN make all of their matrix NaN. */

@@ -2,17 +2,17 @@
 // optimizer step that takes them (include/mtdao_ops.h).
 //
 // Numbers.  Every factor of a product is held as the sum of two fp16 numbers,
-// x 2^e = hi + lo: hi is x 2^e rounded to eleven bits, lo the rest rounded to
-// eleven bits, so that together they are off by 2^-24 |x| at most, as an fp32 number is.
-// A product is hi hi + hi lo + lo hi in the fp16 matrix instructions, each
-// term exact and summed in fp32; lo lo, 2^-24 of the product at most, is left out.
-// That is three matrix instructions for a product of fp32's precision, at a
+// x 2^e = hi + lo: hi is x 2^e rounded to eleven bits, lo the rest, of thirteen bits, rounded to
+// eleven, so that together they are off by 2^-23 |x| at most (their root mean square is 2^-24.5 |x|; an fp32
+// number is off by 2^-24 |x| at most).  A product is hi hi + hi lo + lo hi in the fp16 matrix
+// instructions, each term exact and summed in fp32; lo lo, 2^-22 of the product at most as |lo| <= 2^-11 |x|,
+// is left out.  That is three matrix instructions for a product of fp32's precision, at a
 // sixteenth of the cost of fp32's own each.  (One bf16 term alone leaves the directions
 // with small singular values, which the iteration raises 480-fold, to rounding:
 // errors of 2 (Gaussian) to 40 (low rank and noise) in a hundred of the result.)
 // fp16's exponents suffice because all factors are bounded: the singular values
-// s of X are at most 1.21 from the first product on (the largest of a s + b s^3 + c s^5
-// over [0, 1.27] is 1.2016), so elements of X and A = X X^T stay below 1.21 and 1.46,
+// s of X are at most 1 at the start and 1.21 from the first product on (the largest of a s + b s^3 + c s^5
+// over [0, 1.21] is 1.2024), so elements of X and A = X X^T stay below 1.21 and 1.46,
 // those of b A + c A^2 within 2.81.  e is chosen for these (kX, kA, kB); what lies
 // below 2^-24 of the stored number's unit, 2^-38 of the largest, is lost.
 //
