@@ -183,8 +183,10 @@ __global__ __launch_bounds__(kSmallThreads) void k_embedding_sort(Sort a) {
 // More of them, up to kMiddle: a launch for each digit of BITS bits, a workgroup for each 1024 places.  Every
 // workgroup counts all digits, those of the places before its own apart, rather than wait
 // for another launch to do it: 16384 tokens 10 to 13 us a pass, most of it counting (a digit that many tokens share
-// is counted one after the other).
-constexpr int kMiddle = 65536;
+// is counted one after the other).  That grows with the square of the places.  The whole gradient in us, by passes / by tiles
+// as below, of 64 columns and 50304 rows, tokens as words come and evenly drawn: 4096 29 / 36 and 24 / 31, 16384 42 / 39 and
+// 31 / 33 (of 200000 rows, a tile's pass more: 47 / 52 and 41 / 49), 24576 50 / 42 and 37 / 34, 65536 102 / 61 and 68 / 42.
+constexpr int kMiddle = 16384;
 template <int BITS>
 __global__ __launch_bounds__(kSmallThreads) void k_embedding_pass(Sort a) {
   constexpr int kBins = 1 << BITS, kApart = 4;  // counters of a digit: one for each four waves

@@ -100,6 +100,18 @@ def test_every_kernel_of_the_cross_entropy(instances):
     assert {"k_cross_entropy<float, 256>", "k_cross_entropy<bf16, 256>"} <= set(seen)
 
 
+def test_many_places_are_sorted_in_tiles(instances):
+    """Passes in which every workgroup counts all places take longer than tiles from some 16384 places on."""
+    for n, kernel in ((2049, "k_embedding_pass<8>"), (16384, "k_embedding_pass<8>"), (16385, "k_embedding_move"), (65536, "k_embedding_move")):
+        names = instances(f"""
+        B = 1 << 40
+        need = c.mtdao_embedding_backward_workspace_bytes({n}, 50304, 64)
+        c.mtdao_embedding_backward(B << 14, 0, 64, B, 64, {n}, 1.0, B << 16, 50304, 64, 64, 0, B << 18, need, None)
+        """)
+        sorts = {x for x in names if re.match("k_embedding_(sort|pass|move)", x)}
+        assert sorts == {kernel}, (n, names)
+
+
 def test_every_kernel_of_the_embedding(instances):
     rows = cases_of(test_gpu_embedding.test_lookup, "n,rows,d")
     sums = cases_of(test_gpu_embedding.test_sums, "n,rows,d")
