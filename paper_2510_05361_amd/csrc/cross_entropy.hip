@@ -25,6 +25,7 @@ namespace {
 template <typename T>
 constexpr int kE = 16 / (int)sizeof(T);  // elements of a thread's vector: 16 bytes
 constexpr int kFinish = 1024;  // threads of the kernels over all rows
+constexpr int kOneEach = 256;  // rows of which each has a CU
 
 struct Args {
   int64_t rows, cols, ld, ld_d;
@@ -363,7 +364,7 @@ template <typename T>
 void launch_rows(const Args& k, hipStream_t st) {
   const int64_t c = k.cols;
   // Threads and vectors that hold the row: a wave while it does so with at most 32 logits a lane.  Without a gradient
-  // rows of more than 8192 stream: nothing has to be held.
+  // rows of more than 8192 stream.
   constexpr int W = 8 / kE<T>;  // vectors of eight elements
   if (c <= 512) return launch_held<T, 64, W>(k, st);
   if (c <= 1024) return launch_held<T, 64, 2 * W>(k, st);
@@ -379,8 +380,11 @@ void launch_rows(const Args& k, hipStream_t st) {
       if (c <= 131072) return launch_held<T, 1024, 16>(k, st);
     }
   }
-  // (few rows: more threads each, which takes fewer turns of the loop)
-  if (k.rows < 512 || k.d_logits) hipLaunchKernelGGL((k_cross_entropy<T, 1024>), grid_of(k.rows), dim3(1024), 0, st, k);
+  // Up to a row a CU more threads each, which takes fewer turns of the loop.  Losses in us, 256 / 1024 threads, bf16: 64 x 32003
+  // 8.4 / 6.7, 256 x 50304 12.5 / 10.2, 257 x 50304 12.6 / 14.7, 384 x 32003 10.1 / 12.4, 1024 x 9000 10 / 21 (and 256 x 9000 6.8 / 7.2); fp32:
+  // 256 x 32003 10.4 / 9.3, 257 x 32003 10.5 / 12.7.  With a gradient, which reads the row twice, always: 2000 x 140000 bf16 358 / 284,
+  // 512 x 70000 fp32 108 / 87.
+  if (k.rows <= kOneEach || k.d_logits) hipLaunchKernelGGL((k_cross_entropy<T, 1024>), grid_of(k.rows), dim3(1024), 0, st, k);
   else hipLaunchKernelGGL((k_cross_entropy<T, 256>), grid_of(k.rows), dim3(256), 0, st, k);
 }
 

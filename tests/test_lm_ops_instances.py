@@ -86,6 +86,18 @@ def test_every_kernel_of_the_updates(instances):
     assert set(seen) == in_the_library("k_muon")
 
 
+@pytest.mark.parametrize("cols", [9000, 32003, 50304])
+def test_rows_that_share_cus_have_fewer_threads(instances, cols):
+    """1024 threads a row while each row has a CU, 256 where they share them."""
+    for rows, threads in ((1, 1024), (256, 1024), (257, 256), (384, 256), (4096, 256)):
+        names = instances(f"""
+        B = 1 << 40
+        a = c.CrossEntropyArgs({rows}, {cols}, {cols}, {cols}, 1, 64, 0, 0.0, 1.0, 0, B, B << 14, None, B << 16, None, None)
+        c.mtdao_cross_entropy(a, B << 20, 0, None)
+        """)
+        assert names == [f"k_cross_entropy<bf16, {threads}>"], (rows, names)
+
+
 def test_every_kernel_of_the_cross_entropy(instances):
     cases = [(r, c, d) for r, c in test_gpu_cross_entropy.SIZES for d in (0, 1)] + [(7, c, d) for c in test_gpu_cross_entropy_widths.HELD for d in (0, 1)]
     cases += [(r, c, 0) for r, c in test_gpu_cross_entropy_widths.EVALUATION]
