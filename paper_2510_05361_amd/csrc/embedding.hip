@@ -322,8 +322,14 @@ __global__ __launch_bounds__(kThreads) void k_embedding_runs(const uint32_t* key
 
 // --------------------------------------------------------------------- sums
 
-constexpr int kRun = 32;       // places that a lane adds up, eight in flight: a microsecond each eight
+// Places that a lane adds up, eight in flight.  Pieces of 16 / 32 / 64, the whole gradient in us: 16384 x 2048 into a new one of 50304 rows
+// 134 / 121 / 119, of 8192 rows 79 / 70 / 76, of 256 rows 48 / 45 / 55; 16384 places of one token x 768 173 / 121 / 99; 4096 x 1024 onto 16 rows
+// 23 / 26 / 37, 1999 x 768 onto 50304 21 / 25 / 32.
+constexpr int kRun = 32;
 constexpr int kSlot = kRun / 2;
+// Lanes that work on the same places, a vector of the columns each.  (Groups of 64: the whole gradient, 16384 places, 50304 rows
+// of 64 columns 44.5 us in place of 41.5, of 68 to 2048 the same within 1%.)
+constexpr int kGroup = 16;
 
 struct Sums {
   const uint32_t *key, *place, *first, *last;  // first and last: of a row's places
@@ -336,18 +342,18 @@ struct Sums {
 };
 
 // Adds rows of dy: the group's lanes fetch their places together, and eight rows are in flight.
-template <typename T, int GROUP>
+template <typename T>
 __device__ __forceinline__ void add_rows(const Sums& a, int64_t from, int64_t to, int64_t e, int n, float (&sum)[kSumE]) {
   const T* dy = reinterpret_cast<const T*>(a.dy) + e;
-  const int lane = (int)threadIdx.x % 64, in = lane % GROUP;
-  for (; from < to; from += GROUP) {
-    const int count = to - from < GROUP ? (int)(to - from) : GROUP;
+  const int lane = (int)threadIdx.x % 64, in = lane % kGroup;
+  for (; from < to; from += kGroup) {
+    const int count = to - from < kGroup ? (int)(to - from) : kGroup;
     const uint32_t mine = in < count ? a.place[from + in] : 0;
     for (int i = 0; i < count; i += 8) {
       float v[8][kSumE];
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        const uint32_t place = (uint32_t)__shfl((int)mine, lane - in + (i + t) % GROUP);
+        const uint32_t place = (uint32_t)__shfl((int)mine, lane - in + (i + t) % kGroup);
         if (i + t < count) load_some<kSumE>(dy + (int64_t)place * a.ld_dy, n, v[t]);
       }
 #pragma unroll
@@ -392,17 +398,17 @@ __device__ __forceinline__ bool piece_of(const Sums& a, int64_t slot, Piece& p) 
 // each row of the table, or for each place.  Bound by HBM's writes where the gradient is new: 50304 x 2048
 // from 16384 tokens 74 us, 6.5 TB/s.  (Clearing it in the launch that sorts, and then only the rows that come: 132 us in all
 // in place of 104.)
-template <typename T, int GROUP>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void k_embedding_sums(Sums a) {
-  const int64_t job = this_group() * (kThreads / GROUP) + (int)threadIdx.x / GROUP, at = job / a.chunks;
-  const int64_t e = ((job - at * a.chunks) * GROUP + (int)threadIdx.x % GROUP) * kSumE;
+  const int64_t job = this_group() * (kThreads / kGroup) + (int)threadIdx.x / kGroup, at = job / a.chunks;
+  const int64_t e = ((job - at * a.chunks) * kGroup + (int)threadIdx.x % kGroup) * kSumE;
   const int n = a.d - e > kSumE ? kSumE : a.d > e ? (int)(a.d - e) : 0;
   float sum[kSumE] = {};
   if (at < a.slots) {
     Piece p;
     if (!piece_of(a, at, p)) return;
     const int64_t from = p.s + p.j * kRun, end = p.s + p.c;
-    add_rows<T, GROUP>(a, from, from + kRun < end ? from + kRun : end, e, n, sum);
+    add_rows<T>(a, from, from + kRun < end ? from + kRun : end, e, n, sum);
     if (n > 0) store_some<kSumE>(a.pieces + at * a.d + e, n, sum);
     return;
   }
@@ -417,7 +423,7 @@ __global__ __launch_bounds__(kThreads) void k_embedding_sums(Sums a) {
   }
   const int64_t s = a.first[row], c = (int64_t)a.last[row] - s;
   if (c > kRun) return;
-  add_rows<T, GROUP>(a, s, s + c, e, n, sum);
+  add_rows<T>(a, s, s + c, e, n, sum);
   store_sum(a, row, e, n, sum);
 }
 
@@ -608,14 +614,12 @@ int32_t mtdao_embedding_backward(const void* dy, int32_t dy_dtype, int64_t ld_dy
   if (!accumulate)
     hipLaunchKernelGGL(k_embedding_runs, grid_of(over(rows + 1, kThreads)), block, 0, st, words(l.key[at]), (uint32_t)n_tokens, rows, words(l.first));
   const int64_t vectors = over(d, kSumE);
-  const bool wide = vectors > 16;
   Sums s = {words(l.key[at]), words(l.place[at]), words(l.first), accumulate ? words(l.last) : words(l.first) + 1, dy, dw, reinterpret_cast<float*>(w + l.pieces), n_tokens, rows, d, ld_dy, ld_dw,
-            n_tokens > kRun ? l.slots : 0, over(vectors, wide ? 64 : 16), scale, accumulate};
+            n_tokens > kRun ? l.slots : 0, over(vectors, kGroup), scale, accumulate};
   auto go = [&](auto t) {
     using T = decltype(t);
     const int64_t jobs = (s.slots + (accumulate ? n_tokens : rows)) * s.chunks;
-    if (wide) hipLaunchKernelGGL((k_embedding_sums<T, 64>), grid_of(over(jobs, kThreads / 64)), block, 0, st, s);
-    else hipLaunchKernelGGL((k_embedding_sums<T, 16>), grid_of(over(jobs, kThreads / 16)), block, 0, st, s);
+    hipLaunchKernelGGL(k_embedding_sums<T>, grid_of(over(jobs, kThreads / kGroup)), block, 0, st, s);
     if (s.slots > 0) hipLaunchKernelGGL(k_embedding_join, grid_of(over(s.slots * vectors, kThreads)), block, 0, st, s);
   };
   if (dy_dtype == MTDAO_BF16) go(bf16_t{});
