@@ -363,8 +363,18 @@ void launch_held(const Args& k, hipStream_t st) {
 template <typename T>
 void launch_rows(const Args& k, hipStream_t st) {
   const int64_t c = k.cols;
-  // Threads and vectors that hold the row: a wave while it does so with at most 32 logits a lane.  Without a gradient
-  // rows of more than 8192 stream.
+  // Threads and vectors that hold the row: a wave while it does so with at most 32 logits a lane, then as few threads as do so with
+  // 32 each.  Loss and gradient in us by two forms (threads x vectors of eight), first of 64 rows, then of 0.4 to 0.8 GB of rows:
+  //   columns                     bf16               fp32
+  //     512   64 x 1,  256 x 1    5.2 4.2,  42  94   4.3  4.0,  49  97
+  //    2048   64 x 4,  256 x 1    5.4 4.1,  92 147   6.0  4.3, 180 171
+  //    4096   64 x 8,  256 x 2    7.5 4.5, 179 198   8.3  4.8, 284 261
+  //    8192  256 x 4,  512 x 2    5.5 4.8, 265 293   6.0  5.1, 265 276
+  //   16384  256 x 8,  512 x 4    7.7 6.1, 282 279   8.6  6.7, 298 285
+  //   32768  512 x 8, 1024 x 4    8.8 8.0, 300 311  10.7  9.9, 281 295
+  //   57344 1024 x 7, 1024 x 8   11.7 12.0, 297 350  14.8 15.0, 314 317   (streaming, read twice: 13.1, 379; 16.1, 373)
+  // Without a gradient rows of more than 8192 stream.  Streaming and held: 0.8 GB of 16384 columns bf16 147 147, fp32 162 151, of 50304
+  // 166 142 and 164 176; 64 rows of 50304 8.5 7.7 and 8.7 10.2.
   constexpr int W = 8 / kE<T>;  // vectors of eight elements
   if (c <= 512) return launch_held<T, 64, W>(k, st);
   if (c <= 1024) return launch_held<T, 64, 2 * W>(k, st);

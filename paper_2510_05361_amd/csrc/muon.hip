@@ -618,7 +618,8 @@ __global__ __launch_bounds__(256) void k_muon_join(Gemms all) {
 // also in registers, as the fp32 it is formed in.  Wave w has the w-th 32 columns of X, the first one
 // to three waves the blocks of A on and above the diagonal.  MB: blocks of X's rows.
 // Bound by latency, of the steps' four or five meetings, chains of matrix instructions and what is written both ways: 64 x 64
-// 24 us, 64 x 256 38 us; 100 x 37 25 us, through the launches that large matrices take 85 us.
+// 24 us, 64 x 256 38 us; 100 x 37 25 us.  (Replayed, so / through the launches that large matrices take: 64 x 64 28 / 85 us,
+// 64 x 256 44 / 89, 200 of them 50 / 241, 1000 182 / 1149.)
 constexpr int kTinyM = 64, kTinyN = 256, kTinyThreads = 512;
 
 // Parts of X's lines in which A = X X^T is formed: eight waves among its one or three blocks.
@@ -923,7 +924,9 @@ struct Shape {
 // 3 m^2 n + (4 k - 3) m^3: five as 3 + 2 instead take 38 in place of 65 m^3 for n = 4 m (2048 x 8192,
 // one matrix: 2.1 ms, one by one 3.0).  Errors of A grow in P A P, where those of X X^T do not: of five steps from 2.2e-6 of the
 // result's norm to 3.1e-6 at 512 x 2048 (fp32 arithmetic throughout: 2.8e-6), but from 1.2e-6 to 5.3e-6 at
-// 37 x 100, and below 512 latency counts, not operations.  Three come first, then two, then one at a
+// 37 x 100, and below 512 latency counts, not operations (one of 256 x 1024 115 us one by one, 117 so).  Where n is little
+// more than m it does so above, too: one by one / several at once, 512 x 768 149 / 157 us, 1024 x 1536 255 / 253, 2048 x 2560 954 / 960, 2048 x 3200
+// 1075 / 1013, four of these 3387 / 3075.  Three come first, then two, then one at a
 // time: once singular values have arrived near 1 errors grow faster (six steps as 3 + 3 1.4e-5).
 bool several_at_once(int64_t m, int64_t n) { return m >= 512 && 2 * n >= 3 * m; }
 Shape shape_of(int64_t rows, int64_t cols) {
@@ -1019,7 +1022,8 @@ constexpr int kBig = 256, kMid = 128, kLittle = 64;
 constexpr int64_t kMostLittle = 1000, kMostMid = 1024;
 
 // A = X X^T of few tiles, up to kFewTiles, and many lines is formed in parts of at least kLeastPart lines, as many as
-// occupy the CUs once, and joined: 300 x 8000 396 -> 244 us, 1 x 8192 332 -> 153 us.
+// occupy the CUs once, and joined: 300 x 8000 396 -> 244 us, 1 x 8192 332 -> 153 us; three of 448 x 4096 (108 tiles) 259 -> 245,
+// of 448 x 1024 178 -> 180, one of 1000 x 4000 (136 tiles) 317 either way.
 constexpr int64_t kFewTiles = 128, kParts = 256, kLeastPart = 8, kManyLines = 32;
 constexpr int64_t kPartialBytes = kParts * kLittle * kLittle * 4;
 
