@@ -365,8 +365,6 @@ dim3 chunk_grid(int64_t chunks) {
 }
 
 int64_t chunks_of(int64_t numel) { return (numel + kChunk - 1) / kChunk; }
-int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
-size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 // How a pass goes over its elements.  Workgroups of one CU and, for states of
 // 32 bits, spread pieces set how many DRAM pages are open at once.  Measured for

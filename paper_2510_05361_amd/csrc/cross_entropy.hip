@@ -39,10 +39,6 @@ struct Args {
   int32_t each;         // d_loss has a number for each row
 };
 
-__device__ __forceinline__ int64_t id_of(const void* ids, int32_t wide, int64_t i) {
-  return wide ? reinterpret_cast<const int64_t*>(ids)[i] : (int64_t) reinterpret_cast<const int32_t*>(ids)[i];
-}
-
 // Largest and sum over the THREADS threads of a row (a wave, or the workgroup), in each.
 template <int THREADS>
 __device__ __forceinline__ float row_max(float x, float* part) {
@@ -310,9 +306,6 @@ __global__ __launch_bounds__(kFinish) void k_cross_entropy_sum(const float* loss
 }
 
 // --------------------------------------------------------------------- host
-
-size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
 
 int32_t check(const mtdao_cross_entropy_args* a, std::string* e) {
   if (!a) return fail(e, MTDAO_ERR_INVALID_ARG, "args is NULL");

@@ -25,9 +25,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kSumE = 4;  // elements of a lane's vector of the gradient: 16 bytes of fp32, so that a wave stores whole lines at once
 
-__device__ __forceinline__ int64_t id_of(const void* ids, int32_t wide, int64_t i) {
-  return wide ? reinterpret_cast<const int64_t*>(ids)[i] : (int64_t) reinterpret_cast<const int32_t*>(ids)[i];
-}
 __device__ __forceinline__ int64_t this_group() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
 // ------------------------------------------------------------------- lookup
@@ -453,8 +450,6 @@ __global__ __launch_bounds__(kThreads) void k_embedding_join(Sums a) {
 
 // --------------------------------------------------------------------- host
 
-size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
 int64_t over(int64_t n, int64_t m) { return (n + m - 1) / m; }
 
 int32_t check_sizes(int64_t n, int64_t rows, int64_t d, std::string* e) {

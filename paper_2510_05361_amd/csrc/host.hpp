@@ -65,6 +65,9 @@ inline int32_t fail(std::string* sink, int32_t code, const char* fmt, ...) noexc
   return code;
 }
 
+inline int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }  // bytes of an element
+inline size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
 inline bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 inline bool aligned16(const void* p) { return aligned_to(p, 16); }
 

@@ -52,7 +52,6 @@ constexpr int kStepNT = 3;     // nontemporal hints of the local step (bit 0 loa
 constexpr bool kMeanNT = true; // nontemporal hints of the replica mean
 constexpr int kNormU = 8;      // vector slots per thread in the norm pass
 
-int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
 bool has_v(const mtdao_config& c) { return c.form != MTDAO_SGDM; }
 
 // Elements of a 16-byte slot.  Every row length takes vector slots: rows

@@ -908,8 +908,6 @@ __global__ __launch_bounds__(kRowsAtOnce) void k_muon_table(Rows in, int at, int
 // --------------------------------------------------------------------- host
 
 int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
-size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
 
 // A matrix's factors: X [m][n] and X^T [n][m] with m <= n, X^T's next value,
 // and the products of X with itself.

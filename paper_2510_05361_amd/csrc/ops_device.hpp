@@ -148,6 +148,11 @@ struct Raw<float, NT> {
   }
 };
 
+// The i-th of tokens or targets of 32 or 64 (wide) bits.
+__device__ __forceinline__ int64_t id_of(const void* ids, int32_t wide, int64_t i) {
+  return wide ? reinterpret_cast<const int64_t*>(ids)[i] : (int64_t) reinterpret_cast<const int32_t*>(ids)[i];
+}
+
 // A wave-uniform value that no running kernel writes, through the scalar
 // cache.
 template <typename T>

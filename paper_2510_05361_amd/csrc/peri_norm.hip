@@ -489,7 +489,6 @@ __global__ __launch_bounds__(kCols * 32) void k_peri_columns(Args a, int64_t blo
 
 // --------------------------------------------------------------------- host
 
-int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
 bool is_type(int32_t dt) { return dt == MTDAO_F32 || dt == MTDAO_BF16; }
 // (rows_per_gate may be any number: nothing is added to it)
 int64_t gates_of(const mtdao_peri_norm_args& a) {

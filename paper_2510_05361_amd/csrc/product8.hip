@@ -872,7 +872,6 @@ Mat mat_of(const mtdao_matrix8* q) {
 }
 
 int64_t scale_bytes(const mtdao_matrix8& q) { return up(q.cols, 4 * kBlock8) / (4 * kBlock8) * q.scale_ld; }
-int64_t esize(int32_t dt) { return dt == MTDAO_BF16 ? 2 : 4; }
 
 // A [rows][cols] input with row stride ld.
 int32_t check_input(const void* x, int32_t dtype, int64_t rows, int64_t cols, int64_t ld, const char* name, std::string* e) {
