@@ -134,9 +134,9 @@ __global__ __launch_bounds__(kSmallThreads) void k_embedding_sort(Sort a) {
         const uint64_t same = same_digit<BITS>(digit, live);
         const uint32_t before = live ? mine[digit] : 0;
         rank[r] = (uint16_t)(before + below(same));
-        __builtin_amdgcn_wave_barrier();
+        lanes_done();
         if (live && below(same) == 0) mine[digit] = before + (uint32_t)__popcll(same);
-        __builtin_amdgcn_wave_barrier();
+        lanes_done();
       }
     }
     __syncthreads();

@@ -276,10 +276,6 @@ struct Last {
 // LDS of the wave's own: 32 lines, then 32 rows of 33 words to turn a fragment.  (Pieces of 16 bytes straight from the
 // lanes take four times as many cycles of the CU's path to memory.)
 constexpr int kStaged = 32 * 128, kOwn = kStaged + 32 * 33 * 4;
-__device__ __forceinline__ void lanes_done() {  // (LDS serves a wave in order; only the compiler has to keep it)
-  __builtin_amdgcn_wave_barrier();
-  asm volatile("" ::: "memory");
-}
 __device__ __forceinline__ u32x4* staged_at(uint8_t* mine, int row, int chunk) {
   return reinterpret_cast<u32x4*>(mine + row * 128 + ((chunk ^ row_key(row)) << 4));
 }

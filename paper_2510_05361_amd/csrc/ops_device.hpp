@@ -160,6 +160,13 @@ __device__ __forceinline__ T uniform_load(const T* p) {
   return *(const __attribute__((address_space(4))) T*)p;
 }
 
+// What lanes of a wave have written to LDS the others read behind this.  LDS serves a wave in order;
+// the compiler has to keep it, and the barrier alone does not bind memory.
+__device__ __forceinline__ void lanes_done() {
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // ---------------------------------------------------------- wave reductions
 
 // x of the lane that a DPP control names (all lanes of the row take part).
